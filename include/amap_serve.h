@@ -208,7 +208,8 @@ int amap_rope_append(const amap_rope_t *plan, const amap_append_args *args /* ho
  * Scores, maximum, sum and output are kept in 32 bits.
  *
  * workspace: amap_attend_workspace() bytes, 256-byte aligned, ZEROED before its first use; every call leaves
- * it ready for the next.  Calls that share a workspace must be ordered (one stream, or events).
+ * it ready for the next.  Calls that share a workspace must have the same q_heads, cache.heads and cache.head_dim and be
+ * ordered (one stream, or events); n_requests may be anything up to what the workspace was sized for.
  * ------------------------------------------------------------------------- */
 typedef struct amap_attend_args {
   int32_t n_requests;

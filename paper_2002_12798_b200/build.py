@@ -34,7 +34,7 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
         return LIB
     tmp = LIB + ".tmp%d" % os.getpid()
     cmd = [
-        _nvcc(), "-std=c++17", "-O3", "-lineinfo", "-shared", "-Xcompiler", "-fPIC,-Wall,-Wextra",
+        _nvcc(), "--threads", "0", "-std=c++17", "-O3", "-lineinfo", "-shared", "-Xcompiler", "-fPIC,-Wall,-Wextra",
         "-gencode", "arch=compute_100a,code=sm_100a", "-cudart", "static",
         "-I", INCLUDE, "-I", CSRC, "-o", tmp,
     ] + [os.path.join(CSRC, s) for s in SOURCES]

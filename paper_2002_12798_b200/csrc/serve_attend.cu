@@ -1,5 +1,26 @@
-// Attention of one new token per request over a paged cache.
+// Attention of one new token per request over a paged cache, split over the cache's length and joined in one launch.
+//
+// Mathematics.  For a cache head and the (up to 8 NT) q heads that share it, with S^T = K Q^T (tokens x heads) and the
+// running maximum m, sum l and O^T = V^T P^T (head elements x heads) of a softmax in base 2:
+//   m' = max(m, max S),  P = 2^(S - m'),  l' = l 2^(m-m') + sum P,  O' = O 2^(m-m') + P V;  parts with their own
+//   (m, l, O) join the same way, and out = O / l, lse = (m + log2 l) ln 2.
+//
+// Bound: HBM.  Every K and V element of a live token is read once and meets 2 x group multiply-adds; the tokens take the
+// M side of the matrix instructions (K as it lies, V through transposing loads), so that 8 q heads fill the N side
+// whatever the group size and the tensor pipe stays a small part of the time.  The matrix instructions are warp-wide
+// mma.sync: a product of 16 tokens by 8 heads is far below the 128 rows a tcgen05 tile wants, and at 2 x 8 multiply-adds
+// per element the legacy rate is several times what HBM can feed.
+//
+// Split.  The tiles (64 tokens) of all requests and heads form one line, cut into equal pieces, one per resident block:
+// balanced to a tile whatever the lengths are, and computed by every block for itself from seq_lens (no plan, no host).
+// A block that has a part of an item writes it to the workspace; the last to arrive joins them in the order of the
+// tokens, so the result does not depend on who that is.
+//
+// Pipeline.  Each of a block's four warps streams its own quarter (16 tokens) of every tile through its own ring of
+// shared memory with 16-byte asynchronous copies, page numbers fetched one step ahead of the copies; nothing but the
+// end of an item synchronises warps.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 
 #include "serve_common.cuh"
@@ -8,84 +29,660 @@ using namespace amap_serve;
 
 namespace {
 
-constexpr int kThreads = 128;
+constexpr int kWarps = 4, kThreads = 32 * kWarps;
+constexpr int kRows = 16;               // tokens per warp and step
+constexpr int kTile = kRows * kWarps;   // tokens per tile
+constexpr int kMostBlocksPerSm = 4;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-__device__ __forceinline__ float to_float(const char *p, int64_t at, int dtype) {
-  if (dtype == AMAP_BF16) return __bfloat162float(reinterpret_cast<const __nv_bfloat16 *>(p)[at]);
-  if (dtype == AMAP_FP16) return __half2float(reinterpret_cast<const __half *>(p)[at]);
-  return __half2float(__half(__nv_cvt_fp8_to_halfraw(reinterpret_cast<const uint8_t *>(p)[at], __NV_E4M3)));
+struct Params {
+  amap_attend_args a;
+  int32_t group, blocks_per_head, items_per_request;  // q heads per cache head; blocks of 8 NT of them; cache heads x blocks
+  uint32_t div_mul, div_shift;                        // token / page_size (0 mul: a power of two)
+  int32_t q_pairs, out_pairs;                         // two elements at a time are aligned
+  float *part_o, *part_ml;
+  int32_t *arrived;
+};
+
+// bytes of a row in shared memory; stages of the ring that make about 96 KB a block (two resident blocks then hold
+// about 128 KB in flight per multiprocessor: latency times bandwidth is about 50)
+template <int ROW_BYTES> constexpr int kStages = ROW_BYTES >= 256 ? 3 : 6;
+
+__device__ __forceinline__ uint32_t smem_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool live) {
+  const int n = live ? 16 : 0;  // nothing is read where the row is not live: the 16 bytes become zeros
+  asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ void load4(uint32_t at, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void load4_transposed(uint32_t at, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t v) {
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+template <int CT>
+__device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if constexpr (CT == AMAP_BF16)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float exp2_of(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// two e4m3 (the low 16 bits) as two fp16: exact
+__device__ __forceinline__ uint32_t halves_of(uint32_t two) {
+  uint32_t r;
+  asm("{ .reg .b16 t; cvt.u16.u32 t, %1; cvt.rn.f16x2.e4m3x2 %0, t; }" : "=r"(r) : "r"(two));
+  return r;
 }
 
-// One block per request and q head; 128 tokens a round: a thread scores one token, then owns columns of the output.
-__global__ void __launch_bounds__(kThreads) attend_kernel(const __grid_constant__ amap_attend_args A) {
-  __shared__ float q[256], score[kThreads], part[kThreads / 32];
-  __shared__ int64_t where[kThreads];
+// P in two 16-bit terms, truncated and remainder: 15 bits and more of it enter P V (one 16-bit term would add an error
+// as large as the rounding of a 16-bit output).  The remainder is kept above zero, so that an infinity in V meets no
+// zero that P has not got.  fp16 terms carry P times 2^12, out of the way of fp16's smallest numbers.
+template <int CT> constexpr float kLift = CT == AMAP_FP16 ? 12.0f : 0.0f;
+template <int CT>
+__device__ __forceinline__ void two_terms(float p0, float p1, uint32_t *hi, uint32_t *lo) {
+  if constexpr (CT == AMAP_BF16) {
+    const uint32_t u0 = __float_as_uint(p0), u1 = __float_as_uint(p1);
+    *hi = __byte_perm(u0, u1, 0x7632);
+    const float r0 = fmaxf(p0 - __uint_as_float(u0 & 0xFFFF0000u), 0x1p-126f), r1 = fmaxf(p1 - __uint_as_float(u1 & 0xFFFF0000u), 0x1p-126f);
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(*lo) : "f"(r1), "f"(r0));
+  } else {
+    asm("cvt.rz.f16x2.f32 %0, %1, %2;" : "=r"(*hi) : "f"(p1), "f"(p0));
+    const __half2 h = *reinterpret_cast<const __half2 *>(hi);
+    const float r0 = fmaxf(p0 - __low2float(h), 0x1p-24f), r1 = fmaxf(p1 - __high2float(h), 0x1p-24f);
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(*lo) : "f"(r1), "f"(r0));
+  }
+}
+
+// Walks the line of tiles: request by request, its heads (blocks of them) one after another, a head's tiles in order.
+// A request without tokens counts one tile, so that somebody writes its zeros.
+struct Cursor {
+  int r, h, n, low, t, left, n_next;
+
+  static __device__ __forceinline__ int clamped(const Params &P, int len) {
+    return (int)min((int64_t)max(len, 0), (int64_t)P.a.max_pages * P.a.cache.page_size);
+  }
+  static __device__ __forceinline__ int lowest(const Params &P, int n) { return P.a.window > 0 ? max(0, n - P.a.window) : 0; }
+  static __device__ __forceinline__ int tiles(const Params &P, int n) {
+    return max(1, (n + kTile - 1) / kTile - lowest(P, n) / kTile);
+  }
+  __device__ __forceinline__ void enter(const Params &P) {
+    low = lowest(P, n);
+    t = low & ~(kTile - 1);
+    left = tiles(P, n);
+  }
+  __device__ __forceinline__ void start(const Params &P, int r0, int h0, int tile) {
+    r = r0;
+    h = h0;
+    n = clamped(P, P.a.seq_lens[r]);
+    n_next = P.a.seq_lens[min(r + 1, P.a.n_requests - 1)];
+    enter(P);
+    t += tile * kTile;
+    left -= tile;
+  }
+  __device__ __forceinline__ void advance(const Params &P) {
+    if (--left > 0) {
+      t += kTile;
+      return;
+    }
+    if (++h == P.items_per_request) {
+      h = 0;
+      ++r;
+      n = clamped(P, n_next);
+      n_next = P.a.seq_lens[min(r + 1, P.a.n_requests - 1)];  // read an item ahead of its use
+    }
+    enter(P);
+  }
+};
+
+template <int CT, bool FP8, int DP, int NT>
+__global__ void __launch_bounds__(kThreads, DP == 256 && !FP8 ? 1 : 2) attend_kernel(const __grid_constant__ Params P) {
+  constexpr int ES = FP8 ? 1 : 2, RB = DP * ES, CH = RB / 16, S = kStages<RB>;
+  constexpr int MT = DP / 16;            // 16-element steps of a head
+  constexpr int HB = 8 * NT;             // q heads of a block
+  constexpr int kStage = 2 * kRows * RB; // K then V
+  constexpr int kPitch = DP + 4;         // floats between heads in `joint`: the writes of a warp meet all banks once,
+                                         // and a warp's (m, l) of a head has room behind its O
+  extern __shared__ __align__(128) char smem[];
+  float *joint = reinterpret_cast<float *>(smem + kWarps * S * kStage);  // [warps][8][kPitch]
+  __shared__ int64_t sums[kWarps], first_unit;
+  __shared__ int begin[3], last;
+  __shared__ uint32_t live_rows[kWarps][S];
+
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
+  const amap_cache &C = P.a.cache;
+  const int D = C.head_dim;
+  if (D < DP) {  // chunks behind the head's end are never copied over: zeros for K's products
+    for (int i = tid; i < kWarps * S * kStage / 16; i += kThreads) reinterpret_cast<uint4 *>(smem)[i] = make_uint4(0, 0, 0, 0);
+    __syncthreads();
+  }
   pdl_begin();
-  const int r = blockIdx.y, h = blockIdx.x, tid = threadIdx.x;
-  const amap_cache &C = A.cache;
-  const int group = A.q_heads / C.heads, kvh = h / group, D = C.head_dim;
-  for (int d = tid; d < D; d += kThreads) q[d] = to_float(static_cast<const char *>(A.q), r * A.q_row + h * A.q_head + d, A.dtype);
-  const int n = (int)min((int64_t)max(A.seq_lens[r], 0), (int64_t)A.max_pages * C.page_size);
-  const int low = A.window > 0 ? max(0, n - A.window) : 0;
-  float top = -INFINITY, sum = 0.0f, o[2] = {0.0f, 0.0f};
+
+  // ---- where this block's piece of the line begins ----
+  const int R = P.a.n_requests, per = (R + kThreads - 1) / kThreads, r_first = tid * per, r_last = min(R, r_first + per);
+  int64_t mine = 0;
+  for (int r = r_first; r < r_last; ++r) mine += Cursor::tiles(P, Cursor::clamped(P, P.a.seq_lens[r]));
+  mine *= P.items_per_request;
+  int64_t upto = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int64_t v = __shfl_up_sync(~0u, upto, d);
+    if (lane >= d) upto += v;
+  }
+  if (lane == 31) sums[warp] = upto;
   __syncthreads();
-  for (int base = low; base < n; base += kThreads) {
-    const int t = base + tid;
-    float s = -INFINITY;
-    int64_t v_at = -1;
-    if (t < n) {
-      const int page = A.block_table[r * A.table_stride + t / C.page_size], off = t % C.page_size;
-      if (page >= 0 && page < C.n_pages) {
-        const int64_t k_at = page * C.k_page + off * C.k_token + kvh * C.k_head;
-        v_at = page * C.v_page + off * C.v_token + kvh * C.v_head;
-        s = 0.0f;
-        for (int d = 0; d < D; ++d) s += q[d] * to_float(static_cast<const char *>(C.k), k_at + d, C.dtype);
-        s *= A.scale * C.k_scale;
-        if (A.softcap > 0) s = A.softcap * tanhf(s / A.softcap);
+  int64_t total = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    if (w < warp) upto += sums[w];
+    total += sums[w];
+  }
+  const int64_t pieces = min((int64_t)gridDim.x, total);  // none of them empty
+  if (blockIdx.x >= pieces) return;
+  const int64_t u0 = total * blockIdx.x / pieces, u1 = total * (blockIdx.x + 1) / pieces;
+  if (upto > u0 && upto - mine <= u0) {
+    int64_t u = upto - mine;
+    for (int r = r_first; r < r_last; ++r) {
+      const int tiles = Cursor::tiles(P, Cursor::clamped(P, P.a.seq_lens[r]));
+      const int64_t units = (int64_t)tiles * P.items_per_request;
+      if (u + units > u0) {
+        const int in = (int)(u0 - u);
+        begin[0] = r;
+        begin[1] = in / tiles;
+        begin[2] = in % tiles;
+        first_unit = u + (int64_t)begin[1] * tiles;  // of the item that u0 is in
+        break;
+      }
+      u += units;
+    }
+  }
+  __syncthreads();
+  const int steps = (int)(u1 - u0);
+  Cursor ahead, at;
+  ahead.start(P, begin[0], begin[1], begin[2]);
+  at = ahead;
+  int64_t item_first = first_unit;
+
+  // ---- the ring ----
+  char *const ring = smem + warp * (S * kStage);
+  const uint32_t ring_at = smem_at(ring);
+  const int my_row = lane & 15;
+  int entry = -1, offset = 0, kv_head = 0;  // of the step whose copies are issued next
+  bool in_range = false;
+  int looked = 0;
+  auto look = [&]() {  // fetch the page number of my row for the next step
+    in_range = false;
+    if (looked < steps) {
+      const int token = ahead.t + warp * kRows + my_row;
+      in_range = token < ahead.n && token >= ahead.low;
+      kv_head = ahead.h / P.blocks_per_head;
+      if (in_range) {
+        const uint32_t page = P.div_mul ? __umulhi((uint32_t)token, P.div_mul) >> P.div_shift : (uint32_t)token >> P.div_shift;
+        offset = token - (int)page * C.page_size;
+        entry = P.a.block_table[(int64_t)ahead.r * P.a.table_stride + page];
+      }
+      ++looked;
+      ahead.advance(P);
+    }
+  };
+  int write = 0;
+  auto copy = [&]() {
+    const bool live = in_range && (uint32_t)entry < (uint32_t)C.n_pages;
+    const int64_t ko = live ? (int64_t)entry * C.k_page + (int64_t)offset * C.k_token + (int64_t)kv_head * C.k_head : 0;
+    const int64_t vo = live ? (int64_t)entry * C.v_page + (int64_t)offset * C.v_token + (int64_t)kv_head * C.v_head : 0;
+    const uint32_t rows = __ballot_sync(~0u, live) & 0xFFFFu;
+    if (lane == 0) live_rows[warp][write] = rows;
+    const uint32_t stage = ring_at + write * kStage;
+    constexpr int LPR = CH < 32 ? CH : 32;  // lanes per row
+    constexpr int RPI = 32 / LPR;           // rows per instruction
+    if (rows) {
+#pragma unroll
+      for (int i = 0; i < kRows / RPI; ++i) {
+        const int row = i * RPI + lane / LPR;
+        const int64_t k_row = __shfl_sync(~0u, ko, row), v_row = __shfl_sync(~0u, vo, row);
+        const bool row_live = (rows >> row) & 1;
+#pragma unroll
+        for (int c0 = 0; c0 < CH; c0 += LPR) {
+          const int c = c0 + lane % LPR;
+          const int swizzled = RB >= 128 ? c ^ (row & 7) : c ^ ((row >> 1) & (CH - 1));
+          const uint32_t dst = stage + row * RB + swizzled * 16;
+          if (c * 16 < D * ES) {
+            copy16(dst, static_cast<const char *>(C.k) + k_row * ES + c * 16, row_live);
+            copy16(dst + kRows * RB, static_cast<const char *>(C.v) + v_row * ES + c * 16, row_live);
+          }
+        }
       }
     }
-    where[tid] = v_at;
-    float m = s;
-    for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
-    if ((tid & 31) == 0) part[tid >> 5] = m;
-    __syncthreads();
-    m = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
-    const float now = fmaxf(top, m);
-    const float keep = now == -INFINITY ? 1.0f : expf(top - now);
-    score[tid] = v_at < 0 ? 0.0f : expf(s - now);
-    top = now;
-    __syncthreads();
-    sum *= keep;
-    o[0] *= keep;
-    o[1] *= keep;
-    for (int i = 0; i < kThreads; ++i) {
-      if (where[i] < 0) continue;
-      sum += score[i];
-      for (int k = 0; k < 2; ++k) {
-        const int d = tid + k * kThreads;
-        if (d < D) o[k] += score[i] * to_float(static_cast<const char *>(C.v), where[i] + d, C.dtype);
+    copies_commit();
+    write = write + 1 == S ? 0 : write + 1;
+  };
+
+  // ---- q of an item, as the B operand: element pairs (2 t4, +8) of head g; e4m3: 4 t4 .. +3, K's order there ----
+  uint32_t q[NT][MT][2];
+  float to_log2[NT][2];  // scores times this are exponents of 2 (before a softcap: the score itself)
+  const float unit = (P.a.softcap > 0 ? 1.0f : kLog2e) * P.a.scale * C.k_scale;
+  auto load_q = [&](int r, int h) {
+    const int first = h / P.blocks_per_head * P.group, in_group = h % P.blocks_per_head * HB;
+    const uint16_t *row = static_cast<const uint16_t *>(P.a.q) + (int64_t)r * P.a.q_row;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int head = in_group + nt * 8 + g;
+      const bool there = head < P.group;
+      const uint16_t *x = row + (int64_t)(first + (there ? head : 0)) * P.a.q_head;
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int d = m * 16 + (FP8 ? 4 * t4 + 2 * k : 2 * t4 + 8 * k);
+          uint32_t v = 0;
+          if (there && d < D) {
+            if (P.q_pairs) v = *reinterpret_cast<const uint32_t *>(x + d);
+            else v = x[d] | (uint32_t)x[d + 1] << 16;
+          }
+          q[nt][m][k] = v;
+        }
+      }
+      to_log2[nt][0] = to_log2[nt][1] = unit;
+      if constexpr (FP8) {  // q as fp16 times a power of two that brings its largest element near 1
+        float big = 0.0f;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            float2 f;
+            if (P.a.dtype == AMAP_BF16) f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&q[nt][m][k]));
+            else f = __half22float2(*reinterpret_cast<const __half2 *>(&q[nt][m][k]));
+            big = fmaxf(big, fmaxf(fabsf(f.x), fabsf(f.y)));
+          }
+        }
+        big = fmaxf(big, __shfl_xor_sync(~0u, big, 1));
+        big = fmaxf(big, __shfl_xor_sync(~0u, big, 2));
+        // 2^e <= big < 2^(e+1); e within what 2^-e and 2^e are normal numbers for
+        const int e = min(max((int)(__float_as_uint(big) >> 23) - 127, -120), 120);
+        const float down = __uint_as_float((uint32_t)(127 - e) << 23), up = __uint_as_float((uint32_t)(127 + e) << 23);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            float2 f;
+            if (P.a.dtype == AMAP_BF16) f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&q[nt][m][k]));
+            else f = __half22float2(*reinterpret_cast<const __half2 *>(&q[nt][m][k]));
+            const __half2 h2 = __floats2half2_rn(f.x * down, f.y * down);
+            q[nt][m][k] = *reinterpret_cast<const uint32_t *>(&h2);
+          }
+        }
+        to_log2[nt][0] *= __shfl_sync(~0u, up, 8 * t4);  // of heads 2 t4 and 2 t4 + 1: the columns of S^T here
+        to_log2[nt][1] *= __shfl_sync(~0u, up, 8 * t4 + 4);
       }
     }
-    __syncthreads();
+  };
+
+  float o[NT][MT][4], m[NT][2], l[NT][2];
+  auto clear = [&]() {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      m[nt][0] = m[nt][1] = -INFINITY;
+      l[nt][0] = l[nt][1] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < MT; ++i) o[nt][i][0] = o[nt][i][1] = o[nt][i][2] = o[nt][i][3] = 0.0f;
+    }
+  };
+
+  look();
+#pragma unroll 1
+  for (int i = 0; i < S - 1; ++i) {
+    copy();
+    look();
   }
-  for (int k = 0; k < 2; ++k) {
-    const int d = tid + k * kThreads;
-    if (d >= D) break;
-    const float y = sum > 0 ? o[k] / sum * C.v_scale : sum == 0 ? 0.0f : sum;
-    const int64_t at = r * A.out_row + h * A.out_head + d;
-    if (A.dtype == AMAP_BF16) static_cast<__nv_bfloat16 *>(A.out)[at] = __float2bfloat16_rn(y);
-    else static_cast<__half *>(A.out)[at] = __float2half_rn(y);
+  load_q(at.r, at.h);
+  clear();
+
+  int read = 0;
+#pragma unroll 1
+  for (int step = 0; step < steps; ++step) {
+    copies_wait<S - 2>();
+    __syncwarp();
+    copy();  // into the stage that the step before this one has read
+    look();
+    const uint32_t rows = live_rows[warp][read];
+    if (rows) {
+      const uint32_t k_at = ring_at + read * kStage, v_at = k_at + kRows * RB;
+      float s[NT][4];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.0f;
+      const int row_at = my_row * RB, row_swizzle = RB >= 128 ? my_row & 7 : (my_row >> 1) & (CH - 1);
+      if constexpr (!FP8) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          if (i * 16 >= D) break;
+          uint32_t a[4];
+          load4(k_at + row_at + (((2 * i + (lane >> 4)) ^ row_swizzle) * 16), a);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) mma<CT>(s[nt], a[0], a[1], a[2], a[3], q[nt][i][0], q[nt][i][1]);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < MT; i += 2) {
+          if (i * 16 >= D) break;
+          uint32_t a[4];
+          load4(k_at + row_at + (((i + (lane >> 4)) ^ row_swizzle) * 16), a);
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const uint32_t a0 = halves_of(a[2 * j]), a2 = halves_of(a[2 * j] >> 16), a1 = halves_of(a[2 * j + 1]), a3 = halves_of(a[2 * j + 1] >> 16);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) mma<CT>(s[nt], a0, a1, a2, a3, q[nt][i + j][0], q[nt][i + j][1]);
+          }
+        }
+      }
+      const bool live0 = (rows >> g) & 1, live1 = (rows >> (g + 8)) & 1;
+      bool higher = false;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          float x = s[nt][c] * to_log2[nt][c & 1];
+          if (P.a.softcap > 0) {
+            const float e = exp2_of(x * (2.0f * kLog2e / P.a.softcap));
+            x = (1.0f - __fdividef(2.0f, e + 1.0f)) * (P.a.softcap * kLog2e);  // tanh
+          }
+          s[nt][c] = (c < 2 ? live0 : live1) ? x : -INFINITY;
+        }
+        higher |= fmaxf(s[nt][0], s[nt][2]) > m[nt][0] || fmaxf(s[nt][1], s[nt][3]) > m[nt][1];
+      }
+      if (__any_sync(~0u, higher)) {  // seldom after the first tiles
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            float top = fmaxf(s[nt][c], s[nt][c + 2]);
+            top = fmaxf(top, __shfl_xor_sync(~0u, top, 4));
+            top = fmaxf(top, __shfl_xor_sync(~0u, top, 8));
+            top = fmaxf(top, __shfl_xor_sync(~0u, top, 16));
+            top = fmaxf(top, m[nt][c]);
+            const float keep = top == -INFINITY ? 1.0f : exp2_of(m[nt][c] - top);
+            m[nt][c] = top;
+            l[nt][c] *= keep;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+              o[nt][i][c] *= keep;
+              o[nt][i][c + 2] *= keep;
+            }
+          }
+        }
+      }
+      uint32_t hi[NT][2], lo[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const float top = m[nt][c & 1];
+          s[nt][c] = exp2_of(s[nt][c] - (top == -INFINITY ? 0.0f : top) + kLift<CT>);
+        }
+        l[nt][0] += s[nt][0] + s[nt][2];
+        l[nt][1] += s[nt][1] + s[nt][3];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          two_terms<CT>(s[nt][2 * k], s[nt][2 * k + 1], &hi[nt][k], &lo[nt][k]);
+          hi[nt][k] = transposed(hi[nt][k]);
+          lo[nt][k] = transposed(lo[nt][k]);
+        }
+      }
+      if constexpr (!FP8) {
+        const int v_row = (lane & 7) + (lane >> 4) * 8, v_swizzle = RB >= 128 ? v_row & 7 : (v_row >> 1) & (CH - 1);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          if (i * 16 >= D) break;
+          uint32_t a[4];
+          load4_transposed(v_at + v_row * RB + (((2 * i + ((lane >> 3) & 1)) ^ v_swizzle) * 16), a);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            mma<CT>(o[nt][i], a[0], a[1], a[2], a[3], hi[nt][0], hi[nt][1]);
+            mma<CT>(o[nt][i], a[0], a[1], a[2], a[3], lo[nt][0], lo[nt][1]);
+          }
+        }
+      } else {  // rows g and g + 8 of the product are elements 2g and 2g + 1
+#pragma unroll
+        for (int i = 0; i < MT; i += 2) {
+          if (i * 16 >= D) break;
+          uint32_t a[4];
+          load4_transposed(v_at + row_at + (((i + (lane >> 4)) ^ row_swizzle) * 16), a);
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const uint32_t x = __byte_perm(a[2 * j], 0, 0x3120), y = __byte_perm(a[2 * j + 1], 0, 0x3120);
+            const uint32_t a0 = halves_of(x), a1 = halves_of(x >> 16), a2 = halves_of(y), a3 = halves_of(y >> 16);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              mma<CT>(o[nt][i + j], a0, a1, a2, a3, hi[nt][0], hi[nt][1]);
+              mma<CT>(o[nt][i + j], a0, a1, a2, a3, lo[nt][0], lo[nt][1]);
+            }
+          }
+        }
+      }
+    }
+    read = read + 1 == S ? 0 : read + 1;
+
+    if (at.left > 1 && step + 1 < steps) {
+      at.advance(P);
+      continue;
+    }
+    // ---- the end of an item, or of this block's part of it: join the warps ----
+    const int r = at.r, h = at.h, tiles = Cursor::tiles(P, at.n);
+    const int64_t item_end = item_first + tiles;
+    const bool whole = item_first >= u0 && item_end <= u1;
+    const int first = h / P.blocks_per_head * P.group, in_group = h % P.blocks_per_head * HB;
+    const int heads = min(HB, P.group - in_group);
+    const int slot = 2 * blockIdx.x + (item_first >= u0 ? 1 : 0);  // a block has at most two parts: its first item's and its last's
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      if (nt * 8 >= heads) break;
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        float sum = l[nt][c];
+        sum += __shfl_xor_sync(~0u, sum, 4);
+        sum += __shfl_xor_sync(~0u, sum, 8);
+        sum += __shfl_xor_sync(~0u, sum, 16);
+        if (g == 0) *reinterpret_cast<float2 *>(joint + (warp * 8 + 2 * t4 + c) * kPitch + DP) = make_float2(m[nt][c], sum);
+      }
+      __syncthreads();
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const float *ml = joint + (2 * t4 + c) * kPitch + DP;
+        const float top = fmaxf(fmaxf(ml[0], ml[8 * kPitch]), fmaxf(ml[16 * kPitch], ml[24 * kPitch]));
+        const float f = top == -INFINITY ? 1.0f : exp2_of(m[nt][c] - top);
+        float *to = joint + (warp * 8 + 2 * t4 + c) * kPitch;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          to[i * 16 + (FP8 ? 2 * g : g)] = o[nt][i][c] * f;
+          to[i * 16 + (FP8 ? 2 * g + 1 : g + 8)] = o[nt][i][c + 2] * f;
+        }
+      }
+      __syncthreads();
+      const int n_heads = min(8, heads - nt * 8);
+      for (int i = tid; i < n_heads * (D / 2); i += kThreads) {
+        const int in = i / (D / 2), d = (i - in * (D / 2)) * 2, head = nt * 8 + in;
+        const float *ml = joint + in * kPitch + DP;
+        const float top = fmaxf(fmaxf(ml[0], ml[8 * kPitch]), fmaxf(ml[16 * kPitch], ml[24 * kPitch]));
+        float sum = 0.0f;
+        float2 y = make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+          sum += ml[w * 8 * kPitch + 1] * (top == -INFINITY ? 1.0f : exp2_of(ml[w * 8 * kPitch] - top));
+          const float2 v = *reinterpret_cast<const float2 *>(joint + (w * 8 + in) * kPitch + d);
+          y.x += v.x;
+          y.y += v.y;
+        }
+        if (whole) {
+          const float f = sum == 0.0f ? 0.0f : C.v_scale / sum;
+          const int64_t to = (int64_t)r * P.a.out_row + (int64_t)(first + in_group + head) * P.a.out_head + d;
+          if (P.a.dtype == AMAP_BF16) {
+            __nv_bfloat16 *out = static_cast<__nv_bfloat16 *>(P.a.out) + to;
+            const __nv_bfloat162 v = __floats2bfloat162_rn(y.x * f, y.y * f);
+            if (P.out_pairs) *reinterpret_cast<__nv_bfloat162 *>(out) = v;
+            else out[0] = v.x, out[1] = v.y;
+          } else {
+            __half *out = static_cast<__half *>(P.a.out) + to;
+            const __half2 v = __floats2half2_rn(y.x * f, y.y * f);
+            if (P.out_pairs) *reinterpret_cast<__half2 *>(out) = v;
+            else out[0] = v.x, out[1] = v.y;
+          }
+          if (d == 0 && P.a.lse)
+            P.a.lse[(int64_t)r * P.a.lse_row + first + in_group + head] = sum == 0.0f ? -INFINITY : (top - kLift<CT> + log2f(sum)) * kLn2;
+        } else {
+          *reinterpret_cast<float2 *>(P.part_o + ((int64_t)slot * HB + head) * DP + d) = y;
+          if (d == 0) *reinterpret_cast<float2 *>(P.part_ml + ((int64_t)slot * HB + head) * 2) = make_float2(top, sum);
+        }
+      }
+      __syncthreads();
+    }
+    if (!whole) {  // uniform over the block
+      const int64_t item = (int64_t)r * P.items_per_request + h;
+      const int from = (int)(((item_first + 1) * pieces - 1) / total), to = (int)((item_end * pieces - 1) / total);
+      __threadfence();
+      __syncthreads();
+      if (tid == 0) {
+        last = atomicAdd(P.arrived + item, 1) == to - from;
+        if (last) P.arrived[item] = 0;  // ready for the next call
+      }
+      __syncthreads();
+      if (last) {
+        __threadfence();
+        // parts from .. to, in this order; part `from` began in its block (slot 1), the others before theirs (slot 0)
+        for (int i = tid; i < heads * (D / 4); i += kThreads) {
+          const int head = i / (D / 4), d = (i - head * (D / 4)) * 4;
+          float top = -INFINITY, sum = 0.0f;
+          float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          for (int b = from; b <= to; ++b) {
+            const int64_t part = (int64_t)(2 * b + (b == from ? 1 : 0)) * HB + head;
+            const float2 ml = __ldcg(reinterpret_cast<const float2 *>(P.part_ml + part * 2));
+            const float4 v = __ldcg(reinterpret_cast<const float4 *>(P.part_o + part * DP + d));
+            const float now = fmaxf(top, ml.x);
+            const float keep = now == -INFINITY ? 1.0f : exp2_of(top - now), f = now == -INFINITY ? 1.0f : exp2_of(ml.x - now);
+            sum = sum * keep + ml.y * f;
+            y.x = y.x * keep + v.x * f;
+            y.y = y.y * keep + v.y * f;
+            y.z = y.z * keep + v.z * f;
+            y.w = y.w * keep + v.w * f;
+            top = now;
+          }
+          const float f = sum == 0.0f ? 0.0f : C.v_scale / sum;
+          const float e[4] = {y.x * f, y.y * f, y.z * f, y.w * f};
+          const int64_t to_at = (int64_t)r * P.a.out_row + (int64_t)(first + in_group + head) * P.a.out_head + d;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            if (P.a.dtype == AMAP_BF16) static_cast<__nv_bfloat16 *>(P.a.out)[to_at + j] = __float2bfloat16_rn(e[j]);
+            else static_cast<__half *>(P.a.out)[to_at + j] = __float2half_rn(e[j]);
+          }
+          if (d == 0 && P.a.lse)
+            P.a.lse[(int64_t)r * P.a.lse_row + first + in_group + head] = sum == 0.0f ? -INFINITY : (top - kLift<CT> + log2f(sum)) * kLn2;
+        }
+      }
+    }
+    if (step + 1 < steps) {
+      at.advance(P);
+      item_first = item_end;
+      load_q(at.r, at.h);
+      clear();
+    }
   }
-  if (A.lse && tid == 0) A.lse[r * A.lse_row + h] = sum == 0 ? -INFINITY : top + logf(sum);
+}
+
+template <int CT, bool FP8, int DP, int NT>
+int run(Params &P, void *stream) {
+  constexpr int RB = DP * (FP8 ? 1 : 2);
+  constexpr size_t smem = (size_t)kWarps * kStages<RB> * 2 * kRows * RB + sizeof(float) * kWarps * 8 * (DP + 4);
+  // the block's shared memory is asked for, and how many blocks a multiprocessor then holds, once per device
+  static std::atomic<int> known[64];
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess || dev >= 64) {
+    cudaGetLastError();
+    return refuse(AMAP_ECUDA, e != cudaSuccess ? cudaGetErrorString(e) : "device number");
+  }
+  int blocks = known[dev].load(std::memory_order_relaxed);
+  if (blocks == 0) {
+    int per_sm = 0;
+    e = cudaFuncSetAttribute(attend_kernel<CT, FP8, DP, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, attend_kernel<CT, FP8, DP, NT>, kThreads, smem);
+    if (e != cudaSuccess || per_sm < 1) {
+      cudaGetLastError();
+      return refuse(AMAP_ECUDA, e != cudaSuccess ? cudaGetErrorString(e) : "the kernel does not fit a multiprocessor");
+    }
+    blocks = device_sms() * std::min(per_sm, kMostBlocksPerSm);
+    known[dev].store(blocks, std::memory_order_relaxed);
+  }
+  const int64_t most = (int64_t)P.a.n_requests * P.items_per_request * std::max<int64_t>(1, ((int64_t)P.a.max_pages * P.a.cache.page_size + kTile - 1) / kTile);
+  return launch(attend_kernel<CT, FP8, DP, NT>, dim3((unsigned)std::min<int64_t>(blocks, most)), kThreads, smem, stream, P);
+}
+
+template <int CT, bool FP8, int DP>
+int run_heads(Params &P, int nt, void *stream) {
+  switch (nt) {
+    case 1: return run<CT, FP8, DP, 1>(P, stream);
+    case 2: return run<CT, FP8, DP, 2>(P, stream);
+    default:
+      if constexpr (DP < 256) return run<CT, FP8, DP, 4>(P, stream);
+      else return run<CT, FP8, DP, 2>(P, stream);
+  }
+}
+
+template <int CT, bool FP8>
+int run_dim(Params &P, int dp, int nt, void *stream) {
+  switch (dp) {
+    case 64: return run_heads<CT, FP8, 64>(P, nt, stream);
+    case 128: return run_heads<CT, FP8, 128>(P, nt, stream);
+    default: return run_heads<CT, FP8, 256>(P, nt, stream);
+  }
+}
+
+// head sizes are padded to what a kernel is built for (in shared memory only: no more is read)
+int padded_dim(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
+// eights of q heads that share a pass over the cache: all of a group where its accumulators fit the registers
+int eights(int group, int dp) {
+  const int most = dp < 256 ? 4 : 2;
+  return group <= 8 ? 1 : group <= 16 || most == 2 ? 2 : 4;
+}
+
+
+
+int check_shape(int32_t n_requests, int32_t q_heads, int32_t kv_heads, int32_t head_dim) {
+  SERVE_REQUIRE(n_requests >= 1 && n_requests <= 0xFFFF, AMAP_EINVAL, "requests: 1 .. 65535");
+  SERVE_REQUIRE(q_heads >= 1 && q_heads <= 0xFFFF && kv_heads >= 1 && q_heads % kv_heads == 0, AMAP_EINVAL, "q heads: a multiple of the cache's heads");
+  SERVE_REQUIRE(head_dim >= 8 && head_dim <= 256 && head_dim % 8 == 0, AMAP_EUNSUPPORTED, "head size: a multiple of 8, up to 256");
+  return AMAP_OK;
+}
+
+struct Workspace {
+  int64_t arrived, ml, bytes;  // offsets; the partial outputs come first
+};
+Workspace workspace(int32_t n_requests, int32_t q_heads, int32_t kv_heads, int32_t head_dim) {
+  const int dp = padded_dim(head_dim), group = q_heads / kv_heads, hb = 8 * eights(group, dp);
+  const int64_t slots = 2 * (int64_t)device_sms() * kMostBlocksPerSm, items = (int64_t)n_requests * kv_heads * ((group + hb - 1) / hb);
+  Workspace w;
+  w.ml = slots * hb * dp * 4;
+  w.arrived = w.ml + slots * hb * 8;
+  w.bytes = (w.arrived + items * 4 + 255) / 256 * 256;
+  return w;
 }
 
 }  // namespace
 
 extern "C" int amap_attend_workspace(int32_t n_requests, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int64_t *bytes) {
   SERVE_REQUIRE(bytes, AMAP_EINVAL, "null pointer");
-  SERVE_REQUIRE(n_requests >= 1 && q_heads >= 1 && kv_heads >= 1 && q_heads % kv_heads == 0, AMAP_EINVAL, "q heads: a multiple of the cache's heads");
-  SERVE_REQUIRE(head_dim >= 8 && head_dim <= 256 && head_dim % 8 == 0, AMAP_EUNSUPPORTED, "head size: a multiple of 8, up to 256");
-  *bytes = 256;
+  if (const int rc = check_shape(n_requests, q_heads, kv_heads, head_dim)) return rc;
+  *bytes = workspace(n_requests, q_heads, kv_heads, head_dim).bytes;
   return accept();
 }
 
@@ -93,9 +690,7 @@ extern "C" int amap_attend(const amap_attend_args *a, void *cuda_stream) {
   SERVE_REQUIRE(a, AMAP_EINVAL, "null pointer");
   if (const int rc = check_cache(a->cache)) return rc;
   const amap_cache &c = a->cache;
-  int64_t need = 0;
-  if (const int rc = amap_attend_workspace(a->n_requests, a->q_heads, c.heads, c.head_dim, &need)) return rc;
-  SERVE_REQUIRE(a->n_requests <= 0xFFFF, AMAP_EINVAL, "at most 65535 requests");
+  if (const int rc = check_shape(a->n_requests, a->q_heads, c.heads, c.head_dim)) return rc;
   SERVE_REQUIRE(a->dtype == AMAP_BF16 || a->dtype == AMAP_FP16, AMAP_EINVAL, "type: bf16 or fp16");
   SERVE_REQUIRE(c.dtype == AMAP_E4M3 || c.dtype == a->dtype, AMAP_EINVAL, "a 16-bit cache has the type of q");
   SERVE_REQUIRE(a->q && a->out && a->block_table && a->seq_lens && a->workspace, AMAP_EINVAL, "null pointer");
@@ -103,7 +698,6 @@ extern "C" int amap_attend(const amap_attend_args *a, void *cuda_stream) {
   SERVE_REQUIRE((int64_t)a->max_pages * c.page_size <= 0x7FFFFFFF, AMAP_EOVERFLOW, "a table row holds more than 2^31-1 tokens");
   SERVE_REQUIRE(std::isfinite(a->scale) && std::isfinite(a->softcap) && a->softcap >= 0 && a->window >= 0 && a->reserved == 0, AMAP_EINVAL,
                 "scale is finite, softcap and window are not negative");
-  SERVE_REQUIRE(a->workspace_bytes >= need, AMAP_EINVAL, "workspace too small");
   const int es = dtype_bytes(c.dtype), per16 = 16 / es;
   SERVE_REQUIRE(c.head_dim % per16 == 0, AMAP_EUNSUPPORTED, "head size: whole 16-byte chunks");
   for (const int64_t s : {c.k_page, c.k_token, c.k_head, c.v_page, c.v_token, c.v_head})
@@ -118,5 +712,29 @@ extern "C" int amap_attend(const amap_attend_args *a, void *cuda_stream) {
   os.add(a->n_requests, a->out_row, 2);
   os.add(a->q_heads, a->out_head, 2);
   SERVE_REQUIRE(!overlap(a->q, qs, a->out, os), AMAP_EINVAL, "q and out overlap");
-  return launch(attend_kernel, dim3(a->q_heads, a->n_requests), kThreads, 0, cuda_stream, *a);
+
+  const Workspace w = workspace(a->n_requests, a->q_heads, c.heads, c.head_dim);
+  SERVE_REQUIRE(a->workspace_bytes >= w.bytes, AMAP_EINVAL, "workspace too small");
+  const int dp = padded_dim(c.head_dim);
+  Params P = {};
+  P.a = *a;
+  P.group = a->q_heads / c.heads;
+  const int nt = eights(P.group, dp);
+  P.blocks_per_head = (P.group + 8 * nt - 1) / (8 * nt);
+  P.items_per_request = c.heads * P.blocks_per_head;
+  SERVE_REQUIRE((int64_t)a->n_requests * P.items_per_request <= 0x7FFFFFFF, AMAP_EOVERFLOW, "more than 2^31-1 pairs of request and head");
+  // token / page_size for tokens below 2^31: a shift, or the high word of a product with ceil(2^(32+s) / page_size),
+  // s = floor(log2 page_size), whose excess over 2^(32+s) is at most page_size - 1 < 2^(s+1): exact up to 2^31
+  int s = 0;
+  while ((2u << s) <= (uint32_t)c.page_size) ++s;
+  P.div_shift = s;
+  if (c.page_size != 1 << s) P.div_mul = (uint32_t)((((uint64_t)1 << (32 + s)) + c.page_size - 1) / c.page_size);
+  P.q_pairs = aligned(a->q, 4) && a->q_row % 2 == 0 && a->q_head % 2 == 0;
+  P.out_pairs = aligned(a->out, 4) && a->out_row % 2 == 0 && a->out_head % 2 == 0;
+  char *ws = static_cast<char *>(a->workspace);
+  P.part_o = reinterpret_cast<float *>(ws);
+  P.part_ml = reinterpret_cast<float *>(ws + w.ml);
+  P.arrived = reinterpret_cast<int32_t *>(ws + w.arrived);
+  if (c.dtype == AMAP_E4M3) return run_dim<AMAP_FP16, true>(P, dp, nt, cuda_stream);
+  return c.dtype == AMAP_BF16 ? run_dim<AMAP_BF16, false>(P, dp, nt, cuda_stream) : run_dim<AMAP_FP16, false>(P, dp, nt, cuda_stream);
 }

@@ -525,8 +525,9 @@ def test_a_decoding_step_in_a_graph(ops):
     def step():
         s = ops.pages_extend(new, seq, table, free, count, page, n)
         q = rope.append(fused[:, :q_heads], fused[:, q_heads : q_heads + heads], fused[:, q_heads + heads :], s.positions, s.slots, cache)
-        rows = torch.zeros_like(q).index_copy_(0, s.requests.clamp(min=0).long(), q)
-        out = attention.attend(rows, cache, table, s.seq_lens)
+        rows = torch.zeros(n + 1, q_heads, dim, device="cuda", dtype=q.dtype)  # the last takes what is no request's
+        rows[torch.where(s.requests < 0, n, s.requests).long()] = q
+        out = attention.attend(rows[:n], cache, table, s.seq_lens)
         seq.copy_(s.seq_lens)
         count.copy_(s.free_count)
         return q, out, s
