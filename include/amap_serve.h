@@ -173,6 +173,14 @@ typedef struct amap_cache {
   float k_scale, v_scale; /* an element stands for its value times the scale (1 for 16-bit caches) */
 } amap_cache;
 
+/* What amap_attend's copies need to know of a cache, encoded once where the cache is set up (host memory, any alignment;
+ * to be encoded anew when the cache's description changes). */
+typedef struct amap_cache_maps {
+  uint64_t k_map[16], v_map[16];
+  int32_t box_shift, usable;
+} amap_cache_maps;
+int amap_cache_encode(const amap_cache *cache /* host */, amap_cache_maps *out /* host */);
+
 /* amap_rope_append: a step's q, k, v [rows][heads][head_dim] in one launch.
  *   q_out = rotated q;  K[slots[i]] = rotated k of row i;  V[slots[i]] = v of row i.
  * A slot outside [0, n_pages*page_size) writes nothing to the cache (its q is rotated all the same).  Slots must be
@@ -207,6 +215,9 @@ int amap_rope_append(const amap_rope_t *plan, const amap_append_args *args /* ho
  * part, so what lies behind a request's end may be anything, NaN included.
  * Scores, maximum, sum and output are kept in 32 bits.
  *
+ * Every wait inside the kernel ends: one that has lasted two seconds is given up, and the int32 at byte
+ * amap_attend_workspace()'s *failed of the workspace becomes 1 (the outputs are then worth nothing).
+ *
  * workspace: amap_attend_workspace() bytes, 256-byte aligned, ZEROED before its first use; every call leaves
  * it ready for the next.  Calls that share a workspace must have the same q_heads, cache.heads and cache.head_dim and be
  * ordered (one stream, or events); n_requests may be anything up to what the workspace was sized for.
@@ -229,11 +240,13 @@ typedef struct amap_attend_args {
   int32_t reserved; /* 0 */
   void *workspace;
   int64_t workspace_bytes;
+  const amap_cache_maps *maps; /* host; of `cache`; NULL: encoded in the call */
   amap_cache cache; /* head_dim a multiple of 8 (e4m3: 16), up to 256; rows aligned to 16 bytes */
 } amap_attend_args;
 int amap_attend(const amap_attend_args *args /* host */, void *cuda_stream);
-/* bytes of workspace for up to n_requests requests on the current device */
-int amap_attend_workspace(int32_t n_requests, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int64_t *bytes);
+/* bytes of workspace for up to n_requests requests on the current device, and where in it the mark of a failure is */
+int amap_attend_workspace(int32_t n_requests, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int64_t *bytes,
+                          int64_t *failed /* may be NULL */);
 
 #ifdef __cplusplus
 }

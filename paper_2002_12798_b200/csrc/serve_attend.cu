@@ -14,14 +14,18 @@
 // Split.  The tiles (64 tokens) of all requests and heads form one line, cut into equal pieces, one per resident block:
 // balanced to a tile whatever the lengths are, and computed by every block for itself from seq_lens (no plan, no host).
 // A block that has a part of an item writes it to the workspace; the last to arrive joins them in the order of the
-// tokens, so the result does not depend on who that is.
+// tokens (beyond 32 parts in groups of 16 blocks first), so the result does not depend on who that is.
 //
-// Pipeline.  Each of a block's four warps streams its own quarter (16 tokens) of every tile through its own ring of
-// shared memory with 16-byte asynchronous copies, page numbers fetched one step ahead of the copies; nothing but the
-// end of an item synchronises warps.
+// Pipeline.  A producer warp looks up pages, one tile ahead, and fills a ring of tiles; four warps take 16 tokens of each
+// tile.  Pages of 8 n tokens arrive by tensor copies (TMA) of whole 8 to 64 token boxes, others row by row with 16-byte
+// asynchronous copies; both lay 128-byte rows out with the same swizzle, chunk ^ (row mod 8), so that the matrix loads
+// meet every bank once.  Only the end of an item synchronises the four warps.
+#include <cuda.h>
+
 #include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <cstring>
 
 #include "serve_common.cuh"
 
@@ -29,32 +33,68 @@ using namespace amap_serve;
 
 namespace {
 
-constexpr int kWarps = 4, kThreads = 32 * kWarps;
+constexpr int kWarps = 4, kThreads = 32 * kWarps, kBlock = kThreads + 32;  // the last warp is the producer
 constexpr int kRows = 16;               // tokens per warp and step
 constexpr int kTile = kRows * kWarps;   // tokens per tile
-constexpr int kMostBlocksPerSm = 4;
+constexpr int kMostBlocksPerSm = 3;
+constexpr int kGroup = 16;              // blocks whose parts are joined first, where an item has more than kDirect of them
+constexpr int kDirect = 32;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct Params {
+  alignas(64) CUtensorMap k_map, v_map;  // [page][head][token][element], boxes of 128 bytes x 2^box_shift tokens
   amap_attend_args a;
   int32_t group, blocks_per_head, items_per_request;  // q heads per cache head; blocks of 8 NT of them; cache heads x blocks
   uint32_t div_mul, div_shift;                        // token / page_size (0 mul: a power of two)
+  int32_t tensor_copies, box_shift;
   int32_t q_pairs, out_pairs;                         // two elements at a time are aligned
   float *part_o, *part_ml;
-  int32_t *arrived;
+  int32_t *failed, *grouped, *arrived;
 };
 
-// bytes of a row in shared memory; stages of the ring that make about 96 KB a block (two resident blocks then hold
-// about 128 KB in flight per multiprocessor: latency times bandwidth is about 50)
+// stages of the ring: about 96 KB a block (two resident blocks then hold about 128 KB in flight per multiprocessor:
+// latency times bandwidth is about 50)
 template <int ROW_BYTES> constexpr int kStages = ROW_BYTES >= 256 ? 3 : 6;
 
 __device__ __forceinline__ uint32_t smem_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool live) {
   const int n = live ? 16 : 0;  // nothing is read where the row is not live: the 16 bytes become zeros
-  asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
 }
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void copies_arrive(uint32_t bar) {  // when this thread's copies so far have landed
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tensor_copy(uint32_t dst, const CUtensorMap *map, int x, int token, int head, int page, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+               "l"(map), "r"(x), "r"(token), "r"(head), "r"(page), "r"(bar)
+               : "memory");
+}
+__device__ __forceinline__ void bar_init(uint32_t bar, int n) { asm volatile("mbarrier.init.shared.b64 [%0], %1;" ::"r"(bar), "r"(n) : "memory"); }
+__device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ void bar_arrive_bytes(uint32_t bar, int n) {
+  asm volatile("mbarrier.arrive.expect_tx.shared.b64 _, [%0], %1;" ::"r"(bar), "r"(n) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+// Every wait ends: after two seconds it gives up, marks the workspace, and later waits of the warp return at once, so that
+// the block still walks through its steps and barriers (on what lies in shared memory) and ends.
+__device__ __noinline__ bool bar_wait_slow(uint32_t bar, uint32_t parity, int32_t *failed) {
+  uint64_t begin, now;
+  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(begin));
+  do {
+    if (bar_try(bar, parity)) return true;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(now));
+  } while (now - begin < 2000000000ull);
+  *failed = 1;
+  return false;
+}
+__device__ __forceinline__ void bar_wait(uint32_t bar, uint32_t parity, int32_t *failed, bool &alive) {
+  if (!bar_try(bar, parity) && alive) alive = bar_wait_slow(bar, parity, failed);
+}
+__device__ __forceinline__ void sync_consumers() { asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory"); }
 
 __device__ __forceinline__ void load4(uint32_t at, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
@@ -148,31 +188,122 @@ struct Cursor {
   }
 };
 
-template <int CT, bool FP8, int DP, int NT>
-__global__ void __launch_bounds__(kThreads, DP == 256 && !FP8 ? 1 : 2) attend_kernel(const __grid_constant__ Params P) {
-  constexpr int ES = FP8 ? 1 : 2, RB = DP * ES, CH = RB / 16, S = kStages<RB>;
-  constexpr int MT = DP / 16;            // 16-element steps of a head
-  constexpr int HB = 8 * NT;             // q heads of a block
-  constexpr int kStage = 2 * kRows * RB; // K then V
-  constexpr int kPitch = DP + 4;         // floats between heads in `joint`: the writes of a warp meet all banks once,
-                                         // and a warp's (m, l) of a head has room behind its O
-  extern __shared__ __align__(128) char smem[];
-  float *joint = reinterpret_cast<float *>(smem + kWarps * S * kStage);  // [warps][8][kPitch]
-  __shared__ int64_t sums[kWarps], first_unit;
-  __shared__ int begin[3], last;
-  __shared__ uint32_t live_rows[kWarps][S];
+__device__ __forceinline__ void write_pair(const Params &P, int64_t at, float x, float y) {
+  if (P.a.dtype == AMAP_BF16) {
+    __nv_bfloat16 *out = static_cast<__nv_bfloat16 *>(P.a.out) + at;
+    const __nv_bfloat162 v = __floats2bfloat162_rn(x, y);
+    if (P.out_pairs) *reinterpret_cast<__nv_bfloat162 *>(out) = v;
+    else out[0] = v.x, out[1] = v.y;
+  } else {
+    __half *out = static_cast<__half *>(P.a.out) + at;
+    const __half2 v = __floats2half2_rn(x, y);
+    if (P.out_pairs) *reinterpret_cast<__half2 *>(out) = v;
+    else out[0] = v.x, out[1] = v.y;
+  }
+}
 
+// Joins n <= kDirect parts of an item, the i-th in slot slot_of(i), in this order: into the output, or (final: false) into
+// slot slot_of(0), which nobody else reads before this block has arrived for it.  All four warps.
+template <int CT, int DP, int HB, typename F>
+__device__ void join(const Params &P, float2 (*ml)[8], int n, F slot_of, int heads, bool final, int r, int first_head) {
+  const int tid = threadIdx.x, D = P.a.cache.head_dim;
+  for (int h0 = 0; h0 < heads; h0 += 8) {
+    sync_consumers();
+    for (int i = tid >> 3; i < n; i += kThreads / 8) ml[i][tid & 7] = __ldcg(reinterpret_cast<const float2 *>(P.part_ml) + (int64_t)slot_of(i) * HB + h0 + (tid & 7));
+    sync_consumers();
+    const int n_heads = min(8, heads - h0);
+    for (int item = tid; item < n_heads * (D / 4); item += kThreads) {
+      const int in = item / (D / 4), d = (item - in * (D / 4)) * 4;
+      float top = -INFINITY;
+      for (int i = 0; i < n; ++i) top = fmaxf(top, ml[i][in].x);
+      float sum = 0.0f;
+      float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      const float4 *part = reinterpret_cast<const float4 *>(P.part_o + (int64_t)(h0 + in) * DP + d);
+      for (int i0 = 0; i0 < n; i0 += 8) {
+        float4 v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = i0 + j < n ? __ldcg(part + (int64_t)slot_of(i0 + j) * (HB * DP / 4)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (i0 + j >= n) break;
+          const float2 own = ml[i0 + j][in];
+          const float f = top == -INFINITY ? 1.0f : exp2_of(own.x - top);
+          sum += own.y * f;
+          y.x += v[j].x * f;
+          y.y += v[j].y * f;
+          y.z += v[j].z * f;
+          y.w += v[j].w * f;
+        }
+      }
+      if (final) {
+        const float f = sum == 0.0f ? 0.0f : P.a.cache.v_scale / sum;
+        const int64_t to = (int64_t)r * P.a.out_row + (int64_t)(first_head + h0 + in) * P.a.out_head + d;
+        write_pair(P, to, y.x * f, y.y * f);
+        write_pair(P, to + 2, y.z * f, y.w * f);
+        if (d == 0 && P.a.lse) P.a.lse[(int64_t)r * P.a.lse_row + first_head + h0 + in] = sum == 0.0f ? -INFINITY : (top - kLift<CT> + log2f(sum)) * kLn2;
+      } else {
+        const int64_t to = (int64_t)slot_of(0) * HB + h0 + in;
+        *reinterpret_cast<float4 *>(P.part_o + to * DP + d) = y;
+        if (d == 0) reinterpret_cast<float2 *>(P.part_ml)[to] = make_float2(top, sum);
+      }
+    }
+  }
+}
+
+// whether this block is the last of n to arrive at the counter, which then is ready for the next call; all four warps
+__device__ __forceinline__ bool last_of(int32_t *counter, int n, int *told) {
+  __threadfence();
+  sync_consumers();
+  if (threadIdx.x == 0) {
+    const int before = atomicAdd(counter, 1);
+    if (before == n - 1) *counter = 0;
+    *told = before == n - 1;
+  }
+  sync_consumers();
+  const bool last = *told != 0;
+  if (last) __threadfence();
+  return last;
+}
+
+template <int S> struct Small {
+  uint64_t full[S], empty[S];
+  int64_t sums[kWarps], first_unit;
+  uint32_t rows_there[S][2];  // rows of a stage whose page is there
+  int begin[3], told;
+};
+
+template <int CT, bool FP8, int DP, int NT>
+__global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_kernel(const __grid_constant__ Params P) {
+  constexpr int ES = FP8 ? 1 : 2, RB = DP * ES, NB = RB / 128, S = kStages<RB>;
+  constexpr int MT = DP / 16;                  // 16-element steps of a head
+  constexpr int HB = 8 * NT;                   // q heads of a block
+  constexpr int kBox = kTile * 128;            // bytes of 64 rows of 128
+  constexpr int kStage = 2 * NB * kBox;        // K then V
+  constexpr int kPitch = DP + 4;               // floats between heads in `joint`: the writes of a warp meet all banks once,
+                                               // and a warp's (m, l) of a head has room behind its O
+  extern __shared__ __align__(1024) char smem[];
+  float *joint = reinterpret_cast<float *>(smem + S * kStage);  // [warps][8][kPitch]
+  // all in one piece: static shared memory ahead of it would cost its 1024-byte alignment, and with it the second block
+  Small<S> &small = *reinterpret_cast<Small<S> *>(joint + kWarps * 8 * kPitch);
+  float2(*const joined)[8] = reinterpret_cast<float2(*)[8]>(joint);  // [kDirect][8], while `joint` is idle
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
   const amap_cache &C = P.a.cache;
   const int D = C.head_dim;
-  if (D < DP) {  // chunks behind the head's end are never copied over: zeros for K's products
-    for (int i = tid; i < kWarps * S * kStage / 16; i += kThreads) reinterpret_cast<uint4 *>(smem)[i] = make_uint4(0, 0, 0, 0);
-    __syncthreads();
+  if (tid == 0) {
+    for (int i = 0; i < S; ++i) {
+      bar_init(smem_at(&small.full[i]), P.tensor_copies ? 1 : 33);
+      bar_init(smem_at(&small.empty[i]), kWarps);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (!P.tensor_copies && D < DP) {  // what lies behind a head's end is never copied over: zeros (tensor copies bring their own)
+    for (int i = tid; i < S * kStage / 16; i += kBlock) reinterpret_cast<uint4 *>(smem)[i] = make_uint4(0, 0, 0, 0);
   }
   pdl_begin();
 
   // ---- where this block's piece of the line begins ----
-  const int R = P.a.n_requests, per = (R + kThreads - 1) / kThreads, r_first = tid * per, r_last = min(R, r_first + per);
+  const int R = P.a.n_requests, per = (R + kThreads - 1) / kThreads, r_first = warp < kWarps ? min(R, tid * per) : R, r_last = min(R, r_first + per);
   int64_t mine = 0;
   for (int r = r_first; r < r_last; ++r) mine += Cursor::tiles(P, Cursor::clamped(P, P.a.seq_lens[r]));
   mine *= P.items_per_request;
@@ -182,28 +313,28 @@ __global__ void __launch_bounds__(kThreads, DP == 256 && !FP8 ? 1 : 2) attend_ke
     const int64_t v = __shfl_up_sync(~0u, upto, d);
     if (lane >= d) upto += v;
   }
-  if (lane == 31) sums[warp] = upto;
+  if (lane == 31 && warp < kWarps) small.sums[warp] = upto;
   __syncthreads();
   int64_t total = 0;
 #pragma unroll
   for (int w = 0; w < kWarps; ++w) {
-    if (w < warp) upto += sums[w];
-    total += sums[w];
+    if (w < warp) upto += small.sums[w];
+    total += small.sums[w];
   }
   const int64_t pieces = min((int64_t)gridDim.x, total);  // none of them empty
   if (blockIdx.x >= pieces) return;
   const int64_t u0 = total * blockIdx.x / pieces, u1 = total * (blockIdx.x + 1) / pieces;
-  if (upto > u0 && upto - mine <= u0) {
+  if (warp < kWarps && upto > u0 && upto - mine <= u0) {
     int64_t u = upto - mine;
     for (int r = r_first; r < r_last; ++r) {
       const int tiles = Cursor::tiles(P, Cursor::clamped(P, P.a.seq_lens[r]));
       const int64_t units = (int64_t)tiles * P.items_per_request;
       if (u + units > u0) {
         const int in = (int)(u0 - u);
-        begin[0] = r;
-        begin[1] = in / tiles;
-        begin[2] = in % tiles;
-        first_unit = u + (int64_t)begin[1] * tiles;  // of the item that u0 is in
+        small.begin[0] = r;
+        small.begin[1] = in / tiles;
+        small.begin[2] = in % tiles;
+        small.first_unit = u + (int64_t)small.begin[1] * tiles;  // of the item that u0 is in
         break;
       }
       u += units;
@@ -211,64 +342,117 @@ __global__ void __launch_bounds__(kThreads, DP == 256 && !FP8 ? 1 : 2) attend_ke
   }
   __syncthreads();
   const int steps = (int)(u1 - u0);
-  Cursor ahead, at;
-  ahead.start(P, begin[0], begin[1], begin[2]);
-  at = ahead;
-  int64_t item_first = first_unit;
+  Cursor at;
+  at.start(P, small.begin[0], small.begin[1], small.begin[2]);
+  bool alive = true;
 
-  // ---- the ring ----
-  char *const ring = smem + warp * (S * kStage);
-  const uint32_t ring_at = smem_at(ring);
-  const int my_row = lane & 15;
-  int entry = -1, offset = 0, kv_head = 0;  // of the step whose copies are issued next
-  bool in_range = false;
-  int looked = 0;
-  auto look = [&]() {  // fetch the page number of my row for the next step
-    in_range = false;
-    if (looked < steps) {
-      const int token = ahead.t + warp * kRows + my_row;
-      in_range = token < ahead.n && token >= ahead.low;
-      kv_head = ahead.h / P.blocks_per_head;
-      if (in_range) {
+  if (warp == kWarps) {
+    // ---- the producer ----
+    const int boxes = kTile >> P.box_shift;
+    int entry = -1, offset = 0, there = 0;
+    auto look = [&](int row) {  // the page of a row of the tile at `at`, if any of the row's box takes part
+      const int token = at.t + row;
+      there = token < at.n && token + (P.tensor_copies ? 1 << P.box_shift : 1) > at.low;
+      if (there) {
         const uint32_t page = P.div_mul ? __umulhi((uint32_t)token, P.div_mul) >> P.div_shift : (uint32_t)token >> P.div_shift;
         offset = token - (int)page * C.page_size;
-        entry = P.a.block_table[(int64_t)ahead.r * P.a.table_stride + page];
+        entry = P.a.block_table[(int64_t)at.r * P.a.table_stride + page];
       }
-      ++looked;
-      ahead.advance(P);
-    }
-  };
-  int write = 0;
-  auto copy = [&]() {
-    const bool live = in_range && (uint32_t)entry < (uint32_t)C.n_pages;
-    const int64_t ko = live ? (int64_t)entry * C.k_page + (int64_t)offset * C.k_token + (int64_t)kv_head * C.k_head : 0;
-    const int64_t vo = live ? (int64_t)entry * C.v_page + (int64_t)offset * C.v_token + (int64_t)kv_head * C.v_head : 0;
-    const uint32_t rows = __ballot_sync(~0u, live) & 0xFFFFu;
-    if (lane == 0) live_rows[warp][write] = rows;
-    const uint32_t stage = ring_at + write * kStage;
-    constexpr int LPR = CH < 32 ? CH : 32;  // lanes per row
-    constexpr int RPI = 32 / LPR;           // rows per instruction
-    if (rows) {
+    };
+    int stage = 0;
+    uint32_t parity = 1;  // the first round of waits finds every stage empty
+    if (P.tensor_copies) {
+      const int row = lane << P.box_shift;
+      if (lane < boxes) look(row);
+      for (int step = 0; step < steps; ++step) {
+        const int head = at.h / P.blocks_per_head;
+        const bool live = lane < boxes && there && (uint32_t)entry < (uint32_t)C.n_pages;
+        const int page = live ? entry : C.n_pages;  // a page beyond the last: zeros, and nothing is read
+        const int token = live ? offset : 0;
+        const uint32_t low_rows = __ballot_sync(~0u, __shfl_sync(~0u, live, lane >> P.box_shift));
+        const uint32_t high_rows = __ballot_sync(~0u, __shfl_sync(~0u, live, (lane + 32) >> P.box_shift));
+        if (step + 1 < steps) {
+          at.advance(P);
+          there = 0;
+          if (lane < boxes) look(row);
+        }
+        bar_wait(smem_at(&small.empty[stage]), parity, P.failed, alive);
+        if (!__all_sync(~0u, alive)) break;
+        const uint32_t bar = smem_at(&small.full[stage]), to = smem_at(smem + stage * kStage) + row * 128;
+        if (lane == 0) {
+          small.rows_there[stage][0] = low_rows;
+          small.rows_there[stage][1] = high_rows;
+          bar_arrive_bytes(bar, kStage);
+        }
+        __syncwarp();
+        if (lane < boxes) {
 #pragma unroll
-      for (int i = 0; i < kRows / RPI; ++i) {
-        const int row = i * RPI + lane / LPR;
-        const int64_t k_row = __shfl_sync(~0u, ko, row), v_row = __shfl_sync(~0u, vo, row);
-        const bool row_live = (rows >> row) & 1;
-#pragma unroll
-        for (int c0 = 0; c0 < CH; c0 += LPR) {
-          const int c = c0 + lane % LPR;
-          const int swizzled = RB >= 128 ? c ^ (row & 7) : c ^ ((row >> 1) & (CH - 1));
-          const uint32_t dst = stage + row * RB + swizzled * 16;
-          if (c * 16 < D * ES) {
-            copy16(dst, static_cast<const char *>(C.k) + k_row * ES + c * 16, row_live);
-            copy16(dst + kRows * RB, static_cast<const char *>(C.v) + v_row * ES + c * 16, row_live);
+          for (int b = 0; b < NB; ++b) {
+            tensor_copy(to + b * kBox, &P.k_map, b * (128 / ES), token, head, page, bar);
+            tensor_copy(to + (NB + b) * kBox, &P.v_map, b * (128 / ES), token, head, page, bar);
           }
         }
+        if (++stage == S) stage = 0, parity ^= 1;
+      }
+    } else {
+      // a lane looks up two rows; the copies of a row are 8 lanes' 16 bytes of its 128
+      int entries[2], offsets[2];
+      bool theres[2];
+      auto look2 = [&]() {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          look(lane + 32 * k);
+          entries[k] = entry, offsets[k] = offset, theres[k] = there;
+        }
+      };
+      look2();
+      for (int step = 0; step < steps; ++step) {
+        const int head = at.h / P.blocks_per_head;
+        int64_t k_at[2], v_at[2];
+        uint32_t mask[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const bool live = theres[k] && (uint32_t)entries[k] < (uint32_t)C.n_pages;
+          mask[k] = __ballot_sync(~0u, live);
+          k_at[k] = live ? (int64_t)entries[k] * C.k_page + (int64_t)offsets[k] * C.k_token + (int64_t)head * C.k_head : 0;
+          v_at[k] = live ? (int64_t)entries[k] * C.v_page + (int64_t)offsets[k] * C.v_token + (int64_t)head * C.v_head : 0;
+        }
+        if (step + 1 < steps) {
+          at.advance(P);
+          look2();
+        }
+        bar_wait(smem_at(&small.empty[stage]), parity, P.failed, alive);
+        if (!__all_sync(~0u, alive)) break;
+        const uint32_t bar = smem_at(&small.full[stage]), to = smem_at(smem + stage * kStage);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+#pragma unroll 2
+          for (int i = 0; i < 8; ++i) {
+            const int src = i * 4 + (lane >> 3), row = 32 * k + src;
+            const int64_t k_row = __shfl_sync(~0u, k_at[k], src), v_row = __shfl_sync(~0u, v_at[k], src);
+            const bool live = (mask[k] >> src) & 1;
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+              const int c = b * 128 + (lane & 7) * 16;
+              const uint32_t dst = to + b * kBox + row * 128 + (((lane & 7) ^ (row & 7)) * 16);
+              if (c < D * ES) {
+                copy16(dst, static_cast<const char *>(C.k) + k_row * ES + c, live);
+                copy16(dst + NB * kBox, static_cast<const char *>(C.v) + v_row * ES + c, live);
+              }
+            }
+          }
+        }
+        copies_arrive(bar);
+        if (lane == 0) {
+          small.rows_there[stage][0] = mask[0];
+          small.rows_there[stage][1] = mask[1];
+          bar_arrive(bar);
+        }
+        if (++stage == S) stage = 0, parity ^= 1;
       }
     }
-    copies_commit();
-    write = write + 1 == S ? 0 : write + 1;
-  };
+    return;
+  }
 
   // ---- q of an item, as the B operand: element pairs (2 t4, +8) of head g; e4m3: 4 t4 .. +3, K's order there ----
   uint32_t q[NT][MT][2];
@@ -341,44 +525,52 @@ __global__ void __launch_bounds__(kThreads, DP == 256 && !FP8 ? 1 : 2) attend_ke
     }
   };
 
-  look();
-#pragma unroll 1
-  for (int i = 0; i < S - 1; ++i) {
-    copy();
-    look();
-  }
   load_q(at.r, at.h);
   clear();
+  int64_t item_first = small.first_unit;
+  // where a lane's row of the matrix loads lies in a tile, and its chunk 2j (+1 for the upper lanes) swizzled
+  uint32_t lane_at[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) lane_at[j] = (warp * kRows + (lane & 15)) * 128 + (((2 * j) ^ ((lane >> 4) ^ (lane & 7))) * 16);
+  const uint32_t ring = smem_at(smem);
 
-  int read = 0;
+  int stage = 0;
+  uint32_t parity = 0;
 #pragma unroll 1
   for (int step = 0; step < steps; ++step) {
-    copies_wait<S - 2>();
-    __syncwarp();
-    copy();  // into the stage that the step before this one has read
-    look();
-    const uint32_t rows = live_rows[warp][read];
+    // tokens of mine that take part: a range of rows, without those of pages that are not there
+    const int row0 = at.t + warp * kRows, upper = min(max(at.n - row0, 0), kRows), lower = min(max(at.low - row0, 0), kRows);
+    uint32_t rows = ((1u << upper) - 1) & ~((1u << lower) - 1);
+    bar_wait(smem_at(&small.full[stage]), parity, P.failed, alive);
+    const uint32_t k_at = ring + stage * kStage, v_at = k_at + NB * kBox;
+    rows &= small.rows_there[stage][warp >> 1] >> ((warp & 1) * 16);
     if (rows) {
-      const uint32_t k_at = ring_at + read * kStage, v_at = k_at + kRows * RB;
+      if (rows != 0xFFFFu) {
+        // P is zero in the other rows, but what lies there may be anything: zeros to V
+        for (int i = lane; i < kRows * 8 * NB; i += 32) {
+          const int row = (i >> 3) & (kRows - 1);
+          if (!((rows >> row) & 1))
+            asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(v_at + (i / (kRows * 8)) * kBox + (warp * kRows + row) * 128 + (i & 7) * 16), "r"(0) : "memory");
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // before the tensor copies that come to lie there
+        __syncwarp();
+      }
       float s[NT][4];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.0f;
-      const int row_at = my_row * RB, row_swizzle = RB >= 128 ? my_row & 7 : (my_row >> 1) & (CH - 1);
       if constexpr (!FP8) {
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-          if (i * 16 >= D) break;
           uint32_t a[4];
-          load4(k_at + row_at + (((2 * i + (lane >> 4)) ^ row_swizzle) * 16), a);
+          load4(k_at + lane_at[i & 3] + (i >> 2) * kBox, a);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) mma<CT>(s[nt], a[0], a[1], a[2], a[3], q[nt][i][0], q[nt][i][1]);
         }
       } else {
 #pragma unroll
         for (int i = 0; i < MT; i += 2) {
-          if (i * 16 >= D) break;
           uint32_t a[4];
-          load4(k_at + row_at + (((i + (lane >> 4)) ^ row_swizzle) * 16), a);
+          load4(k_at + lane_at[(i >> 1) & 3] + (i >> 3) * kBox, a);
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             const uint32_t a0 = halves_of(a[2 * j]), a2 = halves_of(a[2 * j] >> 16), a1 = halves_of(a[2 * j + 1]), a3 = halves_of(a[2 * j + 1] >> 16);
@@ -441,24 +633,21 @@ __global__ void __launch_bounds__(kThreads, DP == 256 && !FP8 ? 1 : 2) attend_ke
         }
       }
       if constexpr (!FP8) {
-        const int v_row = (lane & 7) + (lane >> 4) * 8, v_swizzle = RB >= 128 ? v_row & 7 : (v_row >> 1) & (CH - 1);
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-          if (i * 16 >= D) break;
           uint32_t a[4];
-          load4_transposed(v_at + v_row * RB + (((2 * i + ((lane >> 3) & 1)) ^ v_swizzle) * 16), a);
+          load4_transposed(v_at + lane_at[i & 3] + (i >> 2) * kBox, a);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
-            mma<CT>(o[nt][i], a[0], a[1], a[2], a[3], hi[nt][0], hi[nt][1]);
-            mma<CT>(o[nt][i], a[0], a[1], a[2], a[3], lo[nt][0], lo[nt][1]);
+            mma<CT>(o[nt][i], a[0], a[2], a[1], a[3], hi[nt][0], hi[nt][1]);
+            mma<CT>(o[nt][i], a[0], a[2], a[1], a[3], lo[nt][0], lo[nt][1]);
           }
         }
       } else {  // rows g and g + 8 of the product are elements 2g and 2g + 1
 #pragma unroll
         for (int i = 0; i < MT; i += 2) {
-          if (i * 16 >= D) break;
           uint32_t a[4];
-          load4_transposed(v_at + row_at + (((i + (lane >> 4)) ^ row_swizzle) * 16), a);
+          load4_transposed(v_at + lane_at[(i >> 1) & 3] + (i >> 3) * kBox, a);
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             const uint32_t x = __byte_perm(a[2 * j], 0, 0x3120), y = __byte_perm(a[2 * j + 1], 0, 0x3120);
@@ -472,7 +661,9 @@ __global__ void __launch_bounds__(kThreads, DP == 256 && !FP8 ? 1 : 2) attend_ke
         }
       }
     }
-    read = read + 1 == S ? 0 : read + 1;
+    __syncwarp();
+    if (lane == 0) bar_arrive(smem_at(&small.empty[stage]));
+    if (++stage == S) stage = 0, parity ^= 1;
 
     if (at.left > 1 && step + 1 < steps) {
       at.advance(P);
@@ -496,7 +687,7 @@ __global__ void __launch_bounds__(kThreads, DP == 256 && !FP8 ? 1 : 2) attend_ke
         sum += __shfl_xor_sync(~0u, sum, 16);
         if (g == 0) *reinterpret_cast<float2 *>(joint + (warp * 8 + 2 * t4 + c) * kPitch + DP) = make_float2(m[nt][c], sum);
       }
-      __syncthreads();
+      sync_consumers();
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         const float *ml = joint + (2 * t4 + c) * kPitch + DP;
@@ -509,7 +700,7 @@ __global__ void __launch_bounds__(kThreads, DP == 256 && !FP8 ? 1 : 2) attend_ke
           to[i * 16 + (FP8 ? 2 * g + 1 : g + 8)] = o[nt][i][c + 2] * f;
         }
       }
-      __syncthreads();
+      sync_consumers();
       const int n_heads = min(8, heads - nt * 8);
       for (int i = tid; i < n_heads * (D / 2); i += kThreads) {
         const int in = i / (D / 2), d = (i - in * (D / 2)) * 2, head = nt * 8 + in;
@@ -526,67 +717,33 @@ __global__ void __launch_bounds__(kThreads, DP == 256 && !FP8 ? 1 : 2) attend_ke
         }
         if (whole) {
           const float f = sum == 0.0f ? 0.0f : C.v_scale / sum;
-          const int64_t to = (int64_t)r * P.a.out_row + (int64_t)(first + in_group + head) * P.a.out_head + d;
-          if (P.a.dtype == AMAP_BF16) {
-            __nv_bfloat16 *out = static_cast<__nv_bfloat16 *>(P.a.out) + to;
-            const __nv_bfloat162 v = __floats2bfloat162_rn(y.x * f, y.y * f);
-            if (P.out_pairs) *reinterpret_cast<__nv_bfloat162 *>(out) = v;
-            else out[0] = v.x, out[1] = v.y;
-          } else {
-            __half *out = static_cast<__half *>(P.a.out) + to;
-            const __half2 v = __floats2half2_rn(y.x * f, y.y * f);
-            if (P.out_pairs) *reinterpret_cast<__half2 *>(out) = v;
-            else out[0] = v.x, out[1] = v.y;
-          }
+          write_pair(P, (int64_t)r * P.a.out_row + (int64_t)(first + in_group + head) * P.a.out_head + d, y.x * f, y.y * f);
           if (d == 0 && P.a.lse)
             P.a.lse[(int64_t)r * P.a.lse_row + first + in_group + head] = sum == 0.0f ? -INFINITY : (top - kLift<CT> + log2f(sum)) * kLn2;
         } else {
           *reinterpret_cast<float2 *>(P.part_o + ((int64_t)slot * HB + head) * DP + d) = y;
-          if (d == 0) *reinterpret_cast<float2 *>(P.part_ml + ((int64_t)slot * HB + head) * 2) = make_float2(top, sum);
+          if (d == 0) reinterpret_cast<float2 *>(P.part_ml)[(int64_t)slot * HB + head] = make_float2(top, sum);
         }
       }
-      __syncthreads();
+      sync_consumers();
     }
     if (!whole) {  // uniform over the block
-      const int64_t item = (int64_t)r * P.items_per_request + h;
       const int from = (int)(((item_first + 1) * pieces - 1) / total), to = (int)((item_end * pieces - 1) / total);
-      __threadfence();
-      __syncthreads();
-      if (tid == 0) {
-        last = atomicAdd(P.arrived + item, 1) == to - from;
-        if (last) P.arrived[item] = 0;  // ready for the next call
-      }
-      __syncthreads();
-      if (last) {
-        __threadfence();
-        // parts from .. to, in this order; part `from` began in its block (slot 1), the others before theirs (slot 0)
-        for (int i = tid; i < heads * (D / 4); i += kThreads) {
-          const int head = i / (D / 4), d = (i - head * (D / 4)) * 4;
-          float top = -INFINITY, sum = 0.0f;
-          float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-          for (int b = from; b <= to; ++b) {
-            const int64_t part = (int64_t)(2 * b + (b == from ? 1 : 0)) * HB + head;
-            const float2 ml = __ldcg(reinterpret_cast<const float2 *>(P.part_ml + part * 2));
-            const float4 v = __ldcg(reinterpret_cast<const float4 *>(P.part_o + part * DP + d));
-            const float now = fmaxf(top, ml.x);
-            const float keep = now == -INFINITY ? 1.0f : exp2_of(top - now), f = now == -INFINITY ? 1.0f : exp2_of(ml.x - now);
-            sum = sum * keep + ml.y * f;
-            y.x = y.x * keep + v.x * f;
-            y.y = y.y * keep + v.y * f;
-            y.z = y.z * keep + v.z * f;
-            y.w = y.w * keep + v.w * f;
-            top = now;
-          }
-          const float f = sum == 0.0f ? 0.0f : C.v_scale / sum;
-          const float e[4] = {y.x * f, y.y * f, y.z * f, y.w * f};
-          const int64_t to_at = (int64_t)r * P.a.out_row + (int64_t)(first + in_group + head) * P.a.out_head + d;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            if (P.a.dtype == AMAP_BF16) static_cast<__nv_bfloat16 *>(P.a.out)[to_at + j] = __float2bfloat16_rn(e[j]);
-            else static_cast<__half *>(P.a.out)[to_at + j] = __float2half_rn(e[j]);
-          }
-          if (d == 0 && P.a.lse)
-            P.a.lse[(int64_t)r * P.a.lse_row + first + in_group + head] = sum == 0.0f ? -INFINITY : (top - kLift<CT> + log2f(sum)) * kLn2;
+      // part `from` began in its block (the second slot), the others before theirs (the first)
+      auto slot_of_block = [&](int b) { return 2 * b + (b == from ? 1 : 0); };
+      int32_t *item = P.arrived + (int64_t)r * P.items_per_request + h;
+      if (to - from < kDirect) {
+        if (last_of(item, to - from + 1, &small.told))
+          join<CT, DP, HB>(P, joined, to - from + 1, [&](int i) { return slot_of_block(from + i); }, heads, true, r, first + in_group);
+      } else {
+        // of the items with parts in a group of blocks, one at most began before the group and one at most, among those
+        // with more than kDirect parts, begins in it: two counters
+        const int group = blockIdx.x / kGroup, b0 = max(from, group * kGroup), b1 = min(to, group * kGroup + kGroup - 1);
+        if (last_of(P.grouped + 2 * group + (from >= group * kGroup ? 1 : 0), b1 - b0 + 1, &small.told)) {
+          join<CT, DP, HB>(P, joined, b1 - b0 + 1, [&](int i) { return slot_of_block(b0 + i); }, heads, false, r, first + in_group);
+          const int g0 = from / kGroup, g1 = to / kGroup;
+          if (last_of(item, g1 - g0 + 1, &small.told))
+            join<CT, DP, HB>(P, joined, g1 - g0 + 1, [&](int i) { return slot_of_block(max(from, (g0 + i) * kGroup)); }, heads, true, r, first + in_group);
         }
       }
     }
@@ -602,7 +759,7 @@ __global__ void __launch_bounds__(kThreads, DP == 256 && !FP8 ? 1 : 2) attend_ke
 template <int CT, bool FP8, int DP, int NT>
 int run(Params &P, void *stream) {
   constexpr int RB = DP * (FP8 ? 1 : 2);
-  constexpr size_t smem = (size_t)kWarps * kStages<RB> * 2 * kRows * RB + sizeof(float) * kWarps * 8 * (DP + 4);
+  constexpr size_t smem = (size_t)kStages<RB> * 2 * kTile * RB + sizeof(float) * kWarps * 8 * (DP + 4) + sizeof(Small<kStages<RB>>);
   // the block's shared memory is asked for, and how many blocks a multiprocessor then holds, once per device
   static std::atomic<int> known[64];
   int dev = 0;
@@ -615,7 +772,7 @@ int run(Params &P, void *stream) {
   if (blocks == 0) {
     int per_sm = 0;
     e = cudaFuncSetAttribute(attend_kernel<CT, FP8, DP, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, attend_kernel<CT, FP8, DP, NT>, kThreads, smem);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, attend_kernel<CT, FP8, DP, NT>, kBlock, smem);
     if (e != cudaSuccess || per_sm < 1) {
       cudaGetLastError();
       return refuse(AMAP_ECUDA, e != cudaSuccess ? cudaGetErrorString(e) : "the kernel does not fit a multiprocessor");
@@ -624,7 +781,7 @@ int run(Params &P, void *stream) {
     known[dev].store(blocks, std::memory_order_relaxed);
   }
   const int64_t most = (int64_t)P.a.n_requests * P.items_per_request * std::max<int64_t>(1, ((int64_t)P.a.max_pages * P.a.cache.page_size + kTile - 1) / kTile);
-  return launch(attend_kernel<CT, FP8, DP, NT>, dim3((unsigned)std::min<int64_t>(blocks, most)), kThreads, smem, stream, P);
+  return launch(attend_kernel<CT, FP8, DP, NT>, dim3((unsigned)std::min<int64_t>(blocks, most)), kBlock, smem, stream, P);
 }
 
 template <int CT, bool FP8, int DP>
@@ -641,14 +798,15 @@ int run_heads(Params &P, int nt, void *stream) {
 template <int CT, bool FP8>
 int run_dim(Params &P, int dp, int nt, void *stream) {
   switch (dp) {
-    case 64: return run_heads<CT, FP8, 64>(P, nt, stream);
+    case 64:
+      if constexpr (!FP8) return run_heads<CT, FP8, 64>(P, nt, stream);
     case 128: return run_heads<CT, FP8, 128>(P, nt, stream);
     default: return run_heads<CT, FP8, 256>(P, nt, stream);
   }
 }
 
-// head sizes are padded to what a kernel is built for (in shared memory only: no more is read)
-int padded_dim(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
+// head sizes are padded to what a kernel is built for (in shared memory only: no more is read): whole rows of 128 bytes
+int padded_dim(int d, int es) { return d * es <= 128 ? 128 / es : d <= 128 ? 128 : 256; }
 // eights of q heads that share a pass over the cache: all of a group where its accumulators fit the registers
 int eights(int group, int dp) {
   const int most = dp < 256 ? 4 : 2;
@@ -665,30 +823,102 @@ int check_shape(int32_t n_requests, int32_t q_heads, int32_t kv_heads, int32_t h
 }
 
 struct Workspace {
-  int64_t arrived, ml, bytes;  // offsets; the partial outputs come first
+  int64_t ml, failed, grouped, arrived, bytes;  // offsets; the partial outputs come first
 };
 Workspace workspace(int32_t n_requests, int32_t q_heads, int32_t kv_heads, int32_t head_dim) {
-  const int dp = padded_dim(head_dim), group = q_heads / kv_heads, hb = 8 * eights(group, dp);
-  const int64_t slots = 2 * (int64_t)device_sms() * kMostBlocksPerSm, items = (int64_t)n_requests * kv_heads * ((group + hb - 1) / hb);
+  const int dp = head_dim <= 128 ? 128 : 256, group = q_heads / kv_heads, hb = 8 * eights(group, dp);
+  const int64_t blocks = (int64_t)device_sms() * kMostBlocksPerSm, items = (int64_t)n_requests * kv_heads * ((group + hb - 1) / hb);
   Workspace w;
-  w.ml = slots * hb * dp * 4;
-  w.arrived = w.ml + slots * hb * 8;
+  w.ml = 2 * blocks * hb * dp * 4;
+  w.failed = w.ml + 2 * blocks * hb * 8;
+  w.grouped = w.failed + 16;
+  w.arrived = w.grouped + (blocks / kGroup + 1) * 2 * 4;
   w.bytes = (w.arrived + items * 4 + 255) / 256 * 256;
   return w;
 }
 
+using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                            const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+Encode encoder() {
+  static std::atomic<Encode> known{nullptr};
+  Encode f = known.load(std::memory_order_relaxed);
+  if (!f) {
+    void *p = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) {
+      cudaGetLastError();
+      return nullptr;
+    }
+    f = reinterpret_cast<Encode>(p);
+    known.store(f, std::memory_order_relaxed);
+  }
+  return f;
+}
+
+bool encode(const amap_cache &c, void *base, int64_t page, int64_t token, int64_t head, int box, CUtensorMap *out) {
+  const Encode f = encoder();
+  if (!f) return false;
+  const int64_t es = dtype_bytes(c.dtype), row = c.head_dim * es;
+  const cuuint64_t dims[4] = {(cuuint64_t)c.head_dim, (cuuint64_t)c.page_size, (cuuint64_t)c.heads, (cuuint64_t)c.n_pages};
+  cuuint64_t strides[3];
+  const int64_t given[3] = {token * es, head * es, page * es};
+  for (int i = 0; i < 3; ++i) {
+    if (dims[i + 1] == 1) strides[i] = (cuuint64_t)row;  // a stride that no element uses
+    else if (given[i] <= 0 || given[i] >= ((int64_t)1 << 40)) return false;
+    else strides[i] = (cuuint64_t)given[i];
+  }
+  const cuuint32_t boxes[4] = {(cuuint32_t)(128 / es), (cuuint32_t)box, 1, 1}, ones[4] = {1, 1, 1, 1};
+  const CUtensorMapDataType type = c.dtype == AMAP_E4M3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : c.dtype == AMAP_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+  return f(out, type, 4, base, dims, strides, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+int check_readable(const amap_cache &c) {
+  if (const int rc = check_cache(c)) return rc;
+  const int es = dtype_bytes(c.dtype), per16 = 16 / es;
+  SERVE_REQUIRE(c.head_dim >= 8 && c.head_dim <= 256 && c.head_dim % per16 == 0, AMAP_EUNSUPPORTED, "head size: whole 16-byte chunks, up to 256 elements");
+  for (const int64_t s : {c.k_page, c.k_token, c.k_head, c.v_page, c.v_token, c.v_head})
+    SERVE_REQUIRE(s % per16 == 0, AMAP_EALIGN, "cache strides: whole 16-byte chunks");
+  SERVE_REQUIRE(aligned(c.k, 16) && aligned(c.v, 16), AMAP_EALIGN, "cache: aligned to 16 bytes");
+  return AMAP_OK;
+}
+
+void encode_both(const amap_cache &c, amap_cache_maps *out) {
+  static_assert(sizeof(out->k_map) == sizeof(CUtensorMap), "a tensor map is 128 bytes");
+  memset(out, 0, sizeof *out);
+  if (c.page_size % 8) return;
+  int shift = 3;
+  while (shift < 6 && c.page_size % (2 << shift) == 0) ++shift;
+  CUtensorMap k, v;  // aligned to 64 bytes, as the encoder wants them
+  if (!encode(c, c.k, c.k_page, c.k_token, c.k_head, 1 << shift, &k) || !encode(c, c.v, c.v_page, c.v_token, c.v_head, 1 << shift, &v)) return;
+  memcpy(out->k_map, &k, sizeof k);
+  memcpy(out->v_map, &v, sizeof v);
+  out->box_shift = shift;
+  out->usable = 1;
+}
+
 }  // namespace
 
-extern "C" int amap_attend_workspace(int32_t n_requests, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int64_t *bytes) {
+extern "C" int amap_attend_workspace(int32_t n_requests, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int64_t *bytes, int64_t *failed) {
   SERVE_REQUIRE(bytes, AMAP_EINVAL, "null pointer");
   if (const int rc = check_shape(n_requests, q_heads, kv_heads, head_dim)) return rc;
-  *bytes = workspace(n_requests, q_heads, kv_heads, head_dim).bytes;
+  const Workspace w = workspace(n_requests, q_heads, kv_heads, head_dim);
+  *bytes = w.bytes;
+  if (failed) *failed = w.failed;
+  return accept();
+}
+
+extern "C" int amap_cache_encode(const amap_cache *cache, amap_cache_maps *out) {
+  SERVE_REQUIRE(cache && out, AMAP_EINVAL, "null pointer");
+  if (const int rc = check_readable(*cache)) return rc;
+  encode_both(*cache, out);
   return accept();
 }
 
 extern "C" int amap_attend(const amap_attend_args *a, void *cuda_stream) {
   SERVE_REQUIRE(a, AMAP_EINVAL, "null pointer");
-  if (const int rc = check_cache(a->cache)) return rc;
+  if (const int rc = check_readable(a->cache)) return rc;
   const amap_cache &c = a->cache;
   if (const int rc = check_shape(a->n_requests, a->q_heads, c.heads, c.head_dim)) return rc;
   SERVE_REQUIRE(a->dtype == AMAP_BF16 || a->dtype == AMAP_FP16, AMAP_EINVAL, "type: bf16 or fp16");
@@ -698,11 +928,6 @@ extern "C" int amap_attend(const amap_attend_args *a, void *cuda_stream) {
   SERVE_REQUIRE((int64_t)a->max_pages * c.page_size <= 0x7FFFFFFF, AMAP_EOVERFLOW, "a table row holds more than 2^31-1 tokens");
   SERVE_REQUIRE(std::isfinite(a->scale) && std::isfinite(a->softcap) && a->softcap >= 0 && a->window >= 0 && a->reserved == 0, AMAP_EINVAL,
                 "scale is finite, softcap and window are not negative");
-  const int es = dtype_bytes(c.dtype), per16 = 16 / es;
-  SERVE_REQUIRE(c.head_dim % per16 == 0, AMAP_EUNSUPPORTED, "head size: whole 16-byte chunks");
-  for (const int64_t s : {c.k_page, c.k_token, c.k_head, c.v_page, c.v_token, c.v_head})
-    SERVE_REQUIRE(s % per16 == 0, AMAP_EALIGN, "cache strides: whole 16-byte chunks");
-  SERVE_REQUIRE(aligned(c.k, 16) && aligned(c.v, 16), AMAP_EALIGN, "cache: aligned to 16 bytes");
   SERVE_REQUIRE(aligned(a->q, 2) && aligned(a->out, 2) && aligned(a->lse, 4) && aligned(a->block_table, 4) && aligned(a->seq_lens, 4) &&
                     aligned(a->workspace, 256), AMAP_EALIGN, "misaligned pointer");
   Span qs, os;
@@ -715,7 +940,7 @@ extern "C" int amap_attend(const amap_attend_args *a, void *cuda_stream) {
 
   const Workspace w = workspace(a->n_requests, a->q_heads, c.heads, c.head_dim);
   SERVE_REQUIRE(a->workspace_bytes >= w.bytes, AMAP_EINVAL, "workspace too small");
-  const int dp = padded_dim(c.head_dim);
+  const int dp = padded_dim(c.head_dim, dtype_bytes(c.dtype));
   Params P = {};
   P.a = *a;
   P.group = a->q_heads / c.heads;
@@ -734,7 +959,22 @@ extern "C" int amap_attend(const amap_attend_args *a, void *cuda_stream) {
   char *ws = static_cast<char *>(a->workspace);
   P.part_o = reinterpret_cast<float *>(ws);
   P.part_ml = reinterpret_cast<float *>(ws + w.ml);
+  P.failed = reinterpret_cast<int32_t *>(ws + w.failed);
+  P.grouped = reinterpret_cast<int32_t *>(ws + w.grouped);
   P.arrived = reinterpret_cast<int32_t *>(ws + w.arrived);
+  amap_cache_maps made;
+  const amap_cache_maps *maps = a->maps;
+  if (!maps) {
+    encode_both(c, &made);
+    maps = &made;
+  }
+  P.tensor_copies = maps->usable;
+  P.box_shift = maps->box_shift;
+  if (maps->usable) {
+    SERVE_REQUIRE(maps->box_shift >= 3 && maps->box_shift <= 6 && c.page_size % (1 << maps->box_shift) == 0, AMAP_EINVAL, "maps of another cache");
+    memcpy(&P.k_map, maps->k_map, sizeof P.k_map);
+    memcpy(&P.v_map, maps->v_map, sizeof P.v_map);
+  }
   if (c.dtype == AMAP_E4M3) return run_dim<AMAP_FP16, true>(P, dp, nt, cuda_stream);
   return c.dtype == AMAP_BF16 ? run_dim<AMAP_BF16, false>(P, dp, nt, cuda_stream) : run_dim<AMAP_FP16, false>(P, dp, nt, cuda_stream);
 }

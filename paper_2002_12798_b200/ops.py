@@ -26,7 +26,8 @@ from .binding import AmapError, LIBRARY_PATH
 
 EXPORTS = [
     "amap_pages_extend", "amap_pages_release", "amap_rope_plan", "amap_rope_destroy", "amap_rope_rotate",
-    "amap_rope_append", "amap_attend", "amap_attend_workspace", "amap_serve_error",
+    "amap_rope_append", "amap_cache_encode", "amap_attend", "amap_attend_workspace",
+    "amap_serve_error",
 ]
 _BF16, _FP16, _FP32, _E4M3 = 1, 2, 3, 4
 _DTYPES = {torch.bfloat16: _BF16, torch.float16: _FP16, torch.float32: _FP32, torch.float8_e4m3fn: _E4M3}
@@ -39,8 +40,9 @@ _RELEASE = struct.Struct("4iq7P")  # amap_pages_release_args
 _ROTATE = struct.Struct("2iqP2q2i")  # amap_rope_args up to part[]
 _PART = struct.Struct("2P4q2i")  # amap_rope_part
 _APPEND = struct.Struct("q2i4P8qP2q2iP")  # amap_append_args up to cache
-_ATTEND = struct.Struct("4i3P5qPqP2f2iPq")  # amap_attend_args up to cache
+_ATTEND = struct.Struct("4i3P5qPqP2f2iPqP")  # amap_attend_args up to cache
 _CACHE = struct.Struct("2P6q4ii2f4x")  # amap_cache
+_MAPS = struct.Struct("32Q2i")  # amap_cache_maps
 
 
 def _load():
@@ -52,7 +54,8 @@ def _load():
     for name in ("amap_rope_rotate", "amap_rope_append"):
         getattr(lib, name).argtypes = [c_void_p, c_char_p, c_void_p]
     lib.amap_attend.argtypes = [c_char_p, c_void_p]
-    lib.amap_attend_workspace.argtypes = [c_int32, c_int32, c_int32, c_int32, POINTER(c_int64)]
+    lib.amap_cache_encode.argtypes = [c_char_p, c_void_p]
+    lib.amap_attend_workspace.argtypes = [c_int32, c_int32, c_int32, c_int32, POINTER(c_int64), POINTER(c_int64)]
     lib.amap_rope_plan.argtypes = [c_int32, c_int32, POINTER(c_double), POINTER(c_int32), c_int32, c_int32, c_float, POINTER(c_void_p)]
     lib.amap_rope_destroy.argtypes = [c_void_p]
     lib.amap_rope_destroy.restype = None
@@ -168,6 +171,9 @@ class PagedCache:
         self.dtype, self.device = k.dtype, k.device
         self._args = _CACHE.pack(k.data_ptr(), v.data_ptr(), *k.stride()[:3], *v.stride()[:3], *k.shape, _DTYPES[k.dtype],
                                  self.k_scale, self.v_scale)
+        self._maps = ctypes.create_string_buffer(_MAPS.size)  # for attention; a cache that it refuses is refused there
+        readable = _lib.amap_cache_encode(self._args, self._maps) == 0
+        self._maps_at = ctypes.addressof(self._maps) if readable else 0
 
 
 # ----------------------------------------------------------------------------------------------------------------------
@@ -314,13 +320,19 @@ class AttendPlan:
         self.scale = float(scale) if scale is not None else 1.0 / math.sqrt(head_dim)
         self.window, self.softcap = int(window), float(softcap)
         self.device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
-        n = c_int64()
+        n, failed = c_int64(), c_int64()
         with torch.cuda.device(self.device):
-            _check(_lib.amap_attend_workspace(max_requests, q_heads, kv_heads, head_dim, byref(n)), "amap_attend_workspace")
-            self._bytes = n.value
+            _check(_lib.amap_attend_workspace(max_requests, q_heads, kv_heads, head_dim, byref(n), byref(failed)), "amap_attend_workspace")
+            self._bytes, self._failed = n.value, failed.value
             self._stream = torch.cuda.current_stream()
             self._workspace = torch.zeros(self._bytes, dtype=torch.uint8, device=self.device)
         self._raw = self._stream.cuda_stream
+
+    def failed(self):
+        """Whether a wait inside a kernel of this plan has ever run out (after two seconds: its outputs are worth
+        nothing).  Waits for the device."""
+        torch.cuda.synchronize(self.device)
+        return bool(self._workspace[self._failed : self._failed + 4].any())
 
     def _order(self, s):
         if torch.cuda.is_current_stream_capturing():
@@ -356,6 +368,6 @@ class AttendPlan:
                 args = _ATTEND.pack(n, self.q_heads, _DTYPES.get(q.dtype, 0), block_table.shape[1], q.data_ptr(), out.data_ptr(),
                                     lse.data_ptr() if return_lse else 0, q.stride(0), q.stride(1), out.stride(0), out.stride(1), self.q_heads,
                                     block_table.data_ptr(), block_table.stride(0), _ints("seq_lens", seq_lens, (n,)), self.scale, self.softcap,
-                                    self.window, 0, self._workspace.data_ptr(), self._bytes) + cache._args
+                                    self.window, 0, self._workspace.data_ptr(), self._bytes, cache._maps_at) + cache._args
                 _check(_lib.amap_attend(args, s.cuda_stream), "amap_attend")
         return (out, lse) if return_lse else out

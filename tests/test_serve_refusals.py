@@ -34,7 +34,7 @@ def test_packed_structs_are_as_long_as_the_header_says(tmp_path):
     sizes = {"amap_pages_extend_args": ops._EXTEND.size, "amap_pages_release_args": ops._RELEASE.size,
              "amap_rope_args": ops._ROTATE.size + 4 * ops._PART.size, "amap_rope_part": ops._PART.size,
              "amap_append_args": ops._APPEND.size + ops._CACHE.size, "amap_attend_args": ops._ATTEND.size + ops._CACHE.size,
-             "amap_cache": ops._CACHE.size}
+             "amap_cache": ops._CACHE.size, "amap_cache_maps": ops._MAPS.size}
     checks = "".join("_Static_assert(sizeof(%s) == %d, \"%s\");\n" % (n, s, n) for n, s in sizes.items())
     src = tmp_path / "sizes.c"
     src.write_text('#include "amap_serve.h"\n' + checks + "int main(void) { return 0; }\n")  # the header is C, too
@@ -139,7 +139,7 @@ def test_append(change, code, why):
 
 
 ATTEND = dict(n=4, qh=8, dtype=1, max_pages=8, q=0x1000, out=0x11000, lse=0x21000, qr=512, qhs=64, outr=512, ouths=64, lser=8, table=0x31000, stride=8,
-              lens=0x32000, scale=0.125, softcap=0.0, window=0, res=0, ws=0x400000, bytes=2**40)
+              lens=0x32000, scale=0.125, softcap=0.0, window=0, res=0, ws=0x400000, bytes=2**40, maps=0)
 
 
 @pytest.mark.parametrize("change,code,why", [
@@ -153,6 +153,16 @@ ATTEND = dict(n=4, qh=8, dtype=1, max_pages=8, q=0x1000, out=0x11000, lse=0x2100
 def test_attend(change, code, why):
     a, c = split(change, ATTEND)
     refused(lib.amap_attend(ops._ATTEND.pack(*a.values()) + ops._CACHE.pack(*c.values()), None), code, why)
+
+
+def test_cache_encode():
+    out = ctypes.create_string_buffer(ops._MAPS.size)
+    for change, code, why in ((dict(c_v=0), EINVAL, "null"), (dict(c_dim=260), EUNSUPPORTED, "head size"), (dict(c_kh=65), EALIGN, "strides"), (dict(c_v=0x200002), EALIGN, "16 bytes")):
+        refused(lib.amap_cache_encode(ops._CACHE.pack(*split(change, {})[1].values()), out), code, why)
+    refused(lib.amap_cache_encode(ops._CACHE.pack(*CACHE.values()), None), EINVAL, "null")
+    # pages of 3 tokens have no maps; that is no refusal
+    assert lib.amap_cache_encode(ops._CACHE.pack(*split(dict(c_page=3), {})[1].values()), out) == OK
+    assert ops._MAPS.unpack(out.raw)[-1] == 0
 
 
 def test_python_checks_its_tensors():
