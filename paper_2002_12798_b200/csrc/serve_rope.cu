@@ -4,8 +4,10 @@
 // 64-bit fraction of a turn; p times that fraction wraps modulo a full turn exactly, so the angle's error is
 // p * 2^-65 turns whatever p is, and sincospi takes it from there in 32 bits.
 //
-// Bound: memory, every element is read and written once (a cos/sin pair serves all heads of a token, so the angles
-// are 1/heads of the work and never leave the chip).
+// Bound: memory, every element is read and written once.  A block takes a few tokens of one part (q, k or v): its
+// threads issue their loads, compute the tokens' cos and sin once for all heads while those are under way, and turn
+// and store.  An item is VEC pairs (two 16-byte accesses each way where alignment allows), two per thread.
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 #include <new>
@@ -25,18 +27,36 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxHalf = AMAP_ROPE_MAX_DIM / 2;
+constexpr int kUnroll = 2;      // items per thread whose loads are issued together
+constexpr int kBlocks = 4;      // resident per multiprocessor
+constexpr int kMaxTokens = 16;  // per block
 
 // where a part's rows go
 enum { kRows = 0, kCacheTurned = 1, kCacheCopied = 2 };
+
+// n / d for n below 2^31: the high word of a product with ceil(2^(32+s) / d), s = floor(log2 d)
+struct Div {
+  uint32_t mul, shift, d;
+};
+Div div_by(uint32_t d) {
+  Div f = {0, 0, d};
+  while ((2ull << f.shift) <= d) ++f.shift;
+  if (d != 1u << f.shift) f.mul = (uint32_t)((((uint64_t)1 << (32 + f.shift)) + d - 1) / d);
+  return f;
+}
+__device__ __forceinline__ uint32_t quotient(uint32_t n, const Div &f) { return f.mul ? __umulhi(n, f.mul) >> f.shift : n >> f.shift; }
 
 struct Part {
   const char *x;
   char *y;
   int64_t x_row, x_head, y_row, y_head;  // elements; cache: y_row is the page stride
   int64_t y_token;
-  int32_t first_head;  // heads of the parts before this one
+  int32_t heads;
   int32_t kind;
   float inv_scale;
+  int32_t tokens;        // per block
+  uint32_t first_block;  // blocks of the parts before this one
+  Div by_heads;
 };
 
 struct Params {
@@ -47,24 +67,33 @@ struct Params {
   const int32_t *slots;
   int64_t position_axis, position_row;
   int64_t rows;
-  int32_t n_parts, heads;  // heads of all parts together
+  int32_t n_parts;
   int32_t half, head_dim;
-  int32_t items;  // per head: half/VEC chunks of pairs, then the chunks behind rotary_dim two at a time
-  int32_t wide_positions, page_size, n_slots, e4m3;
+  Div by_items, by_half, by_page;  // items of a head: half/VEC chunks of pairs, then the chunks behind rotary_dim two at a time
+  int32_t wide_positions, n_slots, e4m3;
   float scale, sign;
 };
 
 template <int DT, int VEC>
-__device__ __forceinline__ void load(const char *p, int64_t at, float (&v)[VEC]) {
+__device__ __forceinline__ void unpack(const typename Raw<VEC * sizeof(typename Elem<DT>::T)>::T &raw, float (&v)[VEC]) {
   using E = Elem<DT>;
-  constexpr int ES = sizeof(typename E::T);
   union {
-    typename Raw<VEC * ES>::T raw;
+    typename Raw<VEC * sizeof(typename E::T)>::T raw;
     typename E::T e[VEC];
   } u;
-  u.raw = *reinterpret_cast<const typename Raw<VEC * ES>::T *>(p + at * ES);
+  u.raw = raw;
 #pragma unroll
   for (int j = 0; j < VEC; ++j) v[j] = E::to(u.e[j]);
+}
+
+// two values as two elements in one word: the packed conversion runs on the arithmetic pipes, the single one on the
+// special-function unit at a quarter of their rate
+template <int DT>
+__device__ __forceinline__ uint32_t pack2(float x, float y) {
+  uint32_t r;
+  if constexpr (DT == AMAP_BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(y), "f"(x));
+  else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(y), "f"(x));
+  return r;
 }
 
 template <int DT, int VEC>
@@ -74,101 +103,175 @@ __device__ __forceinline__ void store(char *p, int64_t at, const float (&v)[VEC]
   if (e4m3) {
     union {
       typename Raw<VEC>::T raw;
-      uint8_t e[VEC];
+      uint16_t two[(VEC + 1) / 2];
     } u;
+    if constexpr (VEC == 1) {
+      u.raw = to_e4m3(v[0] * inv_scale);
+    } else {
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) u.e[j] = to_e4m3(v[j] * inv_scale);
+      for (int j = 0; j < VEC; j += 2) u.two[j / 2] = __nv_cvt_float2_to_fp8x2(make_float2(v[j] * inv_scale, v[j + 1] * inv_scale), __NV_SATFINITE, __NV_E4M3);
+    }
     *reinterpret_cast<typename Raw<VEC>::T *>(p + at) = u.raw;
   } else {
     union {
       typename Raw<VEC * ES>::T raw;
       typename E::T e[VEC];
+      uint32_t two[(VEC + 1) / 2];
     } u;
+    if constexpr (ES == 4 || VEC == 1) {
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) u.e[j] = E::from(v[j]);
+      for (int j = 0; j < VEC; ++j) u.e[j] = E::from(v[j]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < VEC; j += 2) u.two[j / 2] = pack2<DT>(v[j], v[j + 1]);
+    }
     *reinterpret_cast<typename Raw<VEC * ES>::T *>(p + at * ES) = u.raw;
   }
 }
 
-// One block per token: the threads first compute the token's cos and sin once, then walk its heads.  An item is VEC
-// pairs: two chunks of VEC elements, half a rotary dimension apart (PAIRS_HALF) or side by side.
-template <int DT, int VEC, int PAIRS>
-__global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ Params P) {
-  __shared__ float2 turn[kMaxHalf];
-  pdl_begin();
-  const int64_t row = blockIdx.x;
-  for (int i = threadIdx.x; i < P.half; i += kThreads) {
-    const int64_t at = P.axis[i] * P.position_axis + row * P.position_row;
-    const int64_t pos = P.wide_positions ? static_cast<const int64_t *>(P.positions)[at] : static_cast<const int32_t *>(P.positions)[at];
-    const int32_t turns = (int32_t)(((uint64_t)pos * P.phase[i]) >> 32);  // in units of 2^-32 turns, [-1/2, 1/2)
-    float s, c;
-    sincospif((float)turns * 0x1p-31f, &s, &c);
-    turn[i] = make_float2(c * P.scale, s * P.scale * P.sign);
-  }
-  __syncthreads();
-  int64_t slot = -1;
-  if (P.slots) {
-    slot = P.slots[row];
-    if (slot < 0 || slot >= P.n_slots) slot = -1;
-  }
-  const int chunks = P.half / VEC;
-  for (int item = threadIdx.x; item < P.heads * P.items; item += kThreads) {
-    const int head = item / P.items, c = item - head * P.items;
-    int k = 0;
-    while (k + 1 < P.n_parts && head >= P.part[k + 1].first_head) ++k;
-    const Part &part = P.part[k];
-    const int h = head - part.first_head;
-    const int64_t x = row * part.x_row + h * part.x_head;
-    int64_t y;
-    bool e4m3 = false;
-    if (part.kind == kRows) {
-      y = row * part.y_row + h * part.y_head;
+// Where pair i's cos (and sin) of a token is kept: the VEC values of a chunk in fours, a four of all chunks side by side,
+// so that neighbouring lanes read neighbouring 16 bytes.
+template <int VEC>
+__device__ __forceinline__ int place(int i, int half) {
+  if constexpr (VEC < 4) return i;
+  else return (i % VEC) / 4 * (half / VEC * 4) + i / VEC * 4 + i % 4;
+}
+
+template <int VEC>
+__device__ __forceinline__ void fetch(const float *row, int c, int half, float (&v)[VEC]) {
+#pragma unroll
+  for (int j = 0; j < VEC; j += VEC < 4 ? 1 : 4) {
+    if constexpr (VEC < 4) {
+      v[j] = row[c * VEC + j];
     } else {
-      if (slot < 0) continue;
-      y = slot / P.page_size * part.y_row + slot % P.page_size * part.y_token + h * part.y_head;
-      e4m3 = P.e4m3;
+      const float4 f = *reinterpret_cast<const float4 *>(row + j / 4 * (half / VEC * 4) + c * 4);
+      v[j] = f.x, v[j + 1] = f.y, v[j + 2] = f.z, v[j + 3] = f.w;
     }
-    if (c < chunks) {
-      const int first = PAIRS == AMAP_PAIRS_HALF ? c * VEC : 2 * c * VEC;
-      const int second = PAIRS == AMAP_PAIRS_HALF ? P.half + c * VEC : first + VEC;
-      float a[VEC], b[VEC];
-      load<DT, VEC>(part.x, x + first, a);
-      load<DT, VEC>(part.x, x + second, b);
-      if (part.kind != kCacheCopied) {
+  }
+}
+
+template <int DT, int VEC, int PAIRS>
+__global__ void __launch_bounds__(kThreads, kBlocks) rope_kernel(const __grid_constant__ Params P) {
+  __shared__ __align__(16) float turn_cos[kMaxTokens * kMaxHalf], turn_sin[kMaxTokens * kMaxHalf];
+  constexpr int ES = sizeof(typename Elem<DT>::T);
+  using Chunk = typename Raw<VEC * ES>::T;
+  int k = 0;
+  while (k + 1 < P.n_parts && blockIdx.x >= P.part[k + 1].first_block) ++k;
+  const Part part = P.part[k];  // a copy: the fields stay in registers
+  const int half = P.half, chunks = half / VEC, items = P.by_items.d;
+  const int64_t row0 = (int64_t)(blockIdx.x - part.first_block) * part.tokens;
+  const int tokens = (int)min((int64_t)part.tokens, P.rows - row0), n = tokens * part.heads * items;
+  const bool turns = part.kind != kCacheCopied;
+  const char *const x0 = part.x + row0 * part.x_row * ES;
+  char *const y0 = part.kind == kRows ? part.y + row0 * part.y_row * ES : part.y;
+  pdl_begin();
+
+  Chunk a[kUnroll], b[kUnroll];
+  int64_t to[kUnroll];  // of the head's first element
+  int chunk[kUnroll], token[kUnroll];
+  bool live[kUnroll];
+  auto load = [&](int base) {
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int item = base + u * kThreads;
+      live[u] = item < n;
+      if (!live[u]) continue;
+      const uint32_t row = quotient(item, P.by_items);
+      chunk[u] = item - row * items;
+      token[u] = quotient(row, part.by_heads);
+      const uint32_t head = row - token[u] * part.heads;
+      if (part.kind == kRows) {
+        to[u] = (uint32_t)token[u] * part.y_row + head * part.y_head;
+      } else {
+        const int32_t slot = P.slots[row0 + token[u]];
+        live[u] = slot >= 0 && slot < P.n_slots;
+        if (!live[u]) continue;
+        const uint32_t page = quotient(slot, P.by_page);
+        to[u] = page * part.y_row + (uint32_t)(slot - page * P.by_page.d) * part.y_token + head * part.y_head;
+      }
+      const bool tail = chunk[u] >= chunks;
+      const int first = tail ? 2 * half + 2 * (chunk[u] - chunks) * VEC : PAIRS == AMAP_PAIRS_HALF ? chunk[u] * VEC : 2 * chunk[u] * VEC;
+      const int gap = tail || PAIRS != AMAP_PAIRS_HALF ? VEC : half;
+      const char *p = x0 + ((uint32_t)token[u] * part.x_row + head * part.x_head + first) * ES;
+      a[u] = *reinterpret_cast<const Chunk *>(p);
+      if (first + gap < P.head_dim) b[u] = *reinterpret_cast<const Chunk *>(p + gap * ES);
+    }
+  };
+  auto finish = [&]() {
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      if (!live[u]) continue;
+      float v[VEC], w[VEC];
+      unpack<DT, VEC>(a[u], v);
+      unpack<DT, VEC>(b[u], w);
+      const bool tail = chunk[u] >= chunks;
+      const int first = tail ? 2 * half + 2 * (chunk[u] - chunks) * VEC : PAIRS == AMAP_PAIRS_HALF ? chunk[u] * VEC : 2 * chunk[u] * VEC;
+      const int gap = tail || PAIRS != AMAP_PAIRS_HALF ? VEC : half;
+      if (turns && !tail) {
+        float c[VEC], s[VEC];
+        fetch<VEC>(turn_cos + token[u] * half, chunk[u], half, c);
+        fetch<VEC>(turn_sin + token[u] * half, chunk[u], half, s);
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
-          const float2 t = turn[c * VEC + j];
-          if constexpr (PAIRS == AMAP_PAIRS_HALF) {
-            const float u = a[j], w = b[j];
-            a[j] = u * t.x - w * t.y;
-            b[j] = w * t.x + u * t.y;
-          } else {
-            float &e0 = 2 * j < VEC ? a[(2 * j) % VEC] : b[(2 * j) % VEC];
-            float &e1 = 2 * j + 1 < VEC ? a[(2 * j + 1) % VEC] : b[(2 * j + 1) % VEC];
-            const float u = e0, w = e1;
-            e0 = u * t.x - w * t.y;
-            e1 = w * t.x + u * t.y;
-          }
+          float &e0 = PAIRS == AMAP_PAIRS_HALF ? v[j] : 2 * j < VEC ? v[(2 * j) % VEC] : w[(2 * j) % VEC];
+          float &e1 = PAIRS == AMAP_PAIRS_HALF ? w[j] : 2 * j + 1 < VEC ? v[(2 * j + 1) % VEC] : w[(2 * j + 1) % VEC];
+          const float p = e0, q = e1;
+          e0 = p * c[j] - q * s[j];
+          e1 = q * c[j] + p * s[j];
         }
       }
-      store<DT, VEC>(part.y, y + first, a, e4m3, part.inv_scale);
-      store<DT, VEC>(part.y, y + second, b, e4m3, part.inv_scale);
-    } else {
-      for (int q = 0; q < 2; ++q) {
-        const int at = 2 * P.half + (2 * (c - chunks) + q) * VEC;
-        if (at >= P.head_dim) break;
-        float a[VEC];
-        load<DT, VEC>(part.x, x + at, a);
-        store<DT, VEC>(part.y, y + at, a, e4m3, part.inv_scale);
-      }
+      const bool e4m3 = part.kind != kRows && P.e4m3;
+      store<DT, VEC>(y0, to[u] + first, v, e4m3, part.inv_scale);
+      if (first + gap < P.head_dim) store<DT, VEC>(y0, to[u] + first + gap, w, e4m3, part.inv_scale);
     }
+  };
+
+  load(threadIdx.x);
+  if (turns) {
+    // the tables lie in the kernel's parameters; read as constants, a warp's 32 addresses would be served one by one,
+    // as memory they are two lines
+    const uint64_t *phases = P.phase;
+    const uint8_t *axes = P.axis;
+    asm volatile("" : "+l"(phases), "+l"(axes));
+    for (int i = threadIdx.x; i < tokens * half; i += kThreads) {
+      const int at = quotient(i, P.by_half), pair = i - at * half;
+      const int64_t from = axes[pair] * P.position_axis + (row0 + at) * P.position_row;
+      const int64_t pos = P.wide_positions ? static_cast<const int64_t *>(P.positions)[from] : static_cast<const int32_t *>(P.positions)[from];
+      const int32_t fraction = (int32_t)(((uint64_t)pos * phases[pair]) >> 32);  // in units of 2^-32 turns, [-1/2, 1/2)
+      float s, c;
+      sincospif((float)fraction * 0x1p-31f, &s, &c);
+      turn_cos[at * half + place<VEC>(pair, half)] = c * P.scale;
+      turn_sin[at * half + place<VEC>(pair, half)] = s * P.scale * P.sign;
+    }
+    __syncthreads();
+  }
+  finish();
+  for (int base = threadIdx.x + kUnroll * kThreads; base < n; base += kUnroll * kThreads) {  // many heads a token
+    load(base);
+    finish();
   }
 }
 
 template <int DT, int VEC>
 int run(const amap_rope_t &plan, Params &P, void *stream) {
-  P.items = P.half / VEC + ((P.head_dim - 2 * P.half) / VEC + 1) / 2;
-  const dim3 grid((unsigned)P.rows);
+  const int items = P.half / VEC + ((P.head_dim - 2 * P.half) / VEC + 1) / 2;
+  P.by_items = div_by(items);
+  P.by_half = div_by(std::max(P.half, 1));
+  // tokens per block: two items a thread, but no fewer than two blocks a multiprocessor where there is that much work
+  const int sms = device_sms();
+  int64_t all = 0;
+  for (int k = 0; k < P.n_parts; ++k) all += P.rows * P.part[k].heads * items;
+  const int64_t per_block = std::min<int64_t>(kUnroll * kThreads, std::max<int64_t>(all / (2 * sms), 1));
+  int64_t blocks = 0;
+  for (int k = 0; k < P.n_parts; ++k) {
+    Part &part = P.part[k];
+    part.by_heads = div_by(part.heads);
+    part.tokens = (int32_t)std::max<int64_t>(1, std::min<int64_t>(kMaxTokens, per_block / ((int64_t)part.heads * items)));
+    part.first_block = (uint32_t)blocks;
+    blocks += (P.rows + part.tokens - 1) / part.tokens;
+  }
+  SERVE_REQUIRE(blocks <= 0x7FFFFFFF, AMAP_EOVERFLOW, "too many rows");
+  const dim3 grid((unsigned)blocks);
   return plan.pairs == AMAP_PAIRS_HALF ? launch(rope_kernel<DT, VEC, AMAP_PAIRS_HALF>, grid, kThreads, 0, stream, P)
                                        : launch(rope_kernel<DT, VEC, AMAP_PAIRS_ADJACENT>, grid, kThreads, 0, stream, P);
 }
@@ -280,7 +383,6 @@ extern "C" int amap_rope_rotate(const amap_rope_t *plan, const amap_rope_args *a
   if (a->rows == 0) return accept();
   const int es = dtype_bytes(a->dtype);
   Params P = {};
-  int64_t heads = 0;
   for (int k = 0; k < a->n_parts; ++k) {
     const amap_rope_part &s = a->part[k];
     SERVE_REQUIRE(s.x && s.y, AMAP_EINVAL, "part: null pointer");
@@ -288,8 +390,7 @@ extern "C" int amap_rope_rotate(const amap_rope_t *plan, const amap_rope_args *a
     SERVE_REQUIRE(aligned(s.x, es) && aligned(s.y, es), AMAP_EALIGN, "part: misaligned");
     SERVE_REQUIRE((a->rows == 1 || s.y_row != 0) && (s.heads == 1 || s.y_head != 0), AMAP_EINVAL, "part: rows of y lie on one another");
     P.part[k] = {static_cast<const char *>(s.x), static_cast<char *>(s.y), s.x_row, s.x_head, s.y_row, s.y_head, 0,
-                 (int32_t)heads, kRows, 1.0f};
-    heads += s.heads;
+                 s.heads, kRows, 1.0f, 0, 0, {}};
   }
   // an output laid over an input is a race, unless the part is turned in place; parts turned in place may interleave in
   // one buffer (q and k of a fused projection), whose byte ranges overlap without sharing an element
@@ -304,7 +405,6 @@ extern "C" int amap_rope_rotate(const amap_rope_t *plan, const amap_rope_args *a
     }
   }
   P.n_parts = a->n_parts;
-  P.heads = (int32_t)heads;
   P.rows = a->rows;
   P.positions = a->positions;
   P.position_axis = a->position_axis;
@@ -342,14 +442,14 @@ extern "C" int amap_rope_append(const amap_rope_t *plan, const amap_append_args 
                         !overlap(a->v, rows_span(a->rows, a->v_row, c.heads, a->v_head, plan->head_dim, es), a->q_out, ys),
                     AMAP_EINVAL, "q_out overlaps q, k or v");
     }
-    P.part[n++] = {static_cast<const char *>(a->q), static_cast<char *>(a->q_out), a->q_row, a->q_head, a->q_out_row, a->q_out_head, 0, 0, kRows, 1.0f};
+    P.part[n++] = {static_cast<const char *>(a->q), static_cast<char *>(a->q_out), a->q_row, a->q_head, a->q_out_row, a->q_out_head, 0, a->q_heads, kRows,
+                   1.0f, 0, 0, {}};
   }
-  P.part[n++] = {static_cast<const char *>(a->k), static_cast<char *>(c.k), a->k_row, a->k_head, c.k_page, c.k_head, c.k_token, a->q_heads,
-                 kCacheTurned, 1.0f / c.k_scale};
+  P.part[n++] = {static_cast<const char *>(a->k), static_cast<char *>(c.k), a->k_row, a->k_head, c.k_page, c.k_head, c.k_token, c.heads,
+                 kCacheTurned, 1.0f / c.k_scale, 0, 0, {}};
   P.part[n++] = {static_cast<const char *>(a->v), static_cast<char *>(c.v), a->v_row, a->v_head, c.v_page, c.v_head, c.v_token,
-                 a->q_heads + c.heads, kCacheCopied, 1.0f / c.v_scale};
+                 c.heads, kCacheCopied, 1.0f / c.v_scale, 0, 0, {}};
   P.n_parts = n;
-  P.heads = a->q_heads + 2 * c.heads;
   P.rows = a->rows;
   P.positions = a->positions;
   P.position_axis = a->position_axis;
@@ -357,7 +457,7 @@ extern "C" int amap_rope_append(const amap_rope_t *plan, const amap_append_args 
   P.wide_positions = a->position_bits == 64;
   P.sign = 1.0f;
   P.slots = a->slots;
-  P.page_size = c.page_size;
+  P.by_page = div_by(c.page_size);
   P.n_slots = c.n_pages * c.page_size;
   P.e4m3 = c.dtype == AMAP_E4M3;
   return run_typed(*plan, P, a->dtype, ces, cuda_stream);

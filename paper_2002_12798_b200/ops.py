@@ -13,8 +13,8 @@ it; tensors it makes belong to that stream.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
+import functools
 import math
 import struct
 from collections import namedtuple
@@ -78,22 +78,50 @@ def _require(ok, why):
         raise ValueError(why)
 
 
-def _current(stream, device):
-    """(stream object, context in which tensors are made for it)."""
-    if stream is None:
-        return torch.cuda.current_stream(device), contextlib.nullcontext()
-    return stream, torch.cuda.stream(stream)
+_raw_stream = torch._C._cuda_getCurrentRawStream  # by device number: a fortieth of what a Stream object costs
+_current_device = torch._C._cuda_getDevice
 
 
-def _ints(name, t, shape):
-    if t.dtype is not torch.int32 or not t.is_cuda or t.shape != shape or not t.is_contiguous():
-        raise ValueError("%s: a contiguous int32 CUDA tensor of shape %s" % (name, tuple(shape)))
+def _enqueues(call):
+    """Adds `stream=None` to a call that works on the current stream: it is made the current one for the call, so that
+    what the call allocates belongs to it, too."""
+
+    @functools.wraps(call)
+    def wrapped(*args, stream=None, **kw):
+        if stream is None:
+            return call(*args, **kw)
+        with torch.cuda.stream(stream):
+            return call(*args, **kw)
+
+    return wrapped
+
+
+def _stream_of(device):
+    """The current stream of device number `device`, which has to be the current device: kernels are launched there."""
+    if device != _current_device():
+        raise ValueError("the tensors are on %s, the current device is another (torch.cuda.device)"
+                         % ("cuda:%d" % device if device >= 0 else "the CPU"))
+    return _raw_stream(device)
+
+
+_INT32 = torch.int32
+
+
+def _ints(name, t, n, device):
+    """Address of n int32 numbers that lie side by side on device number `device`."""
+    if t.dtype is not _INT32 or t.get_device() != device or t.numel() != n or not t.is_contiguous():
+        raise ValueError("%s: %d contiguous int32 numbers on the device of the other tensors" % (name, n))
     return t.data_ptr()
 
 
 def _table(t):
-    if t.dtype is not torch.int32 or not t.is_cuda or t.dim() != 2 or t.stride(1) != 1:
-        raise ValueError("block_table: an int32 CUDA tensor [requests, pages] with contiguous rows")
+    """(address, rows, entries of a row, stride of a row) of a block table."""
+    if t.dtype is not _INT32 or not t.is_cuda or t.dim() != 2:
+        raise ValueError("block_table: an int32 CUDA tensor [requests, pages]")
+    (rows, entries), (stride, one) = t.shape, t.stride()
+    if one != 1 and entries > 1:
+        raise ValueError("block_table: rows are contiguous")
+    return t.data_ptr(), rows, entries, stride if rows > 1 else max(stride, entries)
 
 
 # ----------------------------------------------------------------------------------------------------------------------
@@ -102,7 +130,8 @@ def _table(t):
 PagesStep = namedtuple("PagesStep", "query_start slots positions requests seq_lens free_count status")
 
 
-def pages_extend(new_lens, seq_lens, block_table, free_pages, free_count, page_size, max_tokens, *, n_pages=None, out=None, stream=None):
+@_enqueues
+def pages_extend(new_lens, seq_lens, block_table, free_pages, free_count, page_size, max_tokens, *, n_pages=None, out=None):
     """Gives every request room for new_lens[r] more tokens (amap_pages_extend).
 
     new_lens, seq_lens: int32 [R]; block_table: int32 [R, pages], extended in place; free_pages: int32 stack of free
@@ -111,46 +140,50 @@ def pages_extend(new_lens, seq_lens, block_table, free_pages, free_count, page_s
     (-1, 0, -1 behind the last token); seq_lens [R] and free_count [1], to be used from now on in place of the inputs
     (which are unchanged); status [R] (0 granted, 1 too long, 2 no pages, 3 no room in the step).  `out`: a PagesStep
     to write to."""
-    _table(block_table)
-    n, row = block_table.shape
-    device = block_table.device
-    s, made = _current(stream, device)
+    table, n, row, stride = _table(block_table)
+    device = block_table.get_device()
+    raw = _stream_of(device)
+    sizes = (n + 1, max_tokens, max_tokens, max_tokens, n, 1, n)
     if out is None:
-        with made:
-            whole = torch.empty(3 * n + 2 + 3 * max_tokens, dtype=torch.int32, device=device)
-        out = PagesStep(*whole.split([n + 1, max_tokens, max_tokens, max_tokens, n, 1, n]))
+        whole = torch.empty(3 * n + 2 + 3 * max_tokens, dtype=_INT32, device=block_table.device)
+        out = PagesStep._make(whole.split_with_sizes(sizes))
+        start = whole.data_ptr()
+        slots = start + 4 * (n + 1)
+        positions = slots + 4 * max_tokens
+        requests = positions + 4 * max_tokens
+        seq_out = requests + 4 * max_tokens
+        to = (start, slots, positions, requests, seq_out, seq_out + 4 * n, seq_out + 4 * n + 4)
+    else:
+        to = tuple(_ints(name, t, m, device) for name, t, m in zip(PagesStep._fields, out, sizes))
     capacity = free_pages.numel()
-    one = (1,)
-    per_request, per_token = (n,), (max_tokens,)
     args = _EXTEND.pack(
-        n, row, page_size, capacity if n_pages is None else n_pages, capacity, max_tokens, block_table.stride(0),
-        _ints("new_lens", new_lens, per_request), _ints("seq_lens", seq_lens, per_request), block_table.data_ptr(),
-        _ints("free_pages", free_pages, (capacity,)), _ints("free_count", free_count, one),
-        _ints("query_start", out.query_start, (n + 1,)), _ints("slots", out.slots, per_token),
-        _ints("positions", out.positions, per_token), _ints("requests", out.requests, per_token),
-        _ints("seq_lens", out.seq_lens, per_request), _ints("free_count", out.free_count, one), _ints("status", out.status, per_request))
-    _check(_lib.amap_pages_extend(args, s.cuda_stream), "amap_pages_extend")
+        n, row, page_size, capacity if n_pages is None else n_pages, capacity, max_tokens, stride, _ints("new_lens", new_lens, n, device),
+        _ints("seq_lens", seq_lens, n, device), table, _ints("free_pages", free_pages, capacity, device),
+        _ints("free_count", free_count, 1, device), *to)
+    rc = _lib.amap_pages_extend(args, raw)
+    if rc:
+        _check(rc, "amap_pages_extend")
     return out
 
 
-def pages_release(done, seq_lens, block_table, free_pages, free_count, page_size, *, stream=None):
+@_enqueues
+def pages_release(done, seq_lens, block_table, free_pages, free_count, page_size):
     """Puts the pages of the requests with done[r] (bool or uint8 [R]) back on the stack free_pages, in place
     (amap_pages_release).  Returns (seq_lens, free_count) to be used from now on in place of the inputs."""
-    _table(block_table)
-    n, row = block_table.shape
-    device = block_table.device
-    _require(done.dtype in (torch.bool, torch.uint8) and done.is_cuda and done.shape == (n,) and done.is_contiguous(),
-             "done: a contiguous bool or uint8 CUDA tensor [requests]")
-    s, made = _current(stream, device)
-    with made:
-        whole = torch.empty(n + 1, dtype=torch.int32, device=device)
-    seq_out, count_out = whole.split([n, 1])
+    table, n, row, stride = _table(block_table)
+    device = block_table.get_device()
+    raw = _stream_of(device)
+    if done.dtype not in (torch.bool, torch.uint8) or done.get_device() != device or done.numel() != n or not done.is_contiguous():
+        raise ValueError("done: %d contiguous bool or uint8 values on the device of the other tensors" % n)
+    whole = torch.empty(n + 1, dtype=_INT32, device=block_table.device)
+    to = whole.data_ptr()
     capacity = free_pages.numel()
-    args = _RELEASE.pack(n, row, page_size, capacity, block_table.stride(0), done.data_ptr(), _ints("seq_lens", seq_lens, (n,)),
-                         block_table.data_ptr(), _ints("free_pages", free_pages, (capacity,)), _ints("free_count", free_count, (1,)),
-                         seq_out.data_ptr(), count_out.data_ptr())
-    _check(_lib.amap_pages_release(args, s.cuda_stream), "amap_pages_release")
-    return seq_out, count_out
+    args = _RELEASE.pack(n, row, page_size, capacity, stride, done.data_ptr(), _ints("seq_lens", seq_lens, n, device), table,
+                         _ints("free_pages", free_pages, capacity, device), _ints("free_count", free_count, 1, device), to, to + 4 * n)
+    rc = _lib.amap_pages_release(args, raw)
+    if rc:
+        _check(rc, "amap_pages_release")
+    return tuple(whole.split_with_sizes((n, 1)))
 
 
 # ----------------------------------------------------------------------------------------------------------------------
@@ -180,22 +213,25 @@ class PagedCache:
 # rotary positions
 # ----------------------------------------------------------------------------------------------------------------------
 def _heads(name, x, dim):
-    if not x.is_cuda or x.dim() != 3 or x.shape[2] != dim or x.stride(2) != 1:
+    """((tokens, heads, dim), (stride of a token, stride of a head, 1)) of a tensor of heads."""
+    shape, stride = x.shape, x.stride()
+    if not x.is_cuda or len(shape) != 3 or shape[2] != dim or (stride[2] != 1 and dim > 1):
         raise ValueError("%s: a CUDA tensor [tokens, heads, %d] whose heads are contiguous" % (name, dim))
+    return shape, stride
 
 
 class _Rotate(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, plan, positions, inverse, stream, *xs):
+    def forward(ctx, plan, positions, inverse, *xs):
         ctx.save_for_backward(positions)
         ctx.plan, ctx.inverse = plan, inverse
-        return tuple(plan._rotate(xs, positions, inverse, None, stream))
+        return tuple(plan._rotate(xs, positions, inverse, None))
 
     @staticmethod
     def backward(ctx, *grads):
         (positions,) = ctx.saved_tensors
         grads = [g if g.stride(2) == 1 else g.contiguous() for g in grads]
-        return (None, None, None, None) + tuple(ctx.plan._rotate(grads, positions, not ctx.inverse, None, None))
+        return (None, None, None) + tuple(ctx.plan._rotate(grads, positions, not ctx.inverse, None))
 
 
 class RopePlan:
@@ -230,77 +266,82 @@ class RopePlan:
             _lib.amap_rope_destroy(self._h)
             self._h = None
 
-    def _positions(self, positions, tokens):
+    def _positions(self, positions, tokens, device):
         """(pointer, stride of an axis, stride of a token, bits) of int32 / int64 positions [tokens] or [axes, tokens]."""
-        d = positions.dim()
-        if not positions.is_cuda or d not in (1, 2) or positions.shape[-1] != tokens or (d == 2 and positions.shape[0] < self.n_axes) \
-                or (d == 1 and self.n_axes > 1):
-            raise ValueError("positions: a CUDA tensor [%stokens] with one position per token" % ("axes, " if self.n_axes > 1 else ""))
-        bits = 32 if positions.dtype is torch.int32 else 64 if positions.dtype is torch.int64 else 0
-        _require(bits, "positions: int32 or int64")
-        return positions.data_ptr(), positions.stride(0) if d == 2 else 0, positions.stride(-1), bits
+        shape, stride = positions.shape, positions.stride()
+        d = len(shape)
+        if d not in (1, 2) or shape[-1] != tokens or (shape[0] if d == 2 else 1) < self.n_axes or positions.get_device() != device:
+            raise ValueError("positions: [%stokens] with one position per token, on the device of the other tensors"
+                             % ("axes, " if self.n_axes > 1 else ""))
+        bits = 32 if positions.dtype is _INT32 else 64 if positions.dtype is torch.int64 else 0
+        if not bits:
+            raise ValueError("positions: int32 or int64")
+        return positions.data_ptr(), stride[0] if d == 2 else 0, stride[-1], bits
 
-    def _rotate(self, xs, positions, inverse, outs, stream):
-        _require(1 <= len(xs) <= 4, "rotate takes 1 to 4 tensors")
+    def _rotate(self, xs, positions, inverse, outs):
+        n, dim = len(xs), self.head_dim
+        _require(1 <= n <= 4, "rotate takes 1 to 4 tensors")
         first = xs[0]
-        dtype = _DTYPES.get(first.dtype, 0)
-        s, made = _current(stream, first.device)
+        dtype, device, tokens = first.dtype, first.get_device(), first.shape[0]
+        raw = _stream_of(device)
         if outs is None:
-            with made:
-                outs = [torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in xs]
-        _require(len(outs) == len(xs), "outs: one per tensor")
-        parts = []
+            outs = [torch.empty_like(x) for x in xs]
+        _require(len(outs) == n, "outs: one per tensor")
+        parts = b""
         for x, y in zip(xs, outs):
-            _heads("x", x, self.head_dim)
-            _heads("out", y, self.head_dim)
-            _require(x.dtype is first.dtype and y.dtype is x.dtype and x.shape[0] == first.shape[0] and y.shape == x.shape
-                     and x.device == first.device, "rotate: tensors of one type and token count, each with an output like itself")
-            parts.append(_PART.pack(x.data_ptr(), y.data_ptr(), x.stride(0), x.stride(1), y.stride(0), y.stride(1), x.shape[1], 0))
-        tokens = first.shape[0]
-        p, axis, row, bits = self._positions(positions, tokens)
+            shape, xs_ = _heads("x", x, dim)
+            y_shape, ys_ = _heads("out", y, dim)
+            if x.dtype is not dtype or y.dtype is not dtype or shape[0] != tokens or y_shape != shape or x.get_device() != device or y.get_device() != device:
+                raise ValueError("rotate: tensors of one type, token count and device, each with an output like itself")
+            parts += _PART.pack(x.data_ptr(), y.data_ptr(), xs_[0], xs_[1], ys_[0], ys_[1], shape[1], 0)
+        at = self._positions(positions, tokens, device)
         if tokens == 0:
             return outs
-        args = _ROTATE.pack(len(parts), dtype, tokens, p, axis, row, bits, 1 if inverse else 0) + b"".join(parts)
-        args += bytes((4 - len(parts)) * _PART.size)
-        _check(_lib.amap_rope_rotate(self._h, args, s.cuda_stream), "amap_rope_rotate")
+        rc = _lib.amap_rope_rotate(self._h, _ROTATE.pack(n, _DTYPES.get(dtype, 0), tokens, *at, inverse) + parts + bytes((4 - n) * _PART.size), raw)
+        if rc:
+            _check(rc, "amap_rope_rotate")
         return outs
 
-    def rotate(self, xs, positions, *, inverse=False, outs=None, stream=None):
+    @_enqueues
+    def rotate(self, xs, positions, *, inverse=False, outs=None):
         """Turns up to four tensors [tokens, heads, head_dim] (q and k) by the same positions in one launch; returns
         the results in a list.  inverse=True turns back, which is the gradient; tensors that require one are
         differentiated through.  outs: tensors to write to (an x itself for in place)."""
-        if torch.is_grad_enabled() and any(x.requires_grad for x in xs):
-            _require(outs is None, "rotate: no outs where a gradient is required")
-            return list(_Rotate.apply(self, positions, inverse, stream, *xs))
-        return self._rotate(xs, positions, inverse, outs, stream)
+        if torch.is_grad_enabled():
+            for x in xs:
+                if x.requires_grad:
+                    _require(outs is None, "rotate: no outs where a gradient is required")
+                    return list(_Rotate.apply(self, positions, bool(inverse), *xs))
+        return self._rotate(xs, positions, bool(inverse), outs)
 
-    def append(self, q, k, v, positions, slots, cache, *, out=None, stream=None):
+    @_enqueues
+    def append(self, q, k, v, positions, slots, cache, *, out=None):
         """One step of a decoder layer before its attention (amap_rope_append): returns the rotated q [tokens, heads,
         head_dim] and writes the rotated k and the v [tokens, cache.heads, head_dim] to the slots (int32 [tokens], -1
         for none) of the cache.  Views of a fused projection are taken as they are.  Not differentiable."""
-        dim = self.head_dim
-        _heads("q", q, dim)
-        _heads("k", k, dim)
-        _heads("v", v, dim)
-        tokens = q.shape[0]
-        _require(k.shape == v.shape and k.shape[0] == tokens and k.shape[1] == cache.heads and k.dtype is q.dtype and v.dtype is q.dtype,
-                 "append: q, k and v of one type and token count, k and v with the cache's heads")
-        _require(q.device == cache.device, "append: the cache is on another device")
-        s, made = _current(stream, q.device)
+        dim, dtype, device = self.head_dim, q.dtype, q.get_device()
+        raw = _stream_of(device)
+        (tokens, heads, _), qs = _heads("q", q, dim)
+        k_shape, ks = _heads("k", k, dim)
+        v_shape, vs = _heads("v", v, dim)
+        if k_shape != v_shape or k_shape[0] != tokens or k_shape[1] != cache.heads or k.dtype is not dtype or v.dtype is not dtype:
+            raise ValueError("append: q, k and v of one type and token count, k and v with the cache's heads")
+        if not device == k.get_device() == v.get_device() == cache.device.index:
+            raise ValueError("append: q, k, v and the cache on one device")
         if out is None:
-            with made:
-                out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        else:
-            _heads("out", out, dim)
-            _require(out.shape == q.shape and out.dtype is q.dtype, "out: like q")
-        p, axis, row, bits = self._positions(positions, tokens)
-        at = _ints("slots", slots, (tokens,))
+            out = torch.empty_like(q)
+        out_shape, outs = _heads("out", out, dim)
+        if out.dtype is not dtype or out_shape != q.shape or out.get_device() != device:
+            raise ValueError("out: like q")
+        at = self._positions(positions, tokens, device)
+        where = _ints("slots", slots, tokens, device)
         if tokens == 0:
             return out
-        args = _APPEND.pack(tokens, _DTYPES.get(q.dtype, 0), q.shape[1], q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
-                            q.stride(0), q.stride(1), k.stride(0), k.stride(1), v.stride(0), v.stride(1), out.stride(0), out.stride(1),
-                            p, axis, row, bits, 0, at) + cache._args
-        _check(_lib.amap_rope_append(self._h, args, s.cuda_stream), "amap_rope_append")
+        args = _APPEND.pack(tokens, _DTYPES.get(dtype, 0), heads, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), qs[0], qs[1], ks[0],
+                            ks[1], vs[0], vs[1], outs[0], outs[1], *at, 0, where) + cache._args
+        rc = _lib.amap_rope_append(self._h, args, raw)
+        if rc:
+            _check(rc, "amap_rope_append")
         return out
 
 
@@ -319,13 +360,15 @@ class AttendPlan:
         self.max_requests, self.q_heads, self.kv_heads, self.head_dim = max_requests, q_heads, kv_heads, head_dim
         self.scale = float(scale) if scale is not None else 1.0 / math.sqrt(head_dim)
         self.window, self.softcap = int(window), float(softcap)
-        self.device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+        device = torch.device("cuda" if device is None else device)
+        self.device = device if device.index is not None else torch.device("cuda", torch.cuda.current_device())
         n, failed = c_int64(), c_int64()
         with torch.cuda.device(self.device):
             _check(_lib.amap_attend_workspace(max_requests, q_heads, kv_heads, head_dim, byref(n), byref(failed)), "amap_attend_workspace")
             self._bytes, self._failed = n.value, failed.value
             self._stream = torch.cuda.current_stream()
             self._workspace = torch.zeros(self._bytes, dtype=torch.uint8, device=self.device)
+            self._workspace_at = self._workspace.data_ptr()
         self._raw = self._stream.cuda_stream
 
     def failed(self):
@@ -334,40 +377,42 @@ class AttendPlan:
         torch.cuda.synchronize(self.device)
         return bool(self._workspace[self._failed : self._failed + 4].any())
 
-    def _order(self, s):
+    def _order(self):
         if torch.cuda.is_current_stream_capturing():
             return
+        s = torch.cuda.current_stream(self.device)
         s.wait_stream(self._stream)
         self._workspace.record_stream(s)
         self._stream, self._raw = s, s.cuda_stream
 
-    def attend(self, q, cache, block_table, seq_lens, *, out=None, return_lse=False, stream=None):
+    @_enqueues
+    def attend(self, q, cache, block_table, seq_lens, *, out=None, return_lse=False):
         """q: [requests, q_heads, head_dim]; row r is the newest token of the request in row r of block_table (int32
         [requests, pages]), which holds seq_lens[r] tokens (int32), the newest included.  Returns the output, shaped
         like q; with return_lse=True also the fp32 logarithm of the softmax's sum [requests, q_heads].  A request
         without tokens gets zeros and -inf."""
-        _heads("q", q, self.head_dim)
-        _table(block_table)
-        n = q.shape[0]
-        if n > self.max_requests or q.shape[1] != self.q_heads or cache.heads != self.kv_heads or cache.head_dim != self.head_dim:
-            raise ValueError("attend: at most %d requests of %d heads of %d, %d heads in the cache"
-                             % (self.max_requests, self.q_heads, self.head_dim, self.kv_heads))
-        _require(block_table.shape[0] == n, "block_table: a row per request")
-        _require(q.device == self.device and cache.device == self.device, "attend: plan, q and cache on one device")
-        s, made = _current(stream, self.device)
-        with made:
-            if out is None:
-                out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-            else:
-                _heads("out", out, self.head_dim)
-                _require(out.shape == q.shape and out.dtype is q.dtype, "out: like q")
-            lse = torch.empty((n, self.q_heads), dtype=torch.float32, device=q.device) if return_lse else None
-            if n:
-                if s.cuda_stream != self._raw:
-                    self._order(s)
-                args = _ATTEND.pack(n, self.q_heads, _DTYPES.get(q.dtype, 0), block_table.shape[1], q.data_ptr(), out.data_ptr(),
-                                    lse.data_ptr() if return_lse else 0, q.stride(0), q.stride(1), out.stride(0), out.stride(1), self.q_heads,
-                                    block_table.data_ptr(), block_table.stride(0), _ints("seq_lens", seq_lens, (n,)), self.scale, self.softcap,
-                                    self.window, 0, self._workspace.data_ptr(), self._bytes, cache._maps_at) + cache._args
-                _check(_lib.amap_attend(args, s.cuda_stream), "amap_attend")
+        dim, device = self.head_dim, self.device.index
+        raw = _stream_of(device)
+        (n, heads, _), qs = _heads("q", q, dim)
+        table, rows, entries, stride = _table(block_table)
+        if n > self.max_requests or heads != self.q_heads or cache.heads != self.kv_heads or cache.head_dim != dim or rows != n:
+            raise ValueError("attend: at most %d requests of %d heads of %d, %d heads in the cache, a table row per request"
+                             % (self.max_requests, self.q_heads, dim, self.kv_heads))
+        if not device == q.get_device() == cache.device.index == block_table.get_device():
+            raise ValueError("attend: plan, q, block_table and cache on one device")
+        if out is None:
+            out = torch.empty_like(q)
+        out_shape, outs = _heads("out", out, dim)
+        if out.dtype is not q.dtype or out_shape != q.shape or out.get_device() != device:
+            raise ValueError("out: like q")
+        lse = torch.empty((n, heads), dtype=torch.float32, device=self.device) if return_lse else None
+        if n:
+            if raw != self._raw:
+                self._order()
+            args = _ATTEND.pack(n, heads, _DTYPES.get(q.dtype, 0), entries, q.data_ptr(), out.data_ptr(), lse.data_ptr() if return_lse else 0, qs[0],
+                                qs[1], outs[0], outs[1], heads, table, stride, _ints("seq_lens", seq_lens, n, device), self.scale, self.softcap,
+                                self.window, 0, self._workspace_at, self._bytes, cache._maps_at) + cache._args
+            rc = _lib.amap_attend(args, raw)
+            if rc:
+                _check(rc, "amap_attend")
         return (out, lse) if return_lse else out
