@@ -11,10 +11,13 @@
 // mma.sync: a product of 16 tokens by 8 heads is far below the 128 rows a tcgen05 tile wants, and at 2 x 8 multiply-adds
 // per element the legacy rate is several times what HBM can feed.
 //
-// Split.  The tiles (64 tokens) of all requests and heads form one line, cut into equal pieces, one per resident block:
-// balanced to a tile whatever the lengths are, and computed by every block for itself from seq_lens (no plan, no host).
-// A block that has a part of an item writes it to the workspace; the last to arrive joins them in the order of the
-// tokens (beyond 32 parts in groups of 16 blocks first), so the result does not depend on who that is.
+// Split.  The tiles (64 tokens) of all requests form one line, cut into equal pieces: balanced to a tile whatever the
+// lengths are, and computed by every block for itself from seq_lens (no plan, no host).  A piece belongs to a team of
+// blocks, one per cache head (or a divisor of their number, where more teams then fill the device better): what they
+// read lies side by side in caches ordered by token, and they read it at about the same time.
+// An item is a request's tiles of one head.  A block that has a part of an item writes it to the workspace; the last to
+// arrive joins the parts in the order of the tokens (very many of them in groups first), so the result does not depend
+// on who that is.  The part a block begins with is, where it has few others, joined by the producer warp meanwhile.
 //
 // Pipeline.  A producer warp looks up pages, one tile ahead, and fills a ring of tiles; four warps take 16 tokens of each
 // tile.  Pages of 8 n tokens arrive by tensor copies (TMA) of whole 8 to 64 token boxes, others row by row with 16-byte
@@ -37,14 +40,17 @@ constexpr int kWarps = 4, kThreads = 32 * kWarps, kBlock = kThreads + 32;  // th
 constexpr int kRows = 16;               // tokens per warp and step
 constexpr int kTile = kRows * kWarps;   // tokens per tile
 constexpr int kMostBlocksPerSm = 3;
-constexpr int kGroup = 16;              // blocks whose parts are joined first, where an item has more than kDirect of them
-constexpr int kDirect = 32;
+constexpr int kGroup = 16;              // teams whose parts are joined first, where an item has more than kDirect of them
+constexpr int kDirect = 48;
+constexpr int kAside = 4;               // parts that the producer warp joins
+constexpr int kMostMembers = 32;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct Params {
   alignas(64) CUtensorMap k_map, v_map;  // [page][head][token][element], boxes of 128 bytes x 2^box_shift tokens
   amap_attend_args a;
   int32_t group, blocks_per_head, items_per_request;  // q heads per cache head; blocks of 8 NT of them; cache heads x blocks
+  int32_t members, rounds;                            // blocks of a team; items_per_request / members
   uint32_t div_mul, div_shift;                        // token / page_size (0 mul: a power of two)
   int32_t tensor_copies, box_shift;
   int32_t q_pairs, out_pairs;                         // two elements at a time are aligned
@@ -121,17 +127,19 @@ __device__ __forceinline__ float exp2_of(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// two e4m3 (the low 16 bits) as two fp16: exact
-__device__ __forceinline__ uint32_t halves_of(uint32_t two) {
-  uint32_t r;
-  asm("{ .reg .b16 t; cvt.u16.u32 t, %1; cvt.rn.f16x2.e4m3x2 %0, t; }" : "=r"(r) : "r"(two));
-  return r;
+// four e4m3 as four fp16: exact
+__device__ __forceinline__ void halves_of(uint32_t four, uint32_t *low, uint32_t *high) {
+  asm("{ .reg .b16 l, h; mov.b32 {l, h}, %2; cvt.rn.f16x2.e4m3x2 %0, l; cvt.rn.f16x2.e4m3x2 %1, h; }" : "=r"(*low), "=r"(*high) : "r"(four));
 }
 
 // P in two 16-bit terms, truncated and remainder: 15 bits and more of it enter P V (one 16-bit term would add an error
 // as large as the rounding of a 16-bit output).  The remainder is kept above zero, so that an infinity in V meets no
-// zero that P has not got.  fp16 terms carry P times 2^12, out of the way of fp16's smallest numbers.
-template <int CT> constexpr float kLift = CT == AMAP_FP16 ? 12.0f : 0.0f;
+// zero that P has not got.
+// P is taken relative to a maximum that is renewed only when a score passes it by more than kSlack (in powers of 2): the
+// true one moves in most of the early steps, and O would be rescaled each time.  fp16 terms carry P times 2^kLift, out of
+// the way of fp16's smallest numbers; 2^(kLift + kSlack) is below its largest.
+constexpr float kSlack = 8.0f;
+template <int CT> constexpr float kLift = CT == AMAP_FP16 ? 7.0f : 0.0f;
 template <int CT>
 __device__ __forceinline__ void two_terms(float p0, float p1, uint32_t *hi, uint32_t *lo) {
   if constexpr (CT == AMAP_BF16) {
@@ -147,10 +155,10 @@ __device__ __forceinline__ void two_terms(float p0, float p1, uint32_t *hi, uint
   }
 }
 
-// Walks the line of tiles: request by request, its heads (blocks of them) one after another, a head's tiles in order.
+// Walks the line of tiles: request by request, its heads round by round (a round is a team's), a round's tiles in order.
 // A request without tokens counts one tile, so that somebody writes its zeros.
 struct Cursor {
-  int r, h, n, low, t, left, n_next;
+  int r, h, n, low, t, left, n_next;  // h: the round
 
   static __device__ __forceinline__ int clamped(const Params &P, int len) {
     return (int)min((int64_t)max(len, 0), (int64_t)P.a.max_pages * P.a.cache.page_size);
@@ -178,7 +186,7 @@ struct Cursor {
       t += kTile;
       return;
     }
-    if (++h == P.items_per_request) {
+    if (++h == P.rounds) {
       h = 0;
       ++r;
       n = clamped(P, n_next);
@@ -202,18 +210,31 @@ __device__ __forceinline__ void write_pair(const Params &P, int64_t at, float x,
   }
 }
 
-// Joins n <= kDirect parts of an item, the i-th in slot slot_of(i), in this order: into the output, or (final: false) into
-// slot slot_of(0), which nobody else reads before this block has arrived for it.  All four warps.
-template <int CT, int DP, int HB, typename F>
+// Threads that work together: the four warps, or the producer's.
+struct Consumers {
+  static constexpr int kCount = kThreads;
+  static __device__ __forceinline__ int index() { return threadIdx.x; }
+  static __device__ __forceinline__ void sync() { sync_consumers(); }
+};
+struct Producer {
+  static constexpr int kCount = 32;
+  static __device__ __forceinline__ int index() { return threadIdx.x & 31; }
+  static __device__ __forceinline__ void sync() { __syncwarp(); }
+};
+
+// Joins n parts of an item, the i-th in slot slot_of(i), in this order: into the output, or (final: false) into slot
+// slot_of(0), which nobody else reads before this block has arrived for it.  ml: room for n x 8.
+template <typename T, int CT, int DP, int HB, typename F>
 __device__ void join(const Params &P, float2 (*ml)[8], int n, F slot_of, int heads, bool final, int r, int first_head) {
-  const int tid = threadIdx.x, D = P.a.cache.head_dim;
+  const int tid = T::index(), D = P.a.cache.head_dim;
   for (int h0 = 0; h0 < heads; h0 += 8) {
-    sync_consumers();
-    for (int i = tid >> 3; i < n; i += kThreads / 8) ml[i][tid & 7] = __ldcg(reinterpret_cast<const float2 *>(P.part_ml) + (int64_t)slot_of(i) * HB + h0 + (tid & 7));
-    sync_consumers();
+    T::sync();
+    for (int i = tid >> 3; i < n; i += T::kCount / 8) ml[i][tid & 7] = __ldcg(reinterpret_cast<const float2 *>(P.part_ml) + (int64_t)slot_of(i) * HB + h0 + (tid & 7));
+    T::sync();
     const int n_heads = min(8, heads - h0);
-    for (int item = tid; item < n_heads * (D / 4); item += kThreads) {
-      const int in = item / (D / 4), d = (item - in * (D / 4)) * 4;
+    for (int item = tid; item < n_heads * (DP / 4); item += T::kCount) {
+      const int in = item / (DP / 4), d = item % (DP / 4) * 4;
+      if (d >= D) continue;
       float top = -INFINITY;
       for (int i = 0; i < n; ++i) top = fmaxf(top, ml[i][in].x);
       float sum = 0.0f;
@@ -250,26 +271,29 @@ __device__ void join(const Params &P, float2 (*ml)[8], int n, F slot_of, int hea
   }
 }
 
-// whether this block is the last of n to arrive at the counter, which then is ready for the next call; all four warps
+// Whether this block is the last of n to arrive at the counter, which then is ready for the next call.  What the threads
+// have written before is seen by whoever arrives later: the barrier orders it before thread 0's fence, and that before
+// its arrival.
+template <typename T>
 __device__ __forceinline__ bool last_of(int32_t *counter, int n, int *told) {
-  __threadfence();
-  sync_consumers();
-  if (threadIdx.x == 0) {
+  T::sync();
+  if (T::index() == 0) {
+    __threadfence();
     const int before = atomicAdd(counter, 1);
     if (before == n - 1) *counter = 0;
+    __threadfence();
     *told = before == n - 1;
   }
-  sync_consumers();
-  const bool last = *told != 0;
-  if (last) __threadfence();
-  return last;
+  T::sync();
+  return *told != 0;
 }
 
 template <int S> struct Small {
   uint64_t full[S], empty[S];
   int64_t sums[kWarps], first_unit;
   uint32_t rows_there[S][2];  // rows of a stage whose page is there
-  int begin[3], told;
+  int begin[3], told, told_aside;
+  float2 aside[kAside][8];
 };
 
 template <int CT, bool FP8, int DP, int NT>
@@ -286,6 +310,7 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
   // all in one piece: static shared memory ahead of it would cost its 1024-byte alignment, and with it the second block
   Small<S> &small = *reinterpret_cast<Small<S> *>(joint + kWarps * 8 * kPitch);
   float2(*const joined)[8] = reinterpret_cast<float2(*)[8]>(joint);  // [kDirect][8], while `joint` is idle
+  static_assert(kDirect * 64 <= kWarps * 8 * kPitch * 4, "room for the parts of an item");
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
   const amap_cache &C = P.a.cache;
   const int D = C.head_dim;
@@ -306,7 +331,7 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
   const int R = P.a.n_requests, per = (R + kThreads - 1) / kThreads, r_first = warp < kWarps ? min(R, tid * per) : R, r_last = min(R, r_first + per);
   int64_t mine = 0;
   for (int r = r_first; r < r_last; ++r) mine += Cursor::tiles(P, Cursor::clamped(P, P.a.seq_lens[r]));
-  mine *= P.items_per_request;
+  mine *= P.rounds;
   int64_t upto = mine;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
@@ -321,14 +346,15 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
     if (w < warp) upto += small.sums[w];
     total += small.sums[w];
   }
-  const int64_t pieces = min((int64_t)gridDim.x, total);  // none of them empty
-  if (blockIdx.x >= pieces) return;
-  const int64_t u0 = total * blockIdx.x / pieces, u1 = total * (blockIdx.x + 1) / pieces;
+  const int team = blockIdx.x / P.members, member = blockIdx.x - team * P.members;
+  const int64_t pieces = min((int64_t)(gridDim.x / P.members), total);  // none of them empty
+  if (team >= pieces) return;
+  const int64_t u0 = total * team / pieces, u1 = total * (team + 1) / pieces;
   if (warp < kWarps && upto > u0 && upto - mine <= u0) {
     int64_t u = upto - mine;
     for (int r = r_first; r < r_last; ++r) {
       const int tiles = Cursor::tiles(P, Cursor::clamped(P, P.a.seq_lens[r]));
-      const int64_t units = (int64_t)tiles * P.items_per_request;
+      const int64_t units = (int64_t)tiles * P.rounds;
       if (u + units > u0) {
         const int in = (int)(u0 - u);
         small.begin[0] = r;
@@ -345,6 +371,12 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
   Cursor at;
   at.start(P, small.begin[0], small.begin[1], small.begin[2]);
   bool alive = true;
+  // the parts of the item that begins at first_unit: those of the teams `from` to `to`, of which the first began it in
+  // its second slot, the others go on with it in their first
+  const int64_t first_end = small.first_unit + Cursor::tiles(P, at.n);
+  auto team_of = [&](int64_t unit) { return (int)(((unit + 1) * pieces - 1) / total); };
+  const int first_from = team_of(small.first_unit), first_to = team_of(first_end - 1);
+  const bool aside = small.first_unit < u0 && first_end < u1 && first_to - first_from < kAside;
 
   if (warp == kWarps) {
     // ---- the producer ----
@@ -365,7 +397,7 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
       const int row = lane << P.box_shift;
       if (lane < boxes) look(row);
       for (int step = 0; step < steps; ++step) {
-        const int head = at.h / P.blocks_per_head;
+        const int head = (at.h * P.members + member) / P.blocks_per_head;
         const bool live = lane < boxes && there && (uint32_t)entry < (uint32_t)C.n_pages;
         const int page = live ? entry : C.n_pages;  // a page beyond the last: zeros, and nothing is read
         const int token = live ? offset : 0;
@@ -407,7 +439,7 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
       };
       look2();
       for (int step = 0; step < steps; ++step) {
-        const int head = at.h / P.blocks_per_head;
+        const int head = (at.h * P.members + member) / P.blocks_per_head;
         int64_t k_at[2], v_at[2];
         uint32_t mask[2];
 #pragma unroll
@@ -451,6 +483,14 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
         if (++stage == S) stage = 0, parity ^= 1;
       }
     }
+    if (aside && __all_sync(~0u, alive)) {
+      asm volatile("bar.sync 2, %0;" ::"n"(kBlock) : "memory");  // the four warps have written the first item's part
+      const int h = small.begin[1] * P.members + member, r = small.begin[0], in_group = h % P.blocks_per_head * HB;
+      auto slot_of = [&](int i) { return 2 * ((first_from + i) * P.members + member) + (i == 0 ? 1 : 0); };
+      if (last_of<Producer>(P.arrived + (int64_t)r * P.items_per_request + h, first_to - first_from + 1, &small.told_aside))
+        join<Producer, CT, DP, HB>(P, small.aside, first_to - first_from + 1, slot_of, min(HB, P.group - in_group), true, r,
+                                   h / P.blocks_per_head * P.group + in_group);
+    }
     return;
   }
 
@@ -458,7 +498,7 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
   uint32_t q[NT][MT][2];
   float to_log2[NT][2];  // scores times this are exponents of 2 (before a softcap: the score itself)
   const float unit = (P.a.softcap > 0 ? 1.0f : kLog2e) * P.a.scale * C.k_scale;
-  auto load_q = [&](int r, int h) {
+  auto ask_q = [&](int r, int h) {
     const int first = h / P.blocks_per_head * P.group, in_group = h % P.blocks_per_head * HB;
     const uint16_t *row = static_cast<const uint16_t *>(P.a.q) + (int64_t)r * P.a.q_row;
 #pragma unroll
@@ -479,6 +519,11 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
           q[nt][m][k] = v;
         }
       }
+    }
+  };
+  auto take_q = [&]() {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
       to_log2[nt][0] = to_log2[nt][1] = unit;
       if constexpr (FP8) {  // q as fp16 times a power of two that brings its largest element near 1
         float big = 0.0f;
@@ -525,7 +570,8 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
     }
   };
 
-  load_q(at.r, at.h);
+  ask_q(at.r, at.h * P.members + member);
+  take_q();
   clear();
   int64_t item_first = small.first_unit;
   // where a lane's row of the matrix loads lies in a tile, and its chunk 2j (+1 for the upper lanes) swizzled
@@ -555,16 +601,19 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // before the tensor copies that come to lie there
         __syncwarp();
       }
-      float s[NT][4];
+      float s[NT][4], s_odd[NT][4];  // two sums, so that a product need not wait for the one before it
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.0f;
+      for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) s[nt][c] = s_odd[nt][c] = 0.0f;
+      }
       if constexpr (!FP8) {
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
           uint32_t a[4];
           load4(k_at + lane_at[i & 3] + (i >> 2) * kBox, a);
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) mma<CT>(s[nt], a[0], a[1], a[2], a[3], q[nt][i][0], q[nt][i][1]);
+          for (int nt = 0; nt < NT; ++nt) mma<CT>(i & 1 ? s_odd[nt] : s[nt], a[0], a[1], a[2], a[3], q[nt][i][0], q[nt][i][1]);
         }
       } else {
 #pragma unroll
@@ -573,9 +622,11 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
           load4(k_at + lane_at[(i >> 1) & 3] + (i >> 3) * kBox, a);
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            const uint32_t a0 = halves_of(a[2 * j]), a2 = halves_of(a[2 * j] >> 16), a1 = halves_of(a[2 * j + 1]), a3 = halves_of(a[2 * j + 1] >> 16);
+            uint32_t a0, a1, a2, a3;
+            halves_of(a[2 * j], &a0, &a2);
+            halves_of(a[2 * j + 1], &a1, &a3);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) mma<CT>(s[nt], a0, a1, a2, a3, q[nt][i + j][0], q[nt][i + j][1]);
+            for (int nt = 0; nt < NT; ++nt) mma<CT>(j ? s_odd[nt] : s[nt], a0, a1, a2, a3, q[nt][i + j][0], q[nt][i + j][1]);
           }
         }
       }
@@ -585,16 +636,29 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
       for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          float x = s[nt][c] * to_log2[nt][c & 1];
-          if (P.a.softcap > 0) {
-            const float e = exp2_of(x * (2.0f * kLog2e / P.a.softcap));
-            x = (1.0f - __fdividef(2.0f, e + 1.0f)) * (P.a.softcap * kLog2e);  // tanh
-          }
-          s[nt][c] = (c < 2 ? live0 : live1) ? x : -INFINITY;
+          s[nt][c] = (s[nt][c] + s_odd[nt][c]) * to_log2[nt][c & 1];
         }
-        higher |= fmaxf(s[nt][0], s[nt][2]) > m[nt][0] || fmaxf(s[nt][1], s[nt][3]) > m[nt][1];
       }
-      if (__any_sync(~0u, higher)) {  // seldom after the first tiles
+      if (P.a.softcap > 0) {
+        const float in = 2.0f * kLog2e / P.a.softcap, out = P.a.softcap * kLog2e;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) s[nt][c] = (1.0f - __fdividef(2.0f, exp2_of(s[nt][c] * in) + 1.0f)) * out;  // tanh
+        }
+      }
+      if (rows != 0xFFFFu) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) s[nt][c] = (c < 2 ? live0 : live1) ? s[nt][c] : -INFINITY;
+        }
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        higher |= fmaxf(s[nt][0], s[nt][2]) > m[nt][0] + kSlack || fmaxf(s[nt][1], s[nt][3]) > m[nt][1] + kSlack;
+      }
+      if (__any_sync(~0u, higher)) {  // seldom after the first tile
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -618,13 +682,16 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
       uint32_t hi[NT][2], lo[NT][2];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
+        const float from[2] = {(m[nt][0] == -INFINITY ? 0.0f : m[nt][0]) - kLift<CT>, (m[nt][1] == -INFINITY ? 0.0f : m[nt][1]) - kLift<CT>};
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          const float top = m[nt][c & 1];
-          s[nt][c] = exp2_of(s[nt][c] - (top == -INFINITY ? 0.0f : top) + kLift<CT>);
+          s[nt][c] = exp2_of(s[nt][c] - from[c & 1]);
         }
         l[nt][0] += s[nt][0] + s[nt][2];
         l[nt][1] += s[nt][1] + s[nt][3];
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
           two_terms<CT>(s[nt][2 * k], s[nt][2 * k + 1], &hi[nt][k], &lo[nt][k]);
@@ -650,8 +717,9 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
           load4_transposed(v_at + lane_at[(i >> 1) & 3] + (i >> 3) * kBox, a);
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            const uint32_t x = __byte_perm(a[2 * j], 0, 0x3120), y = __byte_perm(a[2 * j + 1], 0, 0x3120);
-            const uint32_t a0 = halves_of(x), a1 = halves_of(x >> 16), a2 = halves_of(y), a3 = halves_of(y >> 16);
+            uint32_t a0, a1, a2, a3;
+            halves_of(__byte_perm(a[2 * j], 0, 0x3120), &a0, &a1);
+            halves_of(__byte_perm(a[2 * j + 1], 0, 0x3120), &a2, &a3);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
               mma<CT>(o[nt][i + j], a0, a1, a2, a3, hi[nt][0], hi[nt][1]);
@@ -670,12 +738,16 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
       continue;
     }
     // ---- the end of an item, or of this block's part of it: join the warps ----
-    const int r = at.r, h = at.h, tiles = Cursor::tiles(P, at.n);
+    const int r = at.r, h = at.h * P.members + member, tiles = Cursor::tiles(P, at.n);
+    if (step + 1 < steps) {
+      at.advance(P);
+      ask_q(at.r, at.h * P.members + member);  // the next item's, under way while this one is put away
+    }
     const int64_t item_end = item_first + tiles;
     const bool whole = item_first >= u0 && item_end <= u1;
     const int first = h / P.blocks_per_head * P.group, in_group = h % P.blocks_per_head * HB;
     const int heads = min(HB, P.group - in_group);
-    const int slot = 2 * blockIdx.x + (item_first >= u0 ? 1 : 0);  // a block has at most two parts: its first item's and its last's
+    const int slot = 2 * (team * P.members + member) + (item_first >= u0 ? 1 : 0);  // a block has at most two parts: its first item's and its last's
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       if (nt * 8 >= heads) break;
@@ -702,8 +774,9 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
       }
       sync_consumers();
       const int n_heads = min(8, heads - nt * 8);
-      for (int i = tid; i < n_heads * (D / 2); i += kThreads) {
-        const int in = i / (D / 2), d = (i - in * (D / 2)) * 2, head = nt * 8 + in;
+      for (int i = tid; i < n_heads * (DP / 2); i += kThreads) {
+        const int in = i / (DP / 2), d = i % (DP / 2) * 2, head = nt * 8 + in;
+        if (d >= D) continue;
         const float *ml = joint + in * kPitch + DP;
         const float top = fmaxf(fmaxf(ml[0], ml[8 * kPitch]), fmaxf(ml[16 * kPitch], ml[24 * kPitch]));
         float sum = 0.0f;
@@ -728,29 +801,32 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
       sync_consumers();
     }
     if (!whole) {  // uniform over the block
-      const int from = (int)(((item_first + 1) * pieces - 1) / total), to = (int)((item_end * pieces - 1) / total);
-      // part `from` began in its block (the second slot), the others before theirs (the first)
-      auto slot_of_block = [&](int b) { return 2 * b + (b == from ? 1 : 0); };
-      int32_t *item = P.arrived + (int64_t)r * P.items_per_request + h;
-      if (to - from < kDirect) {
-        if (last_of(item, to - from + 1, &small.told))
-          join<CT, DP, HB>(P, joined, to - from + 1, [&](int i) { return slot_of_block(from + i); }, heads, true, r, first + in_group);
+      if (aside && item_first < u0) {
+        asm volatile("bar.arrive 2, %0;" ::"n"(kBlock) : "memory");
       } else {
-        // of the items with parts in a group of blocks, one at most began before the group and one at most, among those
-        // with more than kDirect parts, begins in it: two counters
-        const int group = blockIdx.x / kGroup, b0 = max(from, group * kGroup), b1 = min(to, group * kGroup + kGroup - 1);
-        if (last_of(P.grouped + 2 * group + (from >= group * kGroup ? 1 : 0), b1 - b0 + 1, &small.told)) {
-          join<CT, DP, HB>(P, joined, b1 - b0 + 1, [&](int i) { return slot_of_block(b0 + i); }, heads, false, r, first + in_group);
-          const int g0 = from / kGroup, g1 = to / kGroup;
-          if (last_of(item, g1 - g0 + 1, &small.told))
-            join<CT, DP, HB>(P, joined, g1 - g0 + 1, [&](int i) { return slot_of_block(max(from, (g0 + i) * kGroup)); }, heads, true, r, first + in_group);
+        const int from = team_of(item_first), to = team_of(item_end - 1);
+        auto slot_of_team = [&](int b) { return 2 * (b * P.members + member) + (b == from ? 1 : 0); };
+        int32_t *item = P.arrived + (int64_t)r * P.items_per_request + h;
+        if (to - from < kDirect) {
+          if (last_of<Consumers>(item, to - from + 1, &small.told))
+            join<Consumers, CT, DP, HB>(P, joined, to - from + 1, [&](int i) { return slot_of_team(from + i); }, heads, true, r, first + in_group);
+        } else {
+          // of the items with parts in a group of teams, one at most began before the group and one at most, among those
+          // with more than kDirect parts, begins in it: two counters
+          const int group = team / kGroup, b0 = max(from, group * kGroup), b1 = min(to, group * kGroup + kGroup - 1);
+          if (last_of<Consumers>(P.grouped + 2 * (group * P.members + member) + (from >= group * kGroup ? 1 : 0), b1 - b0 + 1, &small.told)) {
+            join<Consumers, CT, DP, HB>(P, joined, b1 - b0 + 1, [&](int i) { return slot_of_team(b0 + i); }, heads, false, r, first + in_group);
+            const int g0 = from / kGroup, g1 = to / kGroup;
+            if (last_of<Consumers>(item, g1 - g0 + 1, &small.told))
+              join<Consumers, CT, DP, HB>(P, joined, g1 - g0 + 1, [&](int i) { return slot_of_team(max(from, (g0 + i) * kGroup)); }, heads, true, r,
+                                          first + in_group);
+          }
         }
       }
     }
     if (step + 1 < steps) {
-      at.advance(P);
       item_first = item_end;
-      load_q(at.r, at.h);
+      take_q();
       clear();
     }
   }
@@ -780,8 +856,12 @@ int run(Params &P, void *stream) {
     blocks = device_sms() * std::min(per_sm, kMostBlocksPerSm);
     known[dev].store(blocks, std::memory_order_relaxed);
   }
-  const int64_t most = (int64_t)P.a.n_requests * P.items_per_request * std::max<int64_t>(1, ((int64_t)P.a.max_pages * P.a.cache.page_size + kTile - 1) / kTile);
-  return launch(attend_kernel<CT, FP8, DP, NT>, dim3((unsigned)std::min<int64_t>(blocks, most)), kBlock, smem, stream, P);
+  // a team's blocks: the largest divisor of the items of a request that leaves no more than a fiftieth of the device idle
+  for (int members = 1; members <= std::min(P.items_per_request, kMostMembers); ++members)
+    if (P.items_per_request % members == 0 && blocks / members * members * 50 >= blocks * 49) P.members = members;
+  P.rounds = P.items_per_request / P.members;
+  const int64_t most = (int64_t)P.a.n_requests * P.rounds * std::max<int64_t>(1, ((int64_t)P.a.max_pages * P.a.cache.page_size + kTile - 1) / kTile);
+  return launch(attend_kernel<CT, FP8, DP, NT>, dim3((unsigned)(std::min<int64_t>(blocks / P.members, most) * P.members)), kBlock, smem, stream, P);
 }
 
 template <int CT, bool FP8, int DP>
@@ -832,7 +912,7 @@ Workspace workspace(int32_t n_requests, int32_t q_heads, int32_t kv_heads, int32
   w.ml = 2 * blocks * hb * dp * 4;
   w.failed = w.ml + 2 * blocks * hb * 8;
   w.grouped = w.failed + 16;
-  w.arrived = w.grouped + (blocks / kGroup + 1) * 2 * 4;
+  w.arrived = w.grouped + (blocks / kGroup + kMostMembers) * 2 * 4;
   w.bytes = (w.arrived + items * 4 + 255) / 256 * 256;
   return w;
 }
