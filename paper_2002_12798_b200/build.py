@@ -1,4 +1,5 @@
-"""Builds libamap.so (host algebra + sm_100a kernels) in-tree with nvcc."""
+"""Builds libamap.so (host algebra + sm_100a kernels) in-tree with nvcc, and _serve_torch.so, the Python entry of the
+serving operators, with g++ against PyTorch's headers."""
 from __future__ import annotations
 
 import os
@@ -10,6 +11,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libamap.so")
+TORCH_ENTRY = os.path.join(HERE, "_serve_torch.so")
 SOURCES = ["builder.cpp", "compose.cpp", "simplify.cpp", "plan_execute.cu", "consume.cu",
            "serve_common.cu", "serve_pages.cu", "serve_rope.cu", "serve_attend.cu"]
 
@@ -25,7 +27,7 @@ def _stale() -> bool:
     if not os.path.exists(LIB):
         return True
     t = os.path.getmtime(LIB)
-    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(INCLUDE, f) for f in os.listdir(INCLUDE)]
+    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f != "serve_torch.cpp"] + [os.path.join(INCLUDE, f) for f in os.listdir(INCLUDE)]
     return any(os.path.getmtime(d) > t for d in deps)
 
 
@@ -46,5 +48,30 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
     return LIB
 
 
+def build_torch_entry(force: bool = False) -> str:
+    """_serve_torch.so; libamap.so, which it calls, is built first and found beside it."""
+    lib = build_library()
+    src = os.path.join(CSRC, "serve_torch.cpp")
+    deps = [src, os.path.join(INCLUDE, "amap.h"), os.path.join(INCLUDE, "amap_serve.h")]
+    if not force and os.path.exists(TORCH_ENTRY) and all(os.path.getmtime(d) <= os.path.getmtime(TORCH_ENTRY) for d in deps):
+        return TORCH_ENTRY
+    import sysconfig
+
+    import torch
+
+    there = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(_nvcc()))
+    tmp = TORCH_ENTRY + ".tmp%d" % os.getpid()
+    cmd = [os.environ.get("CXX", "g++"), "-std=c++17", "-O2", "-shared", "-fPIC", "-fvisibility=hidden", "-Wall", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch.compiled_with_cxx11_abi()]
+    for d in [os.path.join(there, "include"), os.path.join(there, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"], os.path.join(cuda, "include")]:
+        cmd += ["-isystem", d]
+    cmd += ["-I", INCLUDE, src, "-o", tmp]
+    cmd += ["-L", os.path.join(there, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-L", HERE, "-l:" + os.path.basename(lib), "-Wl,-rpath,$ORIGIN"]
+    subprocess.check_call(cmd)
+    os.replace(tmp, TORCH_ENTRY)
+    return TORCH_ENTRY
+
+
 if __name__ == "__main__":
+    build_torch_entry(force="--force" in sys.argv)
     print(build_library(force="--force" in sys.argv, verbose="-v" in sys.argv))

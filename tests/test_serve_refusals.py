@@ -3,6 +3,7 @@ numbers that no call gets as far as using."""
 import ctypes
 import os
 import re
+import struct
 
 import pytest
 import torch
@@ -12,7 +13,19 @@ from paper_2002_12798_b200 import ops
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 OK, EINVAL, EOVERFLOW, EALIGN, EUNSUPPORTED = 0, -1, -6, -7, -9
-lib = ops._lib
+
+# the argument structs of amap_serve.h, with C's alignment
+EXTEND_ARGS, RELEASE_ARGS = struct.Struct("6iq12P"), struct.Struct("4iq7P")
+ROTATE_ARGS, PART_ARGS = struct.Struct("2iqP2q2i"), struct.Struct("2P4q2i")  # up to part[], and one of part[]
+APPEND_ARGS, ATTEND_ARGS = struct.Struct("q2i4P8qP2q2iP"), struct.Struct("4i3P5qPqP2f2iPqP")  # up to cache
+CACHE_ARGS, MAPS_ARGS = struct.Struct("2P6q4ii2f4x"), struct.Struct("32Q2i")
+
+lib = ctypes.CDLL(B.LIBRARY_PATH)
+lib.amap_serve_error.restype = ctypes.c_char_p
+for _name in ("amap_pages_extend", "amap_pages_release", "amap_cache_encode", "amap_attend"):
+    getattr(lib, _name).argtypes = [ctypes.c_char_p, ctypes.c_void_p]
+for _name in ("amap_rope_rotate", "amap_rope_append"):
+    getattr(lib, _name).argtypes = [ctypes.c_void_p, ctypes.c_char_p, ctypes.c_void_p]
 
 
 def test_library_exports_every_declared_symbol():
@@ -31,11 +44,13 @@ def test_packed_structs_are_as_long_as_the_header_says(tmp_path):
     cc = shutil.which("gcc")
     if not cc:
         pytest.skip("no C compiler")
-    sizes = {"amap_pages_extend_args": ops._EXTEND.size, "amap_pages_release_args": ops._RELEASE.size,
-             "amap_rope_args": ops._ROTATE.size + 4 * ops._PART.size, "amap_rope_part": ops._PART.size,
-             "amap_append_args": ops._APPEND.size + ops._CACHE.size, "amap_attend_args": ops._ATTEND.size + ops._CACHE.size,
-             "amap_cache": ops._CACHE.size, "amap_cache_maps": ops._MAPS.size}
+    sizes = {"amap_pages_extend_args": EXTEND_ARGS.size, "amap_pages_release_args": RELEASE_ARGS.size,
+             "amap_rope_args": ROTATE_ARGS.size + 4 * PART_ARGS.size, "amap_rope_part": PART_ARGS.size,
+             "amap_append_args": APPEND_ARGS.size + CACHE_ARGS.size, "amap_attend_args": ATTEND_ARGS.size + CACHE_ARGS.size,
+             "amap_cache": CACHE_ARGS.size, "amap_cache_maps": MAPS_ARGS.size}
     checks = "".join("_Static_assert(sizeof(%s) == %d, \"%s\");\n" % (n, s, n) for n, s in sizes.items())
+    assert sizes["amap_cache"] == ctypes.sizeof(ops._Cache) and sizes["amap_cache_maps"] == ctypes.sizeof(ops._Maps)
+    assert sizes["amap_attend_args"] == ctypes.sizeof(ops._Attend)
     src = tmp_path / "sizes.c"
     src.write_text('#include "amap_serve.h"\n' + checks + "int main(void) { return 0; }\n")  # the header is C, too
     subprocess.check_call([cc, "-std=c11", "-Wall", "-Werror", "-I", os.path.join(ROOT, "include"), "-c", str(src), "-o", str(tmp_path / "sizes.o")])
@@ -57,7 +72,7 @@ EXTEND = dict(n=4, row=8, page=16, pages=64, capacity=64, tokens=100, stride=8, 
     (dict(seq_out=0x20000), EINVAL, "overlaps"), (dict(count_out=0x50000), EINVAL, "overlaps"), (dict(slots=0x80004), EINVAL, "overlaps"),
 ])
 def test_extend(change, code, why):
-    refused(lib.amap_pages_extend(ops._EXTEND.pack(*{**EXTEND, **change}.values()), None), code, why)
+    refused(lib.amap_pages_extend(EXTEND_ARGS.pack(*{**EXTEND, **change}.values()), None), code, why)
 
 
 RELEASE = dict(n=4, row=8, page=16, capacity=64, stride=8, done=0x10001, seq=0x20000, table=0x30000, free=0x40000, count=0x50000,
@@ -69,7 +84,7 @@ RELEASE = dict(n=4, row=8, page=16, capacity=64, stride=8, done=0x10001, seq=0x2
     (dict(seq_out=0x20004), EINVAL, "overlaps"), (dict(free=0x30010), EINVAL, "overlaps"),
 ])
 def test_release(change, code, why):
-    refused(lib.amap_pages_release(ops._RELEASE.pack(*{**RELEASE, **change}.values()), None), code, why)
+    refused(lib.amap_pages_release(RELEASE_ARGS.pack(*{**RELEASE, **change}.values()), None), code, why)
 
 
 @pytest.mark.parametrize("args,why", [
@@ -90,9 +105,9 @@ def test_rope_plan_arguments(args):
 
 
 def rotate(plan, parts, n=None, dtype=1, rows=8, positions=0x100, axis=8, row=1, bits=32, inverse=0):
-    packed = [ops._PART.pack(*p) for p in parts]
-    head = ops._ROTATE.pack(len(parts) if n is None else n, dtype, rows, positions, axis, row, bits, inverse)
-    return lib.amap_rope_rotate(plan._h, head + b"".join(packed) + bytes((4 - len(parts)) * ops._PART.size), None)
+    packed = [PART_ARGS.pack(*p) for p in parts]
+    head = ROTATE_ARGS.pack(len(parts) if n is None else n, dtype, rows, positions, axis, row, bits, inverse)
+    return lib.amap_rope_rotate(plan._h, head + b"".join(packed) + bytes((4 - len(parts)) * PART_ARGS.size), None)
 
 
 def test_rotate():
@@ -111,7 +126,7 @@ def test_rotate():
     refused(rotate(plan, [(0x10000, 0x10002) + part[2:]]), EINVAL, "overlaps")
     refused(rotate(plan, [part, (0x20000, 0x40000) + part[2:]]), EINVAL, "overlaps")  # one part's output is another's input
     refused(rotate(plan, [(0x10000, 0x20000, 256, 64, 256, 0, 4, 0)]), EINVAL, "on one another")
-    refused(lib.amap_rope_rotate(None, bytes(ops._ROTATE.size + 4 * ops._PART.size), None), EINVAL, "null")
+    refused(lib.amap_rope_rotate(None, bytes(ROTATE_ARGS.size + 4 * PART_ARGS.size), None), EINVAL, "null")
     assert rotate(plan, [part], rows=0) == OK  # nothing to do, nothing enqueued
 
 
@@ -135,7 +150,7 @@ def split(change, base):
 def test_append(change, code, why):
     a, c = split(change, APPEND)
     plan = ops.RopePlan(64)
-    refused(lib.amap_rope_append(plan._h, ops._APPEND.pack(*a.values()) + ops._CACHE.pack(*c.values()), None), code, why)
+    refused(lib.amap_rope_append(plan._h, APPEND_ARGS.pack(*a.values()) + CACHE_ARGS.pack(*c.values()), None), code, why)
 
 
 ATTEND = dict(n=4, qh=8, dtype=1, max_pages=8, q=0x1000, out=0x11000, lse=0x21000, qr=512, qhs=64, outr=512, ouths=64, lser=8, table=0x31000, stride=8,
@@ -152,27 +167,30 @@ ATTEND = dict(n=4, qh=8, dtype=1, max_pages=8, q=0x1000, out=0x11000, lse=0x2100
 ])
 def test_attend(change, code, why):
     a, c = split(change, ATTEND)
-    refused(lib.amap_attend(ops._ATTEND.pack(*a.values()) + ops._CACHE.pack(*c.values()), None), code, why)
+    refused(lib.amap_attend(ATTEND_ARGS.pack(*a.values()) + CACHE_ARGS.pack(*c.values()), None), code, why)
 
 
 def test_cache_encode():
-    out = ctypes.create_string_buffer(ops._MAPS.size)
+    out = ctypes.create_string_buffer(MAPS_ARGS.size)
     for change, code, why in ((dict(c_v=0), EINVAL, "null"), (dict(c_dim=260), EUNSUPPORTED, "head size"), (dict(c_kh=65), EALIGN, "strides"), (dict(c_v=0x200002), EALIGN, "16 bytes")):
-        refused(lib.amap_cache_encode(ops._CACHE.pack(*split(change, {})[1].values()), out), code, why)
-    refused(lib.amap_cache_encode(ops._CACHE.pack(*CACHE.values()), None), EINVAL, "null")
+        refused(lib.amap_cache_encode(CACHE_ARGS.pack(*split(change, {})[1].values()), out), code, why)
+    refused(lib.amap_cache_encode(CACHE_ARGS.pack(*CACHE.values()), None), EINVAL, "null")
     # pages of 3 tokens have no maps; that is no refusal
-    assert lib.amap_cache_encode(ops._CACHE.pack(*split(dict(c_page=3), {})[1].values()), out) == OK
-    assert ops._MAPS.unpack(out.raw)[-1] == 0
+    assert lib.amap_cache_encode(CACHE_ARGS.pack(*split(dict(c_page=3), {})[1].values()), out) == OK
+    assert MAPS_ARGS.unpack(out.raw)[-1] == 0
 
 
 def test_python_checks_its_tensors():
+    """Tensors that are on no GPU, no tensors at all, and wrong numbers of them."""
     x = torch.zeros(4, 8, 64)
     i = torch.zeros(4, dtype=torch.int32)
-    with pytest.raises(ValueError):
-        ops.PagedCache(torch.zeros(2, 16, 4, 64), torch.zeros(2, 16, 4, 64))
-    with pytest.raises(ValueError):
-        ops.pages_release(torch.zeros(4, dtype=torch.bool), i, torch.zeros(4, 8, dtype=torch.int32), i, i[:1], 16)
-    with pytest.raises(ValueError):
-        ops.RopePlan(64).rotate([], i)
-    with pytest.raises(ValueError):
-        ops._heads("x", x, 64)  # not on a GPU
+    table = torch.zeros(4, 8, dtype=torch.int32)
+    plan = ops.RopePlan(64)
+    for call in (lambda: ops.PagedCache(torch.zeros(2, 16, 4, 64), torch.zeros(2, 16, 4, 64)),
+                 lambda: ops.pages_extend(i, i, table, i, i[:1], 16, 4),
+                 lambda: ops.pages_extend(i, i, None, i, i[:1], 16, 4),
+                 lambda: ops.pages_release(torch.zeros(4, dtype=torch.bool), i, table, i, i[:1], 16),
+                 lambda: plan.rotate([], i), lambda: plan.rotate([x], i), lambda: plan.rotate([x] * 5, i), lambda: plan.rotate(x, i),
+                 lambda: plan.rotate([None], i), lambda: plan.rotate([x], i, outs=[])):
+        with pytest.raises((ValueError, AttributeError)):
+            call()
