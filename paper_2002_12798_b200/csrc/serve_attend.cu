@@ -11,7 +11,7 @@
 // mma.sync: a product of 16 tokens by 8 heads is far below the 128 rows a tcgen05 tile wants, and at 2 x 8 multiply-adds
 // per element the legacy rate is several times what HBM can feed.
 //
-// Split.  The tiles (64 tokens) of all requests form one line, cut into equal pieces: balanced to a tile whatever the
+// Split.  The tiles (64 or 128 tokens) of all requests form one line, cut into equal pieces: balanced to a tile whatever the
 // lengths are, and computed by every block for itself from seq_lens (no plan, no host).  A piece belongs to a team of
 // blocks, one per cache head (or a divisor of their number, where more teams then fill the device better): what they
 // read lies side by side in caches ordered by token, and they read it at about the same time.
@@ -19,7 +19,7 @@
 // arrive joins the parts in the order of the tokens (very many of them in groups first), so the result does not depend
 // on who that is.  The part a block begins with is, where it has few others, joined by the producer warp meanwhile.
 //
-// Pipeline.  A producer warp looks up pages, one tile ahead, and fills a ring of tiles; four warps take 16 tokens of each
+// Pipeline.  A producer warp looks up pages, one tile ahead, and fills a ring of tiles; four warps take a quarter of each
 // tile.  Pages of 8 n tokens arrive by tensor copies (TMA) of whole 8 to 64 token boxes, others row by row with 16-byte
 // asynchronous copies; both lay 128-byte rows out with the same swizzle, chunk ^ (row mod 8), so that the matrix loads
 // meet every bank once.  Only the end of an item synchronises the four warps.
@@ -37,8 +37,9 @@ using namespace amap_serve;
 namespace {
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps, kBlock = kThreads + 32;  // the last warp is the producer
-constexpr int kRows = 16;               // tokens per warp and step
-constexpr int kTile = kRows * kWarps;   // tokens per tile
+// tokens per warp and step, in sixteens: two where a token's row is 128 bytes, so that a step moves 32 KB either way and two
+// independent products hide each other's latency (128 e4m3 requests: MEASURED_SUB)
+template <int ROW_BYTES> constexpr int kSixteens = ROW_BYTES == 128 ? 2 : 1;
 constexpr int kMostBlocksPerSm = 3;
 constexpr int kGroup = 16;              // teams whose parts are joined first, where an item has more than kDirect of them
 constexpr int kDirect = 48;
@@ -58,9 +59,9 @@ struct Params {
   int32_t *failed, *grouped, *arrived;
 };
 
-// stages of the ring: about 96 KB a block (two resident blocks then hold about 128 KB in flight per multiprocessor:
+// stages of the ring: 96 KB a block, or 192 with heads of 256 16-bit elements (two resident blocks then hold about 128 KB in flight per multiprocessor:
 // latency times bandwidth is about 50)
-template <int ROW_BYTES> constexpr int kStages = ROW_BYTES >= 256 ? 3 : 6;
+constexpr int kStages = 3;
 
 __device__ __forceinline__ uint32_t smem_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool live) {
@@ -155,8 +156,9 @@ __device__ __forceinline__ void two_terms(float p0, float p1, uint32_t *hi, uint
   }
 }
 
-// Walks the line of tiles: request by request, its heads round by round (a round is a team's), a round's tiles in order.
+// Walks the line of tiles of TILE tokens: request by request, its heads round by round (a round is a team's), a round's tiles in order.
 // A request without tokens counts one tile, so that somebody writes its zeros.
+template <int TILE>
 struct Cursor {
   int r, h, n, low, t, left, n_next;  // h: the round
 
@@ -165,11 +167,11 @@ struct Cursor {
   }
   static __device__ __forceinline__ int lowest(const Params &P, int n) { return P.a.window > 0 ? max(0, n - P.a.window) : 0; }
   static __device__ __forceinline__ int tiles(const Params &P, int n) {
-    return max(1, (n + kTile - 1) / kTile - lowest(P, n) / kTile);
+    return max(1, (n + TILE - 1) / TILE - lowest(P, n) / TILE);
   }
   __device__ __forceinline__ void enter(const Params &P) {
     low = lowest(P, n);
-    t = low & ~(kTile - 1);
+    t = low & ~(TILE - 1);
     left = tiles(P, n);
   }
   __device__ __forceinline__ void start(const Params &P, int r0, int h0, int tile) {
@@ -178,12 +180,12 @@ struct Cursor {
     n = clamped(P, P.a.seq_lens[r]);
     n_next = P.a.seq_lens[min(r + 1, P.a.n_requests - 1)];
     enter(P);
-    t += tile * kTile;
+    t += tile * TILE;
     left -= tile;
   }
   __device__ __forceinline__ void advance(const Params &P) {
     if (--left > 0) {
-      t += kTile;
+      t += TILE;
       return;
     }
     if (++h == P.rounds) {
@@ -288,27 +290,29 @@ __device__ __forceinline__ bool last_of(int32_t *counter, int n, int *told) {
   return *told != 0;
 }
 
-template <int S> struct Small {
+template <int S, int TILE> struct Small {
   uint64_t full[S], empty[S];
   int64_t sums[kWarps], first_unit;
-  uint32_t rows_there[S][2];  // rows of a stage whose page is there
+  uint32_t rows_there[S][TILE / 32];  // rows of a stage whose page is there
   int begin[3], told, told_aside;
   float2 aside[kAside][8];
 };
 
 template <int CT, bool FP8, int DP, int NT>
 __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_kernel(const __grid_constant__ Params P) {
-  constexpr int ES = FP8 ? 1 : 2, RB = DP * ES, NB = RB / 128, S = kStages<RB>;
+  constexpr int ES = FP8 ? 1 : 2, RB = DP * ES, NB = RB / 128, S = kStages;
+  constexpr int U = kSixteens<RB>, ROWS = 16 * U, TILE = ROWS * kWarps;  // tokens per warp and step, and per tile
   constexpr int MT = DP / 16;                  // 16-element steps of a head
   constexpr int HB = 8 * NT;                   // q heads of a block
-  constexpr int kBox = kTile * 128;            // bytes of 64 rows of 128
+  constexpr int kBox = TILE * 128;             // bytes of a tile's rows of 128
   constexpr int kStage = 2 * NB * kBox;        // K then V
   constexpr int kPitch = DP + 4;               // floats between heads in `joint`: the writes of a warp meet all banks once,
                                                // and a warp's (m, l) of a head has room behind its O
   extern __shared__ __align__(1024) char smem[];
   float *joint = reinterpret_cast<float *>(smem + S * kStage);  // [warps][8][kPitch]
   // all in one piece: static shared memory ahead of it would cost its 1024-byte alignment, and with it the second block
-  Small<S> &small = *reinterpret_cast<Small<S> *>(joint + kWarps * 8 * kPitch);
+  using Line = Cursor<TILE>;
+  Small<S, TILE> &small = *reinterpret_cast<Small<S, TILE> *>(joint + kWarps * 8 * kPitch);
   float2(*const joined)[8] = reinterpret_cast<float2(*)[8]>(joint);  // [kDirect][8], while `joint` is idle
   static_assert(kDirect * 64 <= kWarps * 8 * kPitch * 4, "room for the parts of an item");
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
@@ -330,7 +334,7 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
   // ---- where this block's piece of the line begins ----
   const int R = P.a.n_requests, per = (R + kThreads - 1) / kThreads, r_first = warp < kWarps ? min(R, tid * per) : R, r_last = min(R, r_first + per);
   int64_t mine = 0;
-  for (int r = r_first; r < r_last; ++r) mine += Cursor::tiles(P, Cursor::clamped(P, P.a.seq_lens[r]));
+  for (int r = r_first; r < r_last; ++r) mine += Line::tiles(P, Line::clamped(P, P.a.seq_lens[r]));
   mine *= P.rounds;
   int64_t upto = mine;
 #pragma unroll
@@ -353,7 +357,7 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
   if (warp < kWarps && upto > u0 && upto - mine <= u0) {
     int64_t u = upto - mine;
     for (int r = r_first; r < r_last; ++r) {
-      const int tiles = Cursor::tiles(P, Cursor::clamped(P, P.a.seq_lens[r]));
+      const int tiles = Line::tiles(P, Line::clamped(P, P.a.seq_lens[r]));
       const int64_t units = (int64_t)tiles * P.rounds;
       if (u + units > u0) {
         const int in = (int)(u0 - u);
@@ -368,19 +372,19 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
   }
   __syncthreads();
   const int steps = (int)(u1 - u0);
-  Cursor at;
+  Line at;
   at.start(P, small.begin[0], small.begin[1], small.begin[2]);
   bool alive = true;
   // the parts of the item that begins at first_unit: those of the teams `from` to `to`, of which the first began it in
   // its second slot, the others go on with it in their first
-  const int64_t first_end = small.first_unit + Cursor::tiles(P, at.n);
+  const int64_t first_end = small.first_unit + Line::tiles(P, at.n);
   auto team_of = [&](int64_t unit) { return (int)(((unit + 1) * pieces - 1) / total); };
   const int first_from = team_of(small.first_unit), first_to = team_of(first_end - 1);
   const bool aside = small.first_unit < u0 && first_end < u1 && first_to - first_from < kAside;
 
   if (warp == kWarps) {
     // ---- the producer ----
-    const int boxes = kTile >> P.box_shift;
+    const int boxes = TILE >> P.box_shift;
     int entry = -1, offset = 0, there = 0;
     auto look = [&](int row) {  // the page of a row of the tile at `at`, if any of the row's box takes part
       const int token = at.t + row;
@@ -401,8 +405,9 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
         const bool live = lane < boxes && there && (uint32_t)entry < (uint32_t)C.n_pages;
         const int page = live ? entry : C.n_pages;  // a page beyond the last: zeros, and nothing is read
         const int token = live ? offset : 0;
-        const uint32_t low_rows = __ballot_sync(~0u, __shfl_sync(~0u, live, lane >> P.box_shift));
-        const uint32_t high_rows = __ballot_sync(~0u, __shfl_sync(~0u, live, (lane + 32) >> P.box_shift));
+        uint32_t rows[TILE / 32];
+#pragma unroll
+        for (int k = 0; k < TILE / 32; ++k) rows[k] = __ballot_sync(~0u, __shfl_sync(~0u, live, (lane + 32 * k) >> P.box_shift));
         if (step + 1 < steps) {
           at.advance(P);
           there = 0;
@@ -412,8 +417,8 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
         if (!__all_sync(~0u, alive)) break;
         const uint32_t bar = smem_at(&small.full[stage]), to = smem_at(smem + stage * kStage) + row * 128;
         if (lane == 0) {
-          small.rows_there[stage][0] = low_rows;
-          small.rows_there[stage][1] = high_rows;
+#pragma unroll
+          for (int k = 0; k < TILE / 32; ++k) small.rows_there[stage][k] = rows[k];
           bar_arrive_bytes(bar, kStage);
         }
         __syncwarp();
@@ -427,23 +432,23 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
         if (++stage == S) stage = 0, parity ^= 1;
       }
     } else {
-      // a lane looks up two rows; the copies of a row are 8 lanes' 16 bytes of its 128
-      int entries[2], offsets[2];
-      bool theres[2];
-      auto look2 = [&]() {
+      // a lane looks up every 32nd row; the copies of a row are 8 lanes' 16 bytes of its 128
+      int entries[TILE / 32], offsets[TILE / 32];
+      bool theres[TILE / 32];
+      auto look_all = [&]() {
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
+        for (int k = 0; k < TILE / 32; ++k) {
           look(lane + 32 * k);
           entries[k] = entry, offsets[k] = offset, theres[k] = there;
         }
       };
-      look2();
+      look_all();
       for (int step = 0; step < steps; ++step) {
         const int head = (at.h * P.members + member) / P.blocks_per_head;
-        int64_t k_at[2], v_at[2];
-        uint32_t mask[2];
+        int64_t k_at[TILE / 32], v_at[TILE / 32];
+        uint32_t mask[TILE / 32];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
+        for (int k = 0; k < TILE / 32; ++k) {
           const bool live = theres[k] && (uint32_t)entries[k] < (uint32_t)C.n_pages;
           mask[k] = __ballot_sync(~0u, live);
           k_at[k] = live ? (int64_t)entries[k] * C.k_page + (int64_t)offsets[k] * C.k_token + (int64_t)head * C.k_head : 0;
@@ -451,13 +456,13 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
         }
         if (step + 1 < steps) {
           at.advance(P);
-          look2();
+          look_all();
         }
         bar_wait(smem_at(&small.empty[stage]), parity, P.failed, alive);
         if (!__all_sync(~0u, alive)) break;
         const uint32_t bar = smem_at(&small.full[stage]), to = smem_at(smem + stage * kStage);
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
+        for (int k = 0; k < TILE / 32; ++k) {
 #pragma unroll 2
           for (int i = 0; i < 8; ++i) {
             const int src = i * 4 + (lane >> 3), row = 32 * k + src;
@@ -476,8 +481,8 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
         }
         copies_arrive(bar);
         if (lane == 0) {
-          small.rows_there[stage][0] = mask[0];
-          small.rows_there[stage][1] = mask[1];
+#pragma unroll
+          for (int k = 0; k < TILE / 32; ++k) small.rows_there[stage][k] = mask[k];
           bar_arrive(bar);
         }
         if (++stage == S) stage = 0, parity ^= 1;
@@ -577,7 +582,7 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
   // where a lane's row of the matrix loads lies in a tile, and its chunk 2j (+1 for the upper lanes) swizzled
   uint32_t lane_at[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) lane_at[j] = (warp * kRows + (lane & 15)) * 128 + (((2 * j) ^ ((lane >> 4) ^ (lane & 7))) * 16);
+  for (int j = 0; j < 4; ++j) lane_at[j] = (warp * ROWS + (lane & 15)) * 128 + (((2 * j) ^ ((lane >> 4) ^ (lane & 7))) * 16);
   const uint32_t ring = smem_at(smem);
 
   int stage = 0;
@@ -585,85 +590,109 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
 #pragma unroll 1
   for (int step = 0; step < steps; ++step) {
     // tokens of mine that take part: a range of rows, without those of pages that are not there
-    const int row0 = at.t + warp * kRows, upper = min(max(at.n - row0, 0), kRows), lower = min(max(at.low - row0, 0), kRows);
-    uint32_t rows = ((1u << upper) - 1) & ~((1u << lower) - 1);
+    const int row0 = at.t + warp * ROWS, upper = min(max(at.n - row0, 0), ROWS), lower = min(max(at.low - row0, 0), ROWS);
+    constexpr uint32_t kAll = ~0u >> (32 - ROWS);
+    uint32_t rows = (upper ? kAll >> (ROWS - upper) : 0) & ~(lower ? kAll >> (ROWS - lower) : 0);
     bar_wait(smem_at(&small.full[stage]), parity, P.failed, alive);
     const uint32_t k_at = ring + stage * kStage, v_at = k_at + NB * kBox;
-    rows &= small.rows_there[stage][warp >> 1] >> ((warp & 1) * 16);
+    rows &= small.rows_there[stage][warp * ROWS / 32] >> (warp * ROWS % 32);
     if (rows) {
-      if (rows != 0xFFFFu) {
+      if (rows != kAll) {
         // P is zero in the other rows, but what lies there may be anything: zeros to V
-        for (int i = lane; i < kRows * 8 * NB; i += 32) {
-          const int row = (i >> 3) & (kRows - 1);
+        for (int i = lane; i < ROWS * 8 * NB; i += 32) {
+          const int row = (i >> 3) & (ROWS - 1);
           if (!((rows >> row) & 1))
-            asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(v_at + (i / (kRows * 8)) * kBox + (warp * kRows + row) * 128 + (i & 7) * 16), "r"(0) : "memory");
+            asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(v_at + (i / (ROWS * 8)) * kBox + (warp * ROWS + row) * 128 + (i & 7) * 16), "r"(0) : "memory");
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // before the tensor copies that come to lie there
         __syncwarp();
       }
-      float s[NT][4], s_odd[NT][4];  // two sums, so that a product need not wait for the one before it
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-        for (int c = 0; c < 4; ++c) s[nt][c] = s_odd[nt][c] = 0.0f;
-      }
-      if constexpr (!FP8) {
-#pragma unroll
-        for (int i = 0; i < MT; ++i) {
-          uint32_t a[4];
-          load4(k_at + lane_at[i & 3] + (i >> 2) * kBox, a);
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) mma<CT>(i & 1 ? s_odd[nt] : s[nt], a[0], a[1], a[2], a[3], q[nt][i][0], q[nt][i][1]);
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < MT; i += 2) {
-          uint32_t a[4];
-          load4(k_at + lane_at[(i >> 1) & 3] + (i >> 3) * kBox, a);
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            uint32_t a0, a1, a2, a3;
-            halves_of(a[2 * j], &a0, &a2);
-            halves_of(a[2 * j + 1], &a1, &a3);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) mma<CT>(j ? s_odd[nt] : s[nt], a0, a1, a2, a3, q[nt][i + j][0], q[nt][i + j][1]);
-          }
-        }
-      }
-      const bool live0 = (rows >> g) & 1, live1 = (rows >> (g + 8)) & 1;
-      bool higher = false;
+      // S^T, sixteen tokens by eight heads each, in two sums where there is but one sixteen: a product then need not wait
+      // for the one before it
+      constexpr int CHAINS = U == 1 ? 2 : 1;
+      float s[U][NT][4], other[CHAINS == 2 ? NT : 1][4];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          s[nt][c] = (s[nt][c] + s_odd[nt][c]) * to_log2[nt][c & 1];
+#pragma unroll
+          for (int u = 0; u < U; ++u) s[u][nt][c] = 0.0f;
+          if constexpr (CHAINS == 2) other[nt][c] = 0.0f;
+        }
+      }
+      if constexpr (!FP8) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            uint32_t a[4];
+            load4(k_at + lane_at[i & 3] + u * 2048 + (i >> 2) * kBox, a);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) mma<CT>(CHAINS == 2 && (i & 1) ? other[nt] : s[u][nt], a[0], a[1], a[2], a[3], q[nt][i][0], q[nt][i][1]);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < MT; i += 2) {
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            uint32_t a[4];
+            load4(k_at + lane_at[(i >> 1) & 3] + u * 2048 + (i >> 3) * kBox, a);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              uint32_t a0, a1, a2, a3;
+              halves_of(a[2 * j], &a0, &a2);
+              halves_of(a[2 * j + 1], &a1, &a3);
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) mma<CT>(CHAINS == 2 && j ? other[nt] : s[u][nt], a0, a1, a2, a3, q[nt][i + j][0], q[nt][i + j][1]);
+            }
+          }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) s[u][nt][c] = (CHAINS == 2 ? s[u][nt][c] + other[nt][c] : s[u][nt][c]) * to_log2[nt][c & 1];
         }
       }
       if (P.a.softcap > 0) {
         const float in = 2.0f * kLog2e / P.a.softcap, out = P.a.softcap * kLog2e;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
+        for (int u = 0; u < U; ++u) {
 #pragma unroll
-          for (int c = 0; c < 4; ++c) s[nt][c] = (1.0f - __fdividef(2.0f, exp2_of(s[nt][c] * in) + 1.0f)) * out;  // tanh
+          for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) s[u][nt][c] = (1.0f - __fdividef(2.0f, exp2_of(s[u][nt][c] * in) + 1.0f)) * out;  // tanh
+          }
         }
       }
-      if (rows != 0xFFFFu) {
+      if (rows != kAll) {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
+        for (int u = 0; u < U; ++u) {
+          const bool live0 = (rows >> (u * 16 + g)) & 1, live1 = (rows >> (u * 16 + g + 8)) & 1;
 #pragma unroll
-          for (int c = 0; c < 4; ++c) s[nt][c] = (c < 2 ? live0 : live1) ? s[nt][c] : -INFINITY;
+          for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) s[u][nt][c] = (c < 2 ? live0 : live1) ? s[u][nt][c] : -INFINITY;
+          }
         }
       }
+      auto highest = [&](int nt, int c) {
+        float top = fmaxf(s[0][nt][c], s[0][nt][c + 2]);
+        if constexpr (U == 2) top = fmaxf(top, fmaxf(s[U - 1][nt][c], s[U - 1][nt][c + 2]));
+        return top;
+      };
+      bool higher = false;
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        higher |= fmaxf(s[nt][0], s[nt][2]) > m[nt][0] + kSlack || fmaxf(s[nt][1], s[nt][3]) > m[nt][1] + kSlack;
-      }
+      for (int nt = 0; nt < NT; ++nt) higher |= highest(nt, 0) > m[nt][0] + kSlack || highest(nt, 1) > m[nt][1] + kSlack;
       if (__any_sync(~0u, higher)) {  // seldom after the first tile
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            float top = fmaxf(s[nt][c], s[nt][c + 2]);
+            float top = highest(nt, c);
             top = fmaxf(top, __shfl_xor_sync(~0u, top, 4));
             top = fmaxf(top, __shfl_xor_sync(~0u, top, 8));
             top = fmaxf(top, __shfl_xor_sync(~0u, top, 16));
@@ -679,51 +708,55 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
           }
         }
       }
-      uint32_t hi[NT][2], lo[NT][2];
+      uint32_t hi[U][NT][2], lo[U][NT][2];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         const float from[2] = {(m[nt][0] == -INFINITY ? 0.0f : m[nt][0]) - kLift<CT>, (m[nt][1] == -INFINITY ? 0.0f : m[nt][1]) - kLift<CT>};
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          s[nt][c] = exp2_of(s[nt][c] - from[c & 1]);
-        }
-        l[nt][0] += s[nt][0] + s[nt][2];
-        l[nt][1] += s[nt][1] + s[nt][3];
-      }
+        for (int u = 0; u < U; ++u) {
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
+          for (int c = 0; c < 4; ++c) s[u][nt][c] = exp2_of(s[u][nt][c] - from[c & 1]);
+          l[nt][0] += s[u][nt][0] + s[u][nt][2];
+          l[nt][1] += s[u][nt][1] + s[u][nt][3];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          two_terms<CT>(s[nt][2 * k], s[nt][2 * k + 1], &hi[nt][k], &lo[nt][k]);
-          hi[nt][k] = transposed(hi[nt][k]);
-          lo[nt][k] = transposed(lo[nt][k]);
+          for (int k = 0; k < 2; ++k) {
+            two_terms<CT>(s[u][nt][2 * k], s[u][nt][2 * k + 1], &hi[u][nt][k], &lo[u][nt][k]);
+            hi[u][nt][k] = transposed(hi[u][nt][k]);
+            lo[u][nt][k] = transposed(lo[u][nt][k]);
+          }
         }
       }
       if constexpr (!FP8) {
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-          uint32_t a[4];
-          load4_transposed(v_at + lane_at[i & 3] + (i >> 2) * kBox, a);
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            mma<CT>(o[nt][i], a[0], a[2], a[1], a[3], hi[nt][0], hi[nt][1]);
-            mma<CT>(o[nt][i], a[0], a[2], a[1], a[3], lo[nt][0], lo[nt][1]);
+          for (int u = 0; u < U; ++u) {
+            uint32_t a[4];
+            load4_transposed(v_at + lane_at[i & 3] + u * 2048 + (i >> 2) * kBox, a);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              mma<CT>(o[nt][i], a[0], a[2], a[1], a[3], hi[u][nt][0], hi[u][nt][1]);
+              mma<CT>(o[nt][i], a[0], a[2], a[1], a[3], lo[u][nt][0], lo[u][nt][1]);
+            }
           }
         }
       } else {  // rows g and g + 8 of the product are elements 2g and 2g + 1
 #pragma unroll
         for (int i = 0; i < MT; i += 2) {
-          uint32_t a[4];
-          load4_transposed(v_at + lane_at[(i >> 1) & 3] + (i >> 3) * kBox, a);
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            uint32_t a0, a1, a2, a3;
-            halves_of(__byte_perm(a[2 * j], 0, 0x3120), &a0, &a1);
-            halves_of(__byte_perm(a[2 * j + 1], 0, 0x3120), &a2, &a3);
+          for (int u = 0; u < U; ++u) {
+            uint32_t a[4];
+            load4_transposed(v_at + lane_at[(i >> 1) & 3] + u * 2048 + (i >> 3) * kBox, a);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              mma<CT>(o[nt][i + j], a0, a1, a2, a3, hi[nt][0], hi[nt][1]);
-              mma<CT>(o[nt][i + j], a0, a1, a2, a3, lo[nt][0], lo[nt][1]);
+            for (int j = 0; j < 2; ++j) {
+              uint32_t a0, a1, a2, a3;
+              halves_of(__byte_perm(a[2 * j], 0, 0x3120), &a0, &a1);
+              halves_of(__byte_perm(a[2 * j + 1], 0, 0x3120), &a2, &a3);
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) {
+                mma<CT>(o[nt][i + j], a0, a1, a2, a3, hi[u][nt][0], hi[u][nt][1]);
+                mma<CT>(o[nt][i + j], a0, a1, a2, a3, lo[u][nt][0], lo[u][nt][1]);
+              }
             }
           }
         }
@@ -738,7 +771,7 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
       continue;
     }
     // ---- the end of an item, or of this block's part of it: join the warps ----
-    const int r = at.r, h = at.h * P.members + member, tiles = Cursor::tiles(P, at.n);
+    const int r = at.r, h = at.h * P.members + member, tiles = Line::tiles(P, at.n);
     if (step + 1 < steps) {
       at.advance(P);
       ask_q(at.r, at.h * P.members + member);  // the next item's, under way while this one is put away
@@ -835,7 +868,8 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
 template <int CT, bool FP8, int DP, int NT>
 int run(Params &P, void *stream) {
   constexpr int RB = DP * (FP8 ? 1 : 2);
-  constexpr size_t smem = (size_t)kStages<RB> * 2 * kTile * RB + sizeof(float) * kWarps * 8 * (DP + 4) + sizeof(Small<kStages<RB>>);
+  constexpr int TILE = 16 * kSixteens<RB> * kWarps;
+  constexpr size_t smem = (size_t)kStages * 2 * TILE * RB + sizeof(float) * kWarps * 8 * (DP + 4) + sizeof(Small<kStages, TILE>);
   // the block's shared memory is asked for, and how many blocks a multiprocessor then holds, once per device
   static std::atomic<int> known[64];
   int dev = 0;
@@ -860,7 +894,7 @@ int run(Params &P, void *stream) {
   for (int members = 1; members <= std::min(P.items_per_request, kMostMembers); ++members)
     if (P.items_per_request % members == 0 && blocks / members * members * 50 >= blocks * 49) P.members = members;
   P.rounds = P.items_per_request / P.members;
-  const int64_t most = (int64_t)P.a.n_requests * P.rounds * std::max<int64_t>(1, ((int64_t)P.a.max_pages * P.a.cache.page_size + kTile - 1) / kTile);
+  const int64_t most = (int64_t)P.a.n_requests * P.rounds * std::max<int64_t>(1, ((int64_t)P.a.max_pages * P.a.cache.page_size + TILE - 1) / TILE);
   return launch(attend_kernel<CT, FP8, DP, NT>, dim3((unsigned)(std::min<int64_t>(blocks / P.members, most) * P.members)), kBlock, smem, stream, P);
 }
 
