@@ -41,8 +41,8 @@ constexpr int kWarps = 4, kThreads = 32 * kWarps, kBlock = kThreads + 32;  // th
 // independent products hide each other's latency (128 e4m3 requests: MEASURED_SUB)
 template <int ROW_BYTES> constexpr int kSixteens = ROW_BYTES == 128 ? 2 : 1;
 constexpr int kMostBlocksPerSm = 3;
-constexpr int kGroup = 16;              // teams whose parts are joined first, where an item has more than kDirect of them
-constexpr int kDirect = 48;
+constexpr int kGroup = 8;               // teams whose parts are joined first, where an item has more than kDirect of them
+constexpr int kDirect = 12;
 constexpr int kAside = 4;               // parts that the producer warp joins
 constexpr int kMostMembers = 32;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -156,11 +156,16 @@ __device__ __forceinline__ void two_terms(float p0, float p1, uint32_t *hi, uint
   }
 }
 
-// Walks the line of tiles of TILE tokens: request by request, its heads round by round (a round is a team's), a round's tiles in order.
-// A request without tokens counts one tile, so that somebody writes its zeros.
+// The line of tiles of TILE tokens: request by request, its heads round by round (a round is a team's), a round's tiles in
+// order.  A request without tokens counts one tile, so that somebody writes its zeros.  Every item (a round of a request)
+// is longer by kEntry places, for what it costs to put the item before it away and to take it up; its tiles are the
+// places behind those.
+constexpr int kEntry = 2;
+
 template <int TILE>
 struct Cursor {
   int r, h, n, low, t, left, n_next;  // h: the round
+  int rest;                           // places from the tile at hand to the end of the piece
 
   static __device__ __forceinline__ int clamped(const Params &P, int len) {
     return (int)min((int64_t)max(len, 0), (int64_t)P.a.max_pages * P.a.cache.page_size);
@@ -174,7 +179,7 @@ struct Cursor {
     t = low & ~(TILE - 1);
     left = tiles(P, n);
   }
-  __device__ __forceinline__ void start(const Params &P, int r0, int h0, int tile) {
+  __device__ __forceinline__ void start(const Params &P, int r0, int h0, int tile, int64_t first_place, int64_t end) {
     r = r0;
     h = h0;
     n = clamped(P, P.a.seq_lens[r]);
@@ -182,8 +187,12 @@ struct Cursor {
     enter(P);
     t += tile * TILE;
     left -= tile;
+    rest = (int)(end - first_place) - tile;
   }
+  __device__ __forceinline__ int stride() const { return left > 1 ? 1 : 1 + kEntry; }
+  __device__ __forceinline__ bool more() const { return rest > stride(); }
   __device__ __forceinline__ void advance(const Params &P) {
+    rest -= stride();
     if (--left > 0) {
       t += TILE;
       return;
@@ -230,22 +239,26 @@ template <typename T, int CT, int DP, int HB, typename F>
 __device__ void join(const Params &P, float2 (*ml)[8], int n, F slot_of, int heads, bool final, int r, int first_head) {
   const int tid = T::index(), D = P.a.cache.head_dim;
   for (int h0 = 0; h0 < heads; h0 += 8) {
+    const int items = min(8, heads - h0) * (DP / 4);
+    float4 v[8];
+    auto ask = [&](int item, int i0) {
+      const float4 *part = reinterpret_cast<const float4 *>(P.part_o + (int64_t)(h0 + item / (DP / 4)) * DP) + item % (DP / 4);
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        v[j] = item < items && i0 + j < n ? __ldcg(part + (int64_t)slot_of(i0 + j) * (HB * DP / 4)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    };
+    ask(tid, 0);  // under way while the parts' (m, l) are shared out
     T::sync();
     for (int i = tid >> 3; i < n; i += T::kCount / 8) ml[i][tid & 7] = __ldcg(reinterpret_cast<const float2 *>(P.part_ml) + (int64_t)slot_of(i) * HB + h0 + (tid & 7));
     T::sync();
-    const int n_heads = min(8, heads - h0);
-    for (int item = tid; item < n_heads * (DP / 4); item += T::kCount) {
+    for (int item = tid; item < items; item += T::kCount) {
       const int in = item / (DP / 4), d = item % (DP / 4) * 4;
-      if (d >= D) continue;
       float top = -INFINITY;
       for (int i = 0; i < n; ++i) top = fmaxf(top, ml[i][in].x);
       float sum = 0.0f;
       float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-      const float4 *part = reinterpret_cast<const float4 *>(P.part_o + (int64_t)(h0 + in) * DP + d);
       for (int i0 = 0; i0 < n; i0 += 8) {
-        float4 v[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = i0 + j < n ? __ldcg(part + (int64_t)slot_of(i0 + j) * (HB * DP / 4)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (item != tid || i0) ask(item, i0);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           if (i0 + j >= n) break;
@@ -258,6 +271,7 @@ __device__ void join(const Params &P, float2 (*ml)[8], int n, F slot_of, int hea
           y.w += v[j].w * f;
         }
       }
+      if (d >= D) continue;
       if (final) {
         const float f = sum == 0.0f ? 0.0f : P.a.cache.v_scale / sum;
         const int64_t to = (int64_t)r * P.a.out_row + (int64_t)(first_head + h0 + in) * P.a.out_head + d;
@@ -274,16 +288,15 @@ __device__ void join(const Params &P, float2 (*ml)[8], int n, F slot_of, int hea
 }
 
 // Whether this block is the last of n to arrive at the counter, which then is ready for the next call.  What the threads
-// have written before is seen by whoever arrives later: the barrier orders it before thread 0's fence, and that before
-// its arrival.
+// have written before is seen by whoever arrives later: the barrier orders it before thread 0's arrival, which releases
+// it and acquires what the others have released.
 template <typename T>
 __device__ __forceinline__ bool last_of(int32_t *counter, int n, int *told) {
   T::sync();
   if (T::index() == 0) {
-    __threadfence();
-    const int before = atomicAdd(counter, 1);
+    int before;
+    asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(counter) : "memory");
     if (before == n - 1) *counter = 0;
-    __threadfence();
     *told = before == n - 1;
   }
   T::sync();
@@ -292,7 +305,7 @@ __device__ __forceinline__ bool last_of(int32_t *counter, int n, int *told) {
 
 template <int S, int TILE> struct Small {
   uint64_t full[S], empty[S];
-  int64_t sums[kWarps], first_unit;
+  int64_t sums[kWarps], first_place;
   uint32_t rows_there[S][TILE / 32];  // rows of a stage whose page is there
   int begin[3], told, told_aside;
   float2 aside[kAside][8];
@@ -334,7 +347,7 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
   // ---- where this block's piece of the line begins ----
   const int R = P.a.n_requests, per = (R + kThreads - 1) / kThreads, r_first = warp < kWarps ? min(R, tid * per) : R, r_last = min(R, r_first + per);
   int64_t mine = 0;
-  for (int r = r_first; r < r_last; ++r) mine += Line::tiles(P, Line::clamped(P, P.a.seq_lens[r]));
+  for (int r = r_first; r < r_last; ++r) mine += kEntry + Line::tiles(P, Line::clamped(P, P.a.seq_lens[r]));
   mine *= P.rounds;
   int64_t upto = mine;
 #pragma unroll
@@ -358,29 +371,31 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
     int64_t u = upto - mine;
     for (int r = r_first; r < r_last; ++r) {
       const int tiles = Line::tiles(P, Line::clamped(P, P.a.seq_lens[r]));
-      const int64_t units = (int64_t)tiles * P.rounds;
-      if (u + units > u0) {
-        const int in = (int)(u0 - u);
+      const int64_t places = (int64_t)(kEntry + tiles) * P.rounds;
+      if (u + places > u0) {
+        const int64_t in = u0 - u;
+        const int round = in <= 0x7FFFFFFF ? (int)in / (kEntry + tiles) : (int)(in / (kEntry + tiles));
+        const int tile = max(0, (int)(in - (int64_t)round * (kEntry + tiles)) - kEntry);
         small.begin[0] = r;
-        small.begin[1] = in / tiles;
-        small.begin[2] = in % tiles;
-        small.first_unit = u + (int64_t)small.begin[1] * tiles;  // of the item that u0 is in
+        small.begin[1] = round;
+        small.begin[2] = tile;
+        small.first_place = u + (int64_t)round * (kEntry + tiles) + kEntry;  // of the item that u0 is in
         break;
       }
-      u += units;
+      u += places;
     }
   }
   __syncthreads();
-  const int steps = (int)(u1 - u0);
   Line at;
-  at.start(P, small.begin[0], small.begin[1], small.begin[2]);
+  at.start(P, small.begin[0], small.begin[1], small.begin[2], small.first_place, u1);
+  if (at.rest <= 0) return;  // a piece between two items
   bool alive = true;
-  // the parts of the item that begins at first_unit: those of the teams `from` to `to`, of which the first began it in
-  // its second slot, the others go on with it in their first
-  const int64_t first_end = small.first_unit + Line::tiles(P, at.n);
-  auto team_of = [&](int64_t unit) { return (int)(((unit + 1) * pieces - 1) / total); };
-  const int first_from = team_of(small.first_unit), first_to = team_of(first_end - 1);
-  const bool aside = small.first_unit < u0 && first_end < u1 && first_to - first_from < kAside;
+  // the parts of the item that the piece begins in: those of the teams `from` to `to`, of which the first began it in its
+  // second slot, the others go on with it in their first
+  const int64_t first_place = small.first_place, first_last = first_place + Line::tiles(P, at.n) - 1;
+  auto team_of = [&](int64_t place) { return (int)(((place + 1) * pieces - 1) / total); };
+  const int first_from = team_of(first_place), first_to = team_of(first_last);
+  const bool aside = first_place < u0 && first_last + 1 + kEntry < u1 && first_to - first_from < kAside;
 
   if (warp == kWarps) {
     // ---- the producer ----
@@ -400,7 +415,7 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
     if (P.tensor_copies) {
       const int row = lane << P.box_shift;
       if (lane < boxes) look(row);
-      for (int step = 0; step < steps; ++step) {
+      for (bool more = true; more;) {
         const int head = (at.h * P.members + member) / P.blocks_per_head;
         const bool live = lane < boxes && there && (uint32_t)entry < (uint32_t)C.n_pages;
         const int page = live ? entry : C.n_pages;  // a page beyond the last: zeros, and nothing is read
@@ -408,7 +423,8 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
         uint32_t rows[TILE / 32];
 #pragma unroll
         for (int k = 0; k < TILE / 32; ++k) rows[k] = __ballot_sync(~0u, __shfl_sync(~0u, live, (lane + 32 * k) >> P.box_shift));
-        if (step + 1 < steps) {
+        more = at.more();
+        if (more) {
           at.advance(P);
           there = 0;
           if (lane < boxes) look(row);
@@ -443,7 +459,7 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
         }
       };
       look_all();
-      for (int step = 0; step < steps; ++step) {
+      for (bool more = true; more;) {
         const int head = (at.h * P.members + member) / P.blocks_per_head;
         int64_t k_at[TILE / 32], v_at[TILE / 32];
         uint32_t mask[TILE / 32];
@@ -454,7 +470,8 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
           k_at[k] = live ? (int64_t)entries[k] * C.k_page + (int64_t)offsets[k] * C.k_token + (int64_t)head * C.k_head : 0;
           v_at[k] = live ? (int64_t)entries[k] * C.v_page + (int64_t)offsets[k] * C.v_token + (int64_t)head * C.v_head : 0;
         }
-        if (step + 1 < steps) {
+        more = at.more();
+        if (more) {
           at.advance(P);
           look_all();
         }
@@ -578,7 +595,7 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
   ask_q(at.r, at.h * P.members + member);
   take_q();
   clear();
-  int64_t item_first = small.first_unit;
+  int64_t item_first = first_place;
   // where a lane's row of the matrix loads lies in a tile, and its chunk 2j (+1 for the upper lanes) swizzled
   uint32_t lane_at[4];
 #pragma unroll
@@ -587,8 +604,9 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
 
   int stage = 0;
   uint32_t parity = 0;
+  bool more = true;
 #pragma unroll 1
-  for (int step = 0; step < steps; ++step) {
+  while (more) {
     // tokens of mine that take part: a range of rows, without those of pages that are not there
     const int row0 = at.t + warp * ROWS, upper = min(max(at.n - row0, 0), ROWS), lower = min(max(at.low - row0, 0), ROWS);
     constexpr uint32_t kAll = ~0u >> (32 - ROWS);
@@ -766,18 +784,19 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
     if (lane == 0) bar_arrive(smem_at(&small.empty[stage]));
     if (++stage == S) stage = 0, parity ^= 1;
 
-    if (at.left > 1 && step + 1 < steps) {
+    more = at.more();
+    if (at.left > 1 && more) {
       at.advance(P);
       continue;
     }
     // ---- the end of an item, or of this block's part of it: join the warps ----
     const int r = at.r, h = at.h * P.members + member, tiles = Line::tiles(P, at.n);
-    if (step + 1 < steps) {
+    if (more) {
       at.advance(P);
       ask_q(at.r, at.h * P.members + member);  // the next item's, under way while this one is put away
     }
-    const int64_t item_end = item_first + tiles;
-    const bool whole = item_first >= u0 && item_end <= u1;
+    const int64_t item_last = item_first + tiles - 1;
+    const bool whole = item_first >= u0 && item_last < u1;
     const int first = h / P.blocks_per_head * P.group, in_group = h % P.blocks_per_head * HB;
     const int heads = min(HB, P.group - in_group);
     const int slot = 2 * (team * P.members + member) + (item_first >= u0 ? 1 : 0);  // a block has at most two parts: its first item's and its last's
@@ -837,7 +856,7 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
       if (aside && item_first < u0) {
         asm volatile("bar.arrive 2, %0;" ::"n"(kBlock) : "memory");
       } else {
-        const int from = team_of(item_first), to = team_of(item_end - 1);
+        const int from = team_of(item_first), to = team_of(item_last);
         auto slot_of_team = [&](int b) { return 2 * (b * P.members + member) + (b == from ? 1 : 0); };
         int32_t *item = P.arrived + (int64_t)r * P.items_per_request + h;
         if (to - from < kDirect) {
@@ -857,8 +876,8 @@ __global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_k
         }
       }
     }
-    if (step + 1 < steps) {
-      item_first = item_end;
+    if (more) {
+      item_first = u1 - at.rest;
       take_q();
       clear();
     }
@@ -895,6 +914,8 @@ int run(Params &P, void *stream) {
     if (P.items_per_request % members == 0 && blocks / members * members * 50 >= blocks * 49) P.members = members;
   P.rounds = P.items_per_request / P.members;
   const int64_t most = (int64_t)P.a.n_requests * P.rounds * std::max<int64_t>(1, ((int64_t)P.a.max_pages * P.a.cache.page_size + TILE - 1) / TILE);
+  SERVE_REQUIRE((int64_t)P.a.n_requests * P.rounds * (((int64_t)P.a.max_pages * P.a.cache.page_size) / TILE + 1 + kEntry) / (blocks / P.members) < 0x7FFFFFFF,
+                AMAP_EOVERFLOW, "more tokens than a block can count");
   return launch(attend_kernel<CT, FP8, DP, NT>, dim3((unsigned)(std::min<int64_t>(blocks / P.members, most) * P.members)), kBlock, smem, stream, P);
 }
 
