@@ -38,7 +38,7 @@ namespace {
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps, kBlock = kThreads + 32;  // the last warp is the producer
 // tokens per warp and step, in sixteens: two where a token's row is 128 bytes, so that a step moves 32 KB either way and two
-// independent products hide each other's latency (128 e4m3 requests: MEASURED_SUB)
+// independent products hide each other's latency (128 e4m3 requests: 103 us with one, 100 with two)
 template <int ROW_BYTES> constexpr int kSixteens = ROW_BYTES == 128 ? 2 : 1;
 constexpr int kMostBlocksPerSm = 3;
 constexpr int kGroup = 8;               // teams whose parts are joined first, where an item has more than kDirect of them
@@ -59,9 +59,12 @@ struct Params {
   int32_t *failed, *grouped, *arrived;
 };
 
-// stages of the ring: 96 KB a block, or 192 with heads of 256 16-bit elements (two resident blocks then hold about 128 KB in flight per multiprocessor:
-// latency times bandwidth is about 50)
-constexpr int kStages = 3;
+// Blocks resident per multiprocessor: two where their registers allow (O and q of 8 heads of up to 128 elements); with 16
+// heads held to half the registers, what spills costs more than the second block brings (32 requests of 8k tokens, 16 q
+// heads per cache head: 131 us against 117).
+template <int DP, int NT> constexpr int kResident = DP == 256 || NT >= 2 ? 1 : 2;
+// Stages of the ring: 192 KB a multiprocessor, of which about two thirds are in flight (latency times bandwidth is 50).
+template <int ROW_BYTES, int RESIDENT> constexpr int kStages = 192 * 1024 / RESIDENT / (2 * 16 * kSixteens<ROW_BYTES> * kWarps * ROW_BYTES);
 
 __device__ __forceinline__ uint32_t smem_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool live) {
@@ -312,8 +315,8 @@ template <int S, int TILE> struct Small {
 };
 
 template <int CT, bool FP8, int DP, int NT>
-__global__ void __launch_bounds__(kBlock, DP == 256 || NT == 4 ? 1 : 2) attend_kernel(const __grid_constant__ Params P) {
-  constexpr int ES = FP8 ? 1 : 2, RB = DP * ES, NB = RB / 128, S = kStages;
+__global__ void __launch_bounds__(kBlock, (kResident<DP, NT>)) attend_kernel(const __grid_constant__ Params P) {
+  constexpr int ES = FP8 ? 1 : 2, RB = DP * ES, NB = RB / 128, S = kStages<RB, kResident<DP, NT>>;
   constexpr int U = kSixteens<RB>, ROWS = 16 * U, TILE = ROWS * kWarps;  // tokens per warp and step, and per tile
   constexpr int MT = DP / 16;                  // 16-element steps of a head
   constexpr int HB = 8 * NT;                   // q heads of a block
@@ -888,7 +891,8 @@ template <int CT, bool FP8, int DP, int NT>
 int run(Params &P, void *stream) {
   constexpr int RB = DP * (FP8 ? 1 : 2);
   constexpr int TILE = 16 * kSixteens<RB> * kWarps;
-  constexpr size_t smem = (size_t)kStages * 2 * TILE * RB + sizeof(float) * kWarps * 8 * (DP + 4) + sizeof(Small<kStages, TILE>);
+  constexpr int S = kStages<RB, kResident<DP, NT>>;
+  constexpr size_t smem = (size_t)S * 2 * TILE * RB + sizeof(float) * kWarps * 8 * (DP + 4) + sizeof(Small<S, TILE>);
   // the block's shared memory is asked for, and how many blocks a multiprocessor then holds, once per device
   static std::atomic<int> known[64];
   int dev = 0;
