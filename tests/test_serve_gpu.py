@@ -564,3 +564,16 @@ def test_a_decoding_step_in_a_graph(ops):
             # k may be rounded to the other neighbour: 2^-11 of each product, on top
             assert (np.abs(f64(out)[r] - want[0]) <= bound[0] + 2 * 2.0**-10 * (size[0, :, None] * mass[0])).all()
         assert not out[1].any()
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+def test_the_example_runs(cache):
+    import os
+    import subprocess
+    import sys
+
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    said = subprocess.run([sys.executable, os.path.join(root, "examples", "decode_step.py"), "--cache", cache, "--steps", "5"],
+                          capture_output=True, text=True, timeout=300)
+    assert said.returncode == 0, said.stderr[-2000:]
+    assert "5 decoding steps" in said.stdout
