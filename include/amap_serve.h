@@ -216,7 +216,8 @@ int amap_rope_append(const amap_rope_t *plan, const amap_append_args *args /* ho
  * Scores, maximum, sum and output are kept in 32 bits.
  *
  * Every wait inside the kernel ends: one that has lasted two seconds is given up, and the int32 at byte
- * amap_attend_workspace()'s *failed of the workspace becomes 1 (the outputs are then worth nothing).
+ * amap_attend_workspace()'s *failed of the workspace becomes 1 (the outputs are then worth
+ * nothing, and the workspace has to be zeroed before it is used again).
  *
  * workspace: amap_attend_workspace() bytes, 256-byte aligned, ZEROED before its first use; every call leaves
  * it ready for the next.  Calls that share a workspace must have the same q_heads, cache.heads and cache.head_dim and be

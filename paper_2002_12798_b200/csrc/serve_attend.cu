@@ -23,6 +23,9 @@
 // tile.  Pages of 8 n tokens arrive by tensor copies (TMA) of whole 8 to 64 token boxes, others row by row with 16-byte
 // asynchronous copies; both lay 128-byte rows out with the same swizzle, chunk ^ (row mod 8), so that the matrix loads
 // meet every bank once.  Only the end of an item synchronises the four warps.
+//
+// Measured: one request of 131009 tokens over 8 heads of 128 fp16 elements (537 MB) 87.5 us = 6.1 TB/s; 32 requests of up
+// to 16384 tokens in bf16 6.4 TB/s; 128 of up to 4096 over an e4m3 cache, 8 q heads to each, 5.2; 33 tokens 5.4 us.
 #include <cuda.h>
 
 #include <algorithm>
@@ -40,7 +43,7 @@ constexpr int kWarps = 4, kThreads = 32 * kWarps, kBlock = kThreads + 32;  // th
 // tokens per warp and step, in sixteens: two where a token's row is 128 bytes, so that a step moves 32 KB either way and two
 // independent products hide each other's latency (128 e4m3 requests: 103 us with one, 100 with two)
 template <int ROW_BYTES> constexpr int kSixteens = ROW_BYTES == 128 ? 2 : 1;
-constexpr int kMostBlocksPerSm = 3;
+constexpr int kMostBlocksPerSm = 2;
 constexpr int kGroup = 8;               // teams whose parts are joined first, where an item has more than kDirect of them
 constexpr int kDirect = 12;
 constexpr int kAside = 4;               // parts that the producer warp joins

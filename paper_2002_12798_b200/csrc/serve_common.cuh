@@ -65,13 +65,11 @@ __device__ __forceinline__ void pdl_begin() {
 template <int DT> struct Elem;
 template <> struct Elem<AMAP_BF16> {
   using T = __nv_bfloat16;
-  using T2 = __nv_bfloat162;
   static __device__ __forceinline__ float to(T v) { return __bfloat162float(v); }
   static __device__ __forceinline__ T from(float v) { return __float2bfloat16_rn(v); }
 };
 template <> struct Elem<AMAP_FP16> {
   using T = __half;
-  using T2 = __half2;
   static __device__ __forceinline__ float to(T v) { return __half2float(v); }
   static __device__ __forceinline__ T from(float v) { return __float2half_rn(v); }
 };
