@@ -403,6 +403,29 @@ def test_attend_one_long_request(ops, q_heads, heads):
     check_attend(ops, q, k, v, table, lens, 32, "bf16")
 
 
+@pytest.mark.parametrize("q_heads,heads", [(64, 64), (37, 37), (80, 40), (70, 35)])
+@pytest.mark.parametrize("page", [3, 16])
+def test_attend_more_heads_than_a_team_has_blocks(ops, q_heads, heads, page):
+    """The heads of a request go round by round through the teams: with requests that end inside pieces, an empty one, and
+    one that many pieces share."""
+    r = np.random.default_rng(heads + page)
+    torch.manual_seed(heads + page)
+    q, k, v, table, lens = attend_inputs(r, [700, 0, 65, 3001, 1, 128], q_heads, heads, 64, page, "bf16", "bf16", "token")
+    check_attend(ops, q, k, v, table, lens, page, "bf16")
+    check_attend(ops, q, k, v, table, lens, page, "bf16", window=300)
+
+
+def test_one_plan_serves_fewer_requests_and_other_caches(ops):
+    """The workspace is left ready by every call, whatever the calls before it split."""
+    r = np.random.default_rng(11)
+    torch.manual_seed(11)
+    plan = ops.AttendPlan(40, 8, 2, 128)
+    for lens, cache_dtype, page in (([9000], "bf16", 16), ([5] * 40, "e4m3", 8), ([4000, 1, 0, 777], "bf16", 5), ([9000], "e4m3", 64), (list(range(0, 4000, 100)), "bf16", 16)):
+        q, k, v, table, lens = attend_inputs(r, lens, 8, 2, 128, page, "bf16", cache_dtype, "token")
+        check_attend(ops, q, k, v, table, lens, page, "bf16", plan=plan)
+    assert not plan.failed()
+
+
 def test_attend_of_empty_requests_only(ops):
     r = np.random.default_rng(0)
     q, k, v, table, lens = attend_inputs(r, [0, 0, -5], 8, 2, 64, 16, "bf16", "bf16", "token")
