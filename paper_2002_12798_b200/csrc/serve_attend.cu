@@ -47,6 +47,8 @@ constexpr int kMostBlocksPerSm = 2;
 constexpr int kGroup = 8;               // teams whose parts are joined first, where an item has more than kDirect of them
 constexpr int kDirect = 12;
 constexpr int kAside = 4;               // parts that the producer warp joins
+template <int DP> constexpr int kJoined = 2 * (DP + 4);  // parts, or groups of them, that the four warps have room to join
+static_assert(kDirect <= kJoined<64>, "parts joined without groups");
 constexpr int kMostMembers = 32;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -240,7 +242,9 @@ struct Producer {
 };
 
 // Joins n parts of an item, the i-th in slot slot_of(i), in this order: into the output, or (final: false) into slot
-// slot_of(0), which nobody else reads before this block has arrived for it.  ml: room for n x 8.
+// slot_of(0), which nobody else reads before this block has arrived for it.  ml: room for n x 8, free again on return:
+// the four warps' lies in `joint`, where the next item's (m, l) go without a barrier ahead of them (with heads of 64
+// elements, those of warp 0's second head over part 8's of the third, which warp 1 reads).
 template <typename T, int CT, int DP, int HB, typename F>
 __device__ void join(const Params &P, float2 (*ml)[8], int n, F slot_of, int heads, bool final, int r, int first_head) {
   const int tid = T::index(), D = P.a.cache.head_dim;
@@ -291,6 +295,7 @@ __device__ void join(const Params &P, float2 (*ml)[8], int n, F slot_of, int hea
       }
     }
   }
+  T::sync();
 }
 
 // Whether this block is the last of n to arrive at the counter, which then is ready for the next call.  What the threads
@@ -332,8 +337,8 @@ __global__ void __launch_bounds__(kBlock, (kResident<DP, NT>)) attend_kernel(con
   // all in one piece: static shared memory ahead of it would cost its 1024-byte alignment, and with it the second block
   using Line = Cursor<TILE>;
   Small<S, TILE> &small = *reinterpret_cast<Small<S, TILE> *>(joint + kWarps * 8 * kPitch);
-  float2(*const joined)[8] = reinterpret_cast<float2(*)[8]>(joint);  // [kDirect][8], while `joint` is idle
-  static_assert(kDirect * 64 <= kWarps * 8 * kPitch * 4, "room for the parts of an item");
+  float2(*const joined)[8] = reinterpret_cast<float2(*)[8]>(joint);  // [kJoined<DP>][8], while `joint` is idle
+  static_assert(sizeof(float2) * 8 * kJoined<DP> <= sizeof(float) * kWarps * 8 * kPitch, "room for the parts of an item");
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
   const amap_cache &C = P.a.cache;
   const int D = C.head_dim;
@@ -914,6 +919,7 @@ int run(Params &P, void *stream) {
       return refuse(AMAP_ECUDA, e != cudaSuccess ? cudaGetErrorString(e) : "the kernel does not fit a multiprocessor");
     }
     blocks = device_sms() * std::min(per_sm, kMostBlocksPerSm);
+    SERVE_REQUIRE((blocks + kGroup - 1) / kGroup <= kJoined<DP>, AMAP_EUNSUPPORTED, "more multiprocessors than an item's parts can be joined from");
     known[dev].store(blocks, std::memory_order_relaxed);
   }
   // a team's blocks: the largest divisor of the items of a request that leaves no more than a fiftieth of the device idle
