@@ -141,26 +141,31 @@ __device__ __forceinline__ void halves_of(uint32_t four, uint32_t *low, uint32_t
   asm("{ .reg .b16 l, h; mov.b32 {l, h}, %2; cvt.rn.f16x2.e4m3x2 %0, l; cvt.rn.f16x2.e4m3x2 %1, h; }" : "=r"(*low), "=r"(*high) : "r"(four));
 }
 
-// P in two 16-bit terms, truncated and remainder: 15 bits and more of it enter P V (one 16-bit term would add an error
-// as large as the rounding of a 16-bit output).  The remainder is kept above zero, so that an infinity in V meets no
-// zero that P has not got.
+// P in 16-bit terms, each what the ones before it leave over, so that P V has the precision of 32-bit P: three terms of
+// bf16's 8 bits, or two of fp16's 11.  A remainder is kept above zero, so that an infinity in V meets no zero that P has
+// not got.
 // P is taken relative to a maximum that is renewed only when a score passes it by more than kSlack (in powers of 2): the
 // true one moves in most of the early steps, and O would be rescaled each time.  fp16 terms carry P times 2^kLift, out of
 // the way of fp16's smallest numbers; 2^(kLift + kSlack) is below its largest.
 constexpr float kSlack = 8.0f;
 template <int CT> constexpr float kLift = CT == AMAP_FP16 ? 7.0f : 0.0f;
+template <int CT> constexpr int kTerms = CT == AMAP_BF16 ? 3 : 2;
 template <int CT>
-__device__ __forceinline__ void two_terms(float p0, float p1, uint32_t *hi, uint32_t *lo) {
+__device__ __forceinline__ void split(float p0, float p1, uint32_t (&term)[kTerms<CT>]) {
   if constexpr (CT == AMAP_BF16) {
-    const uint32_t u0 = __float_as_uint(p0), u1 = __float_as_uint(p1);
-    *hi = __byte_perm(u0, u1, 0x7632);
-    const float r0 = fmaxf(p0 - __uint_as_float(u0 & 0xFFFF0000u), 0x1p-126f), r1 = fmaxf(p1 - __uint_as_float(u1 & 0xFFFF0000u), 0x1p-126f);
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(*lo) : "f"(r1), "f"(r0));
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const uint32_t u0 = __float_as_uint(p0), u1 = __float_as_uint(p1);
+      term[k] = __byte_perm(u0, u1, 0x7632);
+      p0 = fmaxf(p0 - __uint_as_float(u0 & 0xFFFF0000u), 0x1p-126f);
+      p1 = fmaxf(p1 - __uint_as_float(u1 & 0xFFFF0000u), 0x1p-126f);
+    }
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(term[2]) : "f"(p1), "f"(p0));
   } else {
-    asm("cvt.rz.f16x2.f32 %0, %1, %2;" : "=r"(*hi) : "f"(p1), "f"(p0));
-    const __half2 h = *reinterpret_cast<const __half2 *>(hi);
+    asm("cvt.rz.f16x2.f32 %0, %1, %2;" : "=r"(term[0]) : "f"(p1), "f"(p0));
+    const __half2 h = *reinterpret_cast<const __half2 *>(&term[0]);
     const float r0 = fmaxf(p0 - __low2float(h), 0x1p-24f), r1 = fmaxf(p1 - __high2float(h), 0x1p-24f);
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(*lo) : "f"(r1), "f"(r0));
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(term[1]) : "f"(r1), "f"(r0));
   }
 }
 
@@ -737,7 +742,7 @@ __global__ void __launch_bounds__(kBlock, (kResident<DP, NT>)) attend_kernel(con
           }
         }
       }
-      uint32_t hi[U][NT][2], lo[U][NT][2];
+      uint32_t p[U][NT][2][kTerms<CT>];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         const float from[2] = {(m[nt][0] == -INFINITY ? 0.0f : m[nt][0]) - kLift<CT>, (m[nt][1] == -INFINITY ? 0.0f : m[nt][1]) - kLift<CT>};
@@ -749,9 +754,9 @@ __global__ void __launch_bounds__(kBlock, (kResident<DP, NT>)) attend_kernel(con
           l[nt][1] += s[u][nt][1] + s[u][nt][3];
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
-            two_terms<CT>(s[u][nt][2 * k], s[u][nt][2 * k + 1], &hi[u][nt][k], &lo[u][nt][k]);
-            hi[u][nt][k] = transposed(hi[u][nt][k]);
-            lo[u][nt][k] = transposed(lo[u][nt][k]);
+            split<CT>(s[u][nt][2 * k], s[u][nt][2 * k + 1], p[u][nt][k]);
+#pragma unroll
+            for (int w = 0; w < kTerms<CT>; ++w) p[u][nt][k][w] = transposed(p[u][nt][k][w]);
           }
         }
       }
@@ -764,8 +769,8 @@ __global__ void __launch_bounds__(kBlock, (kResident<DP, NT>)) attend_kernel(con
             load4_transposed(v_at + lane_at[i & 3] + u * 2048 + (i >> 2) * kBox, a);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-              mma<CT>(o[nt][i], a[0], a[2], a[1], a[3], hi[u][nt][0], hi[u][nt][1]);
-              mma<CT>(o[nt][i], a[0], a[2], a[1], a[3], lo[u][nt][0], lo[u][nt][1]);
+#pragma unroll
+              for (int w = 0; w < kTerms<CT>; ++w) mma<CT>(o[nt][i], a[0], a[2], a[1], a[3], p[u][nt][0][w], p[u][nt][1][w]);
             }
           }
         }
@@ -783,8 +788,8 @@ __global__ void __launch_bounds__(kBlock, (kResident<DP, NT>)) attend_kernel(con
               halves_of(__byte_perm(a[2 * j + 1], 0, 0x3120), &a2, &a3);
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt) {
-                mma<CT>(o[nt][i + j], a0, a1, a2, a3, hi[u][nt][0], hi[u][nt][1]);
-                mma<CT>(o[nt][i + j], a0, a1, a2, a3, lo[u][nt][0], lo[u][nt][1]);
+#pragma unroll
+                for (int w = 0; w < kTerms<CT>; ++w) mma<CT>(o[nt][i + j], a0, a1, a2, a3, p[u][nt][0][w], p[u][nt][1][w]);
               }
             }
           }
