@@ -43,3 +43,83 @@ def test_attend_keeps_what_two_opposite_values_leave_over(ops, dim, group, dtype
     want, _, _, mass = ref.attend(f64(qq), f64(held[0]), f64(held[1]), table, lens, 1.0)
     off = np.abs(f64(out) - want)
     assert (off <= ref.UNIT[dtype] * np.abs(want) + 2.0**-20 * mass).all(), (off / mass).max()
+
+
+@pytest.mark.parametrize("dtype,cache_dtype", [("fp16", "fp16"), ("bf16", "e4m3"), ("bf16", "bf16")])
+@pytest.mark.parametrize("dim,group", [(64, 8), (128, 1), (128, 16), (256, 8)])
+@pytest.mark.parametrize("where", ["first", "middle", "every 61st", "some heads"])
+def test_attend_beside_a_token_with_nearly_all_the_weight(ops, dim, group, where, dtype, cache_dtype):
+    """One token's score stands 4 to 40 above all others' and its V is zero: the output is what the others have, and every
+    one of them counts.  A score is the product of single elements, exact but for its scale and the subtraction of the
+    maximum: 3 roundings of 2^-24 of at most 40 log2 e, so p is within 2^-17 of itself; requests are many, so that a warp
+    meets most of a request's tokens behind its one."""
+    gaps = [4, 8, 11, 12, 14, 16, 18, 20, 22, 24, 28, 32, 40]
+    n, tokens, page = 13 * 25, 1500, 16
+    row = -(-tokens // page)
+    shape = (2 * row, page, 1, dim)
+    k, v = torch.zeros(shape), torch.full(shape, 448.0 if cache_dtype == "e4m3" else 1024.0)
+    r = np.random.default_rng(dim)
+    at = {"first": [0], "middle": [777], "every 61st": range(0, tokens, 61), "some heads": [3]}[where]
+    flat_k, flat_v = k.view(-1, dim), v.view(-1, dim)
+    for t in at:
+        flat_k[t, 0], flat_v[t] = 1.0, 0.0
+    k.view(2, -1, dim)[1].copy_(k.view(2, -1, dim)[0])  # the second half: the others differ in scores, up to 2 either way
+    k.view(2, -1, dim)[1][:, 1] = torch.from_numpy(r.integers(-8, 9, row * page) / 8.0)
+    v.view(2, -1, dim)[1].copy_(v.view(2, -1, dim)[0])
+    q = torch.zeros(n, group, dim)
+    q[:, :, 0] = torch.tensor(gaps * 25)[:, None]
+    if where == "some heads":
+        q[:, ::3, 0] = 0.0
+    q[:, :, 1] = 1.0
+    table = np.arange(2 * row, dtype=np.int32).reshape(2, row)[np.arange(n) % 2]
+    lens = np.full(n, tokens, dtype=np.int32) - np.arange(n, dtype=np.int32) % 7
+    held = [x.cuda().to(TYPES[cache_dtype]) for x in (k, v)]
+    qq = q.cuda().to(TYPES[dtype])
+    args = qq, ops.PagedCache(*held), torch.from_numpy(table).cuda(), torch.from_numpy(lens).cuda()
+    out, lse = ops.AttendPlan(n, group, 1, dim, scale=1.0).attend(*args, return_lse=True)
+    some = np.arange(0, n, 4)
+    want, want_lse, _, mass = ref.attend(f64(qq)[some], f64(held[0]), f64(held[1]), table[some], lens[some], 1.0)
+    off = np.abs(f64(out)[some] - want)
+    # half of fp16's smallest step, where the output is that small
+    assert (off <= ref.UNIT[dtype] * np.abs(want) + 2.0**-15 * mass + 2.0**-25).all(), (off / mass).max()
+    assert (np.abs(f64(lse)[some] - want_lse) <= 2.0**-16 + 2.0**-22 * np.abs(want_lse)).all()
+
+
+@pytest.mark.parametrize("dim,group", [(64, 8), (128, 16), (256, 3)])
+def test_attend_infinity_beside_a_token_with_nearly_all_the_weight(ops, dim, group):
+    """An infinity in V is one in the output however small its token's weight is (as far as 32 bits hold that), and nothing
+    else; what lies behind a request's end is not."""
+    n, tokens, page = 40, 200, 16
+    k, v = torch.zeros(13, page, 1, dim), torch.ones(13, page, 1, dim)
+    k.view(-1, dim)[5, 0] = 1.0
+    v.view(-1, dim)[[4, 100], [3, 7]] = math.inf
+    v.view(-1, dim)[150, 9] = -math.inf
+    v.view(-1, dim)[tokens:] = math.nan
+    q = torch.zeros(n, group, dim)
+    q[:, :, 0] = torch.arange(n)[:, None]
+    table = torch.arange(13, dtype=torch.int32).repeat(n, 1).cuda()
+    held = [x.cuda().half() for x in (k, v)]
+    out = f64(ops.AttendPlan(n, group, 1, dim, scale=1.0).attend(q.cuda().half(), ops.PagedCache(*held), table, torch.full((n,), tokens, dtype=torch.int32).cuda()))
+    for at, value in ((3, math.inf), (7, math.inf), (9, -math.inf)):
+        assert (out[..., at] == value).all()
+    rest = np.delete(out, [3, 7, 9], 2)
+    assert (np.abs(rest - 1) <= 2.0**-11).all()
+
+
+@pytest.mark.parametrize("dtype,cache_dtype", [("fp16", "fp16"), ("bf16", "e4m3")])
+@pytest.mark.parametrize("spread", [1.0, 8.0, 40.0])
+def test_attend_scores_far_apart_everywhere(ops, spread, dtype, cache_dtype):
+    """Random scores of up to some hundreds of powers of two apart: within the bound of a 32-bit computation."""
+    torch.manual_seed(int(spread))
+    r = np.random.default_rng(int(spread))
+    n, heads, dim, page = 24, 2, 128, 16
+    lens = r.integers(1, 700, n).astype(np.int32)
+    table = r.permutation(n * 44).astype(np.int32).reshape(n, 44)
+    k, v = (torch.randn(n * 44, page, heads, dim, device="cuda").to(TYPES[cache_dtype]) for _ in range(2))
+    q = (torch.randn(n, 16, dim, device="cuda") * spread).to(TYPES[dtype])
+    plan = ops.AttendPlan(n, 16, heads, dim)
+    out, lse = plan.attend(q, ops.PagedCache(k, v), torch.from_numpy(table).cuda(), torch.from_numpy(lens).cuda(), return_lse=True)
+    want, want_lse, size, mass = ref.attend(f64(q), f64(k), f64(v), table, lens, plan.scale)
+    bound, lse_bound = ref.attend_bound(want, size, mass, dim, dtype)
+    assert (np.abs(f64(out) - want) <= bound).all()
+    assert (np.abs(f64(lse) - want_lse) <= lse_bound + 2.0**-22 * np.abs(want_lse)).all()
