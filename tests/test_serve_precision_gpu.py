@@ -123,3 +123,26 @@ def test_attend_scores_far_apart_everywhere(ops, spread, dtype, cache_dtype):
     bound, lse_bound = ref.attend_bound(want, size, mass, dim, dtype)
     assert (np.abs(f64(out) - want) <= bound).all()
     assert (np.abs(f64(lse) - want_lse) <= lse_bound + 2.0**-22 * np.abs(want_lse)).all()
+
+
+@pytest.mark.parametrize("dtype,cache_dtype", [("fp16", "fp16"), ("bf16", "bf16"), ("bf16", "e4m3")])
+@pytest.mark.parametrize("softcap", [1e-40, 1e-6, 0.5, 5.0, 30.0, 50.0, 1e3, 1e5, 1e8, 1e30])
+def test_attend_softcap_of_any_size(ops, softcap, dtype, cache_dtype):
+    """A score that the cap hardly touches is what it is without one: the bound is that of a score in 32 bits, of which the
+    hyperbolic tangent adds 2^-20 of itself (the bound has 16 times 2^-23 to spare for such)."""
+    torch.manual_seed(3)
+    r = np.random.default_rng(3)
+    n, heads, dim, page = 12, 2, 64, 16
+    lens = r.integers(1, 300, n).astype(np.int32)
+    table = r.permutation(n * 19).astype(np.int32).reshape(n, 19)
+    k, v = (torch.randn(n * 19, page, heads, dim, device="cuda").to(TYPES[cache_dtype]) for _ in range(2))
+    q = torch.randn(n, 8, dim, device="cuda").to(TYPES[dtype])
+    q[0], q[1] = 0.0, q[1] * 1e-3
+    plan = ops.AttendPlan(n, 8, heads, dim, softcap=softcap)
+    out, lse = plan.attend(q, ops.PagedCache(k, v), torch.from_numpy(table).cuda(), torch.from_numpy(lens).cuda(), return_lse=True)
+    cap = float(np.float32(softcap))
+    want, want_lse, size, mass = ref.attend(f64(q), f64(k), f64(v), table, lens, plan.scale, softcap=cap)
+    bound, lse_bound = ref.attend_bound(want, size, mass, dim, dtype)
+    off = np.abs(f64(out) - want) / bound
+    assert (off <= 1).all(), off.max()
+    assert (np.abs(f64(lse) - want_lse) <= lse_bound + 2.0**-22 * np.abs(want_lse)).all()
