@@ -583,7 +583,9 @@ __global__ void __launch_bounds__(kBlock, (kResident<DP, NT>)) attend_kernel(con
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       to_log2[nt][0] = to_log2[nt][1] = unit;
-      if constexpr (FP8) {  // q as fp16 times a power of two that brings its largest element near 1
+      // q as fp16 times a power of two that brings its largest element near fp16's largest: elements down to 2^-31 of it are
+      // exact (of fp16's 11 bits, down to 2^-28)
+      if constexpr (FP8) {
         float big = 0.0f;
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
@@ -597,8 +599,8 @@ __global__ void __launch_bounds__(kBlock, (kResident<DP, NT>)) attend_kernel(con
         }
         big = fmaxf(big, __shfl_xor_sync(~0u, big, 1));
         big = fmaxf(big, __shfl_xor_sync(~0u, big, 2));
-        // 2^e <= big < 2^(e+1); e within what 2^-e and 2^e are normal numbers for
-        const int e = min(max((int)(__float_as_uint(big) >> 23) - 127, -120), 120);
+        // 2^14 2^e <= big < 2^15 2^e; e within what 2^-e and 2^e are normal numbers for
+        const int e = min(max((int)(__float_as_uint(big) >> 23) - 127 - 14, -120), 120);
         const float down = __uint_as_float((uint32_t)(127 - e) << 23), up = __uint_as_float((uint32_t)(127 + e) << 23);
 #pragma unroll
         for (int m = 0; m < MT; ++m) {

@@ -146,3 +146,29 @@ def test_attend_softcap_of_any_size(ops, softcap, dtype, cache_dtype):
     off = np.abs(f64(out) - want) / bound
     assert (off <= 1).all(), off.max()
     assert (np.abs(f64(lse) - want_lse) <= lse_bound + 2.0**-22 * np.abs(want_lse)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("power", [10, 16, 20, 26])
+def test_attend_query_elements_far_apart_over_8_bits(ops, power, dtype):
+    """One element of q is 2^power of the others and meets zeros in K: the others count in full."""
+    torch.manual_seed(power)
+    r = np.random.default_rng(power)
+    n, heads, dim, page = 6, 2, 128, 16
+    lens = r.integers(1, 300, n).astype(np.int32)
+    table = r.permutation(n * 19).astype(np.int32).reshape(n, 19)
+    k, v = (torch.randn(n * 19, page, heads, dim, device="cuda") for _ in range(2))
+    k[..., 5] = 0.0
+    held = [x.to(TYPES["e4m3"]) for x in (k, v)]
+    small = 2.0 ** (15 - power) if dtype == "fp16" else 1.0
+    q = (torch.rand(n, 8, dim, device="cuda") + 1) * small * torch.where(torch.rand(n, 8, dim, device="cuda") < 0.5, -1.0, 1.0)
+    q[..., 5] = small * 2.0**power * 1.5
+    q = q.to(TYPES[dtype])
+    assert torch.isfinite(q).all()
+    plan = ops.AttendPlan(n, 8, heads, dim, scale=0.2 / small)
+    out, lse = plan.attend(q, ops.PagedCache(*held), torch.from_numpy(table).cuda(), torch.from_numpy(lens).cuda(), return_lse=True)
+    want, want_lse, size, mass = ref.attend(f64(q), f64(held[0]), f64(held[1]), table, lens, float(np.float32(plan.scale)))
+    bound, lse_bound = ref.attend_bound(want, size, mass, dim, dtype)
+    off = np.abs(f64(out) - want) / bound
+    assert (off <= 1).all(), off.max()
+    assert (np.abs(f64(lse) - want_lse) <= lse_bound + 2.0**-22 * np.abs(want_lse)).all()
