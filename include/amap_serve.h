@@ -184,8 +184,8 @@ int amap_cache_encode(const amap_cache *cache /* host */, amap_cache_maps *out /
 /* amap_rope_append: a step's q, k, v [rows][heads][head_dim] in one launch.
  *   q_out = rotated q;  K[slots[i]] = rotated k of row i;  V[slots[i]] = v of row i.
  * A slot outside [0, n_pages*page_size) writes nothing to the cache (its q is rotated all the same).  Slots must be
- * distinct.  A 16-bit cache has the type of q, k, v; an e4m3 cache takes value/scale, rounded to nearest even and
- * clamped to +-448 (NaN stays NaN). */
+ * distinct.  A 16-bit cache has the type of q, k, v; an e4m3 cache takes value/scale, a division in 32
+ * bits, rounded to nearest even and clamped to +-448 (NaN stays NaN). */
 typedef struct amap_append_args {
   int64_t rows;
   int32_t dtype;   /* AMAP_BF16 or AMAP_FP16 */

@@ -49,6 +49,29 @@ Div div_by(uint32_t d) {
 }
 __device__ __forceinline__ uint32_t quotient(uint32_t n, const Div &f) { return f.mul ? __umulhi(n, f.mul) >> f.shift : n >> f.shift; }
 
+// v / d in 32 bits, correctly rounded where it is a normal number that 8 bits can hold, by Markstein's correction (IBM
+// Journal of Research and Development 34, 1990): with r the rounded reciprocal of d, q = v r is within one unit of the
+// quotient and q + (v - q d) r is the quotient rounded.  d is taken times a power of 2 that brings it near 1, so that any
+// positive number will do.  (A division in the kernel costs the 16-bit caches, which have none, 8 % for its registers.)
+struct Divisor {
+  float pre, d, r;
+};
+Divisor divide_by(float d) {
+  int e = 0;
+  frexpf(d, &e);  // 2^(e-1) <= d < 2^e
+  e = std::max(-126, std::min(126, e - 1));
+  Divisor f;
+  f.pre = ldexpf(1.0f, -e);
+  f.d = d * f.pre;  // exact
+  f.r = 1.0f / f.d;
+  return f;
+}
+__device__ __forceinline__ float quotient(float v, const Divisor &f) {
+  const float x = v * f.pre, q = x * f.r;
+  // outside: zeros of either sign, and what is clamped, infinities and NaN among them
+  return fabsf(q) > 0x1p-20f && fabsf(q) < 1024.0f ? fmaf(fmaf(-q, f.d, x), f.r, q) : q;
+}
+
 struct Part {
   const char *x;
   char *y;
@@ -56,7 +79,7 @@ struct Part {
   int64_t y_token;
   int32_t heads;
   int32_t kind;
-  float inv_scale;
+  Divisor scale;         // cache: what an element of 8 bits is to be multiplied by
   int32_t tokens;        // per block
   uint32_t first_block;  // blocks of the parts before this one
   Div by_heads;
@@ -100,7 +123,7 @@ __device__ __forceinline__ uint32_t pack2(float x, float y) {
 }
 
 template <int DT, int VEC>
-__device__ __forceinline__ void store(char *p, int64_t at, const float (&v)[VEC], bool e4m3, float inv_scale) {
+__device__ __forceinline__ void store(char *p, int64_t at, const float (&v)[VEC], bool e4m3, const Divisor &scale) {
   using E = Elem<DT>;
   constexpr int ES = sizeof(typename E::T);
   if (e4m3) {
@@ -109,10 +132,10 @@ __device__ __forceinline__ void store(char *p, int64_t at, const float (&v)[VEC]
       uint16_t two[(VEC + 1) / 2];
     } u;
     if constexpr (VEC == 1) {
-      u.raw = to_e4m3(v[0] * inv_scale);
+      u.raw = to_e4m3(quotient(v[0], scale));
     } else {
 #pragma unroll
-      for (int j = 0; j < VEC; j += 2) u.two[j / 2] = __nv_cvt_float2_to_fp8x2(make_float2(v[j] * inv_scale, v[j + 1] * inv_scale), __NV_SATFINITE, __NV_E4M3);
+      for (int j = 0; j < VEC; j += 2) u.two[j / 2] = __nv_cvt_float2_to_fp8x2(make_float2(quotient(v[j], scale), quotient(v[j + 1], scale)), __NV_SATFINITE, __NV_E4M3);
     }
     *reinterpret_cast<typename Raw<VEC>::T *>(p + at) = u.raw;
   } else {
@@ -224,8 +247,8 @@ __global__ void __launch_bounds__(kThreads, kBlocks) rope_kernel(const __grid_co
         }
       }
       const bool e4m3 = part.kind != kRows && P.e4m3;
-      store<DT, VEC>(y0, to[u] + first, v, e4m3, part.inv_scale);
-      if (first + gap < P.head_dim) store<DT, VEC>(y0, to[u] + first + gap, w, e4m3, part.inv_scale);
+      store<DT, VEC>(y0, to[u] + first, v, e4m3, part.scale);
+      if (first + gap < P.head_dim) store<DT, VEC>(y0, to[u] + first + gap, w, e4m3, part.scale);
     }
   };
 
@@ -393,7 +416,7 @@ extern "C" int amap_rope_rotate(const amap_rope_t *plan, const amap_rope_args *a
     SERVE_REQUIRE(aligned(s.x, es) && aligned(s.y, es), AMAP_EALIGN, "part: misaligned");
     SERVE_REQUIRE((a->rows == 1 || s.y_row != 0) && (s.heads == 1 || s.y_head != 0), AMAP_EINVAL, "part: rows of y lie on one another");
     P.part[k] = {static_cast<const char *>(s.x), static_cast<char *>(s.y), s.x_row, s.x_head, s.y_row, s.y_head, 0,
-                 s.heads, kRows, 1.0f, 0, 0, {}};
+                 s.heads, kRows, {}, 0, 0, {}};
   }
   // an output laid over an input is a race, unless the part is turned in place; parts turned in place may interleave in
   // one buffer (q and k of a fused projection), whose byte ranges overlap without sharing an element
@@ -446,12 +469,12 @@ extern "C" int amap_rope_append(const amap_rope_t *plan, const amap_append_args 
                     AMAP_EINVAL, "q_out overlaps q, k or v");
     }
     P.part[n++] = {static_cast<const char *>(a->q), static_cast<char *>(a->q_out), a->q_row, a->q_head, a->q_out_row, a->q_out_head, 0, a->q_heads, kRows,
-                   1.0f, 0, 0, {}};
+                   {}, 0, 0, {}};
   }
   P.part[n++] = {static_cast<const char *>(a->k), static_cast<char *>(c.k), a->k_row, a->k_head, c.k_page, c.k_head, c.k_token, c.heads,
-                 kCacheTurned, 1.0f / c.k_scale, 0, 0, {}};
+                 kCacheTurned, divide_by(c.k_scale), 0, 0, {}};
   P.part[n++] = {static_cast<const char *>(a->v), static_cast<char *>(c.v), a->v_row, a->v_head, c.v_page, c.v_head, c.v_token,
-                 c.heads, kCacheCopied, 1.0f / c.v_scale, 0, 0, {}};
+                 c.heads, kCacheCopied, divide_by(c.v_scale), 0, 0, {}};
   P.n_parts = n;
   P.rows = a->rows;
   P.positions = a->positions;

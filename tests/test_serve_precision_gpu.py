@@ -172,3 +172,22 @@ def test_attend_query_elements_far_apart_over_8_bits(ops, power, dtype):
     off = np.abs(f64(out) - want) / bound
     assert (off <= 1).all(), off.max()
     assert (np.abs(f64(lse) - want_lse) <= lse_bound + 2.0**-22 * np.abs(want_lse)).all()
+
+
+@pytest.mark.parametrize("scale", [1.0 / 64, 3.0, 0.7, 1.3, 7.0 / 1024, 11.0, 13.0 / 8, 57.0, 113.0 / 64, 2.0**-126, 2.0**-130, 1e-39, 2.0**-149, 3e38])
+def test_append_divides_by_the_scale(ops, scale):
+    """Every bf16 value and some fp16 ones into an e4m3 cache: the quotient in 32 bits, rounded; exactly."""
+    s = np.float32(scale)
+    every = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(torch.bfloat16)
+    x = every.view(256, 1, 256).cuda()
+    k, v = (torch.zeros(2, 128, 1, 256, device="cuda").to(TYPES["e4m3"]) for _ in range(2))
+    slots, pos = torch.arange(256, dtype=torch.int32, device="cuda"), torch.zeros(256, dtype=torch.int32, device="cuda")
+    ops.RopePlan(256, 0).append(x, x, x, pos, slots, ops.PagedCache(k, v, k_scale=float(s), v_scale=float(s)))
+    with np.errstate(all="ignore"):
+        quotient = every.float().numpy() / s
+    want = torch.from_numpy(np.clip(quotient, -448, 448)).to(TYPES["e4m3"]).view(torch.uint8).numpy().reshape(-1)
+    nan = np.isnan(quotient)
+    for got in (k, v):
+        got = got.view(torch.uint8).cpu().numpy().reshape(-1)
+        assert ((got[nan] & 0x7F) == 0x7F).all()
+        assert np.array_equal(got[~nan], want[~nan]), (got[~nan] != want[~nan]).sum()
