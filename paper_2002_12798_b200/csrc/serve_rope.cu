@@ -2,7 +2,7 @@
 //
 // Pair i of a token at position p (along the pair's axis) turns by p * f_i radians.  The plan keeps f_i / 2pi as a
 // 64-bit fraction of a turn; p times that fraction wraps modulo a full turn exactly, so the angle's error is
-// p * 2^-65 turns whatever p is, and sincospi takes it from there in 32 bits.
+// p * 2^-65 turns whatever p is, and `turn` takes it from there in 32 bits.
 //
 // Bound: memory, every element is read and written once.  A block takes a few tokens of one part (q, k or v): its
 // threads issue their loads, compute the tokens' cos and sin once for all heads while those are under way, and turn
@@ -155,6 +155,24 @@ __device__ __forceinline__ void store(char *p, int64_t at, const float (&v)[VEC]
   }
 }
 
+// sin and cos of a fraction of a turn in units of 2^-64.  For 16-bit elements the nearest half turn is left to sincospif: its
+// argument, a float near half a turn at most, is within 2^-24 pi.  fp32 elements would show that; the nearest quarter turn
+// is taken off in integers for them, which leaves an argument eight times smaller and as much closer.
+template <int DT>
+__device__ __forceinline__ void turn(uint64_t turns, float *s, float *c) {
+  if constexpr (DT != AMAP_FP32) {
+    sincospif((float)(int32_t)(turns >> 32) * 0x1p-31f, s, c);
+  } else {
+    const uint32_t quarter = ((uint32_t)(turns >> 32) + 0x20000000u) >> 30;
+    const int64_t rest = (int64_t)(turns - ((uint64_t)quarter << 62));  // [-1/8, 1/8) turn
+    float x, y;
+    sincospif((float)(int32_t)(rest >> 30) * 0x1p-33f, &x, &y);
+    const float a = quarter & 1 ? y : x, b = quarter & 1 ? x : y;
+    *s = quarter & 2 ? -a : a;
+    *c = (quarter + 1) & 2 ? -b : b;
+  }
+}
+
 // Where pair i's cos (and sin) of a token is kept: the VEC values of a chunk in fours, a four of all chunks side by side,
 // so that neighbouring lanes read neighbouring 16 bytes.
 template <int VEC>
@@ -263,9 +281,9 @@ __global__ void __launch_bounds__(kThreads, kBlocks) rope_kernel(const __grid_co
       const int at = quotient(i, P.by_half), pair = i - at * half;
       const int64_t from = axes[pair] * P.position_axis + (row0 + at) * P.position_row;
       const int64_t pos = P.wide_positions ? static_cast<const int64_t *>(P.positions)[from] : static_cast<const int32_t *>(P.positions)[from];
-      const int32_t fraction = (int32_t)(((uint64_t)pos * phases[pair]) >> 32);  // in units of 2^-32 turns, [-1/2, 1/2)
+      const uint64_t turns = (uint64_t)pos * phases[pair];  // in units of 2^-64 turns
       float s, c;
-      sincospif((float)fraction * 0x1p-31f, &s, &c);
+      turn<DT>(turns, &s, &c);
       turn_cos[at * half + place<VEC>(pair, half)] = c * P.scale;
       turn_sin[at * half + place<VEC>(pair, half)] = s * P.scale * P.sign;
     }

@@ -191,3 +191,25 @@ def test_append_divides_by_the_scale(ops, scale):
         got = got.view(torch.uint8).cpu().numpy().reshape(-1)
         assert ((got[nan] & 0x7F) == 0x7F).all()
         assert np.array_equal(got[~nan], want[~nan]), (got[~nan] != want[~nan]).sum()
+
+
+@pytest.mark.parametrize("base,first", [(10000.0, 0), (1e6, 100000), (10.0, -70)])
+@pytest.mark.parametrize("pairs", ["half", "adjacent"])
+def test_rotate_in_fp32_is_as_exact_as_rounded_cos_and_sin(ops, base, first, pairs):
+    """Over half a million elements, against the same turn with cos and sin of 64 bits rounded once (a tenth more is allowed)."""
+    torch.manual_seed(0)
+    dim, tokens = 128, 1024
+    half = dim // 2
+    plan = ops.RopePlan(dim, base=base, pairs=pairs)
+    pos = torch.arange(first, first + tokens, dtype=torch.int32, device="cuda")
+    x = torch.randn(tokens, 4, dim, device="cuda")
+    (y,) = plan.rotate([x], pos)
+    angle = pos.double()[:, None] * torch.tensor([base ** (-2.0 * i / dim) for i in range(half)], dtype=torch.float64, device="cuda")
+    cos, sin = angle.cos()[:, None], angle.sin()[:, None]
+    a, b = (x[..., :half], x[..., half:]) if pairs == "half" else (x[..., 0::2], x[..., 1::2])
+    got = (y[..., :half], y[..., half:]) if pairs == "half" else (y[..., 0::2], y[..., 1::2])
+    want = torch.stack([a.double() * cos - b.double() * sin, b.double() * cos + a.double() * sin])
+    c, s = cos.float(), sin.float()
+    plain = torch.stack([a * c - b * s, b * c + a * s])
+    off = lambda z: float((z.double() - want).norm() / want.norm())  # noqa: E731
+    assert off(torch.stack(got)) <= 1.1 * off(plain), (off(torch.stack(got)), off(plain))
