@@ -177,11 +177,24 @@ class RopePlan:
         _require(len(inv_freq) == half and len(axes) == half, "inv_freq, axes: rotary_dim/2 values")
         _require(pairs in _PAIRS, 'pairs: "half" or "adjacent"')
         self.head_dim, self.rotary_dim, self.n_axes = head_dim, rotary_dim, 1 + max(axes, default=0)
+        self._made_of = inv_freq, axes, _PAIRS[pairs], scale
+        self._make()
+
+    def _make(self):
         self._h = None
-        h = c_void_p()
-        _check(_lib.amap_rope_plan(head_dim, rotary_dim, (c_double * max(half, 1))(*inv_freq), (c_int32 * max(half, 1))(*axes), self.n_axes,
-                                   _PAIRS[pairs], scale, byref(h)), "amap_rope_plan")
+        inv_freq, axes, pairs, scale = self._made_of
+        n, h = max(len(axes), 1), c_void_p()
+        _check(_lib.amap_rope_plan(self.head_dim, self.rotary_dim, (c_double * n)(*inv_freq), (c_int32 * n)(*axes), self.n_axes, pairs, scale, byref(h)),
+               "amap_rope_plan")
         self._h = h.value
+
+    # a copy (copy, deepcopy, pickle) makes a plan of its own: the handle has one owner
+    def __getstate__(self):
+        return {k: v for k, v in self.__dict__.items() if k != "_h"}
+
+    def __setstate__(self, state):
+        self.__dict__.update(state)
+        self._make()
 
     def __del__(self):
         if getattr(self, "_h", None) and _lib is not None:  # module globals are gone at interpreter shutdown
