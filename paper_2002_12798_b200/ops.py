@@ -17,6 +17,7 @@ import ctypes
 import importlib.machinery
 import importlib.util
 import math
+import threading
 from collections import namedtuple
 from ctypes import POINTER, Structure, byref, c_char_p, c_double, c_float, c_int32, c_int64, c_uint64, c_void_p
 
@@ -234,7 +235,7 @@ class AttendPlan:
     each token sees the last `window` tokens (0: all); softcap: scores are softcap * tanh(score / softcap) (0: none).
 
     Calls of one plan run one after another, also when they come from different streams (the later stream is made to
-    wait).  Inside a graph capture that order is the caller's: a plan captured in a graph should serve that graph."""
+    wait) or threads.  Inside a graph capture that order is the caller's: a plan captured in a graph should serve that graph."""
 
     def __init__(self, max_requests, q_heads, kv_heads, head_dim, *, scale=None, window=0, softcap=0.0, device=None):
         self.max_requests, self.q_heads, self.kv_heads, self.head_dim = max_requests, q_heads, kv_heads, head_dim
@@ -242,16 +243,27 @@ class AttendPlan:
         self.window, self.softcap = int(window), float(softcap)
         device = torch.device("cuda" if device is None else device)
         self.device = device if device.index is not None else torch.device("cuda", torch.cuda.current_device())
+        self._make()
+
+    def _make(self):
         n, failed = c_int64(), c_int64()
         with torch.cuda.device(self.device):
-            _check(_lib.amap_attend_workspace(max_requests, q_heads, kv_heads, head_dim, byref(n), byref(failed)), "amap_attend_workspace")
+            _check(_lib.amap_attend_workspace(self.max_requests, self.q_heads, self.kv_heads, self.head_dim, byref(n), byref(failed)), "amap_attend_workspace")
             self._bytes, self._failed = n.value, failed.value
             self._stream = torch.cuda.current_stream()
             self._workspace = torch.zeros(self._bytes, dtype=torch.uint8, device=self.device)
-        self._raw = self._stream.cuda_stream
-        self._args = _Attend(q_heads=q_heads, scale=self.scale, softcap=self.softcap, window=self.window, workspace=self._workspace.data_ptr(),
-                             workspace_bytes=self._bytes, cache=_Cache(heads=kv_heads, head_dim=head_dim))
+        self._raw, self._lock = self._stream.cuda_stream, threading.Lock()
+        self._args = _Attend(q_heads=self.q_heads, scale=self.scale, softcap=self.softcap, window=self.window, workspace=self._workspace.data_ptr(),
+                             workspace_bytes=self._bytes, cache=_Cache(heads=self.kv_heads, head_dim=self.head_dim))
         self._at, self._device = ctypes.addressof(self._args), self.device.index
+
+    # a copy (copy, deepcopy, pickle) is a plan with a workspace of its own
+    def __getstate__(self):
+        return {k: v for k, v in self.__dict__.items() if k not in ("_bytes", "_failed", "_stream", "_workspace", "_raw", "_lock", "_args", "_at")}
+
+    def __setstate__(self, state):
+        self.__dict__.update(state)
+        self._make()
 
     def failed(self):
         """Whether a wait inside a kernel of this plan has ever run out (after two seconds: its outputs are worth
@@ -275,7 +287,8 @@ class AttendPlan:
         if stream is not None:
             with torch.cuda.stream(stream):
                 return self.attend(q, cache, block_table, seq_lens, out=out, return_lse=return_lse)
-        if _raw_stream(self._device) != self._raw:
-            self._order()
-        return _entry.attend(self._at, self._device, self.max_requests, self.head_dim, q, cache._at, cache._maps_at, cache._device, block_table, seq_lens,
-                             out, return_lse)
+        with self._lock:  # from a call's place in the order to its launch
+            if _raw_stream(self._device) != self._raw:
+                self._order()
+            return _entry.attend(self._at, self._device, self.max_requests, self.head_dim, q, cache._at, cache._maps_at, cache._device, block_table,
+                                 seq_lens, out, return_lse)

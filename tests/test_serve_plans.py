@@ -44,3 +44,61 @@ def test_a_rope_plan_that_was_refused_is_freed_quietly():
     with pytest.raises(B.AmapError):
         ops.RopePlan(64, scale=float("inf"))
     gc.collect()
+
+
+def attend_plan(monkeypatch):
+    """An AttendPlan without its device memory, and a list of what its calls do in which order."""
+    done = []
+
+    def make(plan):
+        plan._lock, plan._raw, plan._at = threading.Lock(), 1, object()
+
+    monkeypatch.setattr(ops.AttendPlan, "_make", make, raising=False)
+    plan = object.__new__(ops.AttendPlan)
+    plan.max_requests, plan.q_heads, plan.kv_heads, plan.head_dim = 4, 8, 2, 64
+    plan.scale, plan.window, plan.softcap, plan.device, plan._device = 0.125, 0, 0.0, torch.device("cuda", 0), 0
+    make(plan)
+    return plan, done
+
+
+@pytest.mark.parametrize("how", [copy.copy, copy.deepcopy, lambda x: pickle.loads(pickle.dumps(x))])
+def test_a_copied_attend_plan_has_a_workspace_of_its_own(how, monkeypatch):
+    plan, _ = attend_plan(monkeypatch)
+    plan.window = 77
+    other = how(plan)
+    assert other._at is not plan._at and other._lock is not plan._lock
+    assert (other.max_requests, other.q_heads, other.kv_heads, other.head_dim, other.scale, other.window, other.device) == (4, 8, 2, 64, 0.125, 77, plan.device)
+
+
+def test_calls_from_two_threads_keep_their_order(monkeypatch):
+    """Between a call's taking its place behind the plan's last stream and its launch, no other call takes one."""
+    plan, done = attend_plan(monkeypatch)
+    streams = {}
+    inside, go_on = threading.Event(), threading.Event()
+
+    def order(self):
+        me = streams[threading.get_ident()]
+        done.append(("waits for", self._raw, me))
+        self._raw = me
+        if me == 2:
+            inside.set()
+            go_on.wait(2)
+
+    monkeypatch.setattr(ops.AttendPlan, "_order", order)
+    monkeypatch.setattr(ops, "_raw_stream", lambda device: streams[threading.get_ident()])
+    monkeypatch.setattr(ops, "_entry", types.SimpleNamespace(attend=lambda *a: done.append(("launched on", streams[threading.get_ident()]))))
+    cache = types.SimpleNamespace(_at=0, _maps_at=0, _device=0)
+
+    def call(stream):
+        streams[threading.get_ident()] = stream
+        plan.attend(None, cache, None, None)
+
+    first, second = threading.Thread(target=call, args=(2,)), threading.Thread(target=call, args=(3,))
+    first.start()
+    assert inside.wait(5)
+    second.start()
+    second.join(0.3)
+    go_on.set()
+    first.join(5)
+    second.join(5)
+    assert done == [("waits for", 1, 2), ("launched on", 2), ("waits for", 2, 3), ("launched on", 3)]
