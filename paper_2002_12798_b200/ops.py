@@ -22,6 +22,7 @@ from collections import namedtuple
 from ctypes import POINTER, Structure, byref, c_char_p, c_double, c_float, c_int32, c_int64, c_uint64, c_void_p
 
 import torch
+from torch.autograd import forward_ad
 
 from . import build as _build
 from .binding import AmapError, LIBRARY_PATH
@@ -142,19 +143,39 @@ class PagedCache:
 # ----------------------------------------------------------------------------------------------------------------------
 # rotary positions
 # ----------------------------------------------------------------------------------------------------------------------
+def _tracked(tensors):
+    """Whether autograd, backward or forward, follows one of the tensors."""
+    if torch.is_grad_enabled():
+        for x in tensors:
+            if x.requires_grad:
+                return True
+    if forward_ad._current_level >= 0:
+        return any(forward_ad.unpack_dual(x).tangent is not None for x in tensors)
+    return False
+
+
 class _Rotate(torch.autograd.Function):
+    """The turn is linear and its own transpose with the angle negated: derivatives are turns again, of every order."""
+
     @staticmethod
     def forward(ctx, plan, positions, inverse, *xs):
         ctx.save_for_backward(positions)
-        ctx.plan, ctx.inverse = plan, inverse
+        ctx.save_for_forward(positions)
+        ctx.plan, ctx.inverse, ctx.like = plan, inverse, [(x.shape, x.dtype, x.device) for x in xs]
         return tuple(_entry.rotate(plan._h, plan.head_dim, plan.n_axes, xs, positions, inverse, None))
 
     @staticmethod
     def backward(ctx, *grads):
         (positions,) = ctx.saved_tensors
         grads = [g if g.stride(2) == 1 else g.contiguous() for g in grads]
-        plan = ctx.plan
-        return (None, None, None, *_entry.rotate(plan._h, plan.head_dim, plan.n_axes, grads, positions, not ctx.inverse, None))
+        return (None, None, None, *_Rotate.apply(ctx.plan, positions, not ctx.inverse, *grads))
+
+    @staticmethod
+    def jvp(ctx, _plan, _positions, _inverse, *tangents):
+        (positions,) = ctx.saved_tensors
+        tangents = [torch.zeros(shape, dtype=dtype, device=device) if t is None else t if t.stride(2) == 1 else t.contiguous()
+                    for t, (shape, dtype, device) in zip(tangents, ctx.like)]
+        return tuple(_Rotate.apply(ctx.plan, positions, ctx.inverse, *tangents))
 
 
 class RopePlan:
@@ -205,15 +226,13 @@ class RopePlan:
     def rotate(self, xs, positions, *, inverse=False, outs=None, stream=None):
         """Turns up to four tensors [tokens, heads, head_dim] (q and k) by the same positions in one launch; returns
         the results in a list.  inverse=True turns back, which is the gradient; tensors that require one are
-        differentiated through.  outs: tensors to write to (an x itself for in place)."""
+        differentiated through, to any order and in either mode.  outs: tensors to write to (an x itself for in place)."""
         if stream is not None:
             with torch.cuda.stream(stream):
                 return self.rotate(xs, positions, inverse=inverse, outs=outs)
-        if torch.is_grad_enabled():
-            for x in xs:
-                if x.requires_grad:
-                    _require(outs is None, "rotate: no outs where a gradient is required")
-                    return list(_Rotate.apply(self, positions, bool(inverse), *xs))
+        if _tracked(xs):
+            _require(outs is None, "rotate: no outs where a gradient is required")
+            return list(_Rotate.apply(self, positions, bool(inverse), *xs))
         return _entry.rotate(self._h, self.head_dim, self.n_axes, xs, positions, inverse, outs)
 
     def append(self, q, k, v, positions, slots, cache, *, out=None, stream=None):

@@ -102,3 +102,85 @@ def test_calls_from_two_threads_keep_their_order(monkeypatch):
     first.join(5)
     second.join(5)
     assert done == [("waits for", 1, 2), ("launched on", 2), ("waits for", 2, 3), ("launched on", 3)]
+
+
+# ----------------------------------------------------------------------------------------------------------------------
+# autograd, with the turn in plain torch in the entry's place
+# ----------------------------------------------------------------------------------------------------------------------
+@pytest.fixture
+def plain_entry(monkeypatch):
+    calls = []
+
+    def rotate(h, dim, axes, xs, positions, inverse, outs):
+        calls.append(("rotate", bool(inverse)))
+        with torch.no_grad():
+            c, s = positions.double().cos()[:, None, None], positions.double().sin()[:, None, None] * (-1 if inverse else 1)
+            got = [torch.cat([x[..., : dim // 2] * c - x[..., dim // 2 :] * s, x[..., dim // 2 :] * c + x[..., : dim // 2] * s], -1) for x in xs]
+            if outs is not None:
+                for o, g in zip(outs, got):
+                    o.copy_(g)
+            return got if outs is None else list(outs)
+
+    def append(h, dim, axes, q, k, v, positions, slots, at, device, out):
+        calls.append(("append",))
+        return q.detach() * 2 if out is None else out
+
+    def attend(*a):
+        calls.append(("attend",))
+        q, lse = a[4], a[11]
+        got = q.detach() * 3
+        return (got, got.sum(-1)) if lse else got
+
+    monkeypatch.setattr(ops, "_entry", types.SimpleNamespace(rotate=rotate, append=append, attend=attend))
+    return calls
+
+
+def doubles(*shape):
+    return torch.randn(*shape, dtype=torch.float64)
+
+
+def test_rotate_has_derivatives_of_every_order(plain_entry):
+    torch.manual_seed(0)
+    plan, pos = ops.RopePlan(4), torch.tensor([0.3, 1.0, 2.0])
+    q, k = doubles(3, 2, 4).requires_grad_(), doubles(3, 1, 4).requires_grad_()
+    assert torch.autograd.gradcheck(lambda q, k: tuple(plan.rotate([q, k], pos)), (q, k))
+    assert torch.autograd.gradgradcheck(lambda q, k: tuple(plan.rotate([q, k], pos)), (q, k))
+    # a penalty on the gradient: its own gradient goes through the gradient's turn
+    weight = doubles(3, 2, 4).requires_grad_()
+    (g,) = torch.autograd.grad((plan.rotate([q], pos)[0] * weight).sum(), [q], create_graph=True)
+    assert g.requires_grad
+    (gw,) = torch.autograd.grad((g * g).sum(), [weight])
+    assert torch.allclose(gw, 2 * weight)  # a turn keeps lengths
+
+
+def test_rotate_carries_tangents(plain_entry):
+    from torch.autograd import forward_ad
+
+    plan, pos = ops.RopePlan(4), torch.tensor([0.3, 1.0, 2.0])
+    q, k, t = doubles(3, 2, 4), doubles(3, 1, 4), doubles(3, 2, 4)
+    with torch.no_grad(), forward_ad.dual_level():
+        a, b = plan.rotate([forward_ad.make_dual(q, t), k], pos, inverse=True)
+        value, tangent = forward_ad.unpack_dual(a)
+        other = forward_ad.unpack_dual(b).tangent
+        assert torch.equal(value, plan.rotate([q], pos, inverse=True)[0])
+        assert torch.equal(tangent, plan.rotate([t], pos, inverse=True)[0])
+        assert other is None or not other.any()
+        with pytest.raises(ValueError, match="outs"):
+            plan.rotate([forward_ad.make_dual(q, t)], pos, outs=[torch.empty_like(q)])
+
+
+@pytest.mark.gpu
+def test_rotate_has_derivatives_on_the_gpu():
+    from torch.autograd import forward_ad
+
+    torch.manual_seed(1)
+    plan, pos = ops.RopePlan(64, 32), torch.arange(7, dtype=torch.int32, device="cuda")
+    q, k, w, t = (torch.randn(7, n, 64, device="cuda") for n in (4, 1, 4, 4))
+    q.requires_grad_(), w.requires_grad_()
+    (g,) = torch.autograd.grad((plan.rotate([q, k], pos)[0] * w).sum(), [q], create_graph=True)
+    (gw,) = torch.autograd.grad((g * g).sum(), [w])
+    assert torch.allclose(gw, 2 * w, rtol=1e-5, atol=1e-5)
+    with torch.no_grad(), forward_ad.dual_level():
+        a, b = plan.rotate([forward_ad.make_dual(q.detach(), t), k], pos)
+        assert torch.equal(forward_ad.unpack_dual(a).tangent, plan.rotate([t], pos)[0])
+        assert not torch.count_nonzero(forward_ad.unpack_dual(b).tangent)
