@@ -8,7 +8,9 @@
 #include <ATen/core/LegacyTypeDispatch.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
+#include <c10/core/AutogradState.h>
 #include <torch/csrc/Exceptions.h>
+#include <torch/csrc/autograd/VariableTypeUtils.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstring>
@@ -126,6 +128,11 @@ inline Positions positions_of(PyObject *o, int64_t tokens, int64_t axes, int dev
   const int bits = t.scalar_type() == at::kInt ? 32 : t.scalar_type() == at::kLong ? 64 : 0;
   require(bits != 0, "positions: int32 or int64");
   return {t.data_ptr(), d == 2 ? t.stride(0) : 0, t.stride(d - 1), bits};
+}
+
+// whether autograd, backward or forward, follows t at this call
+inline bool tracked(const at::Tensor &t) {
+  return (t.requires_grad() && at::GradMode::is_enabled()) || (c10::AutogradState::get_tls_state().get_fw_grad_mode() && torch::autograd::isFwGradDefined(t));
 }
 
 inline PyObject *wrap(at::Tensor t) {
@@ -258,10 +265,12 @@ PyObject *rotate(PyObject *const *a) {
   return all;
 }
 
-// plan, head_dim, axes, q, k, v, positions, slots, cache, its device, out (None) -> out
+// plan, head_dim, axes, q, k, v, positions, slots, cache, its device, out (None) -> out; NotImplemented, and nothing done, where
+// autograd follows an input
 PyObject *append(PyObject *const *a) {
   const int64_t dim = integer(a[1]);
   const at::Tensor &q = tensor(a[3], "q"), &k = tensor(a[4], "k"), &v = tensor(a[5], "v");
+  if (C10_UNLIKELY(tracked(q) || tracked(k) || tracked(v))) Py_RETURN_NOTIMPLEMENTED;
   const int device = cuda_of(q);
   void *stream = stream_of(device);
   heads_of(q, "q", dim, device);
@@ -286,7 +295,7 @@ PyObject *append(PyObject *const *a) {
 }
 
 // the plan's fixed arguments, its device, most requests, head_dim, q, cache, maps, the cache's device, block_table, seq_lens, out (None), lse (bool)
-// -> out, or (out, lse)
+// -> out, or (out, lse); NotImplemented, and nothing done, where autograd follows q
 PyObject *attend(PyObject *const *a) {
   amap_attend_args g;
   memcpy(&g, address<const amap_attend_args>(a[0]), sizeof g);  // q_heads, cache.heads, scale, softcap, window, workspace
@@ -294,6 +303,7 @@ PyObject *attend(PyObject *const *a) {
   void *stream = stream_of(device);
   const int64_t dim = integer(a[3]);
   const at::Tensor &q = tensor(a[4], "q");
+  if (C10_UNLIKELY(tracked(q))) Py_RETURN_NOTIMPLEMENTED;
   heads_of(q, "q", dim, device);
   const Table t = table_of(a[8]);
   const int32_t kv_heads = g.cache.heads;

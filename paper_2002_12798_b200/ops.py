@@ -147,11 +147,33 @@ def _tracked(tensors):
     """Whether autograd, backward or forward, follows one of the tensors."""
     if torch.is_grad_enabled():
         for x in tensors:
-            if x.requires_grad:
+            if getattr(x, "requires_grad", False):  # what is no tensor is refused later
                 return True
-    if forward_ad._current_level >= 0:
-        return any(forward_ad.unpack_dual(x).tangent is not None for x in tensors)
+    if forward_ad._current_level >= 0 and torch._C._is_fwd_grad_enabled():
+        return any(isinstance(x, torch.Tensor) and forward_ad.unpack_dual(x).tangent is not None for x in tensors)
     return False
+
+
+class _NoDerivative(torch.autograd.Function):
+    """A call that has none: its results are as without autograd, and asking for their derivative says so."""
+
+    @staticmethod
+    def forward(ctx, name, call, args, *inputs):
+        ctx.name = name
+        return call(*args)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("%s is not differentiable" % ctx.name)
+
+    @staticmethod
+    def jvp(ctx, *tangents):
+        raise RuntimeError("%s is not differentiable" % ctx.name)
+
+
+def _without_derivative(name, call, args, out, *inputs):  # where the entry has launched nothing, as autograd follows an input
+    _require(out is None, "%s: no out where a gradient is required" % name)
+    return _NoDerivative.apply(name, call, args, *inputs)
 
 
 class _Rotate(torch.autograd.Function):
@@ -238,11 +260,15 @@ class RopePlan:
     def append(self, q, k, v, positions, slots, cache, *, out=None, stream=None):
         """One step of a decoder layer before its attention (amap_rope_append): returns the rotated q [tokens, heads,
         head_dim] and writes the rotated k and the v [tokens, cache.heads, head_dim] to the slots (int32 [tokens], -1
-        for none) of the cache.  Views of a fused projection are taken as they are.  Not differentiable."""
+        for none) of the cache.  Views of a fused projection are taken as they are.  Not differentiable: a result that
+        autograd follows raises when its derivative is asked for."""
         if stream is not None:
             with torch.cuda.stream(stream):
                 return self.append(q, k, v, positions, slots, cache, out=out)
-        return _entry.append(self._h, self.head_dim, self.n_axes, q, k, v, positions, slots, cache._at, cache._device, out)
+        got = _entry.append(self._h, self.head_dim, self.n_axes, q, k, v, positions, slots, cache._at, cache._device, out)
+        if got is not NotImplemented:
+            return got
+        return _without_derivative("append", self.append, (q, k, v, positions, slots, cache), out, q, k, v)
 
 
 # ----------------------------------------------------------------------------------------------------------------------
@@ -302,10 +328,16 @@ class AttendPlan:
         """q: [requests, q_heads, head_dim]; row r is the newest token of the request in row r of block_table (int32
         [requests, pages]), which holds seq_lens[r] tokens (int32), the newest included.  Returns the output, shaped
         like q; with return_lse=True also the fp32 logarithm of the softmax's sum [requests, q_heads].  A request
-        without tokens gets zeros and -inf."""
+        without tokens gets zeros and -inf.  Not differentiable, as append."""
         if stream is not None:
             with torch.cuda.stream(stream):
                 return self.attend(q, cache, block_table, seq_lens, out=out, return_lse=return_lse)
+        got = self._attend(q, cache, block_table, seq_lens, out, return_lse)
+        if got is not NotImplemented:
+            return got
+        return _without_derivative("attend", self._attend, (q, cache, block_table, seq_lens, None, return_lse), out, q)
+
+    def _attend(self, q, cache, block_table, seq_lens, out, return_lse):
         with self._lock:  # from a call's place in the order to its launch
             if _raw_stream(self._device) != self._raw:
                 self._order()

@@ -123,11 +123,15 @@ def plain_entry(monkeypatch):
 
     def append(h, dim, axes, q, k, v, positions, slots, at, device, out):
         calls.append(("append",))
+        if ops._tracked((q, k, v)):
+            return NotImplemented
         return q.detach() * 2 if out is None else out
 
     def attend(*a):
         calls.append(("attend",))
         q, lse = a[4], a[11]
+        if ops._tracked((q,)):
+            return NotImplemented
         got = q.detach() * 3
         return (got, got.sum(-1)) if lse else got
 
@@ -169,6 +173,36 @@ def test_rotate_carries_tangents(plain_entry):
             plan.rotate([forward_ad.make_dual(q, t)], pos, outs=[torch.empty_like(q)])
 
 
+CACHE = types.SimpleNamespace(_at=0, _maps_at=0, _device=0)
+
+
+def test_append_and_attend_say_that_they_have_no_derivative(plain_entry, monkeypatch):
+    """Their results are what they were; asking for the gradient raises instead of leaving it out."""
+    from torch.autograd import forward_ad
+
+    rope, (attention, _) = ops.RopePlan(4), attend_plan(monkeypatch)
+    monkeypatch.setattr(ops, "_raw_stream", lambda device: attention._raw)
+    q, k = doubles(3, 2, 4), doubles(3, 1, 4)
+    for call in (lambda q, k, **o: rope.append(q, k, k, None, None, CACHE, **o), lambda q, k, **o: attention.attend(q, CACHE, None, None, **o)):
+        plain = call(q, k)
+        assert not plain.requires_grad
+        asked = call(q.clone().requires_grad_(), k)
+        assert torch.equal(asked.detach(), plain)
+        with pytest.raises(RuntimeError, match="not differentiable"):
+            asked.sum().backward()
+        with pytest.raises(ValueError, match="out"):
+            call(q.clone().requires_grad_(), k, out=torch.empty_like(q))
+        with torch.no_grad():
+            assert not call(q.clone().requires_grad_(), k).requires_grad
+            with forward_ad.dual_level(), pytest.raises(RuntimeError, match="not differentiable"):
+                call(forward_ad.make_dual(q, q), k)
+    with pytest.raises(RuntimeError, match="not differentiable"):  # k and v, too
+        rope.append(q, k.clone().requires_grad_(), k, None, None, CACHE).sum().backward()
+    out, lse = attention.attend(q.clone().requires_grad_(), CACHE, None, None, return_lse=True)
+    with pytest.raises(RuntimeError, match="not differentiable"):
+        lse.sum().backward()
+
+
 @pytest.mark.gpu
 def test_rotate_has_derivatives_on_the_gpu():
     from torch.autograd import forward_ad
@@ -184,3 +218,18 @@ def test_rotate_has_derivatives_on_the_gpu():
         a, b = plan.rotate([forward_ad.make_dual(q.detach(), t), k], pos)
         assert torch.equal(forward_ad.unpack_dual(a).tangent, plan.rotate([t], pos)[0])
         assert not torch.count_nonzero(forward_ad.unpack_dual(b).tangent)
+
+
+@pytest.mark.gpu
+def test_append_and_attend_say_so_on_the_gpu():
+    k, v = (torch.randn(2, 16, 2, 64, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    cache, rope, attention = ops.PagedCache(k, v), ops.RopePlan(64), ops.AttendPlan(1, 4, 2, 64)
+    q, kk = torch.randn(1, 4, 64, device="cuda", dtype=torch.bfloat16), torch.randn(1, 2, 64, device="cuda", dtype=torch.bfloat16)
+    one = dict(dtype=torch.int32, device="cuda")
+    pos, slot, table, n = torch.tensor([3], **one), torch.tensor([-1], **one), torch.tensor([[1, 0]], **one), torch.tensor([20], **one)
+    for call in (lambda q: rope.append(q, kk, kk, pos, slot, cache), lambda q: attention.attend(q, cache, table, n),
+                 lambda q: attention.attend(q, cache, table, n, return_lse=True)[1]):
+        plain, asked = call(q), call(q.clone().requires_grad_())
+        assert torch.equal(plain, asked.detach()) and not plain.requires_grad
+        with pytest.raises(RuntimeError, match="not differentiable"):
+            asked.float().sum().backward()
