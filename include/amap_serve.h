@@ -142,8 +142,9 @@ int amap_rope_plan(int32_t head_dim,       /* 1 .. AMAP_ROPE_MAX_DIM */
                    int32_t pairs, float scale, amap_rope_t **out);
 void amap_rope_destroy(amap_rope_t *plan);
 
-/* rows x heads x head_dim elements: x is read, y written (y may be x itself with x's strides; else they must not
- * overlap) */
+/* rows x heads x head_dim elements: x is read, y written (y may be x itself with x's strides; else y must not overlap
+ * any part's x).  No element of a y may be one of another part's x or y: parts turned in place may lie side by side in
+ * one buffer, with the same row stride where their bytes interleave. */
 typedef struct amap_rope_part {
   const void *x;
   void *y;

@@ -15,6 +15,7 @@
 #include <cstring>
 #include <new>
 
+#include "serve_alias.hpp"
 #include "serve_common.cuh"
 
 using namespace amap_serve;
@@ -384,6 +385,10 @@ Span rows_span(int64_t rows, int64_t row, int heads, int64_t head, int dim, int 
   return s;
 }
 
+Runs runs(const void *at, int64_t rows, int64_t row, int heads, int64_t head, int es) {
+  return {(int64_t) reinterpret_cast<uintptr_t>(at), rows, row * es, heads, head * es};
+}
+
 }  // namespace
 
 extern "C" int amap_rope_plan(int32_t head_dim, int32_t rotary_dim, const double *inv_freq, const int32_t *axis, int32_t n_axes,
@@ -438,14 +443,21 @@ extern "C" int amap_rope_rotate(const amap_rope_t *plan, const amap_rope_args *a
   }
   // an output laid over an input is a race, unless the part is turned in place; parts turned in place may interleave in
   // one buffer (q and k of a fused projection), whose byte ranges overlap without sharing an element
+  const int64_t width = (int64_t)plan->head_dim * es;
   for (int k = 0; k < a->n_parts; ++k) {
     const amap_rope_part &s = a->part[k];
-    if (s.x == s.y && s.x_row == s.y_row && s.x_head == s.y_head) continue;
+    const bool in_place = s.x == s.y && s.x_row == s.y_row && s.x_head == s.y_head;
     const Span ys = rows_span(a->rows, s.y_row, s.heads, s.y_head, plan->head_dim, es);
+    const Runs y = runs(s.y, a->rows, s.y_row, s.heads, s.y_head, es);
     for (int j = 0; j < a->n_parts; ++j) {
       const amap_rope_part &r = a->part[j];
-      SERVE_REQUIRE(!overlap(s.y, ys, r.x, rows_span(a->rows, r.x_row, r.heads, r.x_head, plan->head_dim, es)), AMAP_EINVAL,
-                    "part: y overlaps an x that is not its own");
+      if (!in_place)
+        SERVE_REQUIRE(!overlap(s.y, ys, r.x, rows_span(a->rows, r.x_row, r.heads, r.x_head, plan->head_dim, es)), AMAP_EINVAL,
+                      "part: y overlaps an x that is not its own");
+      else
+        SERVE_REQUIRE(j == k || !share(y, runs(r.x, a->rows, r.x_row, r.heads, r.x_head, es), width), AMAP_EINVAL,
+                      "parts: a y shares elements with an x that is not its own");
+      SERVE_REQUIRE(j <= k || !share(y, runs(r.y, a->rows, r.y_row, r.heads, r.y_head, es), width), AMAP_EINVAL, "parts: two y share elements");
     }
   }
   P.n_parts = a->n_parts;
@@ -485,6 +497,11 @@ extern "C" int amap_rope_append(const amap_rope_t *plan, const amap_append_args 
                         !overlap(a->k, rows_span(a->rows, a->k_row, c.heads, a->k_head, plan->head_dim, es), a->q_out, ys) &&
                         !overlap(a->v, rows_span(a->rows, a->v_row, c.heads, a->v_head, plan->head_dim, es), a->q_out, ys),
                     AMAP_EINVAL, "q_out overlaps q, k or v");
+    } else {  // in place: beside k and v in one buffer, but not over them
+      const Runs y = runs(a->q_out, a->rows, a->q_out_row, a->q_heads, a->q_out_head, es);
+      const int64_t width = (int64_t)plan->head_dim * es;
+      SERVE_REQUIRE(!share(y, runs(a->k, a->rows, a->k_row, c.heads, a->k_head, es), width) &&
+                        !share(y, runs(a->v, a->rows, a->v_row, c.heads, a->v_head, es), width), AMAP_EINVAL, "q_out overlaps k or v");
     }
     P.part[n++] = {static_cast<const char *>(a->q), static_cast<char *>(a->q_out), a->q_row, a->q_head, a->q_out_row, a->q_out_head, 0, a->q_heads, kRows,
                    {}, 0, 0, {}};
