@@ -205,7 +205,7 @@ struct Cursor {
   }
   static __device__ __forceinline__ int lowest(const Params &P, int n) { return P.a.window > 0 ? max(0, n - P.a.window) : 0; }
   static __device__ __forceinline__ int tiles(const Params &P, int n) {
-    return max(1, (n + TILE - 1) / TILE - lowest(P, n) / TILE);
+    return max(1, n / TILE + (n % TILE != 0) - lowest(P, n) / TILE);  // n may be 2^31 - 1
   }
   __device__ __forceinline__ void enter(const Params &P) {
     low = lowest(P, n);
@@ -439,7 +439,7 @@ __global__ void __launch_bounds__(kBlock, (kResident<DP, NT>)) attend_kernel(con
     int entry = -1, offset = 0, there = 0;
     auto look = [&](int row) {  // the page of a row of the tile at `at`, if any of the row's box takes part
       const int token = at.t + row;
-      there = token < at.n && token + (P.tensor_copies ? 1 << P.box_shift : 1) > at.low;
+      there = token < at.n && token > at.low - (P.tensor_copies ? 1 << P.box_shift : 1);
       if (there) {
         const uint32_t page = P.div_mul ? __umulhi((uint32_t)token, P.div_mul) >> P.div_shift : (uint32_t)token >> P.div_shift;
         offset = token - (int)page * C.page_size;
