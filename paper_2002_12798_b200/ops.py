@@ -311,10 +311,18 @@ class AttendPlan:
         self._make()
 
     def failed(self):
-        """Whether a wait inside a kernel of this plan has ever run out (after two seconds: its outputs are worth
-        nothing).  Waits for the device."""
+        """Whether a wait inside a kernel of this plan has run out (after two seconds: its outputs, and those of the calls
+        after it, are worth nothing until reset()).  Waits for the device."""
         torch.cuda.synchronize(self.device)
         return bool(self._workspace[self._failed : self._failed + 4].any())
+
+    def reset(self):
+        """Zeroes the workspace, after the plan's calls so far: what failed() calls for.  Kernels leave the workspace ready
+        for the next call by themselves, but not one that has given up."""
+        with torch.cuda.device(self.device), self._lock:
+            if _raw_stream(self._device) != self._raw:
+                self._order()
+            self._workspace.zero_()
 
     def _order(self):
         if torch.cuda.is_current_stream_capturing():

@@ -233,3 +233,25 @@ def test_append_and_attend_say_so_on_the_gpu():
         assert torch.equal(plain, asked.detach()) and not plain.requires_grad
         with pytest.raises(RuntimeError, match="not differentiable"):
             asked.float().sum().backward()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("stream", [False, True])
+def test_reset_makes_a_failed_plan_fit_for_use(stream):
+    """A kernel that gave up is played by the host: the mark set, counters and parts left as they may be."""
+    torch.manual_seed(2)
+    n = 5000
+    k, v = (torch.randn(n // 16 + 1, 16, 2, 64, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    cache, attention = ops.PagedCache(k, v), ops.AttendPlan(3, 8, 2, 64)
+    q = torch.randn(3, 8, 64, device="cuda", dtype=torch.bfloat16)
+    table = torch.arange(n // 16 + 1, dtype=torch.int32, device="cuda").repeat(3, 1)
+    lens = torch.tensor([n, 100, n - 7], dtype=torch.int32, device="cuda")
+    want = attention.attend(q, cache, table, lens)
+    assert not attention.failed()
+    attention._workspace.fill_(1)
+    assert attention.failed()
+    side = torch.cuda.Stream() if stream else torch.cuda.current_stream()
+    with torch.cuda.stream(side):
+        attention.reset()
+    got = attention.attend(q, cache, table, lens)
+    assert not attention.failed() and torch.equal(got, want)
