@@ -94,6 +94,9 @@ int amap_pages_extend(const amap_pages_extend_args *args /* host */, void *cuda_
 /* amap_pages_release: the pages of the requests with done[r] != 0 go back on
  * the stack, request by request in the order of their tokens, on top of what
  * is there; seq_lens_out[r] is 0 for them and seq_lens[r] for the others.
+ * A negative table entry is a hole (a page given back earlier, behind a window)
+ * and is passed over; amap_pages_release_within passes over every entry outside
+ * [0, n_pages).
  * free_pages changes only at and above *free_count; what does not fit
  * free_capacity is dropped and not counted.  Table rows keep their entries. */
 typedef struct amap_pages_release_args {
@@ -111,6 +114,7 @@ typedef struct amap_pages_release_args {
   int32_t *free_count_out;
 } amap_pages_release_args;
 int amap_pages_release(const amap_pages_release_args *args /* host */, void *cuda_stream);
+int amap_pages_release_within(const amap_pages_release_args *args /* host */, int32_t n_pages, void *cuda_stream);
 
 /* ---------------------------------------------------------------------------
  * Rotary positions with several axes.  The first rotary_dim elements of a head

@@ -205,7 +205,7 @@ PyObject *extend(PyObject *const *a) {
   return a[8];
 }
 
-// done, seq_lens, block_table, free_pages, free_count, page_size -> seq_lens, free_count
+// done, seq_lens, block_table, free_pages, free_count, page_size, n_pages (None) -> seq_lens, free_count
 PyObject *release(PyObject *const *a) {
   const Table t = table_of(a[2]);
   void *stream = stream_of(t.device);
@@ -222,7 +222,7 @@ PyObject *release(PyObject *const *a) {
   at::AutoDispatchBelowADInplaceOrView plain;
   const at::Tensor whole = at::empty({(int64_t)t.rows + 1}, free_pages.options());
   g.seq_lens_out = static_cast<int32_t *>(whole.data_ptr()), g.free_count_out = g.seq_lens_out + t.rows;
-  check(amap_pages_release(&g, stream), "amap_pages_release");
+  check(amap_pages_release_within(&g, a[6] == Py_None ? INT32_MAX : integer32(a[6]), stream), "amap_pages_release");
   const at::Tensor out[2] = {whole.narrow(0, 0, t.rows), whole.narrow(0, t.rows, 1)};
   return wrap_all(out, 2);
 }
@@ -334,7 +334,7 @@ PyObject *refuse_with(PyObject *, PyObject *error) {
 }
 
 #define ENTRY(name, n) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(&guarded<name, n>)), METH_FASTCALL, nullptr}
-PyMethodDef kMethods[] = {ENTRY(extend, 9), ENTRY(release, 6), ENTRY(rotate, 7), ENTRY(append, 11), ENTRY(attend, 12),
+PyMethodDef kMethods[] = {ENTRY(extend, 9), ENTRY(release, 7), ENTRY(rotate, 7), ENTRY(append, 11), ENTRY(attend, 12),
                           {"refuse_with", refuse_with, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_serve_torch", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 

@@ -28,7 +28,7 @@ from . import build as _build
 from .binding import AmapError, LIBRARY_PATH
 
 EXPORTS = [
-    "amap_pages_extend", "amap_pages_release", "amap_rope_plan", "amap_rope_destroy", "amap_rope_rotate",
+    "amap_pages_extend", "amap_pages_release", "amap_pages_release_within", "amap_rope_plan", "amap_rope_destroy", "amap_rope_rotate",
     "amap_rope_append", "amap_cache_encode", "amap_attend", "amap_attend_workspace", "amap_serve_error",
 ]
 _BF16, _FP16, _FP32, _E4M3 = 1, 2, 3, 4
@@ -108,13 +108,14 @@ def pages_extend(new_lens, seq_lens, block_table, free_pages, free_count, page_s
     return out if out is not None else PagesStep._make(got)
 
 
-def pages_release(done, seq_lens, block_table, free_pages, free_count, page_size, *, stream=None):
+def pages_release(done, seq_lens, block_table, free_pages, free_count, page_size, *, n_pages=None, stream=None):
     """Puts the pages of the requests with done[r] (bool or uint8 [R]) back on the stack free_pages, in place
-    (amap_pages_release).  Returns (seq_lens, free_count) to be used from now on in place of the inputs."""
+    (amap_pages_release).  Negative table entries are holes and are passed over; with n_pages, so is every entry beyond
+    its pages.  Returns (seq_lens, free_count) to be used from now on in place of the inputs."""
     if stream is not None:
         with torch.cuda.stream(stream):
-            return pages_release(done, seq_lens, block_table, free_pages, free_count, page_size)
-    return _entry.release(done, seq_lens, block_table, free_pages, free_count, page_size)
+            return pages_release(done, seq_lens, block_table, free_pages, free_count, page_size, n_pages=n_pages)
+    return _entry.release(done, seq_lens, block_table, free_pages, free_count, page_size, n_pages)
 
 
 # ----------------------------------------------------------------------------------------------------------------------
