@@ -1,11 +1,16 @@
 """Operators on the heads that a composed map has split: rotary positions, a paged key/value cache, and the attention
 of one new token per request (include/amap_serve.h has the definitions; this module marshals arguments).
 
-One decoding step, for every layer the last two lines:
+One decoding step, for every layer the lines from `append` on:
 
     step = ops.pages_extend(new_lens, seq_lens, block_table, free_pages, free_count, page_size, max_tokens)
     q = rope.append(q, k, v, step.positions, step.slots, cache)
-    out = attention.attend(q, cache, block_table, step.seq_lens)
+    rows = q.new_zeros(max_requests + 1, q_heads, 128)
+    rows[step.requests.long()] = q
+    out = attention.attend(rows[:-1], cache, block_table, step.seq_lens)
+
+append takes the step's tokens, one behind the other; attend a row per request, of which some may have no token in the
+step (idle, or refused).  Where every request has one, `rows` is q.
 
 Calls enqueue one kernel on the current CUDA stream (or `stream`) and neither synchronise nor copy to the host, so a
 step can be captured in a CUDA graph.  Tensors a call is given must stay alive and unchanged until that stream has run
