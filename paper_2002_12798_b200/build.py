@@ -48,24 +48,35 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
     return LIB
 
 
+def _entry_stale(mark: str) -> bool:
+    """Older than its sources, or of another PyTorch or Python (it carries the mark of those it was built against)."""
+    if not os.path.exists(TORCH_ENTRY):
+        return True
+    deps = [os.path.join(CSRC, "serve_torch.cpp"), os.path.join(INCLUDE, "amap.h"), os.path.join(INCLUDE, "amap_serve.h")]
+    if any(os.path.getmtime(d) > os.path.getmtime(TORCH_ENTRY) for d in deps):
+        return True
+    with open(TORCH_ENTRY, "rb") as f:
+        return mark.encode() not in f.read()
+
+
 def build_torch_entry(force: bool = False) -> str:
     """_serve_torch.so; libamap.so, which it calls, is built first and found beside it."""
-    lib = build_library()
-    src = os.path.join(CSRC, "serve_torch.cpp")
-    deps = [src, os.path.join(INCLUDE, "amap.h"), os.path.join(INCLUDE, "amap_serve.h")]
-    if not force and os.path.exists(TORCH_ENTRY) and all(os.path.getmtime(d) <= os.path.getmtime(TORCH_ENTRY) for d in deps):
-        return TORCH_ENTRY
     import sysconfig
 
     import torch
 
+    lib = build_library()
+    src = os.path.join(CSRC, "serve_torch.cpp")
+    mark = "built against PyTorch %s, Python %s;" % (torch.__version__, sysconfig.get_config_var("SOABI"))
+    if not force and not _entry_stale(mark):
+        return TORCH_ENTRY
     there = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(_nvcc()))
     tmp = TORCH_ENTRY + ".tmp%d" % os.getpid()
     cmd = [os.environ.get("CXX", "g++"), "-std=c++17", "-O2", "-shared", "-fPIC", "-fvisibility=hidden", "-Wall", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch.compiled_with_cxx11_abi()]
     for d in [os.path.join(there, "include"), os.path.join(there, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"], os.path.join(cuda, "include")]:
         cmd += ["-isystem", d]
-    cmd += ["-I", INCLUDE, src, "-o", tmp]
+    cmd += ["-I", INCLUDE, '-DSERVE_BUILT_AGAINST="%s"' % mark, src, "-o", tmp]
     cmd += ["-L", os.path.join(there, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-L", HERE, "-l:" + os.path.basename(lib), "-Wl,-rpath,$ORIGIN"]
     subprocess.check_call(cmd)
     os.replace(tmp, TORCH_ENTRY)

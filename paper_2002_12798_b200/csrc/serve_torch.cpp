@@ -336,7 +336,9 @@ PyObject *refuse_with(PyObject *, PyObject *error) {
 #define ENTRY(name, n) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(&guarded<name, n>)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {ENTRY(extend, 9), ENTRY(release, 7), ENTRY(rotate, 7), ENTRY(append, 11), ENTRY(attend, 12),
                           {"refuse_with", refuse_with, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
-PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_serve_torch", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
+// the build looks for this text in the library (build.py)
+const char kBuiltAgainst[] = SERVE_BUILT_AGAINST;
+PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_serve_torch", kBuiltAgainst, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 
