@@ -111,6 +111,12 @@ __device__ __noinline__ bool bar_wait_slow(uint32_t bar, uint32_t parity, int32_
 __device__ __forceinline__ void bar_wait(uint32_t bar, uint32_t parity, int32_t *failed, bool &alive) {
   if (!bar_try(bar, parity) && alive) alive = bar_wait_slow(bar, parity, failed);
 }
+// What a warp that has given up does before it ends: it waits, as long again for each stage, for the last copies into the
+// ring, which a block must not leave behind it.  Stages before `stage` were filled last in the lap whose phase has `parity`,
+// the others in the lap before (there is none before the first, and then this wait is over at once).
+__device__ __noinline__ void settle(uint32_t full, int stages, int stage, uint32_t parity, int32_t *failed) {
+  for (int s = 0; s < stages; ++s) bar_wait_slow(full + 8 * s, s < stage ? parity : parity ^ 1, failed);
+}
 __device__ __forceinline__ void sync_consumers() { asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory"); }
 
 __device__ __forceinline__ void load4(uint32_t at, uint32_t (&r)[4]) {
@@ -541,7 +547,11 @@ __global__ void __launch_bounds__(kBlock, (kResident<DP, NT>)) attend_kernel(con
         if (++stage == S) stage = 0, parity ^= 1;
       }
     }
-    if (aside && __all_sync(~0u, alive)) {
+    if (!__all_sync(~0u, alive)) {
+      settle(smem_at(&small.full[0]), S, stage, parity ^ 1, P.failed);
+      return;
+    }
+    if (aside) {
       asm volatile("bar.sync 2, %0;" ::"n"(kBlock) : "memory");  // the four warps have written the first item's part
       const int h = small.begin[1] * P.members + member, r = small.begin[0], in_group = h % P.blocks_per_head * HB;
       auto slot_of = [&](int i) { return 2 * ((first_from + i) * P.members + member) + (i == 0 ? 1 : 0); };
@@ -1014,6 +1024,7 @@ __global__ void __launch_bounds__(kBlock, (kResident<DP, NT>)) attend_kernel(con
       clear();
     }
   }
+  if (!alive) settle(smem_at(&small.full[0]), S, stage, parity, P.failed);
 }
 
 template <int CT, bool FP8, int DP, int NT>

@@ -71,3 +71,28 @@ def test_short_requests_behind_joined_ones(dim, heads, long, parts):
     bound, lse_bound = ref.attend_bound(want, size, mass, dim, "bf16")
     assert (np.abs(f64(out)[some] - want) <= bound).all()
     assert (np.abs(f64(lse)[some] - want_lse) <= lse_bound + 2.0**-22 * np.abs(want_lse)).all()
+
+
+def test_a_warp_that_gave_up_waits_for_the_last_copies():
+    """`settle` on a model of the ring's barriers: for every number of fills it waits for each stage's last, and for no phase
+    that nothing will complete."""
+    text = open(SOURCE).read()
+    assert "bar_wait_slow(full + 8 * s, s < stage ? parity : parity ^ 1, failed)" in text
+    for name, wait in (("consumer", "settle(smem_at(&small.full[0]), S, stage, parity, P.failed)"), ("producer", "settle(smem_at(&small.full[0]), S, stage, parity ^ 1, P.failed)")):
+        assert wait in text, name
+    assert text.count("if (++stage == S) stage = 0, parity ^= 1;") == 3  # a consumer's step, and the producer's in its two forms
+    for stages in (2, 3, 6):
+        for fills in range(4 * stages + 1):
+            stage, parity = 0, 0  # as a consumer counts; the producer's parity is the other one throughout
+            phases = [0] * stages  # completed, once every copy has landed
+            for _ in range(fills):
+                phases[stage] += 1
+                stage += 1
+                if stage == stages:
+                    stage, parity = 0, parity ^ 1
+            for s in range(stages):
+                waits_for = parity if s < stage else parity ^ 1
+                # a wait for a parity is over when the phase at work has the other one; one copy fewer must not be enough
+                over = lambda completed: completed % 2 != waits_for  # noqa: E731
+                assert over(phases[s])
+                assert phases[s] == 0 or not over(phases[s] - 1)
