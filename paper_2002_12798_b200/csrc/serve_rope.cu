@@ -487,6 +487,7 @@ extern "C" int amap_rope_append(const amap_rope_t *plan, const amap_append_args 
   SERVE_REQUIRE((c.n_pages == 1 || (c.k_page && c.v_page)) && (c.page_size == 1 || (c.k_token && c.v_token)) && (c.heads == 1 || (c.k_head && c.v_head)),
                 AMAP_EINVAL, "the cache's rows lie on one another");
   SERVE_REQUIRE(a->q_heads == 0 || ((a->rows == 1 || a->q_out_row) && (a->q_heads == 1 || a->q_out_head)), AMAP_EINVAL, "rows of q_out lie on one another");
+  const bool e4m3 = c.dtype == AMAP_E4M3;
   Params P = {};
   int n = 0;
   if (a->q_heads) {
@@ -507,9 +508,9 @@ extern "C" int amap_rope_append(const amap_rope_t *plan, const amap_append_args 
                    {}, 0, 0, {}};
   }
   P.part[n++] = {static_cast<const char *>(a->k), static_cast<char *>(c.k), a->k_row, a->k_head, c.k_page, c.k_head, c.k_token, c.heads,
-                 kCacheTurned, divide_by(c.k_scale), 0, 0, {}};
+                 kCacheTurned, e4m3 ? divide_by(c.k_scale) : Divisor(), 0, 0, {}};
   P.part[n++] = {static_cast<const char *>(a->v), static_cast<char *>(c.v), a->v_row, a->v_head, c.v_page, c.v_head, c.v_token,
-                 c.heads, kCacheCopied, divide_by(c.v_scale), 0, 0, {}};
+                 c.heads, kCacheCopied, e4m3 ? divide_by(c.v_scale) : Divisor(), 0, 0, {}};
   P.n_parts = n;
   P.rows = a->rows;
   P.positions = a->positions;
@@ -520,6 +521,6 @@ extern "C" int amap_rope_append(const amap_rope_t *plan, const amap_append_args 
   P.slots = a->slots;
   P.by_page = div_by(c.page_size);
   P.n_slots = c.n_pages * c.page_size;
-  P.e4m3 = c.dtype == AMAP_E4M3;
+  P.e4m3 = e4m3;
   return run_typed(*plan, P, a->dtype, ces, cuda_stream);
 }

@@ -11,6 +11,7 @@
 #include <c10/core/AutogradState.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/VariableTypeUtils.h>
+#include <torch/csrc/autograd/forward_grad.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstring>
@@ -130,9 +131,13 @@ inline Positions positions_of(PyObject *o, int64_t tokens, int64_t axes, int dev
   return {t.data_ptr(), d == 2 ? t.stride(0) : 0, t.stride(d - 1), bits};
 }
 
-// whether autograd, backward or forward, follows t at this call
-inline bool tracked(const at::Tensor &t) {
-  return (t.requires_grad() && at::GradMode::is_enabled()) || (c10::AutogradState::get_tls_state().get_fw_grad_mode() && torch::autograd::isFwGradDefined(t));
+// whether autograd, backward or forward, follows a tensor at this call (a view's tangent is asked for only where there can be
+// one: looking for it costs 0.1 us)
+template <typename... T>
+inline bool tracked(const T &...t) {
+  if ((t.requires_grad() || ...) && at::GradMode::is_enabled()) return true;
+  return c10::AutogradState::get_tls_state().get_fw_grad_mode() && torch::autograd::ForwardADLevel::try_get_by_idx(0) &&
+         (torch::autograd::isFwGradDefined(t) || ...);
 }
 
 inline PyObject *wrap(at::Tensor t) {
@@ -270,7 +275,7 @@ PyObject *rotate(PyObject *const *a) {
 PyObject *append(PyObject *const *a) {
   const int64_t dim = integer(a[1]);
   const at::Tensor &q = tensor(a[3], "q"), &k = tensor(a[4], "k"), &v = tensor(a[5], "v");
-  if (C10_UNLIKELY(tracked(q) || tracked(k) || tracked(v))) Py_RETURN_NOTIMPLEMENTED;
+  if (C10_UNLIKELY(tracked(q, k, v))) Py_RETURN_NOTIMPLEMENTED;
   const int device = cuda_of(q);
   void *stream = stream_of(device);
   heads_of(q, "q", dim, device);

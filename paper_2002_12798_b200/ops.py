@@ -19,6 +19,7 @@ it; tensors it makes belong to that stream.
 from __future__ import annotations
 
 import ctypes
+import functools
 import importlib.machinery
 import importlib.util
 import math
@@ -272,9 +273,9 @@ class RopePlan:
             with torch.cuda.stream(stream):
                 return self.append(q, k, v, positions, slots, cache, out=out)
         got = _entry.append(self._h, self.head_dim, self.n_axes, q, k, v, positions, slots, cache._at, cache._device, out)
-        if got is not NotImplemented:
-            return got
-        return _without_derivative("append", self.append, (q, k, v, positions, slots, cache), out, q, k, v)
+        if got is NotImplemented:
+            return _without_derivative("append", self.append, (q, k, v, positions, slots, cache), out, q, k, v)
+        return got
 
 
 # ----------------------------------------------------------------------------------------------------------------------
@@ -346,14 +347,11 @@ class AttendPlan:
         if stream is not None:
             with torch.cuda.stream(stream):
                 return self.attend(q, cache, block_table, seq_lens, out=out, return_lse=return_lse)
-        got = self._attend(q, cache, block_table, seq_lens, out, return_lse)
-        if got is not NotImplemented:
-            return got
-        return _without_derivative("attend", self._attend, (q, cache, block_table, seq_lens, None, return_lse), out, q)
-
-    def _attend(self, q, cache, block_table, seq_lens, out, return_lse):
         with self._lock:  # from a call's place in the order to its launch
             if _raw_stream(self._device) != self._raw:
                 self._order()
-            return _entry.attend(self._at, self._device, self.max_requests, self.head_dim, q, cache._at, cache._maps_at, cache._device, block_table,
-                                 seq_lens, out, return_lse)
+            got = _entry.attend(self._at, self._device, self.max_requests, self.head_dim, q, cache._at, cache._maps_at, cache._device, block_table,
+                                seq_lens, out, return_lse)
+        if got is NotImplemented:
+            return _without_derivative("attend", functools.partial(self.attend, return_lse=return_lse), (q, cache, block_table, seq_lens), out, q)
+        return got
