@@ -216,13 +216,14 @@ int amap_rope_append(const amap_rope_t *plan, const amap_append_args *args /* ho
  *   out = sum_t exp(s_t - lse) V[t],     lse = log sum_t exp(s_t)
  * A request with no token (n <= 0) gets zeros and lse = -inf.  n is clamped to
  * max_pages * page_size; a table entry outside [0, n_pages) is a hole whose
- * tokens take no part.  Nothing is read from the cache but the tokens that take
- * part, so what lies behind a request's end may be anything, NaN included.
+ * tokens take no part.  Only tokens that take part count: of the pages in a
+ * request's row, whole runs of up to 64 tokens may be read, so what lies behind
+ * its end there may be anything, NaN included.  Pages in no row are not read.
  * Scores, maximum, sum and output are kept in 32 bits.
  *
  * Every wait inside the kernel ends: one that has lasted two seconds is given up, and the int32 at byte
- * amap_attend_workspace()'s *failed of the workspace becomes 1 (the outputs are then worth
- * nothing, and the workspace has to be zeroed before it is used again).
+ * amap_attend_workspace()'s *failed of the workspace becomes 1 (the outputs of this call and of later ones are then worth
+ * nothing until the workspace has been zeroed; before it ends, a block lets its copies land, with the same limit).
  *
  * workspace: amap_attend_workspace() bytes, 256-byte aligned, ZEROED before its first use; every call leaves
  * it ready for the next.  Calls that share a workspace must have the same q_heads, cache.heads and cache.head_dim and be

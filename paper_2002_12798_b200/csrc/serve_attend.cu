@@ -24,8 +24,8 @@
 // asynchronous copies; both lay 128-byte rows out with the same swizzle, chunk ^ (row mod 8), so that the matrix loads
 // meet every bank once.  Only the end of an item synchronises the four warps.
 //
-// Measured: one request of 131009 tokens over 8 heads of 128 fp16 elements (537 MB) 87.5 us = 6.1 TB/s; 32 requests of up
-// to 16384 tokens in bf16 6.4 TB/s; 128 of up to 4096 over an e4m3 cache, 8 q heads to each, 5.2; 33 tokens 5.4 us.
+// Measured: one request of 131009 tokens over 8 heads of 128 fp16 elements (537 MB) 89.6 us = 6.0 TB/s; 32 requests of up
+// to 16384 tokens in bf16 6.5 TB/s; 128 of up to 4096 over an e4m3 cache, 8 q heads to each, 5.2; 33 tokens 5.5 us.
 #include <cuda.h>
 
 #include <algorithm>
@@ -68,7 +68,7 @@ struct Params {
 
 // Blocks resident per multiprocessor: two where their registers allow (O and q of 8 heads of up to 128 elements); with 16
 // heads held to half the registers, what spills costs more than the second block brings (32 requests of 8k tokens, 16 q
-// heads per cache head: 131 us against 117).
+// heads per cache head, P in two terms: 131 us against 117; in three 129 with one block).
 template <int DP, int NT> constexpr int kResident = DP == 256 || NT >= 2 ? 1 : 2;
 // Stages of the ring: 192 KB a multiprocessor, of which about two thirds are in flight (latency times bandwidth is 50).
 template <int ROW_BYTES, int RESIDENT> constexpr int kStages = 192 * 1024 / RESIDENT / (2 * 16 * kSixteens<ROW_BYTES> * kWarps * ROW_BYTES);

@@ -7,9 +7,9 @@
 // Bound: memory, every element is read and written once.  A block takes a few tokens of one part (q, k or v): its
 // threads issue their loads, compute the tokens' cos and sin once for all heads while those are under way, and turn
 // and store.  An item is VEC pairs (two 16-byte accesses each way where alignment allows), two per thread: few, so that
-// blocks are short and many overlap (8192 tokens of 40 heads of 128 bf16 elements: 32.5 us = 5.1 TB/s; four items 33.3 us,
+// blocks are short and many overlap (8192 tokens of 40 heads of 128 bf16 elements: 32.2 us = 5.2 TB/s; four items 33.3 us,
 // one item at more blocks 36).  Beside a copy of the same bytes (26 us) it pays for the arithmetic and for the angles,
-// which stand between a block's loads and its stores.  16 tokens into the cache: 2.0 us, latency alone.
+// which stand between a block's loads and its stores.  16 tokens into the cache: 1.9 us, latency alone.
 #include <algorithm>
 #include <cmath>
 #include <cstring>
