@@ -213,3 +213,31 @@ def test_rotate_in_fp32_is_as_exact_as_rounded_cos_and_sin(ops, base, first, pai
     plain = torch.stack([a * c - b * s, b * c + a * s])
     off = lambda z: float((z.double() - want).norm() / want.norm())  # noqa: E731
     assert off(torch.stack(got)) <= 1.1 * off(plain), (off(torch.stack(got)), off(plain))
+
+
+@pytest.mark.parametrize("dtype,cache_dtype", [("fp16", "fp16"), ("bf16", "e4m3"), ("bf16", "bf16")])
+@pytest.mark.parametrize("dim,group,window,softcap", [(64, 32, 0, 0.0), (128, 29, 0, 0.0), (128, 40, 150, 0.0), (256, 17, 0, 40.0), (80, 20, 0, 1e4)])
+def test_attend_many_q_heads_with_scores_far_apart(ops, dim, group, window, softcap, dtype, cache_dtype):
+    """Groups of more than 16 q heads, the kernels with the most of them, over scores near together and far apart, with tokens
+    that take no part in the same steps and pages that end inside them."""
+    torch.manual_seed(dim + group)
+    r = np.random.default_rng(dim + group)
+    page = 24
+    lens = np.array([0, 1, 33, 700, 64, 1500], dtype=np.int32)
+    n, row = len(lens), -(-1500 // page)
+    table = r.permutation(n * row).astype(np.int32).reshape(n, row)
+    table[3, [0, 5, 6]] = -1
+    k, v = (torch.randn(n * row, page, 2, dim, device="cuda").to(TYPES[cache_dtype]) for _ in range(2))
+    q = torch.randn(n, 2 * group, dim, device="cuda")
+    q[:, ::3] *= 12
+    q[:, 1::5] *= 40
+    q = q.to(TYPES[dtype])
+    plan = ops.AttendPlan(n, 2 * group, 2, dim, window=window, softcap=softcap)
+    out, lse = plan.attend(q, ops.PagedCache(k, v), torch.from_numpy(table).cuda(), torch.from_numpy(lens).cuda(), return_lse=True)
+    want, want_lse, size, mass = ref.attend(f64(q), f64(k), f64(v), table, lens, plan.scale, window, softcap)
+    bound, lse_bound = ref.attend_bound(want, size, mass, dim, dtype)
+    off = np.abs(f64(out) - want) / bound
+    assert (off <= 1).all(), off.max()
+    there = np.isfinite(want_lse)
+    assert np.array_equal(there, np.isfinite(f64(lse)))
+    assert (np.abs(f64(lse)[there] - want_lse[there]) <= lse_bound[there] + 2.0**-22 * np.abs(want_lse[there])).all()
