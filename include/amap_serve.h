@@ -255,6 +255,105 @@ int amap_attend(const amap_attend_args *args /* host */, void *cuda_stream);
 int amap_attend_workspace(int32_t n_requests, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int64_t *bytes,
                           int64_t *failed /* may be NULL */);
 
+/* ---------------------------------------------------------------------------
+ * A paged cache of 4 bits.  A head's elements are held in groups of 32 or 64:
+ *   low  = the group's smallest element, rounded down to bf16;
+ *   step = (its largest element - low) / 15, rounded to bf16;
+ *   code = (element - low) / step, rounded to nearest even, within 0 .. 15 (0
+ *          where step is 0), and stands for low + step * code.
+ * A group that holds a NaN or an infinity, or whose low or step is none of
+ * bf16's finite numbers, reads as NaN throughout.
+ *
+ * A page of a head is one run of page_size / 16 cells of 16 tokens, codes and
+ * groups' numbers of K and V together (amap_packed_bytes() in all); what lies
+ * where inside a cell is the library's own.  Memory that no token has been
+ * written to may hold anything.
+ * ------------------------------------------------------------------------- */
+typedef struct amap_packed {
+  void *data;                                  /* aligned to 16 bytes */
+  int64_t page, head;                          /* strides in BYTES between pages and between a page's heads: multiples of 16 */
+  int32_t n_pages, page_size, heads, head_dim; /* page_size a multiple of 16, n_pages * page_size below 2^31; head_dim 64, 96, 128 or 256 */
+  int32_t group;                               /* 32, or 64 where it divides head_dim */
+  int32_t reserved;                            /* 0 */
+} amap_packed;
+/* bytes of a page of a head; 0, with the reason, where there is no such cache */
+int64_t amap_packed_bytes(int32_t page_size, int32_t head_dim, int32_t group);
+
+/* amap_packed_append: a step's q, k, v [rows][heads][head_dim] in one launch, as amap_rope_append: q_out = rotated q, and
+ * the rotated k and the v of row i go to slots[i].  k is quantised as the exact rotation gives it (64 bits).
+ * plan NULL: nothing turns, and positions are not read.  A slot outside [0, n_pages*page_size) writes nothing to the
+ * cache.  Slots must be distinct. */
+typedef struct amap_packed_append_args {
+  int64_t rows;
+  int32_t dtype;   /* AMAP_BF16 or AMAP_FP16 */
+  int32_t q_heads; /* 0: k and v only */
+  const void *q, *k, *v;
+  void *q_out;
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head, q_out_row, q_out_head;
+  const void *positions;
+  int64_t position_axis, position_row;
+  int32_t position_bits;
+  int32_t reserved; /* 0 */
+  const int32_t *slots;
+  amap_packed cache;
+} amap_packed_append_args;
+int amap_packed_append(const amap_rope_t *plan, const amap_packed_append_args *args /* host */, void *cuda_stream);
+
+/* amap_packed_read: k[i], v[i] [heads][head_dim] = what the cache holds at slots[i], in 32 bits and rounded once; zeros for a
+ * slot outside [0, n_pages*page_size). */
+typedef struct amap_packed_read_args {
+  int64_t rows;
+  int32_t dtype;    /* AMAP_BF16, AMAP_FP16 or AMAP_FP32 */
+  int32_t reserved; /* 0 */
+  const int32_t *slots;
+  void *k, *v;
+  int64_t k_row, k_head, v_row, v_head; /* strides */
+  amap_packed cache;
+} amap_packed_read_args;
+int amap_packed_read(const amap_packed_read_args *args /* host */, void *cuda_stream);
+
+/* amap_packed_attend: amap_attend over such a cache; `maps` and `cache` of the arguments are not looked at.  The workspace is
+ * amap_attend's, and may be shared with its calls as those may share it. */
+int amap_packed_attend(const amap_attend_args *args /* host */, const amap_packed *cache /* host */, void *cuda_stream);
+
+/* ---------------------------------------------------------------------------
+ * Sampling: a token for every row of logits, from one uniform number in [0, 1).
+ * With x_i the row's logits, w_i = exp((x_i - max x) / temperature), and tokens
+ * ordered by their logits, ties by their index:
+ *   top_k  keeps the first top_k tokens (0 or less: all);
+ *   min_p  keeps those with w_i >= min_p;
+ *   top_p  keeps, of what these leave, the shortest beginning of the order whose
+ *          sum of w is at least top_p of their sum, one token at least;
+ * the token drawn is the first, by index, whose sum of w over the kept tokens up
+ * to it is above uniform times the sum over all kept ones.  temperature 0 or
+ * less: the largest logit, the first of them.  A NaN counts as -infinity; a row
+ * with no logit above -infinity gives -1; where the largest is +infinity, the
+ * tokens that have it share the weight.
+ * A uniform number outside counts as the nearest inside, NaN as 0.
+ * logprob[r] = log of the probability with which the token was drawn (0 for
+ * temperature 0, -infinity with token -1).
+ * The answer is the definition's in 64 bits: w is kept to 2^-40 of itself (and
+ * to 2^-44 of the largest), sums are whole numbers, in no order.
+ * ------------------------------------------------------------------------- */
+typedef struct amap_sample_args {
+  int32_t rows;    /* 1 .. 65535 */
+  int32_t vocab;   /* 1 .. 2^20 */
+  int32_t dtype;   /* AMAP_BF16, AMAP_FP16 or AMAP_FP32 */
+  int32_t by_row;  /* bits 0 .. 3: temperature, top_k, top_p, min_p are arrays of `rows` numbers, not one */
+  const void *logits;
+  int64_t row;     /* stride between rows */
+  const float *uniform;
+  const float *temperatures; /* with bit 0, else `temperature` counts */
+  const int32_t *top_ks;
+  const float *top_ps, *min_ps;
+  float temperature;
+  int32_t top_k;
+  float top_p, min_p;
+  int32_t *tokens;
+  float *logprobs; /* may be NULL */
+} amap_sample_args;
+int amap_sample(const amap_sample_args *args /* host */, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -13,7 +13,7 @@ INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libamap.so")
 TORCH_ENTRY = os.path.join(HERE, "_serve_torch.so")
 SOURCES = ["builder.cpp", "compose.cpp", "simplify.cpp", "plan_execute.cu", "consume.cu",
-           "serve_common.cu", "serve_pages.cu", "serve_rope.cu", "serve_attend.cu"]
+           "serve_common.cu", "serve_pages.cu", "serve_rope.cu", "serve_attend.cu", "serve_attend_packed.cu", "serve_packed.cu", "serve_sample.cu"]
 
 
 def _nvcc() -> str:

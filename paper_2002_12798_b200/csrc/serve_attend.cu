@@ -42,9 +42,6 @@ using namespace amap_serve;
 namespace {
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps, kBlock = kThreads + 32;  // the last warp is the producer
-// tokens per warp and step, in sixteens: two where a token's row is 128 bytes, so that a step moves 32 KB either way and two
-// independent products hide each other's latency (128 e4m3 requests: 103 us with one, 100 with two)
-template <int ROW_BYTES> constexpr int kSixteens = ROW_BYTES == 128 ? 2 : 1;
 constexpr int kMostBlocksPerSm = 2;
 constexpr int kGroup = 8;               // teams whose parts are joined first, where an item has more than kDirect of them
 constexpr int kDirect = 12;
@@ -66,26 +63,7 @@ struct Params {
   int32_t *failed, *grouped, *arrived;
 };
 
-// Blocks resident per multiprocessor: two where their registers allow (O and q of 8 heads of up to 128 elements); with 16
-// heads held to half the registers, what spills costs more than the second block brings (32 requests of 8k tokens, 16 q
-// heads per cache head, P in two terms: 131 us against 117; in three 129 with one block).
-template <int DP, int NT> constexpr int kResident = DP == 256 || NT >= 2 ? 1 : 2;
-// Stages of the ring: 192 KB a multiprocessor, of which about two thirds are in flight (latency times bandwidth is 50).
-template <int ROW_BYTES, int RESIDENT> constexpr int kStages = 192 * 1024 / RESIDENT / (2 * 16 * kSixteens<ROW_BYTES> * kWarps * ROW_BYTES);
-
 __device__ __forceinline__ uint32_t smem_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool live) {
-  const int n = live ? 16 : 0;  // nothing is read where the row is not live: the 16 bytes become zeros
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
-}
-__device__ __forceinline__ void copies_arrive(uint32_t bar) {  // when this thread's copies so far have landed
-  asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void tensor_copy(uint32_t dst, const CUtensorMap *map, int x, int token, int head, int page, uint32_t bar) {
-  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
-               "l"(map), "r"(x), "r"(token), "r"(head), "r"(page), "r"(bar)
-               : "memory");
-}
 __device__ __forceinline__ void bar_init(uint32_t bar, int n) { asm volatile("mbarrier.init.shared.b64 [%0], %1;" ::"r"(bar), "r"(n) : "memory"); }
 __device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared.b64 _, [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ void bar_arrive_bytes(uint32_t bar, int n) {
@@ -119,17 +97,6 @@ __device__ __noinline__ void settle(uint32_t full, int stages, int stage, uint32
 }
 __device__ __forceinline__ void sync_consumers() { asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory"); }
 
-__device__ __forceinline__ void load4(uint32_t at, uint32_t (&r)[4]) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
-}
-__device__ __forceinline__ void load4_transposed(uint32_t at, uint32_t (&r)[4]) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
-}
-__device__ __forceinline__ uint32_t transposed(uint32_t v) {
-  uint32_t r;
-  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
-  return r;
-}
 template <int CT>
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   if constexpr (CT == AMAP_BF16)
@@ -152,49 +119,6 @@ __device__ __forceinline__ float tanh_of(float x) {
   const float closed = 1.0f - __fdividef(2.0f, exp2_of(x * (2.0f * kLog2e)) + 1.0f);
   return fabsf(x) < 0.3f ? series : closed;
 }
-// four e4m3 as four fp16: exact
-__device__ __forceinline__ void halves_of(uint32_t four, uint32_t *low, uint32_t *high) {
-  asm("{ .reg .b16 l, h; mov.b32 {l, h}, %2; cvt.rn.f16x2.e4m3x2 %0, l; cvt.rn.f16x2.e4m3x2 %1, h; }" : "=r"(*low), "=r"(*high) : "r"(four));
-}
-
-// P in 16-bit terms, each what the ones before it leave over, so that P V has the precision of 32-bit P: three terms of
-// bf16's 8 bits, or two of fp16's 11.  A remainder is no less than `least`, nor (BANDED) is the first term: above zero where
-// V can hold an infinity, so that it meets no zero that P has not got.
-// P is taken relative to a maximum that is renewed only when a score passes it by more than kSlack (in powers of 2): the
-// true one moves in most of the early steps, and O would be rescaled each time.  fp16 terms carry P times 2^kLift, out of
-// the way of fp16's smallest numbers; 2^(kLift + kSlack) is below its largest.  A step with a score further than kDeep
-// below the maximum (beside a token that has nearly all the weight, every one) would still come too near them: such a
-// step goes by bands of kBand powers of 2 from its own highest score down, each lifted to 2^(kLift + kSlack) and scaled
-// back in 32 bits.  In all others P is 2^(kLift - kDeep) at least, 2^12 of fp16's smallest steps.  The three numbers share
-// fp16's 40 powers of 2 out so that bands are rare: with scores of 2.9 (standard deviation, powers of 2) 16 q heads per
-// cache head take 80 us for 32 requests up to 8192 tokens, with 8 + 7, 17 in place of 6 + 9, 21 94 us, without bands 78.  With
-// scores of 11.6 nearly every step goes by bands: 128 e4m3 requests 119 -> 182 us, 32 of fp16 195 -> 276.
-constexpr float kSlack = 6.0f, kDeep = 21.0f, kBand = 24.0f;
-template <int CT> constexpr float kLift = CT == AMAP_FP16 ? 9.0f : 0.0f;
-template <int CT> constexpr int kTerms = CT == AMAP_BF16 ? 3 : 2;
-template <int CT, bool BANDED>
-__device__ __forceinline__ void split(float p0, float p1, float least, uint32_t (&term)[kTerms<CT>]) {
-  if constexpr (CT == AMAP_BF16) {
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const uint32_t u0 = __float_as_uint(p0), u1 = __float_as_uint(p1);
-      term[k] = __byte_perm(u0, u1, 0x7632);
-      p0 = fmaxf(p0 - __uint_as_float(u0 & 0xFFFF0000u), least);
-      p1 = fmaxf(p1 - __uint_as_float(u1 & 0xFFFF0000u), least);
-    }
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(term[2]) : "f"(p1), "f"(p0));
-  } else {
-    asm("cvt.rz.f16x2.f32 %0, %1, %2;" : "=r"(term[0]) : "f"(p1), "f"(p0));
-    __half2 h = *reinterpret_cast<const __half2 *>(&term[0]);
-    if constexpr (BANDED) {
-      h = __hmax2_nan(h, __float2half2_rn(least));
-      term[0] = *reinterpret_cast<const uint32_t *>(&h);
-    }
-    const float r0 = fmaxf(p0 - __low2float(h), least), r1 = fmaxf(p1 - __high2float(h), least);
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(term[1]) : "f"(r1), "f"(r0));
-  }
-}
-
 // The line of tiles of TILE tokens: request by request, its heads round by round (a round is a team's), a round's tiles in
 // order.  A request without tokens counts one tile, so that somebody writes its zeros.  Every item (a round of a request)
 // is longer by kEntry places, for what it costs to put the item before it away and to take it up; its tiles are the
@@ -272,12 +196,12 @@ struct Producer {
   static __device__ __forceinline__ void sync() { __syncwarp(); }
 };
 
-// Joins n parts of an item, the i-th in slot slot_of(i), in this order: into the output, or (final: false) into slot
+// Joins n parts of an item, the i-th in slot slot_of(i), in this order (the parts' O and l are 2^lift times what they stand for): into the output, or (final: false) into slot
 // slot_of(0), which nobody else reads before this block has arrived for it.  ml: room for n x 8, free again on return:
 // the four warps' lies in `joint`, where the next item's (m, l) go without a barrier ahead of them (with heads of 64
 // elements, those of warp 0's second head over part 8's of the third, which warp 1 reads).
-template <typename T, int CT, int DP, int HB, typename F>
-__device__ void join(const Params &P, float2 (*ml)[8], int n, F slot_of, int heads, bool final, int r, int first_head) {
+template <typename T, int DP, int HB, typename F>
+__device__ void join(const Params &P, float2 (*ml)[8], int n, F slot_of, int heads, bool final, int r, int first_head, float lift) {
   const int tid = T::index(), D = P.a.cache.head_dim;
   for (int h0 = 0; h0 < heads; h0 += 8) {
     const int items = min(8, heads - h0) * (DP / 4);
@@ -318,7 +242,7 @@ __device__ void join(const Params &P, float2 (*ml)[8], int n, F slot_of, int hea
         const int64_t to = (int64_t)r * P.a.out_row + (int64_t)(first_head + h0 + in) * P.a.out_head + d;
         write_pair(P, to, y.x * f, y.y * f);
         write_pair(P, to + 2, y.z * f, y.w * f);
-        if (d == 0 && P.a.lse) P.a.lse[(int64_t)r * P.a.lse_row + first_head + h0 + in] = sum == 0.0f ? -INFINITY : (top - kLift<CT> + log2f(sum)) * kLn2;
+        if (d == 0 && P.a.lse) P.a.lse[(int64_t)r * P.a.lse_row + first_head + h0 + in] = sum == 0.0f ? -INFINITY : (top - lift + log2f(sum)) * kLn2;
       } else {
         const int64_t to = (int64_t)slot_of(0) * HB + h0 + in;
         *reinterpret_cast<float4 *>(P.part_o + to * DP + d) = y;
@@ -353,6 +277,337 @@ template <int S, int TILE> struct Small {
   float2 aside[kAside][8];
 };
 
+
+// The piece of the line that a block works through, and the parts of the item that it begins in: those of the teams
+// first_from to first_to, of which the first began it in its second slot, the others go on with it in their first.
+template <int TILE>
+struct Piece {
+  using Line = Cursor<TILE>;
+  Line at;
+  int team, member, first_from, first_to;
+  int64_t total, pieces, u0, u1, first_place;
+  bool aside;  // the producer warp joins the first item's parts
+
+  __device__ __forceinline__ int team_of(int64_t place) const { return (int)(((place + 1) * pieces - 1) / total); }
+
+  // every thread of the block; false: there is nothing to do
+  template <int S>
+  __device__ __forceinline__ bool find(const Params &P, Small<S, TILE> &small) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int R = P.a.n_requests, per = (R + kThreads - 1) / kThreads, r_first = warp < kWarps ? min(R, tid * per) : R, r_last = min(R, r_first + per);
+    int64_t mine = 0;
+    for (int r = r_first; r < r_last; ++r) mine += kEntry + Line::tiles(P, Line::clamped(P, P.a.seq_lens[r]));
+    mine *= P.rounds;
+    int64_t upto = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int64_t v = __shfl_up_sync(~0u, upto, d);
+      if (lane >= d) upto += v;
+    }
+    if (lane == 31 && warp < kWarps) small.sums[warp] = upto;
+    __syncthreads();
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      if (w < warp) upto += small.sums[w];
+      total += small.sums[w];
+    }
+    team = blockIdx.x / P.members, member = blockIdx.x - team * P.members;
+    pieces = min((int64_t)(gridDim.x / P.members), total);  // none of them empty
+    if (team >= pieces) return false;
+    u0 = total * team / pieces, u1 = total * (team + 1) / pieces;
+    if (warp < kWarps && upto > u0 && upto - mine <= u0) {
+      int64_t u = upto - mine;
+      for (int r = r_first; r < r_last; ++r) {
+        const int tiles = Line::tiles(P, Line::clamped(P, P.a.seq_lens[r]));
+        const int64_t places = (int64_t)(kEntry + tiles) * P.rounds;
+        if (u + places > u0) {
+          const int64_t in = u0 - u;
+          const int round = in <= 0x7FFFFFFF ? (int)in / (kEntry + tiles) : (int)(in / (kEntry + tiles));
+          const int tile = max(0, (int)(in - (int64_t)round * (kEntry + tiles)) - kEntry);
+          small.begin[0] = r;
+          small.begin[1] = round;
+          small.begin[2] = tile;
+          small.first_place = u + (int64_t)round * (kEntry + tiles) + kEntry;  // of the item that u0 is in
+          break;
+        }
+        u += places;
+      }
+    }
+    __syncthreads();
+    at.start(P, small.begin[0], small.begin[1], small.begin[2], small.first_place, u1);
+    if (at.rest <= 0) return false;  // a piece between two items
+    first_place = small.first_place;
+    const int64_t first_last = first_place + Line::tiles(P, at.n) - 1;
+    first_from = team_of(first_place), first_to = team_of(first_last);
+    aside = first_place < u0 && first_last + 1 + kEntry < u1 && first_to - first_from < kAside;
+    return true;
+  }
+};
+
+// The producer warp's last work where piece.aside: the join of the item that the piece began in.
+template <int DP, int HB, int S, int TILE>
+__device__ __forceinline__ void join_aside(const Params &P, Small<S, TILE> &small, const Piece<TILE> &piece, float lift) {
+  asm volatile("bar.sync 2, %0;" ::"n"(kBlock) : "memory");  // the four warps have written the first item's part
+  const int member = piece.member, first_from = piece.first_from, parts = piece.first_to - first_from + 1;
+  const int h = small.begin[1] * P.members + member, r = small.begin[0], in_group = h % P.blocks_per_head * HB;
+  auto slot_of = [&](int i) { return 2 * ((first_from + i) * P.members + member) + (i == 0 ? 1 : 0); };
+  if (last_of<Producer>(P.arrived + (int64_t)r * P.items_per_request + h, parts, &small.told_aside))
+    join<Producer, DP, HB>(P, small.aside, parts, slot_of, min(HB, P.group - in_group), true, r, h / P.blocks_per_head * P.group + in_group, lift);
+}
+
+// The four warps' sums for the heads 8 nt .. of an item, which lie in `joint` relative to a common maximum, with each warp's
+// (m, l) behind a head's O: into the output (whole), or into a slot of the workspace.
+template <int DP, int HB>
+__device__ __forceinline__ void sum_warps(const Params &P, const float *joint, int nt, int heads, bool whole, int r, int first_head, int slot, float lift) {
+  constexpr int kPitch = DP + 4;
+  const int n_heads = min(8, heads - nt * 8), D = P.a.cache.head_dim;
+  for (int i = threadIdx.x; i < n_heads * (DP / 2); i += kThreads) {
+    const int in = i / (DP / 2), d = i % (DP / 2) * 2, head = nt * 8 + in;
+    if (d >= D) continue;
+    const float *ml = joint + in * kPitch + DP;
+    const float top = fmaxf(fmaxf(ml[0], ml[8 * kPitch]), fmaxf(ml[16 * kPitch], ml[24 * kPitch]));
+    float sum = 0.0f;
+    float2 y = make_float2(0.0f, 0.0f);
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      sum += ml[w * 8 * kPitch + 1] * (top == -INFINITY ? 1.0f : exp2_of(ml[w * 8 * kPitch] - top));
+      const float2 v = *reinterpret_cast<const float2 *>(joint + (w * 8 + in) * kPitch + d);
+      y.x += v.x;
+      y.y += v.y;
+    }
+    if (whole) {
+      const float f = sum == 0.0f ? 0.0f : P.a.cache.v_scale / sum;
+      write_pair(P, (int64_t)r * P.a.out_row + (int64_t)(first_head + head) * P.a.out_head + d, y.x * f, y.y * f);
+      if (d == 0 && P.a.lse) P.a.lse[(int64_t)r * P.a.lse_row + first_head + head] = sum == 0.0f ? -INFINITY : (top - lift + log2f(sum)) * kLn2;
+    } else {
+      *reinterpret_cast<float2 *>(P.part_o + ((int64_t)slot * HB + head) * DP + d) = y;
+      if (d == 0) reinterpret_cast<float2 *>(P.part_ml)[(int64_t)slot * HB + head] = make_float2(top, sum);
+    }
+  }
+}
+
+// What the four warps do once this block's part of an item (its h-th of request r, places item_first to item_last) lies in
+// the workspace: count it, and join the parts if it is the last.
+template <int DP, int HB, int S, int TILE>
+__device__ __forceinline__ void hand_in(const Params &P, Small<S, TILE> &small, float2 (*joined)[8], const Piece<TILE> &piece, int64_t item_first,
+                                        int64_t item_last, int heads, int r, int h, int first_head, float lift) {
+  if (piece.aside && item_first < piece.u0) {
+    asm volatile("bar.arrive 2, %0;" ::"n"(kBlock) : "memory");
+    return;
+  }
+  const int member = piece.member, from = piece.team_of(item_first), to = piece.team_of(item_last);
+  auto slot_of_team = [&](int b) { return 2 * (b * P.members + member) + (b == from ? 1 : 0); };
+  int32_t *item = P.arrived + (int64_t)r * P.items_per_request + h;
+  if (to - from < kDirect) {
+    if (last_of<Consumers>(item, to - from + 1, &small.told))
+      join<Consumers, DP, HB>(P, joined, to - from + 1, [&](int i) { return slot_of_team(from + i); }, heads, true, r, first_head, lift);
+    return;
+  }
+  // of the items with parts in a group of teams, one at most began before the group and one at most, among those
+  // with more than kDirect parts, begins in it: two counters
+  const int group = piece.team / kGroup, b0 = max(from, group * kGroup), b1 = min(to, group * kGroup + kGroup - 1);
+  if (last_of<Consumers>(P.grouped + 2 * (group * P.members + member) + (from >= group * kGroup ? 1 : 0), b1 - b0 + 1, &small.told)) {
+    join<Consumers, DP, HB>(P, joined, b1 - b0 + 1, [&](int i) { return slot_of_team(b0 + i); }, heads, false, r, first_head, lift);
+    const int g0 = from / kGroup, g1 = to / kGroup;
+    if (last_of<Consumers>(item, g1 - g0 + 1, &small.told))
+      join<Consumers, DP, HB>(P, joined, g1 - g0 + 1, [&](int i) { return slot_of_team(max(from, (g0 + i) * kGroup)); }, heads, true, r, first_head, lift);
+  }
+}
+
+// eights of q heads that share a pass over the cache: all of a group where its accumulators fit the registers
+int eights(int group, int dp) {
+  const int most = dp < 256 ? 4 : 2;
+  return group <= 8 ? 1 : group <= 16 || most == 2 ? 2 : 4;
+}
+
+int check_shape(int32_t n_requests, int32_t q_heads, int32_t kv_heads, int32_t head_dim) {
+  SERVE_REQUIRE(n_requests >= 1 && n_requests <= 0xFFFF, AMAP_EINVAL, "requests: 1 .. 65535");
+  SERVE_REQUIRE(q_heads >= 1 && q_heads <= 0xFFFF && kv_heads >= 1 && q_heads % kv_heads == 0, AMAP_EINVAL, "q heads: a multiple of the cache's heads");
+  SERVE_REQUIRE(head_dim >= 8 && head_dim <= 256 && head_dim % 8 == 0, AMAP_EUNSUPPORTED, "head size: a multiple of 8, up to 256");
+  return AMAP_OK;
+}
+
+struct Workspace {
+  int64_t ml, failed, grouped, arrived, bytes;  // offsets; the partial outputs come first
+};
+Workspace workspace(int32_t n_requests, int32_t q_heads, int32_t kv_heads, int32_t head_dim) {
+  const int dp = head_dim <= 128 ? 128 : 256, group = q_heads / kv_heads, hb = 8 * eights(group, dp);
+  const int64_t blocks = (int64_t)device_sms() * kMostBlocksPerSm, items = (int64_t)n_requests * kv_heads * ((group + hb - 1) / hb);
+  Workspace w;
+  w.ml = 2 * blocks * hb * dp * 4;
+  w.failed = w.ml + 2 * blocks * hb * 8;
+  w.grouped = w.failed + 16;
+  w.arrived = w.grouped + (blocks / kGroup + kMostMembers) * 2 * 4;
+  w.bytes = (w.arrived + items * 4 + 255) / 256 * 256;
+  return w;
+}
+
+
+// Checks of a call that do not depend on how the cache is held; AMAP_OK, or the refusal.
+int check_call(const amap_attend_args &a, int32_t heads, int32_t head_dim, int32_t page_size) {
+  if (const int rc = check_shape(a.n_requests, a.q_heads, heads, head_dim)) return rc;
+  SERVE_REQUIRE(a.dtype == AMAP_BF16 || a.dtype == AMAP_FP16, AMAP_EINVAL, "type: bf16 or fp16");
+  SERVE_REQUIRE(a.q && a.out && a.block_table && a.seq_lens && a.workspace, AMAP_EINVAL, "null pointer");
+  SERVE_REQUIRE(a.max_pages >= 1 && a.table_stride >= a.max_pages, AMAP_EINVAL, "table rows overlap");
+  SERVE_REQUIRE((int64_t)a.max_pages * page_size <= 0x7FFFFFFF, AMAP_EOVERFLOW, "a table row holds more than 2^31-1 tokens");
+  SERVE_REQUIRE(std::isfinite(a.scale) && std::isfinite(a.softcap) && a.softcap >= 0 && a.window >= 0 && a.reserved == 0, AMAP_EINVAL,
+                "scale is finite, softcap and window are not negative");
+  SERVE_REQUIRE(aligned(a.q, 2) && aligned(a.out, 2) && aligned(a.lse, 4) && aligned(a.block_table, 4) && aligned(a.seq_lens, 4) &&
+                    aligned(a.workspace, 256), AMAP_EALIGN, "misaligned pointer");
+  Span qs, os;
+  qs.hi = os.hi = (int64_t)head_dim * 2;
+  qs.add(a.n_requests, a.q_row, 2);
+  qs.add(a.q_heads, a.q_head, 2);
+  os.add(a.n_requests, a.out_row, 2);
+  os.add(a.q_heads, a.out_head, 2);
+  SERVE_REQUIRE(!overlap(a.q, qs, a.out, os), AMAP_EINVAL, "q and out overlap");
+  return AMAP_OK;
+}
+
+// From a checked call (P.a) to a kernel's parameters, for blocks of 8 nt q heads: the items, the division by the page size and
+// the workspace.
+int place(Params &P, int nt) {
+  const amap_cache &c = P.a.cache;
+  const Workspace w = workspace(P.a.n_requests, P.a.q_heads, c.heads, c.head_dim);
+  SERVE_REQUIRE(P.a.workspace_bytes >= w.bytes, AMAP_EINVAL, "workspace too small");
+  P.group = P.a.q_heads / c.heads;
+  P.blocks_per_head = (P.group + 8 * nt - 1) / (8 * nt);
+  P.items_per_request = c.heads * P.blocks_per_head;
+  SERVE_REQUIRE((int64_t)P.a.n_requests * P.items_per_request <= 0x7FFFFFFF, AMAP_EOVERFLOW, "more than 2^31-1 pairs of request and head");
+  // token / page_size for tokens below 2^31: a shift, or the high word of a product with ceil(2^(32+s) / page_size),
+  // s = floor(log2 page_size), whose excess over 2^(32+s) is at most page_size - 1 < 2^(s+1): exact up to 2^31
+  int s = 0;
+  while ((2u << s) <= (uint32_t)c.page_size) ++s;
+  P.div_shift = s;
+  if (c.page_size != 1 << s) P.div_mul = (uint32_t)((((uint64_t)1 << (32 + s)) + c.page_size - 1) / c.page_size);
+  P.q_pairs = aligned(P.a.q, 4) && P.a.q_row % 2 == 0 && P.a.q_head % 2 == 0;
+  P.out_pairs = aligned(P.a.out, 4) && P.a.out_row % 2 == 0 && P.a.out_head % 2 == 0;
+  char *ws = static_cast<char *>(P.a.workspace);
+  P.part_o = reinterpret_cast<float *>(ws);
+  P.part_ml = reinterpret_cast<float *>(ws + w.ml);
+  P.failed = reinterpret_cast<int32_t *>(ws + w.failed);
+  P.grouped = reinterpret_cast<int32_t *>(ws + w.grouped);
+  P.arrived = reinterpret_cast<int32_t *>(ws + w.arrived);
+  return AMAP_OK;
+}
+
+// What a kernel is launched with: its blocks resident on the device (asked for once per device, with the block's shared
+// memory), the teams, and no more blocks than there can be pieces.  P: the part of `args` that the teams are entered in.
+template <int DP, int TILE, typename A>
+int launch_split(void (*kernel)(const A), std::atomic<int> (&known)[64], Params &P, const A &args, size_t smem, void *stream) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess || dev >= 64) {
+    cudaGetLastError();
+    return refuse(AMAP_ECUDA, e != cudaSuccess ? cudaGetErrorString(e) : "device number");
+  }
+  int blocks = known[dev].load(std::memory_order_relaxed);
+  if (blocks == 0) {
+    int per_sm = 0;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kBlock, smem);
+    if (e != cudaSuccess || per_sm < 1) {
+      cudaGetLastError();
+      return refuse(AMAP_ECUDA, e != cudaSuccess ? cudaGetErrorString(e) : "the kernel does not fit a multiprocessor");
+    }
+    blocks = device_sms() * std::min(per_sm, kMostBlocksPerSm);
+    SERVE_REQUIRE((blocks + kGroup - 1) / kGroup <= kJoined<DP>, AMAP_EUNSUPPORTED, "more multiprocessors than an item's parts can be joined from");
+    known[dev].store(blocks, std::memory_order_relaxed);
+  }
+  // a team's blocks: the largest divisor of the items of a request that leaves no more than a fiftieth of the device idle
+  for (int members = 1; members <= std::min(P.items_per_request, kMostMembers); ++members)
+    if (P.items_per_request % members == 0 && blocks / members * members * 50 >= blocks * 49) P.members = members;
+  P.rounds = P.items_per_request / P.members;
+  const int64_t most = (int64_t)P.a.n_requests * P.rounds * std::max<int64_t>(1, ((int64_t)P.a.max_pages * P.a.cache.page_size + TILE - 1) / TILE);
+  SERVE_REQUIRE((int64_t)P.a.n_requests * P.rounds * (((int64_t)P.a.max_pages * P.a.cache.page_size) / TILE + 1 + kEntry) / (blocks / P.members) < 0x7FFFFFFF,
+                AMAP_EOVERFLOW, "more tokens than a block can count");
+  return launch(kernel, dim3((unsigned)(std::min<int64_t>(blocks / P.members, most) * P.members)), kBlock, smem, stream, args);
+}
+
+}  // namespace
+
+// What is above serves the attention over a cache of 4 bits, too (serve_attend_packed.cu).
+#ifndef AMAP_ATTEND_PARTS_ONLY
+
+namespace {
+
+// tokens per warp and step, in sixteens: two where a token's row is 128 bytes, so that a step moves 32 KB either way and two
+// independent products hide each other's latency (128 e4m3 requests: 103 us with one, 100 with two)
+template <int ROW_BYTES> constexpr int kSixteens = ROW_BYTES == 128 ? 2 : 1;
+// Blocks resident per multiprocessor: two where their registers allow (O and q of 8 heads of up to 128 elements); with 16
+// heads held to half the registers, what spills costs more than the second block brings (32 requests of 8k tokens, 16 q
+// heads per cache head, P in two terms: 131 us against 117; in three 129 with one block).
+template <int DP, int NT> constexpr int kResident = DP == 256 || NT >= 2 ? 1 : 2;
+// Stages of the ring: 192 KB a multiprocessor, of which about two thirds are in flight (latency times bandwidth is 50).
+template <int ROW_BYTES, int RESIDENT> constexpr int kStages = 192 * 1024 / RESIDENT / (2 * 16 * kSixteens<ROW_BYTES> * kWarps * ROW_BYTES);
+
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool live) {
+  const int n = live ? 16 : 0;  // nothing is read where the row is not live: the 16 bytes become zeros
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void copies_arrive(uint32_t bar) {  // when this thread's copies so far have landed
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tensor_copy(uint32_t dst, const CUtensorMap *map, int x, int token, int head, int page, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+               "l"(map), "r"(x), "r"(token), "r"(head), "r"(page), "r"(bar)
+               : "memory");
+}
+__device__ __forceinline__ void load4(uint32_t at, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void load4_transposed(uint32_t at, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t v) {
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+// four e4m3 as four fp16: exact
+__device__ __forceinline__ void halves_of(uint32_t four, uint32_t *low, uint32_t *high) {
+  asm("{ .reg .b16 l, h; mov.b32 {l, h}, %2; cvt.rn.f16x2.e4m3x2 %0, l; cvt.rn.f16x2.e4m3x2 %1, h; }" : "=r"(*low), "=r"(*high) : "r"(four));
+}
+
+// P in 16-bit terms, each what the ones before it leave over, so that P V has the precision of 32-bit P: three terms of
+// bf16's 8 bits, or two of fp16's 11.  A remainder is no less than `least`, nor (BANDED) is the first term: above zero where
+// V can hold an infinity, so that it meets no zero that P has not got.
+// P is taken relative to a maximum that is renewed only when a score passes it by more than kSlack (in powers of 2): the
+// true one moves in most of the early steps, and O would be rescaled each time.  fp16 terms carry P times 2^kLift, out of
+// the way of fp16's smallest numbers; 2^(kLift + kSlack) is below its largest.  A step with a score further than kDeep
+// below the maximum (beside a token that has nearly all the weight, every one) would still come too near them: such a
+// step goes by bands of kBand powers of 2 from its own highest score down, each lifted to 2^(kLift + kSlack) and scaled
+// back in 32 bits.  In all others P is 2^(kLift - kDeep) at least, 2^12 of fp16's smallest steps.  The three numbers share
+// fp16's 40 powers of 2 out so that bands are rare: with scores of 2.9 (standard deviation, powers of 2) 16 q heads per
+// cache head take 80 us for 32 requests up to 8192 tokens, with 8 + 7, 17 in place of 6 + 9, 21 94 us, without bands 78.  With
+// scores of 11.6 nearly every step goes by bands: 128 e4m3 requests 119 -> 182 us, 32 of fp16 195 -> 276.
+constexpr float kSlack = 6.0f, kDeep = 21.0f, kBand = 24.0f;
+template <int CT> constexpr float kLift = CT == AMAP_FP16 ? 9.0f : 0.0f;
+template <int CT> constexpr int kTerms = CT == AMAP_BF16 ? 3 : 2;
+template <int CT, bool BANDED>
+__device__ __forceinline__ void split(float p0, float p1, float least, uint32_t (&term)[kTerms<CT>]) {
+  if constexpr (CT == AMAP_BF16) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const uint32_t u0 = __float_as_uint(p0), u1 = __float_as_uint(p1);
+      term[k] = __byte_perm(u0, u1, 0x7632);
+      p0 = fmaxf(p0 - __uint_as_float(u0 & 0xFFFF0000u), least);
+      p1 = fmaxf(p1 - __uint_as_float(u1 & 0xFFFF0000u), least);
+    }
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(term[2]) : "f"(p1), "f"(p0));
+  } else {
+    asm("cvt.rz.f16x2.f32 %0, %1, %2;" : "=r"(term[0]) : "f"(p1), "f"(p0));
+    __half2 h = *reinterpret_cast<const __half2 *>(&term[0]);
+    if constexpr (BANDED) {
+      h = __hmax2_nan(h, __float2half2_rn(least));
+      term[0] = *reinterpret_cast<const uint32_t *>(&h);
+    }
+    const float r0 = fmaxf(p0 - __low2float(h), least), r1 = fmaxf(p1 - __high2float(h), least);
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(term[1]) : "f"(r1), "f"(r0));
+  }
+}
+
 template <int CT, bool FP8, int DP, int NT>
 __global__ void __launch_bounds__(kBlock, (kResident<DP, NT>)) attend_kernel(const __grid_constant__ Params P) {
   constexpr int ES = FP8 ? 1 : 2, RB = DP * ES, NB = RB / 128, S = kStages<RB, kResident<DP, NT>>;
@@ -386,58 +641,12 @@ __global__ void __launch_bounds__(kBlock, (kResident<DP, NT>)) attend_kernel(con
   }
   pdl_begin();
 
-  // ---- where this block's piece of the line begins ----
-  const int R = P.a.n_requests, per = (R + kThreads - 1) / kThreads, r_first = warp < kWarps ? min(R, tid * per) : R, r_last = min(R, r_first + per);
-  int64_t mine = 0;
-  for (int r = r_first; r < r_last; ++r) mine += kEntry + Line::tiles(P, Line::clamped(P, P.a.seq_lens[r]));
-  mine *= P.rounds;
-  int64_t upto = mine;
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const int64_t v = __shfl_up_sync(~0u, upto, d);
-    if (lane >= d) upto += v;
-  }
-  if (lane == 31 && warp < kWarps) small.sums[warp] = upto;
-  __syncthreads();
-  int64_t total = 0;
-#pragma unroll
-  for (int w = 0; w < kWarps; ++w) {
-    if (w < warp) upto += small.sums[w];
-    total += small.sums[w];
-  }
-  const int team = blockIdx.x / P.members, member = blockIdx.x - team * P.members;
-  const int64_t pieces = min((int64_t)(gridDim.x / P.members), total);  // none of them empty
-  if (team >= pieces) return;
-  const int64_t u0 = total * team / pieces, u1 = total * (team + 1) / pieces;
-  if (warp < kWarps && upto > u0 && upto - mine <= u0) {
-    int64_t u = upto - mine;
-    for (int r = r_first; r < r_last; ++r) {
-      const int tiles = Line::tiles(P, Line::clamped(P, P.a.seq_lens[r]));
-      const int64_t places = (int64_t)(kEntry + tiles) * P.rounds;
-      if (u + places > u0) {
-        const int64_t in = u0 - u;
-        const int round = in <= 0x7FFFFFFF ? (int)in / (kEntry + tiles) : (int)(in / (kEntry + tiles));
-        const int tile = max(0, (int)(in - (int64_t)round * (kEntry + tiles)) - kEntry);
-        small.begin[0] = r;
-        small.begin[1] = round;
-        small.begin[2] = tile;
-        small.first_place = u + (int64_t)round * (kEntry + tiles) + kEntry;  // of the item that u0 is in
-        break;
-      }
-      u += places;
-    }
-  }
-  __syncthreads();
-  Line at;
-  at.start(P, small.begin[0], small.begin[1], small.begin[2], small.first_place, u1);
-  if (at.rest <= 0) return;  // a piece between two items
+  Piece<TILE> piece;
+  if (!piece.find(P, small)) return;
+  Line &at = piece.at;
+  const int team = piece.team, member = piece.member;
+  const int64_t u0 = piece.u0, u1 = piece.u1;
   bool alive = true;
-  // the parts of the item that the piece begins in: those of the teams `from` to `to`, of which the first began it in its
-  // second slot, the others go on with it in their first
-  const int64_t first_place = small.first_place, first_last = first_place + Line::tiles(P, at.n) - 1;
-  auto team_of = [&](int64_t place) { return (int)(((place + 1) * pieces - 1) / total); };
-  const int first_from = team_of(first_place), first_to = team_of(first_last);
-  const bool aside = first_place < u0 && first_last + 1 + kEntry < u1 && first_to - first_from < kAside;
 
   if (warp == kWarps) {
     // ---- the producer ----
@@ -551,14 +760,7 @@ __global__ void __launch_bounds__(kBlock, (kResident<DP, NT>)) attend_kernel(con
       settle(smem_at(&small.full[0]), S, stage, parity ^ 1, P.failed);
       return;
     }
-    if (aside) {
-      asm volatile("bar.sync 2, %0;" ::"n"(kBlock) : "memory");  // the four warps have written the first item's part
-      const int h = small.begin[1] * P.members + member, r = small.begin[0], in_group = h % P.blocks_per_head * HB;
-      auto slot_of = [&](int i) { return 2 * ((first_from + i) * P.members + member) + (i == 0 ? 1 : 0); };
-      if (last_of<Producer>(P.arrived + (int64_t)r * P.items_per_request + h, first_to - first_from + 1, &small.told_aside))
-        join<Producer, CT, DP, HB>(P, small.aside, first_to - first_from + 1, slot_of, min(HB, P.group - in_group), true, r,
-                                   h / P.blocks_per_head * P.group + in_group);
-    }
+    if (piece.aside) join_aside<DP, HB>(P, small, piece, kLift<CT>);
     return;
   }
 
@@ -643,7 +845,7 @@ __global__ void __launch_bounds__(kBlock, (kResident<DP, NT>)) attend_kernel(con
   ask_q(at.r, at.h * P.members + member);
   take_q();
   clear();
-  int64_t item_first = first_place;
+  int64_t item_first = piece.first_place;
   // where a lane's row of the matrix loads lies in a tile, and its chunk 2j (+1 for the upper lanes) swizzled
   uint32_t lane_at[4];
 #pragma unroll
@@ -967,57 +1169,10 @@ __global__ void __launch_bounds__(kBlock, (kResident<DP, NT>)) attend_kernel(con
         }
       }
       sync_consumers();
-      const int n_heads = min(8, heads - nt * 8);
-      for (int i = tid; i < n_heads * (DP / 2); i += kThreads) {
-        const int in = i / (DP / 2), d = i % (DP / 2) * 2, head = nt * 8 + in;
-        if (d >= D) continue;
-        const float *ml = joint + in * kPitch + DP;
-        const float top = fmaxf(fmaxf(ml[0], ml[8 * kPitch]), fmaxf(ml[16 * kPitch], ml[24 * kPitch]));
-        float sum = 0.0f;
-        float2 y = make_float2(0.0f, 0.0f);
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-          sum += ml[w * 8 * kPitch + 1] * (top == -INFINITY ? 1.0f : exp2_of(ml[w * 8 * kPitch] - top));
-          const float2 v = *reinterpret_cast<const float2 *>(joint + (w * 8 + in) * kPitch + d);
-          y.x += v.x;
-          y.y += v.y;
-        }
-        if (whole) {
-          const float f = sum == 0.0f ? 0.0f : C.v_scale / sum;
-          write_pair(P, (int64_t)r * P.a.out_row + (int64_t)(first + in_group + head) * P.a.out_head + d, y.x * f, y.y * f);
-          if (d == 0 && P.a.lse)
-            P.a.lse[(int64_t)r * P.a.lse_row + first + in_group + head] = sum == 0.0f ? -INFINITY : (top - kLift<CT> + log2f(sum)) * kLn2;
-        } else {
-          *reinterpret_cast<float2 *>(P.part_o + ((int64_t)slot * HB + head) * DP + d) = y;
-          if (d == 0) reinterpret_cast<float2 *>(P.part_ml)[(int64_t)slot * HB + head] = make_float2(top, sum);
-        }
-      }
+      sum_warps<DP, HB>(P, joint, nt, heads, whole, r, first + in_group, slot, kLift<CT>);
       sync_consumers();
     }
-    if (!whole) {  // uniform over the block
-      if (aside && item_first < u0) {
-        asm volatile("bar.arrive 2, %0;" ::"n"(kBlock) : "memory");
-      } else {
-        const int from = team_of(item_first), to = team_of(item_last);
-        auto slot_of_team = [&](int b) { return 2 * (b * P.members + member) + (b == from ? 1 : 0); };
-        int32_t *item = P.arrived + (int64_t)r * P.items_per_request + h;
-        if (to - from < kDirect) {
-          if (last_of<Consumers>(item, to - from + 1, &small.told))
-            join<Consumers, CT, DP, HB>(P, joined, to - from + 1, [&](int i) { return slot_of_team(from + i); }, heads, true, r, first + in_group);
-        } else {
-          // of the items with parts in a group of teams, one at most began before the group and one at most, among those
-          // with more than kDirect parts, begins in it: two counters
-          const int group = team / kGroup, b0 = max(from, group * kGroup), b1 = min(to, group * kGroup + kGroup - 1);
-          if (last_of<Consumers>(P.grouped + 2 * (group * P.members + member) + (from >= group * kGroup ? 1 : 0), b1 - b0 + 1, &small.told)) {
-            join<Consumers, CT, DP, HB>(P, joined, b1 - b0 + 1, [&](int i) { return slot_of_team(b0 + i); }, heads, false, r, first + in_group);
-            const int g0 = from / kGroup, g1 = to / kGroup;
-            if (last_of<Consumers>(item, g1 - g0 + 1, &small.told))
-              join<Consumers, CT, DP, HB>(P, joined, g1 - g0 + 1, [&](int i) { return slot_of_team(max(from, (g0 + i) * kGroup)); }, heads, true, r,
-                                          first + in_group);
-          }
-        }
-      }
-    }
+    if (!whole) hand_in<DP, HB>(P, small, joined, piece, item_first, item_last, heads, r, h, first + in_group, kLift<CT>);  // uniform over the block
     if (more) {
       item_first = u1 - at.rest;
       take_q();
@@ -1033,35 +1188,8 @@ int run(Params &P, void *stream) {
   constexpr int TILE = 16 * kSixteens<RB> * kWarps;
   constexpr int S = kStages<RB, kResident<DP, NT>>;
   constexpr size_t smem = (size_t)S * 2 * TILE * RB + sizeof(float) * kWarps * 8 * (DP + 4) + sizeof(Small<S, TILE>);
-  // the block's shared memory is asked for, and how many blocks a multiprocessor then holds, once per device
   static std::atomic<int> known[64];
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess || dev >= 64) {
-    cudaGetLastError();
-    return refuse(AMAP_ECUDA, e != cudaSuccess ? cudaGetErrorString(e) : "device number");
-  }
-  int blocks = known[dev].load(std::memory_order_relaxed);
-  if (blocks == 0) {
-    int per_sm = 0;
-    e = cudaFuncSetAttribute(attend_kernel<CT, FP8, DP, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, attend_kernel<CT, FP8, DP, NT>, kBlock, smem);
-    if (e != cudaSuccess || per_sm < 1) {
-      cudaGetLastError();
-      return refuse(AMAP_ECUDA, e != cudaSuccess ? cudaGetErrorString(e) : "the kernel does not fit a multiprocessor");
-    }
-    blocks = device_sms() * std::min(per_sm, kMostBlocksPerSm);
-    SERVE_REQUIRE((blocks + kGroup - 1) / kGroup <= kJoined<DP>, AMAP_EUNSUPPORTED, "more multiprocessors than an item's parts can be joined from");
-    known[dev].store(blocks, std::memory_order_relaxed);
-  }
-  // a team's blocks: the largest divisor of the items of a request that leaves no more than a fiftieth of the device idle
-  for (int members = 1; members <= std::min(P.items_per_request, kMostMembers); ++members)
-    if (P.items_per_request % members == 0 && blocks / members * members * 50 >= blocks * 49) P.members = members;
-  P.rounds = P.items_per_request / P.members;
-  const int64_t most = (int64_t)P.a.n_requests * P.rounds * std::max<int64_t>(1, ((int64_t)P.a.max_pages * P.a.cache.page_size + TILE - 1) / TILE);
-  SERVE_REQUIRE((int64_t)P.a.n_requests * P.rounds * (((int64_t)P.a.max_pages * P.a.cache.page_size) / TILE + 1 + kEntry) / (blocks / P.members) < 0x7FFFFFFF,
-                AMAP_EOVERFLOW, "more tokens than a block can count");
-  return launch(attend_kernel<CT, FP8, DP, NT>, dim3((unsigned)(std::min<int64_t>(blocks / P.members, most) * P.members)), kBlock, smem, stream, P);
+  return launch_split<DP, TILE>(attend_kernel<CT, FP8, DP, NT>, known, P, P, smem, stream);
 }
 
 template <int CT, bool FP8, int DP>
@@ -1087,36 +1215,6 @@ int run_dim(Params &P, int dp, int nt, void *stream) {
 
 // head sizes are padded to what a kernel is built for (in shared memory only: no more is read): whole rows of 128 bytes
 int padded_dim(int d, int es) { return d * es <= 128 ? 128 / es : d <= 128 ? 128 : 256; }
-// eights of q heads that share a pass over the cache: all of a group where its accumulators fit the registers
-int eights(int group, int dp) {
-  const int most = dp < 256 ? 4 : 2;
-  return group <= 8 ? 1 : group <= 16 || most == 2 ? 2 : 4;
-}
-
-
-
-int check_shape(int32_t n_requests, int32_t q_heads, int32_t kv_heads, int32_t head_dim) {
-  SERVE_REQUIRE(n_requests >= 1 && n_requests <= 0xFFFF, AMAP_EINVAL, "requests: 1 .. 65535");
-  SERVE_REQUIRE(q_heads >= 1 && q_heads <= 0xFFFF && kv_heads >= 1 && q_heads % kv_heads == 0, AMAP_EINVAL, "q heads: a multiple of the cache's heads");
-  SERVE_REQUIRE(head_dim >= 8 && head_dim <= 256 && head_dim % 8 == 0, AMAP_EUNSUPPORTED, "head size: a multiple of 8, up to 256");
-  return AMAP_OK;
-}
-
-struct Workspace {
-  int64_t ml, failed, grouped, arrived, bytes;  // offsets; the partial outputs come first
-};
-Workspace workspace(int32_t n_requests, int32_t q_heads, int32_t kv_heads, int32_t head_dim) {
-  const int dp = head_dim <= 128 ? 128 : 256, group = q_heads / kv_heads, hb = 8 * eights(group, dp);
-  const int64_t blocks = (int64_t)device_sms() * kMostBlocksPerSm, items = (int64_t)n_requests * kv_heads * ((group + hb - 1) / hb);
-  Workspace w;
-  w.ml = 2 * blocks * hb * dp * 4;
-  w.failed = w.ml + 2 * blocks * hb * 8;
-  w.grouped = w.failed + 16;
-  w.arrived = w.grouped + (blocks / kGroup + kMostMembers) * 2 * 4;
-  w.bytes = (w.arrived + items * 4 + 255) / 256 * 256;
-  return w;
-}
-
 using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
                             const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
@@ -1200,48 +1298,13 @@ extern "C" int amap_attend(const amap_attend_args *a, void *cuda_stream) {
   SERVE_REQUIRE(a, AMAP_EINVAL, "null pointer");
   if (const int rc = check_readable(a->cache)) return rc;
   const amap_cache &c = a->cache;
-  if (const int rc = check_shape(a->n_requests, a->q_heads, c.heads, c.head_dim)) return rc;
-  SERVE_REQUIRE(a->dtype == AMAP_BF16 || a->dtype == AMAP_FP16, AMAP_EINVAL, "type: bf16 or fp16");
+  if (const int rc = check_call(*a, c.heads, c.head_dim, c.page_size)) return rc;
   SERVE_REQUIRE(c.dtype == AMAP_E4M3 || c.dtype == a->dtype, AMAP_EINVAL, "a 16-bit cache has the type of q");
-  SERVE_REQUIRE(a->q && a->out && a->block_table && a->seq_lens && a->workspace, AMAP_EINVAL, "null pointer");
-  SERVE_REQUIRE(a->max_pages >= 1 && a->table_stride >= a->max_pages, AMAP_EINVAL, "table rows overlap");
-  SERVE_REQUIRE((int64_t)a->max_pages * c.page_size <= 0x7FFFFFFF, AMAP_EOVERFLOW, "a table row holds more than 2^31-1 tokens");
-  SERVE_REQUIRE(std::isfinite(a->scale) && std::isfinite(a->softcap) && a->softcap >= 0 && a->window >= 0 && a->reserved == 0, AMAP_EINVAL,
-                "scale is finite, softcap and window are not negative");
-  SERVE_REQUIRE(aligned(a->q, 2) && aligned(a->out, 2) && aligned(a->lse, 4) && aligned(a->block_table, 4) && aligned(a->seq_lens, 4) &&
-                    aligned(a->workspace, 256), AMAP_EALIGN, "misaligned pointer");
-  Span qs, os;
-  qs.hi = os.hi = (int64_t)c.head_dim * 2;
-  qs.add(a->n_requests, a->q_row, 2);
-  qs.add(a->q_heads, a->q_head, 2);
-  os.add(a->n_requests, a->out_row, 2);
-  os.add(a->q_heads, a->out_head, 2);
-  SERVE_REQUIRE(!overlap(a->q, qs, a->out, os), AMAP_EINVAL, "q and out overlap");
-
-  const Workspace w = workspace(a->n_requests, a->q_heads, c.heads, c.head_dim);
-  SERVE_REQUIRE(a->workspace_bytes >= w.bytes, AMAP_EINVAL, "workspace too small");
   const int dp = padded_dim(c.head_dim, dtype_bytes(c.dtype));
   Params P = {};
   P.a = *a;
-  P.group = a->q_heads / c.heads;
-  const int nt = eights(P.group, dp);
-  P.blocks_per_head = (P.group + 8 * nt - 1) / (8 * nt);
-  P.items_per_request = c.heads * P.blocks_per_head;
-  SERVE_REQUIRE((int64_t)a->n_requests * P.items_per_request <= 0x7FFFFFFF, AMAP_EOVERFLOW, "more than 2^31-1 pairs of request and head");
-  // token / page_size for tokens below 2^31: a shift, or the high word of a product with ceil(2^(32+s) / page_size),
-  // s = floor(log2 page_size), whose excess over 2^(32+s) is at most page_size - 1 < 2^(s+1): exact up to 2^31
-  int s = 0;
-  while ((2u << s) <= (uint32_t)c.page_size) ++s;
-  P.div_shift = s;
-  if (c.page_size != 1 << s) P.div_mul = (uint32_t)((((uint64_t)1 << (32 + s)) + c.page_size - 1) / c.page_size);
-  P.q_pairs = aligned(a->q, 4) && a->q_row % 2 == 0 && a->q_head % 2 == 0;
-  P.out_pairs = aligned(a->out, 4) && a->out_row % 2 == 0 && a->out_head % 2 == 0;
-  char *ws = static_cast<char *>(a->workspace);
-  P.part_o = reinterpret_cast<float *>(ws);
-  P.part_ml = reinterpret_cast<float *>(ws + w.ml);
-  P.failed = reinterpret_cast<int32_t *>(ws + w.failed);
-  P.grouped = reinterpret_cast<int32_t *>(ws + w.grouped);
-  P.arrived = reinterpret_cast<int32_t *>(ws + w.arrived);
+  const int nt = eights(a->q_heads / c.heads, dp);
+  if (const int rc = place(P, nt)) return rc;
   amap_cache_maps made;
   const amap_cache_maps *maps = a->maps;
   if (!maps) {
@@ -1258,3 +1321,5 @@ extern "C" int amap_attend(const amap_attend_args *a, void *cuda_stream) {
   if (c.dtype == AMAP_E4M3) return run_dim<AMAP_FP16, true>(P, dp, nt, cuda_stream);
   return c.dtype == AMAP_BF16 ? run_dim<AMAP_BF16, false>(P, dp, nt, cuda_stream) : run_dim<AMAP_FP16, false>(P, dp, nt, cuda_stream);
 }
+
+#endif  // AMAP_ATTEND_PARTS_ONLY

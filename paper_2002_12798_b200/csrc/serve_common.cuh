@@ -34,24 +34,32 @@ inline int accept() {
 // multiprocessors of the current device
 int device_sms();
 
+// cluster: blocks of a cluster, 1 for none
 template <typename... P, typename... A>
-int launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, void *stream, const A &...args) {
+int launch_clusters(void (*kernel)(P...), dim3 grid, int cluster, int threads, size_t smem, void *stream, const A &...args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = static_cast<cudaStream_t>(stream);
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
   const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
   if (e != cudaSuccess) {
     cudaGetLastError();  // a refused launch leaves no error behind for the caller's next CUDA call
     return refuse(AMAP_ECUDA, cudaGetErrorString(e));
   }
   return accept();
+}
+template <typename... P, typename... A>
+int launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, void *stream, const A &...args) {
+  return launch_clusters(kernel, grid, 1, threads, smem, stream, args...);
 }
 
 // EVERY thread of every kernel calls both, in this order, before it touches a buffer: a block that returned without

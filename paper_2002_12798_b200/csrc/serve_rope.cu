@@ -17,6 +17,7 @@
 
 #include "serve_alias.hpp"
 #include "serve_common.cuh"
+#include "serve_packed.cuh"
 
 using namespace amap_serve;
 
@@ -195,16 +196,16 @@ __device__ __forceinline__ void fetch(const float *row, int c, int half, float (
   }
 }
 
+// A block's work on the rows of a part, the `block`-th of all; turn_cos and turn_sin: kMaxTokens * kMaxHalf floats each.
 template <int DT, int VEC, int PAIRS>
-__global__ void __launch_bounds__(kThreads, kBlocks) rope_kernel(const __grid_constant__ Params P) {
-  __shared__ __align__(16) float turn_cos[kMaxTokens * kMaxHalf], turn_sin[kMaxTokens * kMaxHalf];
+__device__ __forceinline__ void turn_rows(const Params &P, uint32_t block, float *turn_cos, float *turn_sin) {
   constexpr int ES = sizeof(typename Elem<DT>::T);
   using Chunk = typename Raw<VEC * ES>::T;
   int k = 0;
-  while (k + 1 < P.n_parts && blockIdx.x >= P.part[k + 1].first_block) ++k;
+  while (k + 1 < P.n_parts && block >= P.part[k + 1].first_block) ++k;
   const Part part = P.part[k];  // a copy: the fields stay in registers
   const int half = P.half, chunks = half / VEC, items = P.by_items.d;
-  const int64_t row0 = (int64_t)(blockIdx.x - part.first_block) * part.tokens;
+  const int64_t row0 = (int64_t)(block - part.first_block) * part.tokens;
   const int tokens = (int)min((int64_t)part.tokens, P.rows - row0), n = tokens * part.heads * items;
   const bool turns = part.kind != kCacheCopied;
   const char *const x0 = part.x + row0 * part.x_row * ES;
@@ -297,9 +298,15 @@ __global__ void __launch_bounds__(kThreads, kBlocks) rope_kernel(const __grid_co
   }
 }
 
-template <int DT, int VEC>
-int run(const amap_rope_t &plan, Params &P, void *stream) {
-  const int items = P.half / VEC + ((P.head_dim - 2 * P.half) / VEC + 1) / 2;
+template <int DT, int VEC, int PAIRS>
+__global__ void __launch_bounds__(kThreads, kBlocks) rope_kernel(const __grid_constant__ Params P) {
+  __shared__ __align__(16) float turn_cos[kMaxTokens * kMaxHalf], turn_sin[kMaxTokens * kMaxHalf];
+  turn_rows<DT, VEC, PAIRS>(P, blockIdx.x, turn_cos, turn_sin);
+}
+
+// Divides the parts' rows into blocks and returns their number.
+int64_t divide(Params &P, int vec) {
+  const int items = P.half / vec + ((P.head_dim - 2 * P.half) / vec + 1) / 2;
   P.by_items = div_by(items);
   P.by_half = div_by(std::max(P.half, 1));
   // tokens per block: two items a thread, but no fewer than two blocks a multiprocessor where there is that much work
@@ -315,6 +322,12 @@ int run(const amap_rope_t &plan, Params &P, void *stream) {
     part.first_block = (uint32_t)blocks;
     blocks += (P.rows + part.tokens - 1) / part.tokens;
   }
+  return blocks;
+}
+
+template <int DT, int VEC>
+int run(const amap_rope_t &plan, Params &P, void *stream) {
+  const int64_t blocks = divide(P, VEC);
   SERVE_REQUIRE(blocks <= 0x7FFFFFFF, AMAP_EOVERFLOW, "too many rows");
   const dim3 grid((unsigned)blocks);
   return plan.pairs == AMAP_PAIRS_HALF ? launch(rope_kernel<DT, VEC, AMAP_PAIRS_HALF>, grid, kThreads, 0, stream, P)
@@ -337,6 +350,199 @@ int widest(const Params &P, int es, int heads_es) {
   };
   while (vec > 1 && !fits(vec)) vec >>= 1;
   return vec;
+}
+
+// ---- the write into a cache of 4 bits ----
+// A thread has eight elements of a row, the 4 or 8 threads of a group find its smallest and largest by shuffles.  All of it is
+// in 64 bits: between two codes lies a border, and where k falls is the definition's only if k is not a rounding away from it
+// (with 32 bits about one of 2^19 codes would come out as its neighbour, and one of 2^15 steps as another number).  k and
+// v are a fifth of what the launch reads and writes at 4 q heads to a cache head, and the 64-bit units are idle otherwise.
+struct Packing {
+  Params p;  // its one part is q; slots, positions, phases and by_page are k's and v's, too
+  const char *k, *v;
+  int64_t k_row, k_head, v_row, v_head;  // elements
+  char *data;
+  int64_t page, head;  // bytes
+  int32_t heads, slabs, group, tokens;  // tokens of a block
+  uint32_t k_blocks, blocks;            // of k; of k and v: the first of the launch
+  Div by_chunks, by_heads;              // eights of a head; heads
+  int32_t k_wide, v_wide, pad;          // rows in whole 16 bytes; turns of a token in the table
+};
+constexpr int kTurns = kMaxTokens * kMaxHalf / 2;  // cos and sin in 64 bits that fit the two tables of 32
+
+template <int PAIRS>
+__device__ __forceinline__ int turn_place(int i, int pad) {  // neighbouring chunks' turns side by side
+  constexpr int OF = PAIRS == AMAP_PAIRS_HALF ? 8 : 4;
+  return (i % OF) * (pad / OF) + i / OF;
+}
+
+template <int DT>
+__device__ __forceinline__ void eight(const char *row, int d, bool wide, float (&x)[8]) {
+  using T = typename Elem<DT>::T;
+  const T *p = reinterpret_cast<const T *>(row) + d;
+  if (wide) {
+    unpack<DT, 8>(*reinterpret_cast<const uint4 *>(p), x);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = Elem<DT>::to(p[j]);
+  }
+}
+
+template <int DT, int PAIRS>
+__device__ __forceinline__ void pack_rows(const Packing &A, uint32_t block, double *turn_cos, double *turn_sin) {
+  constexpr int ES = sizeof(typename Elem<DT>::T);
+  const Params &P = A.p;
+  const bool is_k = block < A.k_blocks;
+  if (!is_k) block -= A.k_blocks;
+  const int half = is_k ? P.half : 0, chunks = P.head_dim / 8;
+  const int64_t row0 = (int64_t)block * A.tokens;
+  const int tokens = (int)min((int64_t)A.tokens, P.rows - row0), n = tokens * A.heads * chunks;
+  const char *const x0 = (is_k ? A.k : A.v) + row0 * (is_k ? A.k_row : A.v_row) * ES;
+  const int64_t x_row = is_k ? A.k_row : A.v_row, x_head = is_k ? A.k_head : A.v_head;
+  const bool wide = is_k ? A.k_wide : A.v_wide, partner_wide = wide && half % 8 == 0;
+  pdl_begin();
+  if (half) {
+    const uint64_t *phases = P.phase;  // as memory, not as constants (rope_kernel)
+    const uint8_t *axes = P.axis;
+    asm volatile("" : "+l"(phases), "+l"(axes));
+    for (int i = threadIdx.x; i < tokens * half; i += kThreads) {
+      const int at = quotient(i, P.by_half), pair = i - at * half;
+      const int64_t from = axes[pair] * P.position_axis + (row0 + at) * P.position_row;
+      const int64_t pos = P.wide_positions ? static_cast<const int64_t *>(P.positions)[from] : static_cast<const int32_t *>(P.positions)[from];
+      double s, c;
+      sincospi((double)(int64_t)((uint64_t)pos * phases[pair]) * 0x1p-63, &s, &c);
+      turn_cos[at * A.pad + turn_place<PAIRS>(pair, A.pad)] = c * P.scale;
+      turn_sin[at * A.pad + turn_place<PAIRS>(pair, A.pad)] = s * P.scale;
+    }
+    __syncthreads();
+  }
+  for (int base = 0; base < n; base += kThreads) {  // whole warps throughout
+    const int item = min(base + (int)threadIdx.x, n - 1);
+    const int row = quotient(item, A.by_chunks), c = item - row * chunks, token = quotient(row, A.by_heads), head = row - token * A.heads, d0 = c * 8;
+    const char *const from = x0 + ((int64_t)token * x_row + head * x_head) * ES;
+    float f[8];
+    eight<DT>(from, d0, wide, f);
+    double x[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = f[j];
+    if (d0 < 2 * half) {
+      const double *const cos = turn_cos + token * A.pad, *const sin = turn_sin + token * A.pad;
+      if constexpr (PAIRS == AMAP_PAIRS_HALF) {
+        float y[8];
+        if (partner_wide) {
+          eight<DT>(from, d0 < half ? d0 + half : d0 - half, true, y);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int d = d0 + j;
+            y[j] = d < 2 * half ? Elem<DT>::to(reinterpret_cast<const typename Elem<DT>::T *>(from)[d < half ? d + half : d - half]) : 0.0f;
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int d = d0 + j;
+          if (d >= 2 * half) continue;
+          const int at = turn_place<PAIRS>(d < half ? d : d - half, A.pad);
+          x[j] = d < half ? x[j] * cos[at] - y[j] * sin[at] : x[j] * cos[at] + y[j] * sin[at];
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+          if (d0 + j >= 2 * half) continue;
+          const int at = turn_place<PAIRS>((d0 + j) / 2, A.pad);
+          const double a = x[j], b = x[j + 1];
+          x[j] = a * cos[at] - b * sin[at];
+          x[j + 1] = b * cos[at] + a * sin[at];
+        }
+      }
+    }
+    double least = x[0], most = x[0];
+    int finite = 1;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      least = fmin(least, x[j]);
+      most = fmax(most, x[j]);
+      finite &= isfinite(x[j]);
+    }
+#pragma unroll
+    for (int d = 1; d < 8; d <<= 1) {
+      if (8 * d >= A.group) break;
+      least = fmin(least, __shfl_xor_sync(~0u, least, d));
+      most = fmax(most, __shfl_xor_sync(~0u, most, d));
+      finite &= __shfl_xor_sync(~0u, finite, d);
+    }
+    // low is rounded down, so that no element lies below it: twice, which comes to the same as once
+    __nv_bfloat16 low = __float2bfloat16_rd(__double2float_rd(least));
+    __nv_bfloat16 step = __float2bfloat16_rn((float)((most - (double)__bfloat162float(low)) / 15.0));
+    if (!finite || !isfinite(__bfloat162float(low)) || !isfinite(__bfloat162float(step))) {
+      low = __ushort_as_bfloat16(0x7FC0);
+      step = __ushort_as_bfloat16(0);
+    }
+    const double l = __bfloat162float(low), s = __bfloat162float(step), by = s > 0 ? 1.0 / s : 0.0;
+    uint32_t code[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      // rint((x - l) / s): the product with the reciprocal is a rounding off at most, the rest says which way
+      const double over = x[j] - l;
+      double near = rint(over * by);
+      const double rest = 2.0 * fma(-near, s, over);
+      const bool odd = (int)near & 1;
+      if (rest > s || (rest == s && odd)) near += 1.0;
+      else if (rest < -s || (rest == -s && odd)) near -= 1.0;
+      code[j] = s > 0 ? (uint32_t)(int)fmin(near, 15.0) : 0;
+    }
+    const int32_t slot = P.slots[row0 + token];
+    if (base + (int)threadIdx.x >= n || slot < 0 || slot >= P.n_slots) continue;
+    const uint32_t page = quotient(slot, P.by_page), in = slot - page * P.by_page.d;
+    const int t = in % kCell, groups = P.head_dim / A.group;
+    char *const cell = A.data + (int64_t)page * A.page + (int64_t)head * A.head + (int64_t)(in / kCell) * cell_bytes(A.slabs, groups);
+    if (is_k) {
+      uint32_t w = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w |= code[j] << (4 * (j >> 1) + 16 * (j & 1));
+      *reinterpret_cast<uint32_t *>(cell + k_word_at(A.slabs, t, c)) = w;
+    } else {
+      *reinterpret_cast<uint16_t *>(cell + v_half_at(A.slabs, t, 2 * c)) = (uint16_t)(code[0] | code[1] << 4 | code[2] << 8 | code[3] << 12);
+      *reinterpret_cast<uint16_t *>(cell + v_half_at(A.slabs, t, 2 * c + 1)) = (uint16_t)(code[4] | code[5] << 4 | code[6] << 8 | code[7] << 12);
+    }
+    if (d0 % A.group == 0)
+      *reinterpret_cast<uint32_t *>(cell + numbers_at(A.slabs, t, d0 / A.group) + (is_k ? 0 : 8)) = (uint32_t)__bfloat16_as_ushort(low) << 16 | __bfloat16_as_ushort(step);
+  }
+}
+
+template <int DT, int VEC, int PAIRS>
+__global__ void __launch_bounds__(kThreads, 2) pack_kernel(const __grid_constant__ Packing A) {
+  __shared__ __align__(16) double turn_cos[kTurns], turn_sin[kTurns];
+  if (blockIdx.x < A.blocks) pack_rows<DT, PAIRS>(A, blockIdx.x, turn_cos, turn_sin);
+  else turn_rows<DT, VEC, PAIRS>(A.p, blockIdx.x - A.blocks, reinterpret_cast<float *>(turn_cos), reinterpret_cast<float *>(turn_sin));
+}
+
+template <int DT, int VEC>
+int run_packing(int pairs, Packing &A, void *stream) {
+  Params &P = A.p;
+  const int chunks = P.head_dim / 8, of = pairs == AMAP_PAIRS_HALF ? 8 : 4;
+  const int64_t q_blocks = divide(P, VEC);
+  A.by_chunks = div_by(chunks);
+  A.by_heads = div_by(A.heads);
+  A.pad = (P.half + of - 1) / of * of;
+  A.tokens = std::max(1, std::min(kThreads / (A.heads * chunks), kTurns / std::max(A.pad, 1)));
+  const int64_t blocks = (P.rows + A.tokens - 1) / A.tokens;
+  SERVE_REQUIRE(2 * blocks + q_blocks <= 0x7FFFFFFF, AMAP_EOVERFLOW, "too many rows");
+  A.k_blocks = (uint32_t)blocks;
+  A.blocks = (uint32_t)(2 * blocks);
+  const dim3 grid((unsigned)(2 * blocks + q_blocks));
+  return pairs == AMAP_PAIRS_HALF ? launch(pack_kernel<DT, VEC, AMAP_PAIRS_HALF>, grid, kThreads, 0, stream, A)
+                                  : launch(pack_kernel<DT, VEC, AMAP_PAIRS_ADJACENT>, grid, kThreads, 0, stream, A);
+}
+
+template <int DT>
+int run_packing_wide(int vec, int pairs, Packing &A, void *stream) {
+  switch (vec) {
+    case 8: return run_packing<DT, 8>(pairs, A, stream);
+    case 4: return run_packing<DT, 4>(pairs, A, stream);
+    case 2: return run_packing<DT, 2>(pairs, A, stream);
+    default: return run_packing<DT, 1>(pairs, A, stream);
+  }
 }
 
 int run_typed(const amap_rope_t &plan, Params &P, int dtype, int cache_es, void *stream) {
@@ -387,6 +593,27 @@ Span rows_span(int64_t rows, int64_t row, int heads, int64_t head, int dim, int 
 
 Runs runs(const void *at, int64_t rows, int64_t row, int heads, int64_t head, int es) {
   return {(int64_t) reinterpret_cast<uintptr_t>(at), rows, row * es, heads, head * es};
+}
+
+// Where q's result may go: beside its inputs, or over q itself.
+template <typename A>
+int check_q_out(const A &a, int heads, int dim) {
+  const int es = 2;
+  SERVE_REQUIRE((a.rows == 1 || a.q_out_row) && (a.q_heads == 1 || a.q_out_head), AMAP_EINVAL, "rows of q_out lie on one another");
+  if (a.q_out != a.q || a.q_row != a.q_out_row || a.q_head != a.q_out_head) {
+    const Span xs = rows_span(a.rows, a.q_row, a.q_heads, a.q_head, dim, es);
+    const Span ys = rows_span(a.rows, a.q_out_row, a.q_heads, a.q_out_head, dim, es);
+    SERVE_REQUIRE(!overlap(a.q, xs, a.q_out, ys) &&
+                      !overlap(a.k, rows_span(a.rows, a.k_row, heads, a.k_head, dim, es), a.q_out, ys) &&
+                      !overlap(a.v, rows_span(a.rows, a.v_row, heads, a.v_head, dim, es), a.q_out, ys),
+                  AMAP_EINVAL, "q_out overlaps q, k or v");
+  } else {  // in place: beside k and v in one buffer, but not over them
+    const Runs y = runs(a.q_out, a.rows, a.q_out_row, a.q_heads, a.q_out_head, es);
+    const int64_t width = (int64_t)dim * es;
+    SERVE_REQUIRE(!share(y, runs(a.k, a.rows, a.k_row, heads, a.k_head, es), width) &&
+                      !share(y, runs(a.v, a.rows, a.v_row, heads, a.v_head, es), width), AMAP_EINVAL, "q_out overlaps k or v");
+  }
+  return AMAP_OK;
 }
 
 }  // namespace
@@ -486,24 +713,11 @@ extern "C" int amap_rope_append(const amap_rope_t *plan, const amap_append_args 
   const amap_cache &c = a->cache;
   SERVE_REQUIRE((c.n_pages == 1 || (c.k_page && c.v_page)) && (c.page_size == 1 || (c.k_token && c.v_token)) && (c.heads == 1 || (c.k_head && c.v_head)),
                 AMAP_EINVAL, "the cache's rows lie on one another");
-  SERVE_REQUIRE(a->q_heads == 0 || ((a->rows == 1 || a->q_out_row) && (a->q_heads == 1 || a->q_out_head)), AMAP_EINVAL, "rows of q_out lie on one another");
   const bool e4m3 = c.dtype == AMAP_E4M3;
   Params P = {};
   int n = 0;
   if (a->q_heads) {
-    if (a->q_out != a->q || a->q_row != a->q_out_row || a->q_head != a->q_out_head) {
-      const Span xs = rows_span(a->rows, a->q_row, a->q_heads, a->q_head, plan->head_dim, es);
-      const Span ys = rows_span(a->rows, a->q_out_row, a->q_heads, a->q_out_head, plan->head_dim, es);
-      SERVE_REQUIRE(!overlap(a->q, xs, a->q_out, ys) &&
-                        !overlap(a->k, rows_span(a->rows, a->k_row, c.heads, a->k_head, plan->head_dim, es), a->q_out, ys) &&
-                        !overlap(a->v, rows_span(a->rows, a->v_row, c.heads, a->v_head, plan->head_dim, es), a->q_out, ys),
-                    AMAP_EINVAL, "q_out overlaps q, k or v");
-    } else {  // in place: beside k and v in one buffer, but not over them
-      const Runs y = runs(a->q_out, a->rows, a->q_out_row, a->q_heads, a->q_out_head, es);
-      const int64_t width = (int64_t)plan->head_dim * es;
-      SERVE_REQUIRE(!share(y, runs(a->k, a->rows, a->k_row, c.heads, a->k_head, es), width) &&
-                        !share(y, runs(a->v, a->rows, a->v_row, c.heads, a->v_head, es), width), AMAP_EINVAL, "q_out overlaps k or v");
-    }
+    if (const int rc = check_q_out(*a, c.heads, plan->head_dim)) return rc;
     P.part[n++] = {static_cast<const char *>(a->q), static_cast<char *>(a->q_out), a->q_row, a->q_head, a->q_out_row, a->q_out_head, 0, a->q_heads, kRows,
                    {}, 0, 0, {}};
   }
@@ -523,4 +737,61 @@ extern "C" int amap_rope_append(const amap_rope_t *plan, const amap_append_args 
   P.n_slots = c.n_pages * c.page_size;
   P.e4m3 = e4m3;
   return run_typed(*plan, P, a->dtype, ces, cuda_stream);
+}
+
+extern "C" int amap_packed_append(const amap_rope_t *plan, const amap_packed_append_args *a, void *cuda_stream) {
+  SERVE_REQUIRE(a, AMAP_EINVAL, "null pointer");
+  SERVE_REQUIRE(a->dtype == AMAP_BF16 || a->dtype == AMAP_FP16, AMAP_EINVAL, "type: bf16 or fp16");
+  const amap_packed &c = a->cache;
+  SERVE_REQUIRE(a->rows >= 0 && a->rows <= 0x7FFFFFFF, AMAP_EINVAL, "rows: 0 .. 2^31-1");
+  if (plan)
+    if (const int rc = check_rows(a->rows, a->positions, a->position_bits)) return rc;
+  if (const int rc = check_packed(c)) return rc;
+  SERVE_REQUIRE(!plan || c.head_dim == plan->head_dim, AMAP_EINVAL, "the cache's head size differs from the plan's");
+  SERVE_REQUIRE(a->q_heads >= 0 && a->q_heads <= 0xFFFF && a->reserved == 0, AMAP_EINVAL, "at most 65535 heads");
+  if (a->rows == 0) return accept();
+  SERVE_REQUIRE(a->k && a->v && a->slots && (a->q_heads == 0 || (a->q && a->q_out)), AMAP_EINVAL, "null pointer");
+  const int es = 2;
+  SERVE_REQUIRE(aligned(a->q, es) && aligned(a->k, es) && aligned(a->v, es) && aligned(a->q_out, es) && aligned(a->slots, 4), AMAP_EALIGN, "misaligned pointer");
+  Span held;
+  held.hi = amap_packed_bytes(c.page_size, c.head_dim, c.group);
+  held.add(c.n_pages, c.page, 1);
+  held.add(c.heads, c.head, 1);
+  SERVE_REQUIRE(!overlap(a->k, rows_span(a->rows, a->k_row, c.heads, a->k_head, c.head_dim, es), c.data, held) &&
+                    !overlap(a->v, rows_span(a->rows, a->v_row, c.heads, a->v_head, c.head_dim, es), c.data, held),
+                AMAP_EINVAL, "k or v overlaps the cache");
+  Packing A = {};
+  Params &P = A.p;
+  if (a->q_heads) {
+    if (const int rc = check_q_out(*a, c.heads, c.head_dim)) return rc;
+    SERVE_REQUIRE(!overlap(a->q, rows_span(a->rows, a->q_row, a->q_heads, a->q_head, c.head_dim, es), c.data, held) &&
+                      !overlap(a->q_out, rows_span(a->rows, a->q_out_row, a->q_heads, a->q_out_head, c.head_dim, es), c.data, held),
+                  AMAP_EINVAL, "q or q_out overlaps the cache");
+    P.part[P.n_parts++] = {static_cast<const char *>(a->q), static_cast<char *>(a->q_out), a->q_row, a->q_head, a->q_out_row, a->q_out_head, 0, a->q_heads, kRows,
+                           {}, 0, 0, {}};
+  }
+  if (plan) {
+    memcpy(P.phase, plan->phase, sizeof P.phase);
+    memcpy(P.axis, plan->axis, sizeof P.axis);
+  }
+  P.half = plan ? plan->half : 0;
+  P.scale = plan ? plan->scale : 1.0f;
+  P.head_dim = c.head_dim;
+  P.rows = a->rows;
+  P.positions = a->positions;
+  P.position_axis = a->position_axis;
+  P.position_row = a->position_row;
+  P.wide_positions = a->position_bits == 64;
+  P.sign = 1.0f;
+  P.slots = a->slots;
+  P.by_page = div_by(c.page_size);
+  P.n_slots = c.n_pages * c.page_size;
+  A.k = static_cast<const char *>(a->k), A.v = static_cast<const char *>(a->v);
+  A.k_row = a->k_row, A.k_head = a->k_head, A.v_row = a->v_row, A.v_head = a->v_head;
+  A.data = static_cast<char *>(c.data), A.page = c.page, A.head = c.head;
+  A.heads = c.heads, A.slabs = c.head_dim / kSlab, A.group = c.group;
+  A.k_wide = aligned(a->k, 16) && a->k_row % 8 == 0 && a->k_head % 8 == 0;
+  A.v_wide = aligned(a->v, 16) && a->v_row % 8 == 0 && a->v_head % 8 == 0;
+  const int vec = widest(P, es, es), pairs = plan ? plan->pairs : AMAP_PAIRS_HALF;
+  return a->dtype == AMAP_BF16 ? run_packing_wide<AMAP_BF16>(vec, pairs, A, cuda_stream) : run_packing_wide<AMAP_FP16>(vec, pairs, A, cuda_stream);
 }

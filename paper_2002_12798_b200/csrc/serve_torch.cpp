@@ -15,6 +15,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstring>
+#include <type_traits>
 
 #include "amap_serve.h"
 
@@ -272,7 +273,8 @@ PyObject *rotate(PyObject *const *a) {
 
 // plan, head_dim, axes, q, k, v, positions, slots, cache, its device, out (None) -> out; NotImplemented, and nothing done, where
 // autograd follows an input
-PyObject *append(PyObject *const *a) {
+template <typename G, int (*F)(const amap_rope_t *, const G *, void *)>
+PyObject *append_to(PyObject *const *a, const char *where) {
   const int64_t dim = integer(a[1]);
   const at::Tensor &q = tensor(a[3], "q"), &k = tensor(a[4], "k"), &v = tensor(a[5], "v");
   if (C10_UNLIKELY(tracked(q, k, v))) Py_RETURN_NOTIMPLEMENTED;
@@ -281,9 +283,9 @@ PyObject *append(PyObject *const *a) {
   heads_of(q, "q", dim, device);
   heads_of(k, "k", dim, device);
   heads_of(v, "v", dim, device);
-  amap_append_args g;
+  G g;
   memset(&g, 0, sizeof g);
-  memcpy(&g.cache, address<const amap_cache>(a[8]), sizeof g.cache);
+  memcpy(&g.cache, address<const decltype(g.cache)>(a[8]), sizeof g.cache);
   require(k.sizes() == v.sizes() && k.size(0) == q.size(0) && k.size(1) == g.cache.heads && k.scalar_type() == q.scalar_type() && v.scalar_type() == q.scalar_type(),
           "append: q, k and v of one type and token count, k and v with the cache's heads");
   require(integer(a[9]) == device, "append: the cache is on another device");
@@ -295,13 +297,118 @@ PyObject *append(PyObject *const *a) {
   g.q_row = q.stride(0), g.q_head = q.stride(1), g.k_row = k.stride(0), g.k_head = k.stride(1), g.v_row = v.stride(0), g.v_head = v.stride(1);
   g.q_out_row = out.stride(0), g.q_out_head = out.stride(1);
   g.positions = p.at, g.position_axis = p.axis, g.position_row = p.row, g.position_bits = p.bits;
-  if (g.rows) check(amap_rope_append(address<const amap_rope_t>(a[0]), &g, stream), "amap_rope_append");
+  if (g.rows) check(F(address<const amap_rope_t>(a[0]), &g, stream), where);
   return wrap(std::move(out));
+}
+PyObject *append(PyObject *const *a) { return append_to<amap_append_args, amap_rope_append>(a, "amap_rope_append"); }
+PyObject *packed_append(PyObject *const *a) { return append_to<amap_packed_append_args, amap_packed_append>(a, "amap_packed_append"); }
+
+// k, v, slots, cache, its device -> None
+PyObject *packed_write(PyObject *const *a) {
+  const at::Tensor &k = tensor(a[0], "k"), &v = tensor(a[1], "v");
+  amap_packed_append_args g;
+  memset(&g, 0, sizeof g);
+  memcpy(&g.cache, address<const amap_packed>(a[3]), sizeof g.cache);
+  const int device = cuda_of(k);
+  void *stream = stream_of(device);
+  heads_of(k, "k", g.cache.head_dim, device);
+  heads_of(v, "v", g.cache.head_dim, device);
+  require(k.sizes() == v.sizes() && k.size(1) == g.cache.heads && k.scalar_type() == v.scalar_type(), "write: k and v of one type and shape, with the cache's heads");
+  require(integer(a[4]) == device, "write: the cache is on another device");
+  g.slots = ints(a[2], "slots", k.size(0), device);
+  g.rows = k.size(0), g.dtype = type_of(k), g.k = k.data_ptr(), g.v = v.data_ptr();
+  g.k_row = k.stride(0), g.k_head = k.stride(1), g.v_row = v.stride(0), g.v_head = v.stride(1);
+  if (g.rows) check(amap_packed_append(nullptr, &g, stream), "amap_packed_append");
+  Py_RETURN_NONE;
+}
+
+// slots, cache, its device, type (amap_dtype), out (None: made; else (k, v)) -> (k, v)
+PyObject *packed_read(PyObject *const *a) {
+  amap_packed_read_args g;
+  memset(&g, 0, sizeof g);
+  memcpy(&g.cache, address<const amap_packed>(a[1]), sizeof g.cache);
+  const at::Tensor &slots = tensor(a[0], "slots");
+  const int device = cuda_of(slots);
+  void *stream = stream_of(device);
+  require(integer(a[2]) == device, "read: the cache is on another device");
+  g.slots = ints(a[0], "slots", slots.numel(), device);
+  require(slots.dim() == 1, "slots: [tokens]");
+  g.rows = slots.numel(), g.dtype = integer32(a[3]);
+  at::Tensor out[2];
+  if (a[4] == Py_None) {
+    at::AutoDispatchBelowADInplaceOrView plain;
+    const auto type = g.dtype == AMAP_BF16 ? at::kBFloat16 : g.dtype == AMAP_FP16 ? at::kHalf : at::kFloat;
+    for (at::Tensor &t : out) t = at::empty({g.rows, g.cache.heads, g.cache.head_dim}, slots.options().dtype(type));
+  } else {
+    require(PyTuple_Check(a[4]) && PyTuple_GET_SIZE(a[4]) == 2, "out: (k, v)");
+    for (int i = 0; i < 2; ++i) {
+      out[i] = tensor(PyTuple_GET_ITEM(a[4], i), "out");
+      heads_of(out[i], "out", g.cache.head_dim, device);
+      require(type_of(out[i]) == g.dtype && out[i].size(0) == g.rows && out[i].size(1) == g.cache.heads, "out: [tokens, heads, head_dim] of the type asked for");
+    }
+  }
+  g.k = out[0].data_ptr(), g.k_row = out[0].stride(0), g.k_head = out[0].stride(1);
+  g.v = out[1].data_ptr(), g.v_row = out[1].stride(0), g.v_head = out[1].stride(1);
+  if (g.rows) check(amap_packed_read(&g, stream), "amap_packed_read");
+  return wrap_all(out, 2);
+}
+
+// a setting: a number, or a tensor of one per row
+template <typename N>
+inline void setting(PyObject *o, const char *name, at::ScalarType type, int64_t rows, int device, int bit, int32_t *by_row, N *one, const N **each) {
+  if (THPVariable_Check(o)) {
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (C10_UNLIKELY(t.scalar_type() != type || cuda_of(t) != device || t.numel() != rows || !t.is_contiguous()))
+      refuse_value(name, type == at::kInt ? "a number, or contiguous int32 numbers, one per row, on the device of the logits"
+                                          : "a number, or contiguous float32 numbers, one per row, on the device of the logits");
+    *each = static_cast<const N *>(t.data_ptr());
+    *by_row |= 1 << bit;
+  } else if constexpr (std::is_same_v<N, int32_t>) {
+    *one = integer32(o);
+  } else {
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw Raised();
+    *one = (float)v;
+  }
+}
+
+// logits, uniforms, temperature, top_k, top_p, min_p, out (None), logprob (bool) -> tokens, or (tokens, logprobs); NotImplemented, and
+// nothing done, where autograd follows the logits
+PyObject *sample(PyObject *const *a) {
+  const at::Tensor &x = tensor(a[0], "logits");
+  if (C10_UNLIKELY(tracked(x))) Py_RETURN_NOTIMPLEMENTED;
+  const int device = cuda_of(x);
+  void *stream = stream_of(device);
+  require(x.dim() == 2 && (x.stride(1) == 1 || x.size(1) == 1) && x.size(0) <= INT32_MAX && x.size(1) <= INT32_MAX, "logits: [rows, vocab] with contiguous rows");
+  amap_sample_args g;
+  memset(&g, 0, sizeof g);
+  const int64_t rows = x.size(0);
+  g.rows = (int32_t)rows, g.vocab = (int32_t)x.size(1), g.dtype = type_of(x), g.logits = x.data_ptr(), g.row = x.stride(0);
+  const at::Tensor &u = tensor(a[1], "uniforms");
+  if (u.scalar_type() != at::kFloat || cuda_of(u) != device || u.numel() != rows || !u.is_contiguous())
+    refuse_value("uniforms: contiguous float32 numbers, one per row, on the device of the logits");
+  g.uniform = static_cast<const float *>(u.data_ptr());
+  setting(a[2], "temperature", at::kFloat, rows, device, 0, &g.by_row, &g.temperature, &g.temperatures);
+  setting(a[3], "top_k", at::kInt, rows, device, 1, &g.by_row, &g.top_k, &g.top_ks);
+  setting(a[4], "top_p", at::kFloat, rows, device, 2, &g.by_row, &g.top_p, &g.top_ps);
+  setting(a[5], "min_p", at::kFloat, rows, device, 3, &g.by_row, &g.min_p, &g.min_ps);
+  at::Tensor out[2];
+  const bool logprob = PyObject_IsTrue(a[7]) == 1;
+  {
+    at::AutoDispatchBelowADInplaceOrView plain;
+    out[0] = a[6] == Py_None ? at::empty({rows}, x.options().dtype(at::kInt)) : tensor(a[6], "out");
+    if (logprob) out[1] = at::empty({rows}, x.options().dtype(at::kFloat));
+  }
+  g.tokens = a[6] == Py_None ? static_cast<int32_t *>(out[0].data_ptr()) : ints(a[6], "out", rows, device);
+  if (logprob) g.logprobs = static_cast<float *>(out[1].data_ptr());
+  if (rows) check(amap_sample(&g, stream), "amap_sample");
+  return logprob ? wrap_all(out, 2) : wrap(std::move(out[0]));
 }
 
 // the plan's fixed arguments, its device, most requests, head_dim, q, cache, maps, the cache's device, block_table, seq_lens, out (None), lse (bool)
-// -> out, or (out, lse); NotImplemented, and nothing done, where autograd follows q
-PyObject *attend(PyObject *const *a) {
+// -> out, or (out, lse); NotImplemented, and nothing done, where autograd follows q.  PACKED: the cache is an amap_packed, and has no maps
+template <bool PACKED>
+PyObject *attend_over(PyObject *const *a) {
   amap_attend_args g;
   memcpy(&g, address<const amap_attend_args>(a[0]), sizeof g);  // q_heads, cache.heads, scale, softcap, window, workspace
   const int device = (int)integer(a[1]);
@@ -312,7 +419,8 @@ PyObject *attend(PyObject *const *a) {
   heads_of(q, "q", dim, device);
   const Table t = table_of(a[8]);
   const int32_t kv_heads = g.cache.heads;
-  memcpy(&g.cache, address<const amap_cache>(a[5]), sizeof g.cache);
+  if (PACKED) g.cache.heads = address<const amap_packed>(a[5])->heads, g.cache.head_dim = address<const amap_packed>(a[5])->head_dim;
+  else memcpy(&g.cache, address<const amap_cache>(a[5]), sizeof g.cache);
   require(q.size(0) <= integer(a[2]) && t.rows == q.size(0), "attend: no more requests than the plan is for, each with a row of the block table");
   require(q.size(1) == g.q_heads && g.cache.heads == kv_heads && g.cache.head_dim == dim, "attend: the plan is for other heads");
   require(integer(a[7]) == device && t.device == device, "attend: plan, q, block_table and cache on one device");
@@ -328,9 +436,13 @@ PyObject *attend(PyObject *const *a) {
   g.n_requests = t.rows, g.dtype = type_of(q), g.max_pages = t.entries, g.block_table = t.at, g.table_stride = t.stride;
   g.q = q.data_ptr(), g.out = out[0].data_ptr();
   g.q_row = q.stride(0), g.q_head = q.stride(1), g.out_row = out[0].stride(0), g.out_head = out[0].stride(1);
-  if (t.rows) check(amap_attend(&g, stream), "amap_attend");
+  if (t.rows && PACKED) check(amap_packed_attend(&g, address<const amap_packed>(a[5]), stream), "amap_packed_attend");
+  else if (t.rows) check(amap_attend(&g, stream), "amap_attend");
   return lse ? wrap_all(out, 2) : wrap(std::move(out[0]));
 }
+
+PyObject *attend(PyObject *const *a) { return attend_over<false>(a); }
+PyObject *packed_attend(PyObject *const *a) { return attend_over<true>(a); }
 
 PyObject *refuse_with(PyObject *, PyObject *error) {
   Py_INCREF(error);
@@ -339,7 +451,8 @@ PyObject *refuse_with(PyObject *, PyObject *error) {
 }
 
 #define ENTRY(name, n) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(&guarded<name, n>)), METH_FASTCALL, nullptr}
-PyMethodDef kMethods[] = {ENTRY(extend, 9), ENTRY(release, 7), ENTRY(rotate, 7), ENTRY(append, 11), ENTRY(attend, 12),
+PyMethodDef kMethods[] = {ENTRY(extend, 9), ENTRY(release, 7), ENTRY(rotate, 7), ENTRY(append, 11), ENTRY(attend, 12), ENTRY(packed_attend, 12),
+                          ENTRY(packed_append, 11), ENTRY(packed_write, 5), ENTRY(packed_read, 5), ENTRY(sample, 8),
                           {"refuse_with", refuse_with, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 // the build looks for this text in the library (build.py)
 const char kBuiltAgainst[] = SERVE_BUILT_AGAINST;

@@ -35,7 +35,8 @@ from .binding import AmapError, LIBRARY_PATH
 
 EXPORTS = [
     "amap_pages_extend", "amap_pages_release", "amap_pages_release_within", "amap_rope_plan", "amap_rope_destroy", "amap_rope_rotate",
-    "amap_rope_append", "amap_cache_encode", "amap_attend", "amap_attend_workspace", "amap_serve_error",
+    "amap_rope_append", "amap_cache_encode", "amap_attend", "amap_attend_workspace", "amap_serve_error", "amap_packed_bytes",
+    "amap_packed_append", "amap_packed_read", "amap_packed_attend", "amap_sample",
 ]
 _BF16, _FP16, _FP32, _E4M3 = 1, 2, 3, 4
 _DTYPES = {torch.bfloat16: _BF16, torch.float16: _FP16, torch.float32: _FP32, torch.float8_e4m3fn: _E4M3}
@@ -47,6 +48,11 @@ _PAIRS = {"half": 0, "adjacent": 1}
 class _Cache(Structure):  # amap_cache
     _fields_ = [("k", c_void_p), ("v", c_void_p), ("strides", c_int64 * 6), ("n_pages", c_int32), ("page_size", c_int32), ("heads", c_int32),
                 ("head_dim", c_int32), ("dtype", c_int32), ("k_scale", c_float), ("v_scale", c_float)]
+
+
+class _Packed(Structure):  # amap_packed
+    _fields_ = [("data", c_void_p), ("page", c_int64), ("head", c_int64), ("n_pages", c_int32), ("page_size", c_int32), ("heads", c_int32),
+                ("head_dim", c_int32), ("group", c_int32), ("reserved", c_int32)]
 
 
 class _Maps(Structure):  # amap_cache_maps
@@ -66,6 +72,8 @@ def _load():
     lib.amap_serve_error.argtypes = []
     lib.amap_cache_encode.argtypes = [POINTER(_Cache), POINTER(_Maps)]
     lib.amap_attend_workspace.argtypes = [c_int32, c_int32, c_int32, c_int32, POINTER(c_int64), POINTER(c_int64)]
+    lib.amap_packed_bytes.argtypes = [c_int32, c_int32, c_int32]
+    lib.amap_packed_bytes.restype = c_int64
     lib.amap_rope_plan.argtypes = [c_int32, c_int32, POINTER(c_double), POINTER(c_int32), c_int32, c_int32, c_float, POINTER(c_void_p)]
     lib.amap_rope_destroy.argtypes = [c_void_p]
     lib.amap_rope_destroy.restype = None
@@ -145,6 +153,55 @@ class PagedCache:
         self._maps = _Maps()  # for attention, which refuses a cache that this refuses
         readable = _lib.amap_cache_encode(byref(self._args), byref(self._maps)) == 0
         self._at, self._maps_at, self._device = ctypes.addressof(self._args), ctypes.addressof(self._maps) if readable else 0, k.get_device()
+
+
+class PackedCache:
+    """K and V in 4 bits (amap_packed): a group of `group` (32 or 64) elements of a head is held as codes 0 .. 15 that stand for
+    low + step * code, with low (the smallest element, rounded down) and step in bf16.  RopePlan.append quantises into it,
+    AttendPlan.attend reads it as it is, `read` gives tokens back.
+
+    data: uint8 CUDA tensor [pages, heads, page_bytes(page_size, head_dim, group)], of any strides that are multiples of 16
+    with a page of a head contiguous; `zeros` makes one.  page_size is a multiple of 16, head_dim 64, 96, 128 or 256.
+    Keeps the tensor alive."""
+
+    def __init__(self, data, page_size, head_dim, *, group=64):
+        size = self.page_bytes(page_size, head_dim, group)
+        _require(data.is_cuda and data.dim() == 3 and data.dtype == torch.uint8 and data.shape[2] == size and data.stride(2) == 1,
+                 "data: a uint8 CUDA tensor [pages, heads, %d] with contiguous pages of a head" % size)
+        _require(data.data_ptr() % 16 == 0 and data.stride(0) % 16 == 0 and data.stride(1) % 16 == 0, "data: aligned to 16 bytes, as are its strides")
+        self.data, self.page_size, self.head_dim, self.group = data, page_size, head_dim, group
+        self.pages, self.heads, self.device = data.shape[0], data.shape[1], data.device
+        self._args = _Packed(data.data_ptr(), data.stride(0), data.stride(1), self.pages, page_size, self.heads, head_dim, group, 0)
+        self._at, self._maps_at, self._device = ctypes.addressof(self._args), 0, data.get_device()
+
+    @classmethod
+    def zeros(cls, pages, page_size, heads, head_dim, *, group=64, device="cuda"):
+        """A cache of its own memory, all zeros."""
+        return cls(torch.zeros(pages, heads, cls.page_bytes(page_size, head_dim, group), dtype=torch.uint8, device=device), page_size, head_dim, group=group)
+
+    @staticmethod
+    def page_bytes(page_size, head_dim, group=64):
+        """Bytes that a page of one head takes (K and V)."""
+        size = _lib.amap_packed_bytes(page_size, head_dim, group)
+        _require(size > 0, _lib.amap_serve_error().decode())
+        return size
+
+    def write(self, k, v, slots, *, stream=None):
+        """Quantises k and v (bf16 or fp16 [tokens, heads, head_dim]) as they are into the slots (int32 [tokens], -1 for none)."""
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.write(k, v, slots)
+        _entry.packed_write(k, v, slots, self._at, self._device)
+
+    def read(self, slots, *, dtype=torch.bfloat16, out=None, stream=None):
+        """What the cache holds at the slots (int32 [tokens]) as (k, v), each [tokens, heads, head_dim] of dtype (bf16, fp16 or
+        fp32); zeros for a slot that there is not.  out: a pair to write to."""
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.read(slots, dtype=dtype, out=out)
+        code = _DTYPES.get(dtype)
+        _require(code in (_BF16, _FP16, _FP32), "read: bfloat16, float16 or float32")
+        return _entry.packed_read(slots, self._at, self._device, code, None if out is None else tuple(out))
 
 
 # ----------------------------------------------------------------------------------------------------------------------
@@ -267,12 +324,13 @@ class RopePlan:
     def append(self, q, k, v, positions, slots, cache, *, out=None, stream=None):
         """One step of a decoder layer before its attention (amap_rope_append): returns the rotated q [tokens, heads,
         head_dim] and writes the rotated k and the v [tokens, cache.heads, head_dim] to the slots (int32 [tokens], -1
-        for none) of the cache.  Views of a fused projection are taken as they are.  Not differentiable: a result that
+        for none) of the cache (a PackedCache: quantised as the exact rotation gives it).  Views of a fused projection are taken as they are.  Not differentiable: a result that
         autograd follows raises when its derivative is asked for."""
         if stream is not None:
             with torch.cuda.stream(stream):
                 return self.append(q, k, v, positions, slots, cache, out=out)
-        got = _entry.append(self._h, self.head_dim, self.n_axes, q, k, v, positions, slots, cache._at, cache._device, out)
+        entry = _entry.packed_append if isinstance(cache, PackedCache) else _entry.append
+        got = entry(self._h, self.head_dim, self.n_axes, q, k, v, positions, slots, cache._at, cache._device, out)
         if got is NotImplemented:
             return _without_derivative("append", self.append, (q, k, v, positions, slots, cache), out, q, k, v)
         return got
@@ -350,8 +408,31 @@ class AttendPlan:
         with self._lock:  # from a call's place in the order to its launch
             if _raw_stream(self._device) != self._raw:
                 self._order()
-            got = _entry.attend(self._at, self._device, self.max_requests, self.head_dim, q, cache._at, cache._maps_at, cache._device, block_table,
+            entry = _entry.packed_attend if isinstance(cache, PackedCache) else _entry.attend
+            got = entry(self._at, self._device, self.max_requests, self.head_dim, q, cache._at, cache._maps_at, cache._device, block_table,
                                 seq_lens, out, return_lse)
         if got is NotImplemented:
             return _without_derivative("attend", functools.partial(self.attend, return_lse=return_lse), (q, cache, block_table, seq_lens), out, q)
         return got
+
+
+# ----------------------------------------------------------------------------------------------------------------------
+# the next token
+# ----------------------------------------------------------------------------------------------------------------------
+def sample(logits, uniforms, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=None, return_logprob=False, stream=None):
+    """A token for every row of logits (bf16, fp16 or fp32 [rows, vocab]) from uniforms (fp32 [rows], in [0, 1)), as int32 [rows]
+    (amap_sample).  Weights are exp(logit / temperature); top_k (0: all) keeps that many of the largest logits, min_p those
+    with at least this part of the largest one's weight, top_p the fewest of what these leave whose weights are that part of
+    their sum; the token is where the sum over the kept tokens, by index, passes its uniform.  temperature 0 takes the
+    largest logit.  Ties go to the lowest index, NaN is never drawn, a row with no logit above
+    -infinity gives -1.  Every setting is a number, or a tensor with one per row (fp32; top_k int32).  With
+    return_logprob=True also the log of the probability that the token was drawn with, fp32 [rows].  Not differentiable, as
+    append."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return sample(logits, uniforms, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p, out=out, return_logprob=return_logprob)
+    got = _entry.sample(logits, uniforms, temperature, top_k, top_p, min_p, out, return_logprob)
+    if got is NotImplemented:
+        call = functools.partial(sample, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p, return_logprob=return_logprob)
+        return _without_derivative("sample", call, (logits, uniforms), out, logits)
+    return got

@@ -1,0 +1,198 @@
+"""Sampling on the GPU against its definition in 64 bits, row by row and token by token."""
+import numpy as np
+import pytest
+
+import packed_ref as ref
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+TYPES = {"bf16": torch.bfloat16, "fp16": torch.float16, "fp32": torch.float32}
+NEAR = 2.0**-30  # in probability: how near to a border the definition's answer is not looked at (sums of weights of 2^-36)
+
+
+@pytest.fixture(scope="module")
+def ops():
+    from paper_2002_12798_b200 import ops
+
+    return ops
+
+
+def check(ops, logits, u, **settings):
+    token, logprob = ops.sample(logits, u, return_logprob=True, **settings)
+    assert token.dtype == torch.int32 and logprob.dtype == torch.float32
+    x, uu = logits.float().cpu().numpy().astype(np.float64), u.cpu().numpy()
+    each = {n: (v.cpu().numpy() if isinstance(v, torch.Tensor) else np.full(len(x), np.float32(v) if n != "top_k" else v))
+            for n, v in {"temperature": 1.0, "top_k": 0, "top_p": 1.0, "min_p": 0.0, **settings}.items()}
+    skipped = 0
+    for r in range(len(x)):
+        want, want_logprob, near = ref.sample(x[r], uu[r], *(float(each[n][r]) if n != "top_k" else int(each[n][r]) for n in ("temperature", "top_k", "top_p", "min_p")))
+        if near < NEAR and uu[r] > 0:
+            skipped += 1
+            continue
+        assert int(token[r]) == want, (r, int(token[r]), want, near)
+        got = float(logprob[r])
+        assert got == want_logprob or abs(got - want_logprob) <= 2.0**-23 * abs(want_logprob) + 2.0**-30, (r, got, want_logprob)
+    assert skipped <= len(x) // 50
+    return token
+
+
+SETTINGS = [dict(), dict(temperature=0.7), dict(temperature=1.7, top_k=40), dict(top_p=0.9), dict(top_p=0.5, temperature=3.0), dict(min_p=0.1),
+            dict(temperature=0.8, top_k=50, top_p=0.95), dict(top_k=7, top_p=0.3, min_p=0.02), dict(temperature=0.0), dict(top_k=1), dict(top_p=0.0),
+            dict(min_p=1.0), dict(top_k=10**6, top_p=0.999, temperature=20.0), dict(top_k=500, min_p=0.001)]
+
+
+@pytest.mark.parametrize("settings", SETTINGS)
+@pytest.mark.parametrize("rows,vocab,dtype", [(1, 1, "fp32"), (3, 2, "bf16"), (5, 33, "fp16"), (2, 1000, "fp32"), (1, 32000, "fp32"), (9, 50001, "bf16"), (200, 3001, "fp16")])
+def test_sample(ops, settings, rows, vocab, dtype):
+    g = torch.Generator(device="cuda").manual_seed(rows + vocab)
+    x = (torch.randn(rows, vocab, generator=g, device="cuda") * 3).to(TYPES[dtype])
+    check(ops, x, torch.rand(rows, generator=g, device="cuda"), **settings)
+
+
+def test_large_vocabularies_of_each_cluster(ops):
+    """1 to 300 rows: from eight blocks to a row down to one."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    for rows, vocab, dtype in [(1, 262144, "bf16"), (4, 200003, "fp32"), (20, 131072, "fp16"), (40, 65537, "fp32"), (90, 40001, "bf16"), (300, 9001, "fp32")]:
+        x = (torch.randn(rows, vocab, generator=g, device="cuda") * 2).to(TYPES[dtype])
+        u = torch.rand(rows, generator=g, device="cuda")
+        for settings in (dict(), dict(top_p=0.9, temperature=0.8), dict(top_k=100, top_p=0.9)):
+            check(ops, x, u, **settings)
+
+
+def test_settings_by_row(ops):
+    g = torch.Generator(device="cuda").manual_seed(2)
+    rows, vocab = 300, 5003
+    x = (torch.randn(rows, vocab, generator=g, device="cuda") * 3).bfloat16()
+    pick = lambda values, dtype: torch.tensor(values, device="cuda", dtype=dtype)[torch.randint(0, len(values), (rows,), generator=g, device="cuda")]  # noqa: E731
+    check(ops, x, torch.rand(rows, generator=g, device="cuda"), temperature=pick([0.0, 0.3, 1.0, 2.5, -1.0], torch.float32),
+          top_k=pick([0, -1, 1, 5, 80, 5002, 5003, 9999], torch.int32), top_p=pick([1.0, 0.9, 0.5, 0.01], torch.float32), min_p=pick([0.0, 0.05, 0.5], torch.float32))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+def test_ties(ops, dtype):
+    """Few distinct logits: a bound falls among equal ones, of which the first by index are kept."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    rows, vocab = 40, 20011
+    x = torch.randint(0, 4, (rows, vocab), generator=g, device="cuda").to(TYPES[dtype])
+    x[0] = 1.5
+    x[1] = -3.0
+    u = torch.rand(rows, generator=g, device="cuda")
+    for settings in (dict(), dict(top_k=100), dict(top_k=5001), dict(top_p=0.3), dict(top_p=0.9), dict(top_k=6000, top_p=0.7), dict(min_p=0.3, top_k=9000)):
+        check(ops, x, u, **settings)
+
+
+def test_logits_next_to_one_another(ops):
+    """fp32 logits that differ in their last bits, and ones from zero up through all its exponents."""
+    g = torch.Generator(device="cuda").manual_seed(4)
+    u = torch.rand(6, generator=g, device="cuda")
+    x = 7.0 + torch.randint(0, 3000, (6, 30000), generator=g, device="cuda") * 2.0**-21
+    y = torch.exp2(-torch.rand(6, 30000, generator=g, device="cuda") * 140) * torch.where(torch.rand(6, 30000, generator=g, device="cuda") < 0.5, 1, -1)
+    for z in (x, y, -x, torch.cat([x[:, :100], y], 1)):
+        for settings in (dict(top_k=1000), dict(top_p=0.4), dict(top_k=20000, top_p=0.9)):
+            check(ops, z.contiguous(), u, **settings)
+
+
+def test_infinities_and_nan(ops):
+    inf, nan = float("inf"), float("nan")
+    x = torch.randn(9, 777, device="cuda")
+    x[0] = -inf
+    x[1] = nan
+    x[2, ::3] = nan
+    x[3, ::2] = -inf
+    x[4, [5, 70, 700]] = inf
+    x[5] = inf
+    x[6, 5:] = -inf
+    x[7] = torch.finfo(torch.float32).min
+    x[8, 0], x[8, 1] = 3e38, -3e38
+    for dtype in ("fp32", "bf16"):
+        for u in (0.0, 0.4, 0.999):
+            for settings in (dict(), dict(top_k=2), dict(top_p=0.5), dict(temperature=0.0), dict(min_p=0.5)):
+                token = check(ops, x.to(TYPES[dtype]), torch.full((9,), u, device="cuda"), **settings)
+                assert token[0] == -1 and token[1] == -1
+    # what is masked by the type's lowest value is not drawn beside anything else
+    y = torch.full((4, 1000), torch.finfo(torch.bfloat16).min, device="cuda", dtype=torch.bfloat16)
+    y[:, 77] = 0.0
+    assert ops.sample(y, torch.tensor([0.0, 0.3, 0.9, 1.0 - 2.0**-24], device="cuda")).tolist() == [77] * 4
+
+
+def test_uniforms_at_and_beyond_their_ends(ops):
+    x = torch.tensor([[-float("inf"), 1.0, 1.0, -float("inf"), 1.0, -float("inf")]], device="cuda").expand(7, 6).contiguous()
+    u = torch.tensor([0.0, -1.0, float("nan"), 0.5, 1 - 2.0**-24, 1.0, 5.0], device="cuda")
+    assert ops.sample(x, u).tolist() == [1, 1, 1, 2, 4, 4, 4]
+
+
+def test_temperatures_of_every_size(ops):
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x = torch.randn(8, 3000, generator=g, device="cuda") * 5
+    u = torch.rand(8, generator=g, device="cuda")
+    for t in (1e-40, 1e-6, 0.01, 50.0, 1e6, 1e30):
+        for settings in (dict(), dict(top_k=30), dict(top_p=0.5)):
+            check(ops, x, u, temperature=t, **settings)
+    check(ops, x * 1e30, u, temperature=1e30)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_rows_of_any_alignment(ops, dtype):
+    """Rows that begin at every element of a 16-byte piece, and what lies around them is not looked at."""
+    g = torch.Generator(device="cuda").manual_seed(6)
+    for offset in range(9):
+        for stride in (2048, 2051):
+            flat = torch.full((offset + 5 * stride + 64,), 1e4, device="cuda", dtype=TYPES[dtype])
+            x = flat.as_strided((5, 2011), (stride, 1), offset)
+            x.copy_(torch.randn(5, 2011, generator=g, device="cuda") * 3)
+            check(ops, x, torch.rand(5, generator=g, device="cuda"), top_p=0.8, temperature=0.9)
+
+
+def test_a_broadcast_row(ops):
+    x = torch.randn(1, 5000, device="cuda", dtype=torch.float16) * 3
+    check(ops, x.expand(50, 5000), torch.rand(50, device="cuda"), top_k=100)
+
+
+def test_outputs_and_refusals(ops):
+    x, u = torch.randn(4, 100, device="cuda"), torch.rand(4, device="cuda")
+    out = torch.empty(4, device="cuda", dtype=torch.int32)
+    assert ops.sample(x, u, out=out) is not None and torch.equal(out, ops.sample(x, u))
+    assert ops.sample(x[:0], u[:0]).shape == (0,)
+    for bad, why in [((x, u[:3]), "uniforms"), ((x, u.double()), "uniforms"), ((x.t(), u), "contiguous rows"), ((x[0], u), "contiguous rows")]:
+        with pytest.raises(ValueError, match=why):
+            ops.sample(*bad)
+    for bad, why in [(dict(top_k=torch.zeros(4, device="cuda")), "int32"), (dict(temperature=torch.ones(3, device="cuda")), "float32"), (dict(out=out[:3]), "out")]:
+        with pytest.raises(ValueError, match=why):
+            ops.sample(x, u, **bad)
+    from paper_2002_12798_b200.binding import AmapError
+
+    for bad in (dict(top_p=1.5), dict(min_p=-0.1), dict(temperature=float("nan"))):
+        with pytest.raises(AmapError):
+            ops.sample(x, u, **bad)
+    with pytest.raises(AmapError):
+        ops.sample(x.double(), u)
+    y = x.clone().requires_grad_()
+    token, logprob = ops.sample(y, u, return_logprob=True)
+    assert torch.equal(token, ops.sample(x, u))
+    with pytest.raises(RuntimeError, match="not differentiable"):
+        logprob.sum().backward()
+
+
+def test_a_captured_call_on_another_stream(ops):
+    x, u = torch.randn(6, 40000, device="cuda") * 2, torch.rand(6, device="cuda")
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    ops.sample(x, u, top_p=0.9, stream=stream)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        token = ops.sample(x, u, top_p=0.9, top_k=300)
+    for _ in range(3):
+        x.copy_(torch.randn_like(x) * 2)
+        u.copy_(torch.rand_like(u))
+        graph.replay()
+        assert torch.equal(token, ops.sample(x, u, top_p=0.9, top_k=300))
+
+
+def test_drawn_as_often_as_their_weight(ops):
+    """Many uniforms, evenly spaced, over one row: every token as often as its probability says, to within one."""
+    x = torch.randn(1, 50, device="cuda") * 2
+    n = 20000
+    token = ops.sample(x.expand(n, 50), (torch.arange(n, device="cuda") + 0.5) / n, temperature=1.3)
+    p = torch.softmax(x[0].double() / float(np.float32(1.3)), 0).cpu().numpy()
+    assert np.abs(np.bincount(token.cpu().numpy(), minlength=50) - n * p).max() <= 1.0 + n * 2.0**-23
