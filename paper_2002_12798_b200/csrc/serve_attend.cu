@@ -42,7 +42,7 @@ using namespace amap_serve;
 namespace {
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps, kBlock = kThreads + 32;  // the last warp is the producer
-constexpr int kMostBlocksPerSm = 2;
+constexpr int kMostBlocksPerSm = 3;
 constexpr int kGroup = 8;               // teams whose parts are joined first, where an item has more than kDirect of them
 constexpr int kDirect = 12;
 constexpr int kAside = 4;               // parts that the producer warp joins
@@ -97,6 +97,11 @@ __device__ __noinline__ void settle(uint32_t full, int stages, int stage, uint32
 }
 __device__ __forceinline__ void sync_consumers() { asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory"); }
 
+__device__ __forceinline__ uint32_t transposed(uint32_t v) {
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
 template <int CT>
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   if constexpr (CT == AMAP_BF16)
@@ -433,7 +438,7 @@ struct Workspace {
 };
 Workspace workspace(int32_t n_requests, int32_t q_heads, int32_t kv_heads, int32_t head_dim) {
   const int dp = head_dim <= 128 ? 128 : 256, group = q_heads / kv_heads, hb = 8 * eights(group, dp);
-  const int64_t blocks = (int64_t)device_sms() * kMostBlocksPerSm, items = (int64_t)n_requests * kv_heads * ((group + hb - 1) / hb);
+  const int64_t blocks = (int64_t)device_sms() * kMostBlocksPerSm, items = (int64_t)n_requests * kv_heads * ((group + 7) / 8);
   Workspace w;
   w.ml = 2 * blocks * hb * dp * 4;
   w.failed = w.ml + 2 * blocks * hb * 8;
@@ -559,11 +564,6 @@ __device__ __forceinline__ void load4(uint32_t at, uint32_t (&r)[4]) {
 }
 __device__ __forceinline__ void load4_transposed(uint32_t at, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
-}
-__device__ __forceinline__ uint32_t transposed(uint32_t v) {
-  uint32_t r;
-  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
-  return r;
 }
 // four e4m3 as four fp16: exact
 __device__ __forceinline__ void halves_of(uint32_t four, uint32_t *low, uint32_t *high) {

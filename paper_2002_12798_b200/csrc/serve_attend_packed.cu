@@ -26,11 +26,14 @@
 namespace {
 
 constexpr int kPackedTile = 128, kCells = kPackedTile / kCell, kOwn = kCells / kWarps;  // cells of a tile; of a warp
+constexpr int kLook = 32 / kCells;                                                      // tiles whose pages are looked up at a time
 static_assert(kOwn == 2, "a warp's cells of a tile");
-constexpr float kUp = 9.0f, kTop = 0x1p15f;  // P is 2^kUp times what it stands for; a weight above kTop renews the reference
+constexpr float kUp = 9.0f, kTop = 0x1p15f;  // P is 2^kUp times what it stands for; P step_V above kTop renews the reference
 constexpr float kNone = -3e38f;            // the reference before the first token
+constexpr float kLeast = 0x1p-60f;         // a smaller |low| or step counts as this much
+constexpr float kMost = 0x1p80f;           // a sum of P above this renews the reference, too (tokens whose V is constant have no step)
 
-template <int NS, int NT> constexpr int kPackedResident = NS * NT >= 8 ? 1 : 2;
+template <int NS> constexpr int kPackedResident = NS >= 8 ? 1 : 2;
 // Stages of the ring: what a multiprocessor's shared memory has room for beside the rest of its blocks, up to eight.
 constexpr int least(int a, int b) { return a < b ? a : b; }
 template <int NS, int NG, int RESIDENT>
@@ -39,61 +42,78 @@ constexpr int kPackedStages = least(8, (226 * 1024 / RESIDENT - 3072 - (int)size
 struct PackedParams {
   Params p;
   const char *data;
-  int64_t page, head;
+  int64_t page, head;  // bytes
+  int32_t run;         // cells that every page divides into, up to a tile's: 1, 2, 4 or 8
 };
 
 __device__ __forceinline__ void bulk_copy(uint32_t dst, const void *src, int bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 template <int WORDS>
-__device__ __forceinline__ void load_words(uint32_t at, uint32_t *r) {
-  if constexpr (WORDS == 4) asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
-  else if constexpr (WORDS == 2) asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "r"(at) : "memory");
-  else asm volatile("ld.shared.b32 %0, [%1];" : "=r"(r[0]) : "r"(at) : "memory");
+__device__ __forceinline__ void load_words(const char *at, uint32_t *r) {
+  if constexpr (WORDS == 4) {
+    const uint4 v = *reinterpret_cast<const uint4 *>(at);
+    r[0] = v.x, r[1] = v.y, r[2] = v.z, r[3] = v.w;
+  } else if constexpr (WORDS == 2) {
+    const uint2 v = *reinterpret_cast<const uint2 *>(at);
+    r[0] = v.x, r[1] = v.y;
+  } else {
+    r[0] = *reinterpret_cast<const uint32_t *>(at);
+  }
+}
+// the first of a sum of products: nothing has to be set to zero ahead of it
+__device__ __forceinline__ void mma_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+      : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
 }
 // K codes of a lane: slabs side by side, four at a time; three are single words (their rows are 12 bytes)
 template <int NS>
-__device__ __forceinline__ void load_k(uint32_t at, int token, int t4, uint32_t (&r)[NS]) {
+__device__ __forceinline__ void load_k(const char *at, int token, int t4, uint32_t (&r)[NS]) {
 #pragma unroll
   for (int first = 0; first < NS; first += 4) {
-    constexpr int kAll = 4;
-    const int wide = NS - first < kAll ? NS - first : kAll;
-    const uint32_t from = at + first * 256 + (token * 4 + t4) * 4 * wide;
+    const int wide = NS - first < 4 ? NS - first : 4;
+    const char *from = at + first * 256 + (token * 4 + t4) * 4 * wide;
     if (wide == 4) load_words<4>(from, &r[first]);
     else if (wide == 2) load_words<2>(from, &r[first]);
     else
       for (int i = 0; i < wide; ++i) load_words<1>(from + 4 * i, &r[first + i]);
   }
 }
-template <int NS>
-__device__ __forceinline__ void load_v(uint32_t at, int lane, uint32_t (&r)[NS][2]) {
-#pragma unroll
-  for (int first = 0; first < NS; first += 2) {
-    if (NS - first >= 2) {
-      load_words<4>(at + first * 256 + lane * 16, &r[first][0]);
-    } else {
-      load_words<2>(at + first * 256 + lane * 8, &r[first][0]);
-    }
-  }
+// V codes of the COUNT (1 or 2) slabs from `slab` on, which lie side by side where they are two
+template <int NS, int COUNT>
+__device__ __forceinline__ void load_v(const char *at, int lane, int slab, uint32_t (&r)[COUNT][2]) {
+  const int first = slab & ~1, wide = NS - first < 2 ? 1 : 2;
+  const char *from = at + first * 256 + lane * 8 * wide + (slab - first) * 8;
+  if constexpr (COUNT == 2) load_words<4>(from, &r[0][0]);
+  else load_words<2>(from, &r[0][0]);
 }
-__device__ __forceinline__ float step_of(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float step_of(uint32_t w) { return __uint_as_float(w * 0x10000u); }
 __device__ __forceinline__ float low_of(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+// the larger step (the upper halves are not looked at)
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
 
 // a and b as fp16 in one word, and what that leaves over, likewise
 __device__ __forceinline__ void two_terms(float a, float b, uint32_t (&term)[2]) {
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(term[0]) : "f"(b), "f"(a));
-  const float2 h = __half22float2(*reinterpret_cast<const __half2 *>(&term[0]));
-  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(term[1]) : "f"(b - h.y), "f"(a - h.x));
+  float x, y;
+  asm("{ .reg .b16 l, h; mov.b32 {l, h}, %2; sub.f32.f16 %0, l, %3; sub.f32.f16 %1, h, %4; }" : "=f"(x), "=f"(y) : "r"(term[0]), "f"(a), "f"(b));
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(term[1]) : "f"(-y), "f"(-x));
 }
 
-// NS: slabs of 32 elements of a head; SG: slabs of a group; NT: eights of q heads
-template <int NS, int SG, int NT>
-__global__ void __launch_bounds__(kBlock, (kPackedResident<NS, NT>)) attend_packed_kernel(const __grid_constant__ PackedParams PP) {
+// NS: slabs of 32 elements of a head; SG: slabs of a group.  A block has eight q heads: with sixteen, whose sums leave room for one
+// block a multiprocessor, 128 requests of 64 q heads to 4 take 106 us instead of 90, although the codes are then unpacked once.
+template <int NS, int SG>
+__global__ void __launch_bounds__(kBlock, (kPackedResident<NS>)) attend_packed_kernel(const __grid_constant__ PackedParams PP) {
   const Params &P = PP.p;
   constexpr int NG = NS / SG, D = 32 * NS, C = cell_bytes(NS, NG), kStage = kCells * C;
-  constexpr int S = kPackedStages<NS, NG, kPackedResident<NS, NT>>;
-  constexpr int HB = 8 * NT, NM = (NT + 1) / 2;  // sixteens of q heads
-  constexpr int kRows = NT == 1 ? 1 : 2;         // rows of a sixteen that a lane has: heads g, and g + 8
+  constexpr int S = kPackedStages<NS, NG, kPackedResident<NS>>;
+  constexpr int HB = 8;
+  constexpr int kPair = NG % 2 == 0 ? 2 : 1;     // groups whose products are summed at a time
   constexpr int kPitch = D + 4;
   extern __shared__ __align__(1024) char smem[];
   float *joint = reinterpret_cast<float *>(smem + S * kStage);  // [warps][8][kPitch]
@@ -120,41 +140,55 @@ __global__ void __launch_bounds__(kBlock, (kPackedResident<NS, NT>)) attend_pack
   bool alive = true;
 
   if (warp == kWarps) {
-    // ---- the producer: lane i has cell i of the tile ----
-    int entry = -1, offset = 0;
-    bool there = false;
+    // ---- the producer: it looks pages up for kLook tiles of an item at a time, a group of them ahead (a look takes about as
+    // long as four tiles take to come: with one at a time 64 requests were 172 us); a lane has a run of cells that lie
+    // side by side in a page, as many as every page divides into ----
+    const int run = PP.run, ahead = lane / kCells, cell0 = lane % kCells;
+    int entry = -1, offset = 0, from_cell = 0, n_cells = 0, tiles = 0;
     auto look = [&]() {
-      const int token = at.t + lane * kCell;
-      there = lane < kCells && token < at.n && token > at.low - kCell;
-      if (there) {
+      tiles = min(kLook, min(at.left, at.rest));
+      const int token = at.t + ahead * kPackedTile + cell0 * kCell;
+      n_cells = 0;
+      if (ahead < tiles && cell0 % run == 0 && token < at.n && token + run * kCell > at.low) {
         const uint32_t page = P.div_mul ? __umulhi((uint32_t)token, P.div_mul) >> P.div_shift : (uint32_t)token >> P.div_shift;
         offset = token - (int)page * cache.page_size;
         entry = P.a.block_table[(int64_t)at.r * P.a.table_stride + page];
+        from_cell = max(at.low - token, 0) / kCell;
+        n_cells = min(run, (at.n - token + kCell - 1) / kCell) - from_cell;
       }
     };
     int stage = 0;
     uint32_t parity = 1;  // the first round of waits finds every stage empty
     look();
-    for (bool more = true; more;) {
+    for (bool more = true; more && __all_sync(~0u, alive);) {
       const int head = (at.h * P.members + member) / P.blocks_per_head;
-      const bool live = there && (uint32_t)entry < (uint32_t)cache.n_pages;
-      const uint32_t cells = __ballot_sync(~0u, live);
-      const char *from = PP.data + (live ? (int64_t)entry * PP.page + (int64_t)head * PP.head + (int64_t)(offset / kCell) * C : 0);
+      if ((uint32_t)entry >= (uint32_t)cache.n_pages) n_cells = 0;
+      const int count = n_cells, first = cell0 + from_cell, t = at.t, n = at.n, low = at.low, there = tiles;
+      const uint32_t cells = __reduce_or_sync(~0u, count > 0 ? ((1u << count) - 1) << (ahead * kCells + first) : 0u);
+      const char *from = PP.data + (count > 0 ? (int64_t)entry * PP.page + (int64_t)head * PP.head + (int64_t)(offset / kCell + from_cell) * C : 0);
+      at.t += (there - 1) * kPackedTile;
+      at.left -= there - 1;
+      at.rest -= there - 1;
       more = at.more();
       if (more) {
         at.advance(P);
         look();
       }
-      bar_wait(smem_at(&small.empty[stage]), parity, P.failed, alive);
-      if (!__all_sync(~0u, alive)) break;
-      const uint32_t bar = smem_at(&small.full[stage]);
-      if (lane == 0) {
-        small.rows_there[stage][0] = cells;
-        bar_arrive_bytes(bar, __popc(cells) * C);
+      for (int k = 0; k < there; ++k) {
+        // of the lane-th warp: its tokens that take part
+        const int row0 = t + k * kPackedTile + lane * 32, upper = min(max(n - row0, 0), 32), lower = min(max(low - row0, 0), 32);
+        const uint32_t in_tile = cells >> (k * kCells) & ((1u << kCells) - 1), own = in_tile >> (lane * kOwn & 31);
+        const uint32_t rows = (upper ? ~0u >> (32 - upper) : 0) & ~(lower ? ~0u >> (32 - lower) : 0) & ((own & 1 ? 0xFFFFu : 0u) | (own & 2 ? 0xFFFF0000u : 0u));
+        bar_wait(smem_at(&small.empty[stage]), parity, P.failed, alive);
+        if (!__all_sync(~0u, alive)) break;
+        const uint32_t bar = smem_at(&small.full[stage]);
+        if (lane < kWarps) small.rows_there[stage][lane] = rows;
+        __syncwarp();
+        if (lane == 0) bar_arrive_bytes(bar, __popc(in_tile) * C);
+        __syncwarp();
+        if (count > 0 && ahead == k) bulk_copy(smem_at(smem + stage * kStage) + first * C, from, count * C, bar);
+        if (++stage == S) stage = 0, parity ^= 1;
       }
-      __syncwarp();
-      if (live) bulk_copy(smem_at(smem + stage * kStage) + lane * C, from, C, bar);
-      if (++stage == S) stage = 0, parity ^= 1;
     }
     if (!__all_sync(~0u, alive)) {
       settle(smem_at(&small.full[0]), S, stage, parity ^ 1, P.failed);
@@ -164,30 +198,26 @@ __global__ void __launch_bounds__(kBlock, (kPackedResident<NS, NT>)) attend_pack
     return;
   }
 
-  // ---- q of an item, as the A operand: a lane has heads g and g + 8 of a sixteen, of each slab the elements 8 t4 .. +7 ----
-  uint32_t q[NM][kRows][NS][4];
-  float to_log2[NM][kRows], sums[NM][kRows][NG];  // sums of q over a group, as the products count it
+  // ---- q of an item, as the B operand: of head g, of each slab the elements 8 t4 .. +7 ----
+  uint32_t q[NS][4];
+  // of heads 2 t4 and 2 t4 + 1, S^T's columns here: what makes exponents of 2 of the products' sums, never zero (with a softcap
+  // it makes scores, which are brought back to the products' unit once they are capped); sums of q over a group, as the products count it
+  float to_log2[2], sums[NG][2];
   const float unit = (P.a.softcap > 0 ? 1.0f : kLog2e) * P.a.scale;
   auto ask_q = [&](int r, int h) {
     const int first = h / P.blocks_per_head * P.group, in_group = h % P.blocks_per_head * HB;
     const uint16_t *row = static_cast<const uint16_t *>(P.a.q) + (int64_t)r * P.a.q_row;
+    const int head = in_group + g;
+    const bool there = head < P.group;
+    const uint16_t *x = row + (int64_t)(first + (there ? head : 0)) * P.a.q_head;
 #pragma unroll
-    for (int m = 0; m < NM; ++m) {
+    for (int j = 0; j < NS; ++j) {
 #pragma unroll
-      for (int k = 0; k < kRows; ++k) {
-        const int head = in_group + m * 16 + k * 8 + g;
-        const bool there = head < P.group;
-        const uint16_t *x = row + (int64_t)(first + (there ? head : 0)) * P.a.q_head;
-#pragma unroll
-        for (int j = 0; j < NS; ++j) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int d = j * 32 + t4 * 8 + i * 2;
-            uint32_t v = 0;
-            if (there) v = P.q_pairs ? *reinterpret_cast<const uint32_t *>(x + d) : x[d] | (uint32_t)x[d + 1] << 16;
-            q[m][k][j][i] = v;
-          }
-        }
+      for (int i = 0; i < 4; ++i) {
+        const int d = j * 32 + t4 * 8 + i * 2;
+        uint32_t v = 0;
+        if (there) v = P.q_pairs ? *reinterpret_cast<const uint32_t *>(x + d) : x[d] | (uint32_t)x[d + 1] << 16;
+        q[j][i] = v;
       }
     }
   };
@@ -195,62 +225,63 @@ __global__ void __launch_bounds__(kBlock, (kPackedResident<NS, NT>)) attend_pack
     return P.a.dtype == AMAP_BF16 ? make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u)) : __half22float2(*reinterpret_cast<const __half2 *>(&v));
   };
   auto take_q = [&]() {
+    float big = 0.0f;
 #pragma unroll
-    for (int m = 0; m < NM; ++m) {
+    for (int j = 0; j < NS; ++j) {
 #pragma unroll
-      for (int k = 0; k < kRows; ++k) {
-        float big = 0.0f;
+      for (int i = 0; i < 4; ++i) {
+        const float2 f = as_floats(q[j][i]);
+        big = fmaxf(big, fmaxf(fabsf(f.x), fabsf(f.y)));
+      }
+    }
+    big = fmaxf(big, __shfl_xor_sync(~0u, big, 1));
+    big = fmaxf(big, __shfl_xor_sync(~0u, big, 2));
+    // 2^10 2^e <= big < 2^11 2^e; e within what 2^-e and 2^e are normal numbers for
+    const int e = min(max((int)(__float_as_uint(big) >> 23) - 127 - 10, -120), 120);
+    const float down = __uint_as_float((uint32_t)(127 - e) << 23);
+    float up = unit * __uint_as_float((uint32_t)(127 + e) << 23);
+    up = copysignf(fminf(fmaxf(fabsf(up) * 0x1p20f, FLT_MIN), FLT_MAX), up);
+    to_log2[0] = __shfl_sync(~0u, up, 8 * t4);
+    to_log2[1] = __shfl_sync(~0u, up, 8 * t4 + 4);
 #pragma unroll
-        for (int j = 0; j < NS; ++j) {
+    for (int n = 0; n < NG; ++n) {
+      float sum = 0.0f;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float2 f = as_floats(q[m][k][j][i]);
-            big = fmaxf(big, fmaxf(fabsf(f.x), fabsf(f.y)));
-          }
-        }
-        big = fmaxf(big, __shfl_xor_sync(~0u, big, 1));
-        big = fmaxf(big, __shfl_xor_sync(~0u, big, 2));
-        // 2^10 2^e <= big < 2^11 2^e; e within what 2^-e and 2^e are normal numbers for
-        const int e = min(max((int)(__float_as_uint(big) >> 23) - 127 - 10, -120), 120);
-        const float down = __uint_as_float((uint32_t)(127 - e) << 23);
-        to_log2[m][k] = unit * __uint_as_float((uint32_t)(127 + e) << 23);
+      for (int j = n * SG; j < (n + 1) * SG; ++j) {
 #pragma unroll
-        for (int n = 0; n < NG; ++n) {
-          float sum = 0.0f;
-#pragma unroll
-          for (int j = n * SG; j < (n + 1) * SG; ++j) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              float2 f = as_floats(q[m][k][j][i]);
-              f.x *= down;
-              f.y *= down;
-              sum += f.x + f.y;
-              const float kind = i & 1 ? 1.0f : 16.0f;
-              const __half2 h2 = __floats2half2_rn(f.x * kind, f.y * kind);
-              q[m][k][j][i] = *reinterpret_cast<const uint32_t *>(&h2);
-            }
-          }
-          sum += __shfl_xor_sync(~0u, sum, 1);
-          sum += __shfl_xor_sync(~0u, sum, 2);
-          sums[m][k][n] = sum * 0x1p-20f;
+        for (int i = 0; i < 4; ++i) {
+          float2 f = as_floats(q[j][i]);
+          f.x *= down;
+          f.y *= down;
+          sum += f.x + f.y;
+          const float kind = i & 1 ? 1.0f : 16.0f;
+          const __half2 h2 = __floats2half2_rn(f.x * kind, f.y * kind);
+          q[j][i] = *reinterpret_cast<const uint32_t *>(&h2);
         }
       }
+      sum += __shfl_xor_sync(~0u, sum, 1);
+      sum += __shfl_xor_sync(~0u, sum, 2);
+      sum *= 0x1p-20f;
+      sums[n][0] = __shfl_sync(~0u, sum, 8 * t4);
+      sums[n][1] = __shfl_sync(~0u, sum, 8 * t4 + 4);
     }
   };
 
-  // o: codes' part of O^T, elements by heads 2 t4 and 2 t4 + 1; of head g (nt eights on): low's part of a group over this
-  // lane's tokens, the same of l, and the reference
-  float o[NT][2 * NS][4], lows[NT][NG], l[NT], ref[NT];
+  // o: codes' part of O^T, elements by heads 2 t4 and 2 t4 + 1; of these heads: low's part of a group over this lane's tokens,
+  // the same of l, and the reference
+  float o[2 * NS][4], lows[NG][2], l[2], ref[2];
+  bool fresh;  // nothing is in them yet
   auto clear = [&]() {
+    fresh = true;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      l[nt] = 0.0f;
-      ref[nt] = kNone;
+    for (int c = 0; c < 2; ++c) {
+      l[c] = 0.0f;
+      ref[c] = kNone;
 #pragma unroll
-      for (int n = 0; n < NG; ++n) lows[nt][n] = 0.0f;
-#pragma unroll
-      for (int i = 0; i < 2 * NS; ++i) o[nt][i][0] = o[nt][i][1] = o[nt][i][2] = o[nt][i][3] = 0.0f;
+      for (int n = 0; n < NG; ++n) lows[n][c] = 0.0f;
     }
+#pragma unroll
+    for (int i = 0; i < 2 * NS; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
   };
 
   ask_q(at.r, at.h * P.members + member);
@@ -259,205 +290,203 @@ __global__ void __launch_bounds__(kBlock, (kPackedResident<NS, NT>)) attend_pack
   int64_t item_first = piece.first_place;
   int stage = 0;
   uint32_t parity = 0;
+  const int numbers = NS * 512 + g * 8;  // where this lane finds those of token g (of g + 8: 64 bytes behind)
   bool more = true;
 #pragma unroll 1
   while (more) {
-    // this warp's tokens that take part
-    const int row0 = at.t + warp * 32, upper = min(max(at.n - row0, 0), 32), lower = min(max(at.low - row0, 0), 32);
-    uint32_t rows = (upper ? ~0u >> (32 - upper) : 0) & ~(lower ? ~0u >> (32 - lower) : 0);
-    bar_wait(smem_at(&small.full[stage]), parity, P.failed, alive);
-    const uint32_t cells = small.rows_there[stage][0] >> (warp * kOwn);
-    rows &= (cells & 1 ? 0xFFFFu : 0u) | (cells & 2 ? 0xFFFF0000u : 0u);
-    const uint32_t base = smem_at(smem + stage * kStage) + warp * kOwn * C;
-    if (rows) {
-      const bool all = rows == ~0u;
-      float s[kOwn][NT][4];   // head g (+ 8 nt); tokens 2 t4, 2 t4 + 1, + 8, + 9 of a cell
-      float most[kOwn][4];    // of these tokens, the largest |low_V| or step_V
+    const int here = min(at.left, at.rest);  // tiles of the item in this piece
+#pragma unroll 1
+    for (int tile = here; tile > 0; --tile) {
+      bar_wait(smem_at(&small.full[stage]), parity, P.failed, alive);
+      const uint32_t rows = small.rows_there[stage][warp];
+      char *const base = smem + stage * kStage + warp * kOwn * C;
+      if (rows) {
+        float s[kOwn][4];    // tokens g, g + 8 of a cell by heads 2 t4, 2 t4 + 1
+        uint32_t w[kOwn][2][NG];  // V's numbers
+        uint32_t k[kOwn][2][NS];
 #pragma unroll
-      for (int u = 0; u < kOwn; ++u) {
-        const uint32_t cell = base + u * C;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          most[u][i] = 0x1p-60f;
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) s[u][nt][i] = 0.0f;
+        for (int u = 0; u < kOwn; ++u) {
+          load_k<NS>(base + u * C, g, t4, k[u][0]);
+          load_k<NS>(base + u * C, g + 8, t4, k[u][1]);
         }
-        uint32_t k[2][NS];
-        load_k<NS>(cell, g, t4, k[0]);
-        load_k<NS>(cell, g + 8, t4, k[1]);
 #pragma unroll
-        for (int n = 0; n < NG; ++n) {
-          float acc[NM][2][4];
+        for (int n0 = 0; n0 < NG; n0 += kPair) {
+          float acc[kOwn][kPair][4];  // products that need not wait for one another, by turns
 #pragma unroll
-          for (int m = 0; m < NM; ++m) {
+          for (int j = 0; j < SG; ++j) {
 #pragma unroll
-            for (int c = 0; c < 4; ++c) acc[m][0][c] = acc[m][1][c] = 0.0f;
-          }
+            for (int i = 0; i < 4; i += 2) {
 #pragma unroll
-          for (int j = n * SG; j < (n + 1) * SG; ++j) {
+              for (int n = 0; n < kPair; ++n) {
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {  // eight tokens
-              const uint32_t w = k[e][j], w8 = w >> 8;
-#pragma unroll
-              for (int m = 0; m < NM; ++m) {
-                mma<AMAP_FP16>(acc[m][e], q[m][0][j][0], kRows == 2 ? q[m][kRows - 1][j][0] : 0u, q[m][0][j][1], kRows == 2 ? q[m][kRows - 1][j][1] : 0u,
-                               w & 0x000F000Fu, w & 0x00F000F0u);
-                mma<AMAP_FP16>(acc[m][e], q[m][0][j][2], kRows == 2 ? q[m][kRows - 1][j][2] : 0u, q[m][0][j][3], kRows == 2 ? q[m][kRows - 1][j][3] : 0u,
-                               w8 & 0x000F000Fu, w8 & 0x00F000F0u);
+                for (int u = 0; u < kOwn; ++u) {
+                  const int slab = (n0 + n) * SG + j;
+                  const uint32_t w0 = k[u][0][slab] >> (4 * i), w1 = k[u][1][slab] >> (4 * i);
+                  const uint32_t a0 = w0 & 0x000F000Fu, a1 = w1 & 0x000F000Fu, a2 = w0 & 0x00F000F0u, a3 = w1 & 0x00F000F0u;
+                  if (j == 0 && i == 0) mma_first(acc[u][n], a0, a1, a2, a3, q[slab][i], q[slab][i + 1]);
+                  else mma<AMAP_FP16>(acc[u][n], a0, a1, a2, a3, q[slab][i], q[slab][i + 1]);
+                }
               }
             }
           }
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            uint32_t w[4];
-            load_words<4>(cell + NS * 512 + n * 128 + e * 64 + t4 * 16, w);
+          for (int u = 0; u < kOwn; ++u) {
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              const float step = step_of(w[c]), low = low_of(w[c]);
-              most[u][2 * e + c] = fmaxf(most[u][2 * e + c], fmaxf(step_of(w[2 + c]), fabsf(low_of(w[2 + c]))));
+            for (int n = 0; n < kPair; ++n) {
 #pragma unroll
-              for (int m = 0; m < NM; ++m) {
+              for (int e = 0; e < 2; ++e) {
+                const uint2 both = *reinterpret_cast<const uint2 *>(base + u * C + numbers + (n0 + n) * 128 + e * 64);
+                w[u][e][n0 + n] = both.y;
 #pragma unroll
-                for (int r = 0; r < kRows; ++r) {
-                  if (2 * m + r >= NT) continue;
-                  float &x = s[u][2 * m + r][2 * e + c];
-                  x = fmaf(step, acc[m][e][2 * r + c], fmaf(low, sums[m][r][n], x));
+                for (int c = 0; c < 2; ++c) {
+                  float &x = s[u][2 * e + c];
+                  x = n0 + n ? fmaf(low_of(both.x), sums[n0 + n][c], x) : low_of(both.x) * sums[n0 + n][c];
+                  x = fmaf(step_of(both.x), acc[u][n][2 * e + c], x);
                 }
               }
             }
           }
         }
-      }
-#pragma unroll
-      for (int u = 0; u < kOwn; ++u) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) s[u][nt][i] = s[u][nt][i] * 0x1p20f * to_log2[nt / 2][kRows == 2 ? nt & 1 : 0];
-        }
-      }
-      if (P.a.softcap > 0) {
-        const float in = fminf(1.0f / P.a.softcap, FLT_MAX), out = P.a.softcap * kLog2e;
-#pragma unroll
-        for (int u = 0; u < kOwn; ++u) {
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[u][nt][i] = tanh_of(s[u][nt][i] * in) * out;
-          }
-        }
-      }
-      auto live = [&](int u, int i) { return (rows >> (u * kCell + (i >> 1) * 8 + 2 * t4 + (i & 1))) & 1; };
-      if (!all) {  // what lies there of tokens that take no part may be anything
-#pragma unroll
-        for (int u = 0; u < kOwn; ++u) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if (live(u, i)) continue;
-            most[u][i] = 0x1p-60f;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) s[u][nt][i] = -INFINITY;
-          }
-        }
-      }
-      float p[kOwn][NT][4];
-      auto weigh = [&]() {
-        bool higher = false;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          const float from = ref[nt] - kUp;
+        if (P.a.softcap > 0) {
+          const float in = fminf(1.0f / P.a.softcap, FLT_MAX), out = P.a.softcap * kLog2e;
 #pragma unroll
           for (int u = 0; u < kOwn; ++u) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              p[u][nt][i] = exp2_of(s[u][nt][i] - from);
-              higher |= p[u][nt][i] * most[u][i] > kTop;
-            }
+            for (int i = 0; i < 4; ++i) s[u][i] = tanh_of(s[u][i] * to_log2[i & 1] * in) * out / to_log2[i & 1];
           }
         }
-        return __any_sync(~0u, higher);
-      };
-      if (weigh()) {  // seldom after the first tile
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          float top = kNone;
+        if (rows != ~0u) {  // what lies there of tokens that take no part may be anything: their P is zero, and so are V's numbers
 #pragma unroll
           for (int u = 0; u < kOwn; ++u) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) top = fmaxf(top, s[u][nt][i] + __log2f(most[u][i]));
-          }
-          top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
-          top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
-          top = fmaxf(top, ref[nt]);
-          const float keep = exp2_of(ref[nt] - top);
-          ref[nt] = top;
-          l[nt] *= keep;
-#pragma unroll
-          for (int n = 0; n < NG; ++n) lows[nt][n] *= keep;
-          const float keep0 = __shfl_sync(~0u, keep, 8 * t4), keep1 = __shfl_sync(~0u, keep, 8 * t4 + 4);
-#pragma unroll
-          for (int i = 0; i < 2 * NS; ++i) {
-            o[nt][i][0] *= keep0;
-            o[nt][i][1] *= keep1;
-            o[nt][i][2] *= keep0;
-            o[nt][i][3] *= keep1;
-          }
-        }
-        weigh();
-      }
-#pragma unroll
-      for (int u = 0; u < kOwn; ++u) {
-        const uint32_t cell = base + u * C;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) l[nt] += (p[u][nt][0] + p[u][nt][1]) + (p[u][nt][2] + p[u][nt][3]);
-        uint32_t v[NS][2];
-        load_v<NS>(cell + NS * 256, lane, v);
-#pragma unroll
-        for (int n = 0; n < NG; ++n) {
-          uint32_t w[2][2];
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            load_words<2>(cell + NS * 512 + n * 128 + e * 64 + t4 * 16 + 8, w[e]);
-            if (!all) {
-#pragma unroll
-              for (int c = 0; c < 2; ++c) w[e][c] = live(u, 2 * e + c) ? w[e][c] : 0;
-            }
-          }
-          uint32_t b[NT][2][2];  // [eight tokens][term]
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const float p0 = p[u][nt][2 * e], p1 = p[u][nt][2 * e + 1];
-              lows[nt][n] = fmaf(p0, low_of(w[e][0]), fmaf(p1, low_of(w[e][1]), lows[nt][n]));
-              two_terms(p0 * step_of(w[e][0]), p1 * step_of(w[e][1]), b[nt][e]);
+              if ((rows >> (u * kCell + e * 8 + g)) & 1) continue;
+#pragma unroll
+              for (int c = 0; c < 2; ++c) s[u][2 * e + c] = copysignf(INFINITY, -to_log2[c]);
+#pragma unroll
+              for (int n = 0; n < NG; ++n) w[u][e][n] = 0;
+            }
+          }
+        }
+        float step[kOwn][2];      // the largest
+#pragma unroll
+        for (int u = 0; u < kOwn; ++u) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            uint32_t most = w[u][e][0];
+#pragma unroll
+            for (int n = 1; n < NG; ++n) most = larger(most, w[u][e][n]);
+            step[u][e] = step_of(most);
+          }
+        }
+        float p[kOwn][4], sum[2];
+        auto weigh = [&]() {
+          bool beyond = fresh;
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            const float from = kUp - ref[c];
+            float most = 0.0f;
+#pragma unroll
+            for (int u = 0; u < kOwn; ++u) {
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                p[u][2 * e + c] = exp2_of(fmaf(s[u][2 * e + c], to_log2[c], from));
+                most = fmaxf(most, p[u][2 * e + c] * step[u][e]);
+              }
+            }
+            sum[c] = p[0][c] + p[0][c + 2] + (p[1][c] + p[1][c + 2]);
+            beyond |= most > kTop || sum[c] > kMost;
+          }
+          return beyond;
+        };
+        // seldom after the first tile: the reference, and all that is relative to it, go by this step's weights, too
+        auto renew = [&]() {
+          float weight[kOwn][2];  // log2 of the larger of |low| and step
+#pragma unroll
+          for (int u = 0; u < kOwn; ++u) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              float x = fmaxf(kLeast, step[u][e]);
+#pragma unroll
+              for (int n = 0; n < NG; ++n) x = fmaxf(x, fabsf(low_of(w[u][e][n])));
+              weight[u][e] = __log2f(x);
             }
           }
 #pragma unroll
-          for (int j = n * SG; j < (n + 1) * SG; ++j) {
+          for (int c = 0; c < 2; ++c) {
+            float top = kNone;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const uint32_t w0 = v[j][0] >> (8 * i), w1 = v[j][1] >> (8 * i);
-              const uint32_t a0 = w0 & 0x000F000Fu, a1 = w0 & 0x00F000F0u, a2 = w1 & 0x000F000Fu, a3 = w1 & 0x00F000F0u;
+            for (int u = 0; u < kOwn; ++u) top = fmaxf(top, fmaxf(fmaf(s[u][c], to_log2[c], weight[u][0]), fmaf(s[u][c + 2], to_log2[c], weight[u][1])));
+            top = fmaxf(top, __shfl_xor_sync(~0u, top, 4));
+            top = fmaxf(top, __shfl_xor_sync(~0u, top, 8));
+            top = fmaxf(top, __shfl_xor_sync(~0u, top, 16));
+            top = fmaxf(top, ref[c]);
+            const float keep = exp2_of(ref[c] - top);
+            ref[c] = top;
+            l[c] *= keep;
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt) {
-                mma<AMAP_FP16>(o[nt][2 * j + i], a0, a1, a2, a3, b[nt][0][0], b[nt][1][0]);
-                mma<AMAP_FP16>(o[nt][2 * j + i], a0, a1, a2, a3, b[nt][0][1], b[nt][1][1]);
+            for (int n = 0; n < NG; ++n) lows[n][c] *= keep;
+#pragma unroll
+            for (int i = 0; i < 2 * NS; ++i) {
+              o[i][c] *= keep;
+              o[i][c + 2] *= keep;
+            }
+          }
+          fresh = false;
+        };
+        if (__any_sync(~0u, weigh())) {
+          renew();
+          weigh();
+        }
+        l[0] += sum[0];
+        l[1] += sum[1];
+#pragma unroll
+        for (int n = 0; n < NG; ++n) {
+#pragma unroll
+          for (int u = 0; u < kOwn; ++u) {
+            // the second cell's codes are counted down from 15, low + step c = (low + 15 step) - step (15 - c): what the matrix
+            // unit sums then goes up and down by turns, and stays small beside what it cuts off at every step
+            uint32_t b[2][2];  // P step_V, [term][eight tokens]
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float own = step_of(w[u][e][n]), by = u ? -own : own, low = u ? fmaf(15.0f, own, low_of(w[u][e][n])) : low_of(w[u][e][n]);
+              uint32_t term[2];
+              two_terms(p[u][2 * e] * by, p[u][2 * e + 1] * by, term);
+              b[0][e] = transposed(term[0]), b[1][e] = transposed(term[1]);
+#pragma unroll
+              for (int c = 0; c < 2; ++c) lows[n][c] = fmaf(p[u][2 * e + c], low, lows[n][c]);
+            }
+            uint32_t v[SG][2], a[2 * SG][4];
+            load_v<NS, SG>(base + u * C + NS * 256, lane, n * SG, v);
+#pragma unroll
+            for (int j = 0; j < SG; ++j) {
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                // rows g: whole bytes, of which 16 times rows g + 8, the upper codes, is taken off again at the end
+                const uint32_t x0 = u ? ~v[j][0] : v[j][0], x1 = u ? ~v[j][1] : v[j][1];
+                a[2 * j + i][0] = i ? __byte_perm(x0, 0, 0x4341) : x0 & 0x00FF00FFu;
+                a[2 * j + i][1] = (i ? a[2 * j + i][0] : x0) & 0x00F000F0u;
+                a[2 * j + i][2] = i ? __byte_perm(x1, 0, 0x4341) : x1 & 0x00FF00FFu;
+                a[2 * j + i][3] = (i ? a[2 * j + i][2] : x1) & 0x00F000F0u;
+              }
+            }
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+#pragma unroll
+              for (int i = 0; i < 2 * SG; ++i) {
+                mma<AMAP_FP16>(o[2 * n * SG + i], a[i][0], a[i][1], a[i][2], a[i][3], b[t][0], b[t][1]);
               }
             }
           }
         }
       }
+      __syncwarp();
+      if (lane == 0) bar_arrive(smem_at(&small.empty[stage]));
+      if (++stage == S) stage = 0, parity ^= 1;
     }
-    __syncwarp();
-    if (lane == 0) bar_arrive(smem_at(&small.empty[stage]));
-    if (++stage == S) stage = 0, parity ^= 1;
-
+    at.left -= here - 1;
+    at.rest -= here - 1;
     more = at.more();
-    if (at.left > 1 && more) {
-      at.advance(P);
-      continue;
-    }
     // ---- the end of an item, or of this block's part of it: join the warps ----
     const int r = at.r, h = at.h * P.members + member, tiles = Line::tiles(P, at.n);
     if (more) {
@@ -470,36 +499,36 @@ __global__ void __launch_bounds__(kBlock, (kPackedResident<NS, NT>)) attend_pack
     const int heads = min(HB, P.group - in_group);
     const int slot = 2 * (team * P.members + member) + (item_first >= u0 ? 1 : 0);  // a block has at most two parts: its first item's and its last's
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      if (nt * 8 >= heads) break;
-      float sum = l[nt];
-      sum += __shfl_xor_sync(~0u, sum, 1);
-      sum += __shfl_xor_sync(~0u, sum, 2);
-      const float own = ref[nt] == kNone ? -INFINITY : ref[nt];
-      if (t4 == 0) *reinterpret_cast<float2 *>(joint + (warp * 8 + g) * kPitch + D) = make_float2(own, sum);
-      sync_consumers();
-      const float *ml = joint + g * kPitch + D;
+    for (int c = 0; c < 2; ++c) {
+      float sum = l[c];
+      sum += __shfl_xor_sync(~0u, sum, 4);
+      sum += __shfl_xor_sync(~0u, sum, 8);
+      sum += __shfl_xor_sync(~0u, sum, 16);
+      if (ref[c] == kNone) ref[c] = -INFINITY;
+      if (g == 0) *reinterpret_cast<float2 *>(joint + (warp * 8 + 2 * t4 + c) * kPitch + D) = make_float2(ref[c], sum);
+    }
+    sync_consumers();
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const float *ml = joint + (2 * t4 + c) * kPitch + D;
       const float top = fmaxf(fmaxf(ml[0], ml[8 * kPitch]), fmaxf(ml[16 * kPitch], ml[24 * kPitch]));
-      const float f = top == -INFINITY ? 1.0f : exp2_of(own - top);
-      const float f0 = __shfl_sync(~0u, f, 8 * t4), f1 = __shfl_sync(~0u, f, 8 * t4 + 4);
-      float *to = joint + (warp * 8 + 2 * t4) * kPitch;
+      const float f = top == -INFINITY ? 1.0f : exp2_of(ref[c] - top);
+      float *to = joint + (warp * 8 + 2 * t4 + c) * kPitch;
 #pragma unroll
       for (int n = 0; n < NG; ++n) {
-        float low = lows[nt][n];
-        low += __shfl_xor_sync(~0u, low, 1);
-        low += __shfl_xor_sync(~0u, low, 2);
-        const float low0 = __shfl_sync(~0u, low, 8 * t4), low1 = __shfl_sync(~0u, low, 8 * t4 + 4);
+        float low = lows[n][c];
+        low += __shfl_xor_sync(~0u, low, 4);
+        low += __shfl_xor_sync(~0u, low, 8);
+        low += __shfl_xor_sync(~0u, low, 16);
 #pragma unroll
-        for (int i = 2 * n * SG; i < 2 * (n + 1) * SG; ++i) {  // rows g and g + 8 are elements 4g + 2 (i mod 2) and the one behind it
-          const int d = i / 2 * 32 + 4 * g + 2 * (i & 1);
-          *reinterpret_cast<float2 *>(to + d) = make_float2(fmaf(o[nt][i][0], 0x1p24f, low0) * f0, fmaf(o[nt][i][2], 0x1p20f, low0) * f0);
-          *reinterpret_cast<float2 *>(to + kPitch + d) = make_float2(fmaf(o[nt][i][1], 0x1p24f, low1) * f1, fmaf(o[nt][i][3], 0x1p20f, low1) * f1);
-        }
+        for (int i = 2 * n * SG; i < 2 * (n + 1) * SG; ++i)  // rows g and g + 8 are elements 4g + 2 (i mod 2) and the one behind it
+          *reinterpret_cast<float2 *>(to + i / 2 * 32 + 4 * g + 2 * (i & 1)) =
+              make_float2(fmaf(o[i][c] - o[i][c + 2], 0x1p24f, low) * f, fmaf(o[i][c + 2], 0x1p20f, low) * f);
       }
-      sync_consumers();
-      sum_warps<D, HB>(P, joint, nt, heads, whole, r, first + in_group, slot, kUp);
-      sync_consumers();
     }
+    sync_consumers();
+    sum_warps<D, HB>(P, joint, 0, heads, whole, r, first + in_group, slot, kUp);
+    sync_consumers();
     if (!whole) hand_in<D, HB>(P, small, joined, piece, item_first, item_last, heads, r, h, first + in_group, kUp);  // uniform over the block
     if (more) {
       item_first = u1 - at.rest;
@@ -510,23 +539,12 @@ __global__ void __launch_bounds__(kBlock, (kPackedResident<NS, NT>)) attend_pack
   if (!alive) settle(smem_at(&small.full[0]), S, stage, parity, P.failed);
 }
 
-template <int NS, int SG, int NT>
+template <int NS, int SG>
 int run_packed(PackedParams &P, void *stream) {
-  constexpr int S = kPackedStages<NS, NS / SG, kPackedResident<NS, NT>>, D = 32 * NS;
+  constexpr int S = kPackedStages<NS, NS / SG, kPackedResident<NS>>, D = 32 * NS;
   constexpr size_t smem = (size_t)S * kCells * cell_bytes(NS, NS / SG) + sizeof(float) * kWarps * 8 * (D + 4) + sizeof(Small<S, kPackedTile>);
   static std::atomic<int> known[64];
-  return launch_split<D, kPackedTile>(attend_packed_kernel<NS, SG, NT>, known, P.p, P, smem, stream);
-}
-
-template <int NS, int SG>
-int run_packed_heads(PackedParams &P, int nt, void *stream) {
-  switch (nt) {
-    case 1: return run_packed<NS, SG, 1>(P, stream);
-    case 2: return run_packed<NS, SG, 2>(P, stream);
-    default:
-      if constexpr (NS < 8) return run_packed<NS, SG, 4>(P, stream);
-      else return run_packed<NS, SG, 2>(P, stream);
-  }
+  return launch_split<D, kPackedTile>(attend_packed_kernel<NS, SG>, known, P.p, P, smem, stream);
 }
 
 }  // namespace
@@ -544,15 +562,16 @@ extern "C" int amap_packed_attend(const amap_attend_args *a, const amap_packed *
   P.a.cache.n_pages = c.n_pages, P.a.cache.page_size = c.page_size, P.a.cache.heads = c.heads, P.a.cache.head_dim = c.head_dim;
   P.a.cache.k_scale = P.a.cache.v_scale = 1.0f;
   PP.data = static_cast<const char *>(c.data), PP.page = c.page, PP.head = c.head;
-  const int nt = eights(a->q_heads / c.heads, c.head_dim <= 128 ? 128 : 256);
-  if (const int rc = place(P, nt)) return rc;
+  PP.run = 1;
+  while (PP.run < kCells && c.page_size / kCell % (2 * PP.run) == 0) PP.run *= 2;
+  if (const int rc = place(P, 1)) return rc;
   switch (c.head_dim * 2 + (c.group == 64)) {
-    case 128: return run_packed_heads<2, 1>(PP, nt, cuda_stream);
-    case 129: return run_packed_heads<2, 2>(PP, nt, cuda_stream);
-    case 192: return run_packed_heads<3, 1>(PP, nt, cuda_stream);
-    case 256: return run_packed_heads<4, 1>(PP, nt, cuda_stream);
-    case 257: return run_packed_heads<4, 2>(PP, nt, cuda_stream);
-    case 512: return run_packed_heads<8, 1>(PP, nt, cuda_stream);
-    default: return run_packed_heads<8, 2>(PP, nt, cuda_stream);  // check_packed has refused everything else
+    case 128: return run_packed<2, 1>(PP, cuda_stream);
+    case 129: return run_packed<2, 2>(PP, cuda_stream);
+    case 192: return run_packed<3, 1>(PP, cuda_stream);
+    case 256: return run_packed<4, 1>(PP, cuda_stream);
+    case 257: return run_packed<4, 2>(PP, cuda_stream);
+    case 512: return run_packed<8, 1>(PP, cuda_stream);
+    default: return run_packed<8, 2>(PP, cuda_stream);  // check_packed has refused everything else
   }
 }

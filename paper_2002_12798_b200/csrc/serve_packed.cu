@@ -67,8 +67,8 @@ __global__ void __launch_bounds__(kThreads) read_kernel(const __grid_constant__ 
       const uint32_t kw = *reinterpret_cast<const uint32_t *>(cell + k_word_at(NS, token, c));
       const uint32_t v0 = *reinterpret_cast<const uint16_t *>(cell + v_half_at(NS, token, 2 * c));
       const uint32_t v1 = *reinterpret_cast<const uint16_t *>(cell + v_half_at(NS, token, 2 * c + 1));
-      const char *numbers = cell + numbers_at(NS, token, c * 8 >> P.group_shift);
-      const uint32_t kn = *reinterpret_cast<const uint32_t *>(numbers), vn = *reinterpret_cast<const uint32_t *>(numbers + 8);
+      const uint2 numbers = *reinterpret_cast<const uint2 *>(cell + numbers_at(NS, token, c * 8 >> P.group_shift));
+      const uint32_t kn = numbers.x, vn = numbers.y;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         k[i] = fmaf(step_of(kn), (float)(kw >> (4 * (i >> 1) + 16 * (i & 1)) & 15), low_of(kn));

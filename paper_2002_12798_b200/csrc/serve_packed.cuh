@@ -7,8 +7,7 @@
 //             4i + 16 o.  Up to four slabs side by side: [token][t][slab]
 //   V codes   per slab 32 lanes x 8 bytes, lane 4g + t: elements 4g .. 4g+3 (four bits each) of the tokens 2t, 2t+1, 2t+8,
 //             2t+9, 16 bits a token.  Up to two slabs side by side: [lane][slab]
-//   numbers   per group [token / 8][t] four words, of tokens 2t and 2t+1 (+8): K's, K's, V's, V's; a word is step (low 16
-//             bits) and low (high), both bf16
+//   numbers   per group and token K's word and V's; a word is step (low 16 bits) and low (high), both bf16
 // A token's bytes are its own: tokens of one cell are written independently.
 #pragma once
 #include <cstdint>
@@ -39,8 +38,8 @@ AMAP_HD int v_half_at(int slabs, int token, int f) {
   const int slab = f >> 3, first = slab & ~1, wide = slabs - first < 2 ? slabs - first : 2;
   return slabs * 256 + first * 256 + ((f & 7) * 4 + ((token & 7) >> 1)) * 8 * wide + (slab - first) * 8 + (token >> 3) * 4 + (token & 1) * 2;
 }
-// offset of K's word of numbers of a group; V's lies 8 bytes behind
-AMAP_HD int numbers_at(int slabs, int token, int group) { return slabs * 512 + group * 128 + (token >> 3) * 64 + ((token & 7) >> 1) * 16 + (token & 1) * 4; }
+// offset of K's word of numbers of a group; V's lies behind it
+AMAP_HD int numbers_at(int slabs, int token, int group) { return slabs * 512 + group * 128 + token * 8; }
 
 // Checks of a description that every operator on it makes; AMAP_OK, or the refusal.
 int check_packed(const amap_packed &c);

@@ -506,7 +506,7 @@ __device__ __forceinline__ void pack_rows(const Packing &A, uint32_t block, doub
       *reinterpret_cast<uint16_t *>(cell + v_half_at(A.slabs, t, 2 * c + 1)) = (uint16_t)(code[4] | code[5] << 4 | code[6] << 8 | code[7] << 12);
     }
     if (d0 % A.group == 0)
-      *reinterpret_cast<uint32_t *>(cell + numbers_at(A.slabs, t, d0 / A.group) + (is_k ? 0 : 8)) = (uint32_t)__bfloat16_as_ushort(low) << 16 | __bfloat16_as_ushort(step);
+      *reinterpret_cast<uint32_t *>(cell + numbers_at(A.slabs, t, d0 / A.group) + (is_k ? 0 : 4)) = (uint32_t)__bfloat16_as_ushort(low) << 16 | __bfloat16_as_ushort(step);
   }
 }
 

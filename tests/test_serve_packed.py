@@ -86,7 +86,7 @@ def test_a_cell_is_tiled_by_its_tokens(places, dim, group):
     owner = np.full(p["bytes"], -1)
     for kind, size in (("k", 4), ("v", 2), ("n", 4)):
         for (token, _), at in p[kind].items():
-            for first in (at, at + 8) if kind == "n" else (at,):  # V's numbers lie 8 bytes behind K's
+            for first in (at, at + 4) if kind == "n" else (at,):  # V's numbers lie behind K's
                 assert at % size == 0 and (owner[first : first + size] == -1).all()
                 owner[first : first + size] = token
     assert (owner >= 0).all() and p["bytes"] % 128 == 0
@@ -112,8 +112,7 @@ def test_lanes_find_their_operands(places, dim, group):
                     assert p["v"][token, 8 * slab + g] == word + 2 * (token & 1)
         for n in range(dim // group):
             for e in range(2):
-                for c in range(2):
-                    assert p["n"][8 * e + 2 * t4 + c, n] == slabs * 512 + n * 128 + e * 64 + t4 * 16 + 4 * c
+                assert p["n"][8 * e + g, n] == slabs * 512 + g * 8 + n * 128 + e * 64
 
 
 def test_the_reference_quantises_as_defined():
