@@ -332,8 +332,8 @@ int amap_packed_attend(const amap_attend_args *args /* host */, const amap_packe
  * A uniform number outside counts as the nearest inside, NaN as 0.
  * logprob[r] = log of the probability with which the token was drawn (0 for
  * temperature 0, -infinity with token -1).
- * The answer is the definition's in 64 bits: w is kept to 2^-40 of itself (and
- * to 2^-44 of the largest), sums are whole numbers, in no order.
+ * The answer is the definition's in 64 bits: w is rounded to units of 2^-44 (of
+ * the largest), sums are whole numbers, in no order.
  * ------------------------------------------------------------------------- */
 typedef struct amap_sample_args {
   int32_t rows;    /* 1 .. 65535 */

@@ -1,18 +1,22 @@
 // Sampling: temperature, top-k, min-p and top-p, and a token from one uniform number per row (amap_sample).
 //
-// Mathematics.  A token's weight is w = 2^y, y = (x - max) log2(e) / temperature, held as a whole number W of units of 2^-44: y
-// comes out of one 64-bit multiply-add as a fixed-point number with 45 fractional bits, 2^y by table and a polynomial in
-// integers (Tang, ACM Transactions on Mathematical Software 15, 1989): 2^-40 of itself.  Sums of W are whole numbers, so
-// their order does not matter, and the answer is the 64-bit definition's for all but about one row in 10^7: with weights of
-// 24 bits the borders between 10^5 tokens would move by a percent of the distance between them.
+// Mathematics.  A token's weight w = 2^y, y = (x - max) log2(e) / temperature, by a table of 2^(i/1024) and a polynomial of degree 3
+// in 64 bits (Tang, ACM Transactions on Mathematical Software 15, 1989), is rounded to a whole number W of units of 2^-44.
+// Sums of W are whole numbers, so their order does not matter, and the answer is the 64-bit definition's but where the
+// uniform number is within some 2^-35 of a border between two tokens: with weights of 24 bits, rows of 10^5 tokens would often
+// come out otherwise.
 //
 // What the settings keep is a beginning of the order by (logit, index), given by a last logit and how many of the tokens
-// that have it are kept.  It is found by histograms of counts and sums: first over y (bins of 2^-6), then over the bits
-// of the logits in the bin where the bound falls, until that holds one logit.  The draw takes the sums of each warp's run of
-// the row, and goes through one of them.
+// that have it are kept.  A first bound is cheap: min_p gives one; for top_k the top_k-th largest of the threads' own
+// maxima; for top_p alone the weight that all tokens together would need to make up the rest.  The tokens above it, few as
+// a rule, are listed by each warp, and if there are 1024 at most one block sorts them and is done.  More of them, or a row
+// whose lists overflow, go by histograms of counts and sums: first over y (64 bins to a power of two), then over the bits
+// of the logits in the bin where a bound falls, until that holds one logit.  The draw takes the sums of each warp's run of
+// the row (or of its list), and goes through one of them.
 //
-// Bound: memory for many rows; the logits are read once from HBM and two to five times from the second-level cache.  A row
-// is a cluster's, of as many blocks as fill the device, which exchange sums through shared memory.
+// Bound: the weights where all tokens have to be weighed (about 25 instructions, nine of them in 64 bits, each), memory and
+// latency elsewhere; the logits come from HBM once, and from the second-level cache once or twice more.  A row is a
+// cluster's, of as many blocks as fill the device, which exchange sums through shared memory.
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -33,6 +37,8 @@ constexpr int kBins = 2944;             // 46 powers of two in 64 bins each: all
 constexpr int kKeyBins = 2048;
 constexpr int kPoints = 1024;           // of the table of 2^x
 constexpr int kUnit = 44;               // W is in units of 2^-44
+constexpr int kListed = 320;            // tokens of a warp's list
+constexpr int kSorted = 1024;           // tokens that one block sorts
 
 struct Params {
   amap_sample_args a;
@@ -45,19 +51,30 @@ struct Tally {  // of the elements before a bound
 };
 
 struct Shared {
-  uint64_t table[kPoints];
-  uint32_t count[kBins], low[kBins], high[kBins];  // a bin's tokens and the sum of their W
-  uint64_t share_mass[kBins / 2];                  // the cluster's sums of this block's share of the bins
-  uint32_t share_count[kBins / 2];
-  // exchanged with the other blocks; every step has its own
-  uint64_t block_mass, warp_mass[kWarps];
-  uint32_t block_count, warp_equal[kWarps];
+  double table[kPoints];
+  union {
+    struct {
+      uint32_t count[kBins], low[kBins], high[kBins];  // a bin's tokens and the sum of their W
+    };
+    struct {
+      uint64_t order[kSorted];  // key and index of the tokens to be sorted
+      uint64_t sums[kSorted];   // their W
+    };
+  };
+  float list_value[kWarps][kListed];
+  int32_t list_index[kWarps][kListed];
+  // exchanged with the other blocks
+  uint64_t run_mass[kThreads];  // of the bins that a thread adds up
+  uint32_t run_count[kThreads];
+  Tally block_tally[2];
+  uint64_t warp_mass[kWarps];
+  uint32_t warp_equal[kWarps], warp_listed[kWarps];
   float block_max;
   int32_t block_first;
   uint32_t block_least, block_most;
-  uint64_t found_mass;
-  uint32_t found_count, found_bin;
   // this block's
+  Tally found;
+  uint32_t found_run, found_bin;
   uint64_t scan_mass[kWarps];
   uint32_t scan_count[kWarps];
   float warp_max[kWarps];
@@ -65,9 +82,9 @@ struct Shared {
   uint32_t warp_least[kWarps], warp_most[kWarps];
   uint64_t all_mass[kMostBlocks * kWarps];
   uint32_t all_equal[kMostBlocks * kWarps];
-  uint64_t pick_before;
+  uint64_t pick_before, total;
   uint32_t pick_equal;
-  int32_t pick_warp;
+  int32_t pick_warp, kept;
 };
 
 // order of floats as whole numbers
@@ -102,67 +119,86 @@ __device__ __forceinline__ uint64_t share_up(float f, uint64_t m) {
 template <int DT>
 struct Sampler {
   using T = typename Elem<DT>::T;
-  static constexpr int VEC = 16 / sizeof(T), kAhead = 16 / VEC;  // vectors under way in a thread
+  static constexpr int VEC = 16 / sizeof(T), kAhead = 3;  // elements of a vector; vectors under way in a thread
   Shared &S;
   const T *x;
   int vocab, shift;      // shift: elements between the 16-byte boundary at or before x and x
   int begin, end;        // this warp's vectors, counted from that boundary
   int blocks, rank;
-  float top;             // the largest logit
-  bool infinite;         // it is +infinity
-  double by;             // y = (x - top) by
-  float range;           // weights of logits further than this below it are zero
-  uint64_t least;        // smaller weights count as zero (min_p)
+  bool alone;            // only tokens with the largest logit have a weight, as it is +infinity or the lowest float: they count as 0, the
+                         // others as -1
+  float largest;
+  double top, by;        // y = (x - top) by / 1024
+  float least_value;     // smaller logits, and NaN, have no weight, and are taken to be this one
+  uint64_t least;        // smaller W count as zero (min_p)
+  bool listed;           // the tokens are those of the warps' lists
+  int n_listed;
 
-  __device__ __forceinline__ void load(int j, float (&v)[VEC]) const {
+  union Vector {
+    uint4 raw;
+    T e[VEC];
+  };
+  // the j-th vector before `until`; NaN for what lies outside the row
+  __device__ __forceinline__ Vector load(int j, int until) const {
     const int first = j * VEC - shift;
-    if (j < end && first >= 0 && first + VEC <= vocab) {
-      union {
-        uint4 raw;
-        T e[VEC];
-      } u;
+    Vector u;
+    if (j < until && first >= 0 && first + VEC <= vocab) {
       u.raw = *reinterpret_cast<const uint4 *>(x + first);
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) v[i] = Elem<DT>::to(u.e[i]);
     } else {
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) v[i] = j < end && first + i >= 0 && first + i < vocab ? Elem<DT>::to(x[first + i]) : __uint_as_float(0x7FC00000u);
+      for (int i = 0; i < VEC; ++i) u.e[i] = j < until && first + i >= 0 && first + i < vocab ? x[first + i] : Elem<DT>::from(__uint_as_float(0x7FC00000u));
+    }
+    return u;
+  }
+  // f(index, logit) for every element of this lane's vectors among those from `from` to `until`; NaN for those that are none
+  template <typename F>
+  __device__ __forceinline__ void each_between(int from, int until, F f) const {
+    int j = from + (threadIdx.x & 31);
+    Vector ahead[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) ahead[k] = load(j + 32 * k, until);
+#pragma unroll 1
+    for (; j - (int)(threadIdx.x & 31) < until; j += 32) {
+      const Vector u = ahead[0];
+#pragma unroll
+      for (int k = 0; k + 1 < kAhead; ++k) ahead[k] = ahead[k + 1];
+      ahead[kAhead - 1] = load(j + 32 * kAhead, until);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) f(j * VEC - shift + i, Elem<DT>::to(u.e[i]));
     }
   }
-  // f(index, value) for every element of this lane's vectors; NaN for those that are none
+  template <typename F>
+  __device__ __forceinline__ void each_of_row(F f) const { each_between(begin, end, f); }
+  __device__ __forceinline__ float value(float v) const { return fmaxf(alone ? (v == largest ? 0.0f : -1.0f) : v, least_value); }
+  // f(value) for every token, of the row or of the lists
   template <typename F>
   __device__ __forceinline__ void each(F f) const {
-    for (int j = begin + (threadIdx.x & 31); j < end; j += 32 * kAhead) {
-      float v[kAhead][VEC];
-#pragma unroll
-      for (int k = 0; k < kAhead; ++k) load(j + 32 * k, v[k]);
-#pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) f((j + 32 * k) * VEC - shift + i, v[k][i]);
-      }
+    if (listed) {
+      for (int i = threadIdx.x & 31; i < n_listed; i += 32) f(S.list_value[threadIdx.x >> 5][i]);
+    } else {
+      each_of_row([&](int, float v) { f(value(v)); });
     }
   }
 
-  // y + 64 with 45 fractional bits; 0 for what has no weight
-  __device__ __forceinline__ uint64_t place_of(float v) const {
-    if (infinite) return v == top ? 64ull << 45 : 0;
-    if (!(top - v <= range)) return 0;  // NaN and -infinity among them
-    // 192 + y lies between 128 and 256, where a double's last bit is 2^-45
-    return (uint64_t)__double_as_longlong(fma((double)v - (double)top, by, 192.0)) & ((1ull << 52) - 1);
-  }
-  __device__ __forceinline__ uint64_t weight_of(uint64_t place) const {
-    const uint32_t whole = (uint32_t)(place >> 45), point = (uint32_t)(place >> 35) & (kPoints - 1), rest = (uint32_t)(place >> 3);
-    // rest: 32 bits of what is beyond the point, d = rest 2^-42; 2^d - 1 = e + e^2/2 + e^3/6 with e = d ln 2, in units of 2^-42
-    const uint32_t e = __umulhi(rest, 2977044472u), e2 = __umulhi(e, e), e3 = __umulhi(e2, e);
-    const uint32_t p = e + (e2 >> 11) + (__umulhi(e3, 715827883u) >> 20);
-    if (whole < 20) return 0;
-    const uint64_t t = S.table[point];
-    const uint64_t w = (t + ((uint64_t)__umulhi((uint32_t)(t >> 13), p) << 3)) >> (64 - whole);
+  // W of a token, and 1024 y rounded
+  __device__ __forceinline__ uint64_t weight(float v, int *y) const {
+    constexpr double kMagic = 0x1.8p52, kBase = 0x1.8p8;
+    constexpr double c1 = 6.769015435155716e-4, c2 = 2.290978498068816e-7, c3 = 5.169222938345892e-11;  // (ln 2 / 1024)^n / n!
+    const double d = (double)v - top, t = fma(d, by, kMagic), r = fma(d, by, kMagic - t), p = r * fma(r, fma(r, c3, c2), c1);
+    const int i = __double2loint(t);
+    *y = i;
+    const double two = S.table[i & (kPoints - 1)], power = __hiloint2double(__double2hiint(two) + (i >> 10) * (1 << 20), __double2loint(two));
+    // beside 384 the last bit is 2^-44
+    const uint64_t w = (uint64_t)(__double_as_longlong(fma(power, p, power) + kBase) - __double_as_longlong(kBase));
     return w >= least ? w : 0;
   }
-  __device__ __forceinline__ uint64_t weight(float v) const { return weight_of(place_of(v)); }
-  static __device__ __forceinline__ int bin_of(uint64_t place) { return (int)(((64ull << 45) - place) >> 39); }
+  __device__ __forceinline__ uint64_t weight(float v) const {
+    int y;
+    return weight(v, &y);
+  }
+  static __device__ __forceinline__ int bin_of(int y) { return -y >> 4; }
+  // a value that every token with a bin up to this one reaches
+  __device__ __forceinline__ float value_of_bin(int bin) const { return fmaxf(__double2float_rd(top - (16.0 * (bin + 1) + 1.0) / by), least_value); }
 
   __device__ __forceinline__ void clear_bins(int n) const {
     for (int i = threadIdx.x; i < n; i += kThreads) S.count[i] = S.low[i] = S.high[i] = 0;
@@ -191,37 +227,32 @@ struct Sampler {
     return all;
   }
 
-  // The first bin at whose end the tokens so far (by_count) are `want` or more, or their sum `target` or more, and the tally
-  // before it.  Adds the cluster's histograms up on the way: a block has a share of the bins.  There is such a bin.
-  __device__ Tally find_bin(int n, bool by_count, uint32_t want, uint64_t target, int *bin) const {
-    cg::cluster_group cluster = cg::this_cluster();
-    const int per = (n + blocks - 1) / blocks, first = rank * per, mine = max(0, min(per, n - first));
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (blocks > 1) cluster.sync();
+  __device__ __forceinline__ const Shared *block(int b) const { return blocks > 1 ? cg::this_cluster().map_shared_rank(&S, b) : &S; }
+  __device__ __forceinline__ void sync_row() const {
+    if (blocks > 1) cg::this_cluster().sync();
     else __syncthreads();
-    auto get = [&](int i, Tally *t) {  // bin first + i, of the whole cluster
-      if (blocks > 1) *t = {S.share_mass[i], S.share_count[i]};
-      else *t = {(uint64_t)S.high[i] << 32, S.count[i]}, t->mass += S.low[i];
-    };
+  }
+
+  // The first bin at whose end the row's tokens so far (by_count) are `want` or more, or their sum `target` or more, and the
+  // tally before it; there is such a bin.  The blocks exchange sums of runs of bins, and look into the bins of one run.
+  // Between this and what writes to the bins next lies a barrier of the row's blocks.
+  __device__ Tally find_bin(int n, bool by_count, uint32_t want, uint64_t target, int *bin) const {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, run = (n + kThreads - 1) / kThreads;  // at most 8
+    __syncthreads();
     Tally sum = {0, 0};
-    if (blocks > 1) {
-      for (int i = tid; i < mine; i += kThreads) {
-        Tally t = {0, 0};
-        for (int b = 0; b < blocks; ++b) {
-          const Shared *o = cluster.map_shared_rank(&S, b);
-          t.mass += ((uint64_t)o->high[first + i] << 32) + o->low[first + i];
-          t.count += o->count[first + i];
-        }
-        S.share_mass[i] = t.mass, S.share_count[i] = t.count;
-      }
-      __syncthreads();
+    for (int i = min(n, tid * run); i < min(n, (tid + 1) * run); ++i) {
+      sum.mass += ((uint64_t)S.high[i] << 32) + S.low[i];
+      sum.count += S.count[i];
     }
-    // runs of bins: a thread's, side by side
-    const int run = (mine + kThreads - 1) / kThreads, i0 = min(mine, tid * run), i1 = min(mine, i0 + run);
-    for (int i = i0; i < i1; ++i) {
-      Tally t;
-      get(i, &t);
-      sum.mass += t.mass, sum.count += t.count;
+    S.run_mass[tid] = sum.mass, S.run_count[tid] = sum.count;
+    if (tid == 0) S.found = {0, 0}, S.found_run = 0, S.found_bin = 0;
+    sync_row();
+    if (blocks > 1) {
+      sum = {0, 0};
+#pragma unroll
+      for (int b = 0; b < kMostBlocks; ++b) {
+        if (b < blocks) sum.mass += block(b)->run_mass[tid], sum.count += block(b)->run_count[tid];
+      }
     }
     Tally upto = sum;
 #pragma unroll
@@ -230,92 +261,71 @@ struct Sampler {
       const uint32_t c = __shfl_up_sync(~0u, upto.count, d);
       if (lane >= d) upto.mass += m, upto.count += c;
     }
-    __syncthreads();
     if (lane == 31) S.scan_mass[warp] = upto.mass, S.scan_count[warp] = upto.count;
     __syncthreads();
-    Tally whole = {0, 0};
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
       if (w < warp) upto.mass += S.scan_mass[w], upto.count += S.scan_count[w];
-      whole.mass += S.scan_mass[w], whole.count += S.scan_count[w];
-    }
-    if (blocks > 1) {
-      if (tid == 0) S.block_mass = whole.mass, S.block_count = whole.count, S.found_bin = ~0u;
-      cluster.sync();
-      for (int b = 0; b < rank; ++b) {
-        const Shared *o = cluster.map_shared_rank(&S, b);
-        upto.mass += o->block_mass, upto.count += o->block_count;
-      }
-    } else {
-      if (tid == 0) S.found_mass = 0, S.found_count = 0, S.found_bin = 0;
-      __syncthreads();
     }
     auto enough = [&](const Tally &t) { return by_count ? t.count >= want : t.mass >= target; };
-    Tally before = {upto.mass - sum.mass, upto.count - sum.count};
-    if (enough(upto) && !enough(before)) {  // one thread of the cluster
-      for (int i = i0; i < i1; ++i) {
-        Tally t;
-        get(i, &t);
-        t.mass += before.mass, t.count += before.count;
-        if (enough(t)) {
-          S.found_mass = before.mass, S.found_count = before.count, S.found_bin = first + i;
-          break;
-        }
-        before = t;
-      }
-    }
-    if (blocks > 1) {
-      cluster.sync();
+    const Tally before = {upto.mass - sum.mass, upto.count - sum.count};
+    if (enough(upto) && !enough(before)) S.found = before, S.found_run = tid;
+    __syncthreads();
+    if (warp == 0) {  // a bin to each of eight lanes, a block to each of four eights
+      const int i = S.found_run * run + (lane & 7);
       Tally t = {0, 0};
-      *bin = 0;
-      for (int b = 0; b < blocks; ++b) {
-        const Shared *o = cluster.map_shared_rank(&S, b);
-        if (o->found_bin != ~0u) *bin = (int)o->found_bin, t = {o->found_mass, o->found_count};
+      if ((lane & 7) < run && i < n) {
+        for (int b = lane >> 3; b < blocks; b += 4) {
+          const Shared *o = block(b);
+          t.mass += ((uint64_t)o->high[i] << 32) + o->low[i];
+          t.count += o->count[i];
+        }
       }
-      cluster.sync();  // before anybody writes to these again
-      return t;
+#pragma unroll
+      for (int d = 8; d < 32; d <<= 1) t.mass += __shfl_xor_sync(~0u, t.mass, d), t.count += __shfl_xor_sync(~0u, t.count, d);
+      Tally at = S.found, own = t;
+#pragma unroll
+      for (int d = 1; d < 8; d <<= 1) {
+        const uint64_t m = __shfl_up_sync(~0u, t.mass, d, 8);
+        const uint32_t c = __shfl_up_sync(~0u, t.count, d, 8);
+        if ((lane & 7) >= d) t.mass += m, t.count += c;
+      }
+      at.mass += t.mass, at.count += t.count;
+      const Tally ahead = {at.mass - own.mass, at.count - own.count};
+      __syncwarp();
+      if (lane < 8 && enough(at) && !enough(ahead)) S.found = ahead, S.found_bin = i;
     }
     __syncthreads();
     *bin = (int)S.found_bin;
-    const Tally t = {S.found_mass, S.found_count};
-    __syncthreads();
-    return t;
+    return S.found;
   }
 
   // Among the tokens of a bin of y: the logit (as a key) at which `want` tokens or the sum `target` are reached, and the tally
   // before it.
   __device__ Tally refine(int bin, bool by_count, uint32_t want, uint64_t target, uint32_t *key) const {
-    cg::cluster_group cluster = cg::this_cluster();
     uint32_t lo = ~0u, hi = 0;
-    each([&](int, float v) {
-      const uint64_t place = place_of(v);
-      if (place && bin_of(place) == bin && weight_of(place)) lo = min(lo, key_of(v)), hi = max(hi, key_of(v));
+    each([&](float v) {
+      int y;
+      if (weight(v, &y) && bin_of(y) == bin) lo = min(lo, key_of(v)), hi = max(hi, key_of(v));
     });
     lo = __reduce_min_sync(~0u, lo), hi = __reduce_max_sync(~0u, hi);
     if ((threadIdx.x & 31) == 0) S.warp_least[threadIdx.x >> 5] = lo, S.warp_most[threadIdx.x >> 5] = hi;
     __syncthreads();
     lo = ~0u, hi = 0;
     for (int w = 0; w < kWarps; ++w) lo = min(lo, S.warp_least[w]), hi = max(hi, S.warp_most[w]);
-    if (blocks > 1) {
-      if (threadIdx.x == 0) S.block_least = lo, S.block_most = hi;
-      cluster.sync();
-      for (int b = 0; b < blocks; ++b) {
-        const Shared *o = cluster.map_shared_rank(&S, b);
-        lo = min(lo, o->block_least), hi = max(hi, o->block_most);
-      }
-      cluster.sync();
-    }
+    if (threadIdx.x == 0) S.block_least = lo, S.block_most = hi;
+    sync_row();
+    for (int b = 0; b < blocks; ++b) lo = min(lo, block(b)->block_least), hi = max(hi, block(b)->block_most);
     Tally all = {0, 0};
     for (int pass = 0; pass < 3 && lo < hi; ++pass) {  // 11 bits each
       const int down = max(0, 32 - __clz(hi - lo) - 11);  // hi - lo >> down is below kKeyBins
-      __syncthreads();
+      if (pass) sync_row();
       clear_bins(kKeyBins);
-      each([&](int, float v) {
-        const uint64_t place = place_of(v);
-        if (!place || bin_of(place) != bin) return;
+      each([&](float v) {
+        int y;
         const uint32_t k = key_of(v);
-        const uint64_t w = weight_of(place);
-        if (w && k >= lo && k <= hi) add((hi - k) >> down, w);
+        const uint64_t w = weight(v, &y);
+        if (w && bin_of(y) == bin && k >= lo && k <= hi) add((hi - k) >> down, w);
       });
       int at;
       const Tally t = find_bin(kKeyBins, by_count, want - all.count, target - all.mass, &at);
@@ -334,7 +344,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   Shared &S = *reinterpret_cast<Shared *>(smem);
   cg::cluster_group cluster = cg::this_cluster();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, row = blockIdx.x / P.blocks;
-  for (int i = tid; i < kPoints; i += kThreads) S.table[i] = (uint64_t)rint(exp2((double)i / kPoints) * (double)(1ull << kUnit));
+  for (int i = tid; i < kPoints; i += kThreads) S.table[i] = exp2((double)i / kPoints);
   pdl_begin();
   using Z = Sampler<DT>;
   Z z{S};
@@ -348,123 +358,295 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   const int top_k = P.a.by_row & 2 ? P.a.top_ks[row] : P.a.top_k;
   const float top_p = P.a.by_row & 4 ? P.a.top_ps[row] : P.a.top_p, min_p = P.a.by_row & 8 ? P.a.min_ps[row] : P.a.min_p;
 
-  // ---- the largest logit, the first of them ----
-  float best = -INFINITY;
-  int first = 0x7FFFFFFF;
-  z.each([&](int i, float v) {
-    if (v > best) best = v, first = i;
-  });
+  z.listed = false;
+  // ---- the largest logit ----
+  float own = -INFINITY;
+  z.each_of_row([&](int, float v) { own = fmaxf(own, v); });
+  float best = own;
 #pragma unroll
-  for (int d = 16; d; d >>= 1) {
-    const float v = __shfl_xor_sync(~0u, best, d);
-    const int i = __shfl_xor_sync(~0u, first, d);
-    if (v > best || (v == best && i < first)) best = v, first = i;
-  }
-  if (lane == 0) S.warp_max[warp] = best, S.warp_first[warp] = first;
+  for (int d = 16; d; d >>= 1) best = fmaxf(best, __shfl_xor_sync(~0u, best, d));
+  if (lane == 0) S.warp_max[warp] = best;
   __syncthreads();
-  auto better = [&](float v, int i) {
-    if (v > best || (v == best && i < first)) best = v, first = i;
-  };
-  for (int w = 0; w < kWarps; ++w) better(S.warp_max[w], S.warp_first[w]);
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) best = fmaxf(best, S.warp_max[w]);
   if (P.blocks > 1) {
-    if (tid == 0) S.block_max = best, S.block_first = first;
-    cluster.sync();
-    for (int b = 0; b < P.blocks; ++b) {
-      const Shared *o = cluster.map_shared_rank(&S, b);
-      better(o->block_max, o->block_first);
-    }
+    if (tid == 0) S.block_max = best;
+    z.sync_row();
+    for (int b = 0; b < P.blocks; ++b) best = fmaxf(best, z.block(b)->block_max);
   }
   if (!(temperature > 0.0f) || best == -INFINITY) {
+    int first = 0x7FFFFFFF;
+    z.each_of_row([&](int i, float v) {
+      if (v == best && i < first && i >= 0 && i < z.vocab) first = i;
+    });
+    first = __reduce_min_sync(~0u, first);
+    if (lane == 0) S.warp_first[warp] = first;
+    __syncthreads();
+    if (tid == 0) {
+      for (int w = 0; w < kWarps; ++w) first = min(first, S.warp_first[w]);
+      S.block_first = first;
+    }
+    z.sync_row();
     if (z.rank == 0 && tid == 0) {
+      for (int b = 0; b < P.blocks; ++b) first = min(first, z.block(b)->block_first);
       P.a.tokens[row] = best == -INFINITY ? -1 : first;
       if (P.a.logprobs) P.a.logprobs[row] = best == -INFINITY ? -INFINITY : 0.0f;
     }
-    if (P.blocks > 1) cluster.sync();  // nobody leaves while its shared memory is read
+    z.sync_row();  // nobody leaves while its shared memory is read
     return;
   }
-  z.top = best;
-  z.infinite = best == INFINITY;
-  z.by = 1.4426950408889634 / (double)temperature;
-  z.range = fminf(40.0f * temperature, FLT_MAX);  // 2^-57.7
+  // ---- weights ----
+  z.alone = best == INFINITY || best == -FLT_MAX;
+  z.largest = best;
+  const double t = fmin((double)temperature, 1e36);
+  z.top = z.alone ? 0.0f : best;
+  z.by = 1024 * 1.4426950408889634 / t;
+  z.least_value = fmaxf(__double2float_rd(z.top - (z.alone ? 1.0 : 40.0 * t)), -FLT_MAX);  // 2^-57.7
+  if (z.least_value >= (float)z.top) z.least_value = nextafterf((float)z.top, -INFINITY);
+  if (z.alone) z.by = 1024.0 * 100;
+  // where the next smaller float is further away than that, y stays within what `weight` can take
+  z.by = fmin(z.by, 1024.0 * 1000 / (z.top - z.least_value));
   z.least = min_p > 0.0f ? (uint64_t)ceil((double)fminf(min_p, 1.0f) * (double)(1ull << kUnit)) : 1;
 
   // ---- what is kept: tokens with a larger key than `last`, and the first `equal` of those that have it ----
   uint32_t last = 0, equal = ~0u;
   uint64_t last_weight = 0;
   const bool by_k = top_k > 0 && top_k < z.vocab, by_p = top_p < 1.0f;
-  if (by_k || by_p) {
-    z.clear_bins(kBins);
-    Tally all = {0, 0};
-    z.each([&](int, float v) {
-      const uint64_t place = z.place_of(v);
-      if (!place) return;
-      const uint64_t w = z.weight_of(place);
-      if (!w) return;
-      z.add(Z::bin_of(place), w);
-      all.mass += w, ++all.count;
-    });
+  int turn = 0;
+  auto total = [&](Tally all) {  // over the row's blocks
     all = z.block_sum(all);
     if (P.blocks > 1) {
-      if (tid == 0) S.block_mass = all.mass, S.block_count = all.count;
-      cluster.sync();
+      turn ^= 1;  // what is read here is not written to before the next barrier but one
+      if (tid == 0) S.block_tally[turn] = all;
+      z.sync_row();
       all = {0, 0};
-      for (int b = 0; b < P.blocks; ++b) {
-        const Shared *o = cluster.map_shared_rank(&S, b);
-        all.mass += o->block_mass, all.count += o->block_count;
+      for (int b = 0; b < P.blocks; ++b) all.mass += z.block(b)->block_tally[turn].mass, all.count += z.block(b)->block_tally[turn].count;
+    }
+    return all;
+  };
+  if (by_k || by_p || min_p > 0.0f) {
+    // a bound that is easily had
+    float bound = z.least_value;
+    if (min_p > 0.0f) bound = fmaxf(bound, __double2float_rd(z.top + 1024 * (log2((double)fminf(min_p, 1.0f)) - 1e-6) / z.by));
+    if (by_k && top_k <= P.blocks * kThreads) {
+      z.clear_bins(kBins);
+      int y;
+      const uint64_t w = z.weight(z.value(own), &y);
+      if (w) z.add(Z::bin_of(y), w);
+      if (total({w, w != 0}).count >= (uint32_t)top_k) {
+        int bin;
+        z.find_bin(kBins, true, top_k, 0, &bin);
+        bound = fmaxf(bound, z.value_of_bin(bin));
       }
-      cluster.sync();
+    } else if (!by_k && !(min_p > 0.0f)) {
+      Tally all = {0, 0};
+      z.each([&](float v) {
+        const uint64_t w = z.weight(v);
+        all.mass += w, all.count += w != 0;
+      });
+      all = total(all);
+      if (tid == 0) S.total = all.mass;
+      // a token that is kept last has no less than its share of what is to be left out: a thousandth less, for the roundings
+      const double weight = (1.0 - (double)fmaxf(top_p, 0.0f)) * (double)all.mass / all.count * 0.999 / (double)(1ull << kUnit);
+      bound = fmaxf(bound, __double2float_rd(z.top + 1024 * (log2(fmin(weight, 1.0)) - 1e-6) / z.by));
     }
-    uint64_t base = all.mass;  // what top_p is a part of
-    int bin_k = 0, bin_p = 0;
-    Tally k = {0, 0}, p = {0, 0};
-    const bool cut = by_k && (uint32_t)top_k < all.count;
-    // the bins' sums are needed for both bounds, before refining writes over them: top_p's bin is looked for among
-    // the sums that top_k leaves, which refining its bin gives; so the histogram is made anew in between
-    if (cut) {
-      k = z.find_bin(kBins, true, top_k, 0, &bin_k);
-      const Tally in = z.refine(bin_k, true, top_k - k.count, 0, &last);
-      last_weight = z.weight(of_key(last));
-      equal = top_k - k.count - in.count;
-      base = k.mass + in.mass + equal * last_weight;
+    // the tokens that reach it, in their order
+    int n = 0;
+    typename Z::Vector next = z.load(z.begin + lane, z.end);
+#pragma unroll 1
+    for (int j0 = z.begin; j0 < z.end; j0 += 32) {
+      const typename Z::Vector u = next;
+      next = z.load(j0 + 32 + lane, z.end);
+      float v[Z::VEC];
+      uint32_t mine = 0;
+#pragma unroll
+      for (int i = 0; i < Z::VEC; ++i) {
+        v[i] = z.value(Elem<DT>::to(u.e[i]));
+        mine |= (v[i] >= bound && v[i] > z.least_value ? 1u : 0u) << i;
+      }
+      if (!__any_sync(~0u, mine)) continue;
+      const int count = __popc(mine);
+      int at = count;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int o = __shfl_up_sync(~0u, at, d);
+        if (lane >= d) at += o;
+      }
+      const int all = __shfl_sync(~0u, at, 31);
+      at += n - count;
+#pragma unroll
+      for (int i = 0; i < Z::VEC; ++i) {
+        if (!(mine >> i & 1)) continue;
+        if (at < kListed) S.list_value[warp][at] = v[i], S.list_index[warp][at] = (j0 + lane) * Z::VEC - z.shift + i;
+        ++at;
+      }
+      n += all;
     }
-    if (by_p) {
-      const uint64_t target = max(share_up(fmaxf(top_p, 0.0f), base), (uint64_t)1);
-      if (cut) {
+    if (lane == 0) S.warp_listed[warp] = n;
+    __syncwarp();
+    z.sync_row();
+    // how many there are ahead of this warp's and in all, and whether every list has room
+    int ahead = 0, count = 0;
+    bool room = true;
+    for (int w = lane; w < warps; w += 32) {
+      const int c = z.block(w / kWarps)->warp_listed[w % kWarps];
+      room &= c <= kListed;
+      count += c;
+      ahead += w < z.rank * kWarps + warp ? c : 0;
+    }
+    room = __all_sync(~0u, room);
+    count = __reduce_add_sync(~0u, count);
+    ahead = __reduce_add_sync(~0u, ahead);
+    z.listed = room;
+    z.n_listed = n;
+
+    if (room && count <= kSorted) {
+      // ---- few: one block sorts them by key, largest first, then index ----
+      Shared *home = P.blocks > 1 ? cluster.map_shared_rank(&S, 0) : &S;
+      for (int i = lane; i < n; i += 32) home->order[ahead + i] = (uint64_t)key_of(S.list_value[warp][i]) << 32 | (0xFFFFFFFFu - S.list_index[warp][i]);
+      z.sync_row();
+      if (z.rank == 0) {
+        int size = 32;
+        while (size < count) size *= 2;
+        for (int i = count + tid; i < size; i += kThreads) S.order[i] = 0;
+        auto sort = [&]() {  // bitonic, descending
+          for (int run = 2; run <= size; run *= 2) {
+            for (int d = run / 2; d; d /= 2) {
+              __syncthreads();
+              for (int i = tid; i < size / 2; i += kThreads) {
+                const int lo = 2 * i - (i & (d - 1)), hi = lo + d;
+                const uint64_t x = S.order[lo], y = S.order[hi];
+                if ((x < y) == !(lo & run)) S.order[lo] = y, S.order[hi] = x;
+              }
+            }
+          }
+          __syncthreads();
+        };
+        // sums up to each: two to a thread
+        auto scan = [&](uint64_t (&w)[2]) {
+          uint64_t upto = w[0] + w[1];
+#pragma unroll
+          for (int d = 1; d < 32; d <<= 1) {
+            const uint64_t o = __shfl_up_sync(~0u, upto, d);
+            if (lane >= d) upto += o;
+          }
+          __syncthreads();
+          if (lane == 31) S.scan_mass[warp] = upto;
+          __syncthreads();
+          uint64_t all = 0;
+#pragma unroll
+          for (int v = 0; v < kWarps; ++v) {
+            if (v < warp) upto += S.scan_mass[v];
+            all += S.scan_mass[v];
+          }
+          w[0] = upto - w[1];
+          w[1] = upto;
+          return all;
+        };
+        sort();
+        const int most = by_k ? min(count, top_k) : count;
+        uint64_t w[2], upto[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) w[i] = upto[i] = 2 * tid + i < most ? z.weight(of_key((uint32_t)(S.order[2 * tid + i] >> 32))) : 0;
+        const uint64_t base = scan(upto);
+        // of the whole row's, where neither top_k nor min_p leave anything out: the first pass has it (top_p alone)
+        const uint64_t target = by_p ? max(share_up(fmaxf(top_p, 0.0f), by_k || min_p > 0.0f ? base : S.total), (uint64_t)1) : ~0ull;
+        if (tid == 0) S.kept = 0;
         __syncthreads();
-        z.clear_bins(kBins);
-        z.each([&](int, float v) {
-          const uint64_t place = z.place_of(v);
-          if (!place || key_of(v) < last) return;
-          const uint64_t w = z.weight_of(place);
-          if (w) z.add(Z::bin_of(place), w);
-        });
+        int kept = 0;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) kept += w[i] != 0 && upto[i] - w[i] < target;
+        kept = __reduce_add_sync(~0u, kept);
+        if (lane == 0) atomicAdd(&S.kept, kept);
+        __syncthreads();
+        kept = S.kept;
+        // the kept ones, by index (largest first: the sums are taken from the other end)
+        const int size_before = size;
+        size = 32;
+        while (size < kept) size *= 2;
+        for (int i = tid; i < size_before; i += kThreads) {
+          const uint64_t k = S.order[i];
+          if (i < size) S.order[i] = i < kept ? k << 32 | k >> 32 : 0;
+        }
+        sort();
+#pragma unroll
+        for (int i = 0; i < 2; ++i) w[i] = upto[i] = 2 * tid + i < kept ? z.weight(of_key((uint32_t)S.order[2 * tid + i])) : 0;
+        const uint64_t all = scan(upto);
+        const float u = P.a.uniform[row];
+        const uint64_t draw = share_of(u > 0.0f ? fminf(u, 0x1.fffffep-1f) : 0.0f, all);
+        // S.order has ~index in its upper half, largest first, so the lowest index comes first
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          if (w[i] && draw >= upto[i] - w[i] && draw < upto[i]) {
+            P.a.tokens[row] = (int32_t)(0xFFFFFFFFu - (uint32_t)(S.order[2 * tid + i] >> 32));
+            if (P.a.logprobs) P.a.logprobs[row] = (float)log((double)w[i] / (double)all);
+          }
+        }
       }
-      p = z.find_bin(kBins, false, 0, target, &bin_p);
-      const Tally in = z.refine(bin_p, false, 0, target - p.mass, &last);
-      last_weight = z.weight(of_key(last));
-      const uint64_t left = target - p.mass - in.mass;
-      equal = (uint32_t)((left + last_weight - 1) / last_weight);
+      z.sync_row();  // nobody leaves while its shared memory is read
+      return;
+    }
+
+    // ---- many: histograms ----
+    if (by_k || by_p) {
+      z.clear_bins(kBins);  // the lists' barrier lies behind what looked into them last
+      Tally all = {0, 0};
+      auto tally = [&](uint32_t from) {
+        z.each([&](float v) {
+          int y;
+          const uint64_t w = z.weight(v, &y);
+          if (!w || key_of(v) < from) return;
+          z.add(Z::bin_of(y), w);
+          all.mass += w, ++all.count;
+        });
+      };
+      tally(0);
+      all = total(all);
+      uint64_t base = by_k || min_p > 0.0f ? all.mass : S.total;  // what top_p is a part of
+      int bin;
+      const bool cut = by_k && (uint32_t)top_k < all.count;
+      if (cut) {
+        const Tally k = z.find_bin(kBins, true, top_k, 0, &bin);
+        const Tally in = z.refine(bin, true, top_k - k.count, 0, &last);
+        last_weight = z.weight(of_key(last));
+        equal = top_k - k.count - in.count;
+        base = k.mass + in.mass + equal * last_weight;
+      }
+      if (by_p) {
+        const uint64_t target = max(share_up(fmaxf(top_p, 0.0f), base), (uint64_t)1);
+        if (cut) {  // refining has written over the histogram
+          z.sync_row();
+          z.clear_bins(kBins);
+          tally(last);
+        }
+        const Tally p = z.find_bin(kBins, false, 0, target, &bin);
+        const Tally in = z.refine(bin, false, 0, target - p.mass, &last);
+        last_weight = z.weight(of_key(last));
+        equal = (uint32_t)((target - p.mass - in.mass + last_weight - 1) / max(last_weight, (uint64_t)1));
+      }
     }
   }
 
   // ---- the draw ----
   uint64_t mass = 0;
   uint32_t same = 0;
-  z.each([&](int, float v) {
-    const uint64_t place = z.place_of(v);
-    if (!place) return;
+  auto weigh = [&](float v) {
+    const uint64_t w = z.weight(v);
     const uint32_t k = key_of(v);
-    if (k > last) mass += z.weight_of(place);
-    else same += k == last;
-  });
+    mass += k > last ? w : 0;
+    same += k == last;
+  };
+  auto over_warp = [&]() {
 #pragma unroll
-  for (int d = 16; d; d >>= 1) mass += __shfl_xor_sync(~0u, mass, d);
-  same = __reduce_add_sync(~0u, same);
+    for (int d = 16; d; d >>= 1) mass += __shfl_xor_sync(~0u, mass, d);
+    same = __reduce_add_sync(~0u, same);
+  };
+  z.each(weigh);
+  over_warp();
   if (lane == 0) S.warp_mass[warp] = mass, S.warp_equal[warp] = same;
-  if (P.blocks > 1) cluster.sync();
-  else __syncthreads();
+  z.sync_row();
   if (tid < warps) {
-    const Shared *o = P.blocks > 1 ? cluster.map_shared_rank(&S, tid / kWarps) : &S;
+    const Shared *o = z.block(tid / kWarps);
     S.all_mass[tid] = o->warp_mass[tid % kWarps], S.all_equal[tid] = o->warp_equal[tid % kWarps];
   }
   __syncthreads();
@@ -514,62 +696,93 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     if (lane == 0) S.all_mass[0] = all;
   }
   __syncthreads();
-  if (S.pick_warp / kWarps == z.rank && S.pick_warp % kWarps == warp) {
-    const uint64_t target = S.pick_before, all = S.all_mass[0];
-    uint64_t before = 0;
+  if (S.pick_warp / kWarps == z.rank) {
+    // the run of that warp, a part of it to each warp; a list is short enough for one
+    uint64_t target = S.pick_before, before = 0;
+    const uint64_t all = S.all_mass[0];
     uint32_t seen = S.pick_equal;
-    for (int j0 = z.begin; j0 < z.end; j0 += 32) {
-      float v[Z::VEC];
-      z.load(j0 + lane, v);
-      uint32_t equals = 0;
-#pragma unroll
-      for (int i = 0; i < Z::VEC; ++i) equals += z.place_of(v[i]) && key_of(v[i]) == last;
-      uint32_t rank = equals;
-#pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const uint32_t t = __shfl_up_sync(~0u, rank, d);
-        if (lane >= d) rank += t;
+    int from = 0, until = 0, chosen = S.pick_warp % kWarps;
+    if (!z.listed) {
+      const int run = min(vectors, S.pick_warp * per), end = min(vectors, run + per), part = (per / 32 + kWarps - 1) / kWarps * 32;
+      mass = 0, same = 0;
+      z.each_between(min(end, run + warp * part), min(end, run + (warp + 1) * part), [&](int, float v) { weigh(z.value(v)); });
+      over_warp();
+      if (lane == 0) S.scan_mass[warp] = mass, S.scan_count[warp] = same;
+      __syncthreads();
+      for (chosen = 0; chosen + 1 < kWarps; ++chosen) {
+        const uint64_t m = S.scan_mass[chosen] + last_weight * (uint64_t)min(S.scan_count[chosen], equal - min(equal, seen));
+        if (target < before + m) break;
+        before += m;
+        seen += S.scan_count[chosen];
       }
-      const uint32_t row_equals = __shfl_sync(~0u, rank, 31);
-      rank += seen - equals;
-      uint64_t w[Z::VEC], sum = 0;
+      from = min(end, run + chosen * part), until = min(end, run + (chosen + 1) * part);
+    }
+    if (warp == chosen) {
+    // N tokens of each lane, in order: those of a vector, or one of the list
+    auto go = [&](auto width, int from, int to, auto get, auto index) {
+      constexpr int N = decltype(width)::value;
+      for (int j0 = from; j0 < to; j0 += 32) {
+        float v[N];
+        get(j0 + lane, v);
+        uint32_t equals = 0;
 #pragma unroll
-      for (int i = 0; i < Z::VEC; ++i) {
-        w[i] = 0;
-        if (z.place_of(v[i])) {
+        for (int i = 0; i < N; ++i) equals += key_of(v[i]) == last;
+        uint32_t rank = equals;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+          const uint32_t o = __shfl_up_sync(~0u, rank, d);
+          if (lane >= d) rank += o;
+        }
+        const uint32_t row_equals = __shfl_sync(~0u, rank, 31);
+        rank += seen - equals;
+        uint64_t w[N], sum = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
           const uint32_t k = key_of(v[i]);
-          if (k > last) w[i] = z.weight(v[i]);
-          else if (k == last && rank++ < equal) w[i] = last_weight;
+          w[i] = k > last ? z.weight(v[i]) : k == last && rank++ < equal ? last_weight : 0;
+          sum += w[i];
         }
-        sum += w[i];
-      }
-      uint64_t upto = sum;
+        uint64_t upto = sum;
 #pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const uint64_t t = __shfl_up_sync(~0u, upto, d);
-        if (lane >= d) upto += t;
-      }
-      const uint64_t step = __shfl_sync(~0u, upto, 31);
-      upto += before;
-      if (target < before + step) {
-        if (target < upto && target >= upto - sum) {
-          uint64_t at = upto - sum;
+        for (int d = 1; d < 32; d <<= 1) {
+          const uint64_t o = __shfl_up_sync(~0u, upto, d);
+          if (lane >= d) upto += o;
+        }
+        const uint64_t step = __shfl_sync(~0u, upto, 31);
+        upto += before;
+        if (target < before + step) {
+          if (target < upto && target >= upto - sum) {
+            uint64_t at = upto - sum;
 #pragma unroll
-          for (int i = 0; i < Z::VEC; ++i) {
-            if (target >= at && target < at + w[i]) {
-              P.a.tokens[row] = (j0 + lane) * Z::VEC - z.shift + i;
-              if (P.a.logprobs) P.a.logprobs[row] = (float)log((double)w[i] / (double)all);
+            for (int i = 0; i < N; ++i) {
+              if (target >= at && target < at + w[i]) {
+                P.a.tokens[row] = index(j0 + lane, i);
+                if (P.a.logprobs) P.a.logprobs[row] = (float)log((double)w[i] / (double)all);
+              }
+              at += w[i];
             }
-            at += w[i];
           }
+          return;
         }
-        break;
+        before += step;
+        seen += row_equals;
       }
-      before += step;
-      seen += row_equals;
+    };
+    if (z.listed) {
+      go(std::integral_constant<int, 1>(), 0, z.n_listed, [&](int j, float (&v)[1]) { v[0] = j < z.n_listed ? S.list_value[warp][j] : z.least_value; },
+         [&](int j, int) { return S.list_index[warp][j]; });
+    } else {
+      go(std::integral_constant<int, Z::VEC>(), from, until,
+         [&](int j, float (&v)[Z::VEC]) {
+           const typename Z::Vector u = z.load(j, until);
+#pragma unroll
+           for (int i = 0; i < Z::VEC; ++i) v[i] = z.value(Elem<DT>::to(u.e[i]));
+         },
+         [&](int j, int i) { return j * Z::VEC - z.shift + i; });
+    }
     }
   }
-  if (P.blocks > 1) cluster.sync();  // nobody leaves while its shared memory is read
+  z.sync_row();  // nobody leaves while its shared memory is read
 }
 
 template <int DT>
@@ -608,7 +821,7 @@ extern "C" int amap_sample(const amap_sample_args *a, void *cuda_stream) {
   // blocks of a row: as many as fill the device twice over, but none with less than two vectors of 16 bytes a thread
   const int64_t vectors = (int64_t)a->vocab * dtype_bytes(a->dtype) / 16;
   P.blocks = 1;
-  while (P.blocks < kMostBlocks && (int64_t)a->rows * P.blocks * 2 <= 2 * device_sms() && vectors >= P.blocks * 4 * kThreads) P.blocks *= 2;
+  while (P.blocks < kMostBlocks && (int64_t)a->rows * P.blocks * 2 <= 2 * device_sms() && vectors >= P.blocks * 2 * kThreads) P.blocks *= 2;
   switch (a->dtype) {
     case AMAP_BF16: return run<AMAP_BF16>(P, cuda_stream);
     case AMAP_FP16: return run<AMAP_FP16>(P, cuda_stream);
