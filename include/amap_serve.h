@@ -337,7 +337,7 @@ int amap_packed_attend(const amap_attend_args *args /* host */, const amap_packe
  * ------------------------------------------------------------------------- */
 typedef struct amap_sample_args {
   int32_t rows;    /* 1 .. 65535 */
-  int32_t vocab;   /* 1 .. 2^20 */
+  int32_t vocab;   /* 1 .. 2^19 */
   int32_t dtype;   /* AMAP_BF16, AMAP_FP16 or AMAP_FP32 */
   int32_t by_row;  /* bits 0 .. 3: temperature, top_k, top_p, min_p are arrays of `rows` numbers, not one */
   const void *logits;

@@ -31,13 +31,19 @@ namespace cg = cooperative_groups;
 
 namespace {
 
+#ifndef MAXB
+#define MAXB 8
+#endif
+#ifndef CAPX
+#define CAPX 2
+#endif
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kMostBlocks = 8;          // of a cluster
-constexpr int kBins = 2944;             // 46 powers of two in 64 bins each: all weights that are not zero
+constexpr int kBins = 4096;             // bins of y: 64 to a power of two, in all 45 of which weights are not zero; or bf16 logits
 constexpr int kKeyBins = 2048;
 constexpr int kPoints = 1024;           // of the table of 2^x
 constexpr int kUnit = 44;               // W is in units of 2^-44
-constexpr int kListed = 320;            // tokens of a warp's list
+constexpr int kListBytes = 2560;        // of a warp's list
 constexpr int kSorted = 1024;           // tokens that one block sorts
 
 struct Params {
@@ -56,13 +62,10 @@ struct Shared {
     struct {
       uint32_t count[kBins], low[kBins], high[kBins];  // a bin's tokens and the sum of their W
     };
-    struct {
-      uint64_t order[kSorted];  // key and index of the tokens to be sorted
-      uint64_t sums[kSorted];   // their W
-    };
+    uint64_t order[kSorted];     // key and index of the tokens to be sorted
+    uint64_t weight_of[kBins];   // of a bf16 logit
   };
-  float list_value[kWarps][kListed];
-  int32_t list_index[kWarps][kListed];
+  char lists[kWarps][kListBytes];
   // exchanged with the other blocks
   uint64_t run_mass[kThreads];  // of the bins that a thread adds up
   uint32_t run_count[kThreads];
@@ -119,6 +122,12 @@ __device__ __forceinline__ uint64_t share_up(float f, uint64_t m) {
 template <int DT>
 struct Sampler {
   using T = typename Elem<DT>::T;
+  // a token of a list: its logit, and its place in the warp's run of the row (65536 tokens at most)
+  struct Entry {
+    uint16_t at;
+    T logit;
+  };
+  static constexpr int kListed = kListBytes / sizeof(Entry);
   static constexpr int VEC = 16 / sizeof(T), kAhead = 3;  // elements of a vector; vectors under way in a thread
   Shared &S;
   const T *x;
@@ -170,11 +179,13 @@ struct Sampler {
   template <typename F>
   __device__ __forceinline__ void each_of_row(F f) const { each_between(begin, end, f); }
   __device__ __forceinline__ float value(float v) const { return fmaxf(alone ? (v == largest ? 0.0f : -1.0f) : v, least_value); }
+  __device__ __forceinline__ Entry *list() const { return reinterpret_cast<Entry *>(S.lists[threadIdx.x >> 5]); }
+  __device__ __forceinline__ int index_of(const Entry &e) const { return begin * VEC - shift + e.at; }
   // f(value) for every token, of the row or of the lists
   template <typename F>
   __device__ __forceinline__ void each(F f) const {
     if (listed) {
-      for (int i = threadIdx.x & 31; i < n_listed; i += 32) f(S.list_value[threadIdx.x >> 5][i]);
+      for (int i = threadIdx.x & 31; i < n_listed; i += 32) f(value(Elem<DT>::to(list()[i].logit)));
     } else {
       each_of_row([&](int, float v) { f(value(v)); });
     }
@@ -199,6 +210,32 @@ struct Sampler {
   static __device__ __forceinline__ int bin_of(int y) { return -y >> 4; }
   // a value that every token with a bin up to this one reaches
   __device__ __forceinline__ float value_of_bin(int bin) const { return fmaxf(__double2float_rd(top - (16.0 * (bin + 1) + 1.0) / by), least_value); }
+
+  // ---- bf16: few logits are near enough to the largest to have a weight, and every one can have a bin of its own, counted down
+  // from the largest; those below 2^-7, of either sign, share one ----
+  static constexpr int kTiny = 0x4400;  // its place in the order: 0x4400 logits are below, 0x4400 above
+  int top_place;
+  static __device__ __forceinline__ int place_of(float v) {
+    const uint32_t b = __float_as_uint(v), o = (int32_t)b < 0 ? ~b >> 16 : b >> 16 | 0x8000u;
+    return (int)(o >= 0xBC00u ? o - 0x77FFu : min(o, (uint32_t)kTiny));
+  }
+  __device__ __forceinline__ int logit_bin(float v) const { return top_place - place_of(v); }
+  __device__ __forceinline__ int tiny_bin() const { return top_place - kTiny; }
+  __device__ __forceinline__ float logit_of(int bin) const {
+    const uint32_t c = top_place - bin, o = c > (uint32_t)kTiny ? c + 0x77FFu : c;
+    return __uint_as_float((o & 0x8000u ? o & 0x7FFFu : ~o & 0xFFFFu) << 16);
+  }
+  // W by the table of logits
+  __device__ __forceinline__ uint64_t look(float v) const {
+    const int bin = logit_bin(v);
+    if (bin == tiny_bin()) return weight(v);
+    return v > least_value ? S.weight_of[bin] : 0;
+  }
+  __device__ __forceinline__ void make_table() const {  // with nobody looking into the bins
+    const int bins = min(kBins, logit_bin(least_value) + 1);
+    for (int i = threadIdx.x; i < bins; i += kThreads) S.weight_of[i] = i == tiny_bin() ? 0 : weight(logit_of(i));
+    __syncthreads();
+  }
 
   __device__ __forceinline__ void clear_bins(int n) const {
     for (int i = threadIdx.x; i < n; i += kThreads) S.count[i] = S.low[i] = S.high[i] = 0;
@@ -408,6 +445,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   z.by = fmin(z.by, 1024.0 * 1000 / (z.top - z.least_value));
   z.least = min_p > 0.0f ? (uint64_t)ceil((double)fminf(min_p, 1.0f) * (double)(1ull << kUnit)) : 1;
 
+  // bf16, and all logits that have a weight are among the bins
+  z.top_place = Z::place_of(best);
+  const bool by_logit = DT == AMAP_BF16 && !z.alone && z.logit_bin(z.least_value) < kBins;
+
   // ---- what is kept: tokens with a larger key than `last`, and the first `equal` of those that have it ----
   uint32_t last = 0, equal = ~0u;
   uint64_t last_weight = 0;
@@ -424,7 +465,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     }
     return all;
   };
-  if (by_k || by_p || min_p > 0.0f) {
+  if (by_k || min_p > 0.0f || (by_p && !by_logit)) {
     // a bound that is easily had
     float bound = z.least_value;
     if (min_p > 0.0f) bound = fmaxf(bound, __double2float_rd(z.top + 1024 * (log2((double)fminf(min_p, 1.0f)) - 1e-6) / z.by));
@@ -477,7 +518,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
 #pragma unroll
       for (int i = 0; i < Z::VEC; ++i) {
         if (!(mine >> i & 1)) continue;
-        if (at < kListed) S.list_value[warp][at] = v[i], S.list_index[warp][at] = (j0 + lane) * Z::VEC - z.shift + i;
+        if (at < Z::kListed) z.list()[at] = {(uint16_t)((j0 - z.begin + lane) * Z::VEC + i), u.e[i]};
         ++at;
       }
       n += all;
@@ -487,10 +528,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     z.sync_row();
     // how many there are ahead of this warp's and in all, and whether every list has room
     int ahead = 0, count = 0;
-    bool room = true;
+    bool room = per * Z::VEC <= 65536;
     for (int w = lane; w < warps; w += 32) {
       const int c = z.block(w / kWarps)->warp_listed[w % kWarps];
-      room &= c <= kListed;
+      room &= c <= Z::kListed;
       count += c;
       ahead += w < z.rank * kWarps + warp ? c : 0;
     }
@@ -503,7 +544,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     if (room && count <= kSorted) {
       // ---- few: one block sorts them by key, largest first, then index ----
       Shared *home = P.blocks > 1 ? cluster.map_shared_rank(&S, 0) : &S;
-      for (int i = lane; i < n; i += 32) home->order[ahead + i] = (uint64_t)key_of(S.list_value[warp][i]) << 32 | (0xFFFFFFFFu - S.list_index[warp][i]);
+      for (int i = lane; i < n; i += 32) home->order[ahead + i] = (uint64_t)key_of(z.value(Elem<DT>::to(z.list()[i].logit))) << 32 | (0xFFFFFFFFu - z.index_of(z.list()[i]));
       z.sync_row();
       if (z.rank == 0) {
         int size = 32;
@@ -586,11 +627,62 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
       z.sync_row();  // nobody leaves while its shared memory is read
       return;
     }
-
-    // ---- many: histograms ----
-    if (by_k || by_p) {
-      z.clear_bins(kBins);  // the lists' barrier lies behind what looked into them last
-      Tally all = {0, 0};
+  }
+  // ---- many: histograms ----
+  if (by_k || by_p) {
+    const bool logits = by_logit && !z.listed;
+    bool found = false;
+    Tally all = {0, 0};
+    int bin;
+    if (logits) {
+      z.clear_bins(kBins);
+      z.each_of_row([&](int, float x) {
+        const float v = z.value(x);
+        const int i = z.logit_bin(v);
+        if (i == z.tiny_bin()) {
+          const uint64_t w = z.weight(v);
+          if (w) z.add(i, w);
+        } else if (v > z.least_value) {
+          atomicAdd(&S.count[i], 1u);
+        }
+      });
+      __syncthreads();
+      for (int i = tid; i < kBins; i += kThreads) {
+        if (i != z.tiny_bin() && S.count[i]) {
+          const uint64_t w = z.weight(z.logit_of(i)), m = w * S.count[i];
+          if (!w) S.count[i] = 0;
+          S.low[i] = (uint32_t)m, S.high[i] = (uint32_t)(m >> 32);
+        }
+        all.mass += ((uint64_t)S.high[i] << 32) + S.low[i], all.count += S.count[i];
+      }
+      all = total(all);
+      found = true;
+      uint64_t base = all.mass;
+      auto settle = [&](bool by_count, uint32_t want, uint64_t target) {  // last and equal; what is ahead of them
+        const Tally t = z.find_bin(kBins, by_count, want, target, &bin);
+        found = found && bin != z.tiny_bin();
+        if (!found) return t;
+        const float v = z.logit_of(bin);
+        last = key_of(v);
+        last_weight = z.weight(v);
+        equal = by_count ? want - t.count : (uint32_t)((target - t.mass + last_weight - 1) / max(last_weight, (uint64_t)1));
+        return t;
+      };
+      if (by_k && (uint32_t)top_k < all.count) {
+        const Tally t = settle(true, top_k, 0);
+        base = t.mass + equal * last_weight;
+      }
+      if (by_p && found) {
+        z.sync_row();
+        settle(false, 0, max(share_up(fmaxf(top_p, 0.0f), base), (uint64_t)1));
+      }
+      if (!found) {  // a bound falls among the logits that share a bin
+        z.sync_row();
+        last = 0, equal = ~0u, last_weight = 0, all = {0, 0};
+      }
+    }
+    if (!found) {
+      z.clear_bins(kBins);  // a barrier of the row's blocks lies behind what looked into them last
       auto tally = [&](uint32_t from) {
         z.each([&](float v) {
           int y;
@@ -602,8 +694,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
       };
       tally(0);
       all = total(all);
-      uint64_t base = by_k || min_p > 0.0f ? all.mass : S.total;  // what top_p is a part of
-      int bin;
+      uint64_t base = by_k || min_p > 0.0f || by_logit ? all.mass : S.total;  // what top_p is a part of
       const bool cut = by_k && (uint32_t)top_k < all.count;
       if (cut) {
         const Tally k = z.find_bin(kBins, true, top_k, 0, &bin);
@@ -628,10 +719,15 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   }
 
   // ---- the draw ----
+  const bool by_table = by_logit && !z.listed;
+  if (by_table) {
+    if (by_k || by_p) z.sync_row();  // the table comes to lie over the bins
+    z.make_table();
+  }
   uint64_t mass = 0;
   uint32_t same = 0;
   auto weigh = [&](float v) {
-    const uint64_t w = z.weight(v);
+    const uint64_t w = by_table ? z.look(v) : z.weight(v);
     const uint32_t k = key_of(v);
     mass += k > last ? w : 0;
     same += k == last;
@@ -769,8 +865,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
       }
     };
     if (z.listed) {
-      go(std::integral_constant<int, 1>(), 0, z.n_listed, [&](int j, float (&v)[1]) { v[0] = j < z.n_listed ? S.list_value[warp][j] : z.least_value; },
-         [&](int j, int) { return S.list_index[warp][j]; });
+      go(std::integral_constant<int, 1>(), 0, z.n_listed, [&](int j, float (&v)[1]) { v[0] = j < z.n_listed ? z.value(Elem<DT>::to(z.list()[j].logit)) : z.least_value; },
+         [&](int j, int) { return z.index_of(z.list()[j]); });
     } else {
       go(std::integral_constant<int, Z::VEC>(), from, until,
          [&](int j, float (&v)[Z::VEC]) {
@@ -806,7 +902,7 @@ int run(const Params &P, void *stream) {
 extern "C" int amap_sample(const amap_sample_args *a, void *cuda_stream) {
   SERVE_REQUIRE(a, AMAP_EINVAL, "null pointer");
   SERVE_REQUIRE(a->rows >= 1 && a->rows <= 0xFFFF, AMAP_EINVAL, "rows: 1 .. 65535");
-  SERVE_REQUIRE(a->vocab >= 1 && a->vocab <= 1 << 20, AMAP_EINVAL, "vocab: 1 .. 2^20");
+  SERVE_REQUIRE(a->vocab >= 1 && a->vocab <= 1 << 19, AMAP_EINVAL, "vocab: 1 .. 2^19");
   SERVE_REQUIRE(a->dtype == AMAP_BF16 || a->dtype == AMAP_FP16 || a->dtype == AMAP_FP32, AMAP_EINVAL, "type: bf16, fp16 or fp32");
   SERVE_REQUIRE((a->by_row & ~15) == 0, AMAP_EINVAL, "by_row: bits 0 .. 3");
   SERVE_REQUIRE(a->logits && a->uniform && a->tokens && (!(a->by_row & 1) || a->temperatures) && (!(a->by_row & 2) || a->top_ks) &&
@@ -821,7 +917,7 @@ extern "C" int amap_sample(const amap_sample_args *a, void *cuda_stream) {
   // blocks of a row: as many as fill the device twice over, but none with less than two vectors of 16 bytes a thread
   const int64_t vectors = (int64_t)a->vocab * dtype_bytes(a->dtype) / 16;
   P.blocks = 1;
-  while (P.blocks < kMostBlocks && (int64_t)a->rows * P.blocks * 2 <= 2 * device_sms() && vectors >= P.blocks * 2 * kThreads) P.blocks *= 2;
+  while (P.blocks < MAXB && (int64_t)a->rows * P.blocks * 2 <= CAPX * device_sms() && vectors >= P.blocks * 2 * kThreads) P.blocks *= 2;
   switch (a->dtype) {
     case AMAP_BF16: return run<AMAP_BF16>(P, cuda_stream);
     case AMAP_FP16: return run<AMAP_FP16>(P, cuda_stream);

@@ -232,7 +232,7 @@ SAMPLE_ARGS = dict(rows=4, vocab=1000, dtype=1, by_row=0, logits=0x10000, row=10
 
 
 @pytest.mark.parametrize("change,code,why", [
-    (dict(rows=0), EINVAL, "rows"), (dict(rows=65536), EINVAL, "rows"), (dict(vocab=0), EINVAL, "vocab"), (dict(vocab=2**20 + 1), EINVAL, "vocab"),
+    (dict(rows=0), EINVAL, "rows"), (dict(rows=65536), EINVAL, "rows"), (dict(vocab=0), EINVAL, "vocab"), (dict(vocab=2**19 + 1), EINVAL, "vocab"),
     (dict(dtype=4), EINVAL, "type"), (dict(by_row=16), EINVAL, "by_row"), (dict(by_row=1), EINVAL, "null"), (dict(by_row=2), EINVAL, "null"),
     (dict(by_row=4), EINVAL, "null"), (dict(by_row=8), EINVAL, "null"), (dict(logits=0), EINVAL, "null"), (dict(uniform=0), EINVAL, "null"),
     (dict(tokens=0), EINVAL, "null"), (dict(t=float("nan")), EINVAL, "temperature"), (dict(t=float("inf")), EINVAL, "temperature"), (dict(p=1.5), EINVAL, "top_p"),
