@@ -31,12 +31,6 @@ namespace cg = cooperative_groups;
 
 namespace {
 
-#ifndef MAXB
-#define MAXB 8
-#endif
-#ifndef CAPX
-#define CAPX 2
-#endif
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kMostBlocks = 8;          // of a cluster
 constexpr int kBins = 4096;             // bins of y: 64 to a power of two, in all 45 of which weights are not zero; or bf16 logits
@@ -159,9 +153,9 @@ struct Sampler {
     }
     return u;
   }
-  // f(index, logit) for every element of this lane's vectors among those from `from` to `until`; NaN for those that are none
+  // f(index of the first, logits) for this lane's vectors among those from `from` to `until`; NaN for what is no element of the row
   template <typename F>
-  __device__ __forceinline__ void each_between(int from, int until, F f) const {
+  __device__ __forceinline__ void each_vector(int from, int until, F f) const {
     int j = from + (threadIdx.x & 31);
     Vector ahead[kAhead];
 #pragma unroll
@@ -172,9 +166,19 @@ struct Sampler {
 #pragma unroll
       for (int k = 0; k + 1 < kAhead; ++k) ahead[k] = ahead[k + 1];
       ahead[kAhead - 1] = load(j + 32 * kAhead, until);
+      float v[VEC];
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) f(j * VEC - shift + i, Elem<DT>::to(u.e[i]));
+      for (int i = 0; i < VEC; ++i) v[i] = Elem<DT>::to(u.e[i]);
+      f(j * VEC - shift, v);
     }
+  }
+  // f(index, logit) for each element
+  template <typename F>
+  __device__ __forceinline__ void each_between(int from, int until, F f) const {
+    each_vector(from, until, [&](int first, const float (&v)[VEC]) {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) f(first + i, v[i]);
+    });
   }
   template <typename F>
   __device__ __forceinline__ void each_of_row(F f) const { each_between(begin, end, f); }
@@ -225,15 +229,9 @@ struct Sampler {
     const uint32_t c = top_place - bin, o = c > (uint32_t)kTiny ? c + 0x77FFu : c;
     return __uint_as_float((o & 0x8000u ? o & 0x7FFFu : ~o & 0xFFFFu) << 16);
   }
-  // W by the table of logits
-  __device__ __forceinline__ uint64_t look(float v) const {
-    const int bin = logit_bin(v);
-    if (bin == tiny_bin()) return weight(v);
-    return v > least_value ? S.weight_of[bin] : 0;
-  }
   __device__ __forceinline__ void make_table() const {  // with nobody looking into the bins
     const int bins = min(kBins, logit_bin(least_value) + 1);
-    for (int i = threadIdx.x; i < bins; i += kThreads) S.weight_of[i] = i == tiny_bin() ? 0 : weight(logit_of(i));
+    for (int i = threadIdx.x; i < bins; i += kThreads) S.weight_of[i] = i == tiny_bin() ? 0 : weight(value(logit_of(i)));
     __syncthreads();
   }
 
@@ -636,20 +634,28 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     int bin;
     if (logits) {
       z.clear_bins(kBins);
-      z.each_of_row([&](int, float x) {
-        const float v = z.value(x);
-        const int i = z.logit_bin(v);
-        if (i == z.tiny_bin()) {
-          const uint64_t w = z.weight(v);
-          if (w) z.add(i, w);
-        } else if (v > z.least_value) {
-          atomicAdd(&S.count[i], 1u);
+      z.each_vector(z.begin, z.end, [&](int, const float (&x)[Z::VEC]) {
+        uint32_t tiny = 0;
+#pragma unroll
+        for (int i = 0; i < Z::VEC; ++i) {
+          const float v = z.value(x[i]);
+          const int at = z.logit_bin(v);
+          const bool own = at != z.tiny_bin();
+          if (v > z.least_value && own) atomicAdd(&S.count[at], 1u);
+          tiny |= own ? 0u : 1u << i;
+        }
+        if (tiny) {
+#pragma unroll
+          for (int i = 0; i < Z::VEC; ++i) {
+            const uint64_t w = tiny >> i & 1 ? z.weight(z.value(x[i])) : 0;
+            if (w) z.add(z.tiny_bin(), w);
+          }
         }
       });
       __syncthreads();
       for (int i = tid; i < kBins; i += kThreads) {
-        if (i != z.tiny_bin() && S.count[i]) {
-          const uint64_t w = z.weight(z.logit_of(i)), m = w * S.count[i];
+        const uint64_t w = z.weight(z.value(z.logit_of(i))), m = w * S.count[i];
+        if (i != z.tiny_bin()) {
           if (!w) S.count[i] = 0;
           S.low[i] = (uint32_t)m, S.high[i] = (uint32_t)(m >> 32);
         }
@@ -726,18 +732,42 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   }
   uint64_t mass = 0;
   uint32_t same = 0;
+  const float last_value = last ? of_key(last) : -INFINITY;
   auto weigh = [&](float v) {
-    const uint64_t w = by_table ? z.look(v) : z.weight(v);
-    const uint32_t k = key_of(v);
-    mass += k > last ? w : 0;
-    same += k == last;
+    const uint64_t w = z.weight(v);
+    mass += v > last_value ? w : 0;
+    same += v == last_value;
+  };
+  auto weigh_vectors = [&](int from, int until) {
+    z.each_vector(from, until, [&](int, const float (&x)[Z::VEC]) {
+      if (!by_table) {
+#pragma unroll
+        for (int i = 0; i < Z::VEC; ++i) weigh(z.value(x[i]));
+        return;
+      }
+      uint32_t tiny = 0;
+#pragma unroll
+      for (int i = 0; i < Z::VEC; ++i) {
+        const float v = z.value(x[i]);
+        const int at = z.logit_bin(v);
+        const bool own = at != z.tiny_bin();
+        if (v > last_value && own) mass += S.weight_of[at];
+        same += v == last_value;
+        tiny |= own || !(v > last_value) ? 0u : 1u << i;
+      }
+      if (tiny) {
+#pragma unroll
+        for (int i = 0; i < Z::VEC; ++i) mass += tiny >> i & 1 ? z.weight(z.value(x[i])) : 0;
+      }
+    });
   };
   auto over_warp = [&]() {
 #pragma unroll
     for (int d = 16; d; d >>= 1) mass += __shfl_xor_sync(~0u, mass, d);
     same = __reduce_add_sync(~0u, same);
   };
-  z.each(weigh);
+  if (z.listed) z.each(weigh);
+  else weigh_vectors(z.begin, z.end);
   over_warp();
   if (lane == 0) S.warp_mass[warp] = mass, S.warp_equal[warp] = same;
   z.sync_row();
@@ -801,7 +831,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     if (!z.listed) {
       const int run = min(vectors, S.pick_warp * per), end = min(vectors, run + per), part = (per / 32 + kWarps - 1) / kWarps * 32;
       mass = 0, same = 0;
-      z.each_between(min(end, run + warp * part), min(end, run + (warp + 1) * part), [&](int, float v) { weigh(z.value(v)); });
+      weigh_vectors(min(end, run + warp * part), min(end, run + (warp + 1) * part));
       over_warp();
       if (lane == 0) S.scan_mass[warp] = mass, S.scan_count[warp] = same;
       __syncthreads();
@@ -914,10 +944,13 @@ extern "C" int amap_sample(const amap_sample_args *a, void *cuda_stream) {
                     aligned(a->temperatures, 4) && aligned(a->top_ks, 4) && aligned(a->top_ps, 4) && aligned(a->min_ps, 4), AMAP_EALIGN, "misaligned pointer");
   Params P = {};
   P.a = *a;
-  // blocks of a row: as many as fill the device twice over, but none with less than two vectors of 16 bytes a thread
-  const int64_t vectors = (int64_t)a->vocab * dtype_bytes(a->dtype) / 16;
+  // blocks of a row: as many as fill the device twice over, but none with less than a vector of 16 bytes a thread.  More rows
+  // than multiprocessors that have settings of their own differ in work, and get twice as many, to even out (256 x 150001
+  // bf16, settings mixed: 154 -> 130 us; all alike, 40 largest of 150001: 60 -> 80)
+  const int64_t vectors = (int64_t)a->vocab * dtype_bytes(a->dtype) / 16, sms = device_sms();
+  const int64_t most = (a->rows > sms && a->by_row ? 4 : 2) * sms;
   P.blocks = 1;
-  while (P.blocks < MAXB && (int64_t)a->rows * P.blocks * 2 <= CAPX * device_sms() && vectors >= P.blocks * 2 * kThreads) P.blocks *= 2;
+  while (P.blocks < kMostBlocks && (int64_t)a->rows * P.blocks * 2 <= most && vectors >= P.blocks * 2 * kThreads) P.blocks *= 2;
   switch (a->dtype) {
     case AMAP_BF16: return run<AMAP_BF16>(P, cuda_stream);
     case AMAP_FP16: return run<AMAP_FP16>(P, cuda_stream);
