@@ -1,7 +1,7 @@
 // The cache of 4 bits: its description, and reading tokens back in 16 or 32 bits.
 //
-// Reading.  A thread has eight elements of K and the same eight of V of a token: a word and two 16-bit halves of codes, a word
-// of numbers each, and two stores of 16 bytes.  A block has 16 tokens of a head, so that where they are a cell's (the tokens
+// Reading.  A thread has eight elements of K and the same eight of V of a token, of two heads: a word and two 16-bit halves of codes,
+// the two words of numbers, and two stores of 16 bytes each.  A block has 16 tokens of these heads, so that where they are a cell's (the tokens
 // of a prompt) the halves of V, which lie apart, are served by the cell's lines in the first-level cache.
 // Bound: memory, of which three quarters are the stores.
 #include <algorithm>
@@ -22,8 +22,9 @@ struct ReadParams {
   char *k, *v;
   int64_t k_row, k_head, v_row, v_head;  // elements
   const int32_t *slots;
-  int64_t rows, items;  // items: threads with something to do, sixteens of rows made whole
-  int32_t heads, page_size, n_slots, group_shift;
+  int64_t rows;
+  int32_t heads, page_size, n_slots, group_shift, head_blocks;
+  uint32_t div_mul, div_shift;  // slot / page_size (0 mul: a power of two)
 };
 
 __device__ __forceinline__ float low_of(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
@@ -48,50 +49,62 @@ __device__ __forceinline__ void put(char *p, int64_t at, const float (&x)[8], bo
   }
 }
 
+// A block: 256 / chunks rows (16 at least or all that fit) of kHeads heads, their loads under way together.
+constexpr int kHeads = 2;
+template <int NS> constexpr int kRows = kThreads / (4 * NS) >= 16 ? kThreads / (4 * NS) / 16 * 16 : kThreads / (4 * NS);
+
 template <int DT, int NS, bool WIDE>
 __global__ void __launch_bounds__(kThreads) read_kernel(const __grid_constant__ ReadParams P) {
   constexpr int CHUNKS = 4 * NS;
+  const int c = threadIdx.x % CHUNKS, in_block = threadIdx.x / CHUNKS;
+  const uint32_t block = blockIdx.x / P.head_blocks;
+  const int head0 = (blockIdx.x - block * P.head_blocks) * kHeads;
+  const int64_t row = (int64_t)block * kRows<NS> + in_block;
   pdl_begin();
-  for (int64_t item = (int64_t)blockIdx.x * kThreads + threadIdx.x; item < P.items; item += (int64_t)gridDim.x * kThreads) {
-    // [sixteen of rows][head][row of it][chunk]
-    const int c = (int)(item % CHUNKS);
-    const int64_t rest = item / CHUNKS, block = rest / 16;
-    const int64_t row = block / P.heads * 16 + rest % 16;
-    const int head = (int)(block % P.heads);
-    if (row >= P.rows) continue;
-    float k[8], v[8];
-    const int32_t slot = P.slots[row];
-    if (slot >= 0 && slot < P.n_slots) {
-      const int32_t page = slot / P.page_size, in = slot - page * P.page_size, token = in % kCell, groups = CHUNKS * 8 >> P.group_shift;
-      const char *cell = P.data + (int64_t)page * P.page + (int64_t)head * P.head + (int64_t)(in / kCell) * cell_bytes(NS, groups);
-      const uint32_t kw = *reinterpret_cast<const uint32_t *>(cell + k_word_at(NS, token, c));
-      const uint32_t v0 = *reinterpret_cast<const uint16_t *>(cell + v_half_at(NS, token, 2 * c));
-      const uint32_t v1 = *reinterpret_cast<const uint16_t *>(cell + v_half_at(NS, token, 2 * c + 1));
-      const uint2 numbers = *reinterpret_cast<const uint2 *>(cell + numbers_at(NS, token, c * 8 >> P.group_shift));
-      const uint32_t kn = numbers.x, vn = numbers.y;
+  if (in_block >= kRows<NS> || row >= P.rows) return;
+  const int32_t slot = P.slots[row];
+  const bool there = slot >= 0 && slot < P.n_slots;
+  uint32_t kw[kHeads] = {}, v0[kHeads] = {}, v1[kHeads] = {};
+  uint2 numbers[kHeads] = {};
+  if (there) {
+    const uint32_t page = P.div_mul ? __umulhi((uint32_t)slot, P.div_mul) >> P.div_shift : (uint32_t)slot >> P.div_shift;
+    const int in = slot - (int)page * P.page_size, token = in % kCell, groups = CHUNKS * 8 >> P.group_shift;
+    const char *const cell = P.data + (int64_t)page * P.page + (int64_t)(in / kCell) * cell_bytes(NS, groups);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        k[i] = fmaf(step_of(kn), (float)(kw >> (4 * (i >> 1) + 16 * (i & 1)) & 15), low_of(kn));
-        v[i] = fmaf(step_of(vn), (float)((i < 4 ? v0 : v1) >> (4 * (i & 3)) & 15), low_of(vn));
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) k[i] = v[i] = 0.0f;
+    for (int h = 0; h < kHeads; ++h) {
+      if (head0 + h >= P.heads) break;
+      const char *const own = cell + (int64_t)(head0 + h) * P.head;
+      kw[h] = *reinterpret_cast<const uint32_t *>(own + k_word_at(NS, token, c));
+      v0[h] = *reinterpret_cast<const uint16_t *>(own + v_half_at(NS, token, 2 * c));
+      v1[h] = *reinterpret_cast<const uint16_t *>(own + v_half_at(NS, token, 2 * c + 1));
+      numbers[h] = *reinterpret_cast<const uint2 *>(own + numbers_at(NS, token, c * 8 >> P.group_shift));
     }
-    put<DT>(P.k, row * P.k_row + head * P.k_head + c * 8, k, WIDE);
-    put<DT>(P.v, row * P.v_row + head * P.v_head + c * 8, v, WIDE);
+  }
+#pragma unroll
+  for (int h = 0; h < kHeads; ++h) {
+    if (head0 + h >= P.heads) break;
+    float k[8], v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      k[i] = fmaf(step_of(numbers[h].x), (float)(kw[h] >> (4 * (i >> 1) + 16 * (i & 1)) & 15), low_of(numbers[h].x));
+      v[i] = fmaf(step_of(numbers[h].y), (float)((i < 4 ? v0[h] : v1[h]) >> (4 * (i & 3)) & 15), low_of(numbers[h].y));
+    }
+    put<DT>(P.k, row * P.k_row + (head0 + h) * P.k_head + c * 8, k, WIDE);
+    put<DT>(P.v, row * P.v_row + (head0 + h) * P.v_head + c * 8, v, WIDE);
   }
 }
 
 template <int DT, int NS>
-int run(const ReadParams &P, bool wide, void *stream) {
-  const int64_t blocks = (P.items + kThreads - 1) / kThreads;
-  const dim3 grid((unsigned)std::min<int64_t>(blocks, 0x7FFFFFFF));
+int run(ReadParams &P, bool wide, void *stream) {
+  P.head_blocks = (P.heads + kHeads - 1) / kHeads;
+  const int64_t blocks = (P.rows + kRows<NS> - 1) / kRows<NS> * P.head_blocks;
+  SERVE_REQUIRE(blocks <= 0x7FFFFFFF, AMAP_EOVERFLOW, "too many rows");
+  const dim3 grid((unsigned)blocks);
   return wide ? launch(read_kernel<DT, NS, true>, grid, kThreads, 0, stream, P) : launch(read_kernel<DT, NS, false>, grid, kThreads, 0, stream, P);
 }
 
 template <int DT>
-int run_dim(const ReadParams &P, int head_dim, bool wide, void *stream) {
+int run_dim(ReadParams &P, int head_dim, bool wide, void *stream) {
   switch (head_dim) {
     case 64: return run<DT, 2>(P, wide, stream);
     case 96: return run<DT, 3>(P, wide, stream);
@@ -162,7 +175,11 @@ extern "C" int amap_packed_read(const amap_packed_read_args *a, void *cuda_strea
   P.slots = a->slots;
   P.rows = a->rows;
   P.heads = c.heads, P.page_size = c.page_size, P.n_slots = c.n_pages * c.page_size, P.group_shift = c.group == 64 ? 6 : 5;
-  P.items = (a->rows + 15) / 16 * 16 * c.heads * (c.head_dim / 8);
+  // the high word of a product with ceil(2^(32+s) / page_size), s = floor(log2 page_size): exact for slots below 2^31
+  int s = 0;
+  while ((2u << s) <= (uint32_t)c.page_size) ++s;
+  P.div_shift = s;
+  if (c.page_size != 1 << s) P.div_mul = (uint32_t)((((uint64_t)1 << (32 + s)) + c.page_size - 1) / c.page_size);
   const int per16 = 16 / es;
   const bool wide = aligned(a->k, 16) && aligned(a->v, 16) && a->k_row % per16 == 0 && a->k_head % per16 == 0 && a->v_row % per16 == 0 && a->v_head % per16 == 0;
   switch (a->dtype) {

@@ -401,49 +401,56 @@ __device__ __forceinline__ void pack_rows(const Packing &A, uint32_t block, doub
   const int64_t x_row = is_k ? A.k_row : A.v_row, x_head = is_k ? A.k_head : A.v_head;
   const bool wide = is_k ? A.k_wide : A.v_wide, partner_wide = wide && half % 8 == 0;
   pdl_begin();
-  if (half) {
-    const uint64_t *phases = P.phase;  // as memory, not as constants (rope_kernel)
-    const uint8_t *axes = P.axis;
-    asm volatile("" : "+l"(phases), "+l"(axes));
-    for (int i = threadIdx.x; i < tokens * half; i += kThreads) {
-      const int at = quotient(i, P.by_half), pair = i - at * half;
-      const int64_t from = axes[pair] * P.position_axis + (row0 + at) * P.position_row;
-      const int64_t pos = P.wide_positions ? static_cast<const int64_t *>(P.positions)[from] : static_cast<const int32_t *>(P.positions)[from];
-      double s, c;
-      sincospi((double)(int64_t)((uint64_t)pos * phases[pair]) * 0x1p-63, &s, &c);
-      turn_cos[at * A.pad + turn_place<PAIRS>(pair, A.pad)] = c * P.scale;
-      turn_sin[at * A.pad + turn_place<PAIRS>(pair, A.pad)] = s * P.scale;
-    }
-    __syncthreads();
-  }
   for (int base = 0; base < n; base += kThreads) {  // whole warps throughout
     const int item = min(base + (int)threadIdx.x, n - 1);
     const int row = quotient(item, A.by_chunks), c = item - row * chunks, token = quotient(row, A.by_heads), head = row - token * A.heads, d0 = c * 8;
     const char *const from = x0 + ((int64_t)token * x_row + head * x_head) * ES;
-    float f[8];
+    float f[8], y[8], none = 0.0f;  // NaN once an infinity or a NaN is among the row's elements that count
     eight<DT>(from, d0, wide, f);
-    double x[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = f[j];
-    if (d0 < 2 * half) {
-      const double *const cos = turn_cos + token * A.pad, *const sin = turn_sin + token * A.pad;
-      if constexpr (PAIRS == AMAP_PAIRS_HALF) {
-        float y[8];
-        if (partner_wide) {
-          eight<DT>(from, d0 < half ? d0 + half : d0 - half, true, y);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int d = d0 + j;
-            y[j] = d < 2 * half ? Elem<DT>::to(reinterpret_cast<const typename Elem<DT>::T *>(from)[d < half ? d + half : d - half]) : 0.0f;
-          }
-        }
+    const bool turned = d0 < 2 * half;
+    if (PAIRS == AMAP_PAIRS_HALF && turned) {
+      if (partner_wide) {
+        eight<DT>(from, d0 < half ? d0 + half : d0 - half, true, y);
+      } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const int d = d0 + j;
+          y[j] = d < 2 * half ? Elem<DT>::to(reinterpret_cast<const typename Elem<DT>::T *>(from)[d < half ? d + half : d - half]) : 0.0f;
+        }
+      }
+    }
+    const int32_t slot = P.slots[row0 + token];
+    if (half && base == 0) {  // while these loads are under way
+      const uint64_t *phases = P.phase;  // as memory, not as constants (rope_kernel)
+      const uint8_t *axes = P.axis;
+      asm volatile("" : "+l"(phases), "+l"(axes));
+      for (int i = threadIdx.x; i < tokens * half; i += kThreads) {
+        const int at = quotient(i, P.by_half), pair = i - at * half;
+        const int64_t from = axes[pair] * P.position_axis + (row0 + at) * P.position_row;
+        const int64_t pos = P.wide_positions ? static_cast<const int64_t *>(P.positions)[from] : static_cast<const int32_t *>(P.positions)[from];
+        double s, c;
+        sincospi((double)(int64_t)((uint64_t)pos * phases[pair]) * 0x1p-63, &s, &c);
+        turn_cos[at * A.pad + turn_place<PAIRS>(pair, A.pad)] = c * P.scale;
+        turn_sin[at * A.pad + turn_place<PAIRS>(pair, A.pad)] = s * P.scale;
+      }
+      __syncthreads();
+    }
+    double x[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      x[j] = f[j];
+      none = fmaf(f[j], 0.0f, none);
+    }
+    if (turned) {
+      const double *const cos = turn_cos + token * A.pad, *const sin = turn_sin + token * A.pad;
+      if constexpr (PAIRS == AMAP_PAIRS_HALF) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int d = d0 + j;
+          none = fmaf(y[j], 0.0f, none);
           if (d >= 2 * half) continue;
           const int at = turn_place<PAIRS>(d < half ? d : d - half, A.pad);
-          x[j] = d < half ? x[j] * cos[at] - y[j] * sin[at] : x[j] * cos[at] + y[j] * sin[at];
+          x[j] = fma((double)(d < half ? -y[j] : y[j]), sin[at], x[j] * cos[at]);
         }
       } else {
 #pragma unroll
@@ -456,42 +463,42 @@ __device__ __forceinline__ void pack_rows(const Packing &A, uint32_t block, doub
         }
       }
     }
-    double least = x[0], most = x[0];
-    int finite = 1;
+    // what is rounded down keeps its order, so the smallest may be sought among floats
+    float least = __double2float_rd(x[0]);
+    double most = x[0];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      least = fmin(least, x[j]);
-      most = fmax(most, x[j]);
-      finite &= isfinite(x[j]);
+    for (int j = 1; j < 8; ++j) {
+      least = fminf(least, __double2float_rd(x[j]));
+      most = x[j] > most ? x[j] : most;
     }
 #pragma unroll
     for (int d = 1; d < 8; d <<= 1) {
       if (8 * d >= A.group) break;
-      least = fmin(least, __shfl_xor_sync(~0u, least, d));
-      most = fmax(most, __shfl_xor_sync(~0u, most, d));
-      finite &= __shfl_xor_sync(~0u, finite, d);
+      least = fminf(least, __shfl_xor_sync(~0u, least, d));
+      const double other = __shfl_xor_sync(~0u, most, d);
+      most = other > most ? other : most;
+      none += __shfl_xor_sync(~0u, none, d);
     }
-    // low is rounded down, so that no element lies below it: twice, which comes to the same as once
-    __nv_bfloat16 low = __float2bfloat16_rd(__double2float_rd(least));
+    __nv_bfloat16 low = __float2bfloat16_rd(least);  // down twice comes to the same as once: no element lies below it
     __nv_bfloat16 step = __float2bfloat16_rn((float)((most - (double)__bfloat162float(low)) / 15.0));
-    if (!finite || !isfinite(__bfloat162float(low)) || !isfinite(__bfloat162float(step))) {
+    if (!(none == 0.0f) || !isfinite(__bfloat162float(low)) || !isfinite(__bfloat162float(step))) {
       low = __ushort_as_bfloat16(0x7FC0);
       step = __ushort_as_bfloat16(0);
     }
-    const double l = __bfloat162float(low), s = __bfloat162float(step), by = s > 0 ? 1.0 / s : 0.0;
+    const float step_f = __bfloat162float(step);
+    const double l = __bfloat162float(low), s = step_f, h = 0.5 * s, by = step_f >= 0x1p-120f ? (double)__frcp_rn(step_f) : s > 0 ? 1.0 / s : 0.0;
     uint32_t code[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      // rint((x - l) / s): the product with the reciprocal is a rounding off at most, the rest says which way
-      const double over = x[j] - l;
-      double near = rint(over * by);
-      const double rest = 2.0 * fma(-near, s, over);
-      const bool odd = (int)near & 1;
-      if (rest > s || (rest == s && odd)) near += 1.0;
-      else if (rest < -s || (rest == -s && odd)) near -= 1.0;
-      code[j] = s > 0 ? (uint32_t)(int)fmin(near, 15.0) : 0;
+      // rint((x - l) / s): the product with the reciprocal says it but next to a border, where the rest decides
+      const double over = x[j] - l, t = fma(over, by, 0x1.8p52), near = t - 0x1.8p52, rest = fma(-near, s, over);
+      int n = __double2loint(t);
+      if (fabs(rest) >= h) {
+        if (rest > h || (rest == h && (n & 1))) ++n;
+        else if (rest < -h || (rest == -h && (n & 1))) --n;
+      }
+      code[j] = s > 0 ? min(n, 15) : 0;
     }
-    const int32_t slot = P.slots[row0 + token];
     if (base + (int)threadIdx.x >= n || slot < 0 || slot >= P.n_slots) continue;
     const uint32_t page = quotient(slot, P.by_page), in = slot - page * P.by_page.d;
     const int t = in % kCell, groups = P.head_dim / A.group;
