@@ -518,7 +518,7 @@ __device__ __forceinline__ void pack_rows(const Packing &A, uint32_t block, doub
 }
 
 template <int DT, int VEC, int PAIRS>
-__global__ void __launch_bounds__(kThreads, 2) pack_kernel(const __grid_constant__ Packing A) {
+__global__ void __launch_bounds__(kThreads, kBlocks) pack_kernel(const __grid_constant__ Packing A) {
   __shared__ __align__(16) double turn_cos[kTurns], turn_sin[kTurns];
   if (blockIdx.x < A.blocks) pack_rows<DT, PAIRS>(A, blockIdx.x, turn_cos, turn_sin);
   else turn_rows<DT, VEC, PAIRS>(A.p, blockIdx.x - A.blocks, reinterpret_cast<float *>(turn_cos), reinterpret_cast<float *>(turn_sin));
