@@ -42,7 +42,7 @@ using namespace amap_serve;
 namespace {
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps, kBlock = kThreads + 32;  // the last warp is the producer
-constexpr int kMostBlocksPerSm = 3;
+constexpr int kMostBlocksPerSm = 2;
 constexpr int kGroup = 8;               // teams whose parts are joined first, where an item has more than kDirect of them
 constexpr int kDirect = 12;
 constexpr int kAside = 4;               // parts that the producer warp joins

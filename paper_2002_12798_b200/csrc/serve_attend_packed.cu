@@ -4,21 +4,31 @@
 //   s_t = scale sum_g (step_K <q_g, c_tg> + low_K sum(q_g)),   O = sum_t sum_g (P_t step_V) d_tg + P_t low_V
 // so the matrix instructions see the codes themselves.  A code's four bits, masked out where they lie in a 16-bit half, are
 // an fp16 number: code x 2^-24 in bits 0 .. 3, code x 2^-20 in bits 4 .. 7 (fp16 counts evenly from 0 to 2^11 of its
-// smallest steps), exact in the products.  Eight codes cost a shift and four masks, no conversion; q's elements that meet
-// the lower kind are taken 16 times as large, and the two kinds of O's rows are scaled at the end.
+// smallest steps), exact in the products: no conversion.  q's elements that meet the lower kind of K's codes are taken 16
+// times as large.  Of V the lower kind's rows take whole bytes, lower + 16 upper, and what the upper rows have of them is taken off
+// at the end: four operations for eight codes.  Tokens are the M side of both products; P is transposed in between.
 //
 // Precision.  q is fp16 times a power of two that brings its largest element near 2^11 (2^15 where it meets the lower kind):
 // elements down to 2^-27 of it are exact (of fp16's 11 bits, down to 2^-24).  P step_V enters as two fp16 terms of 11 bits, the
-// second what the first leaves over.  They are taken relative to a reference R that follows the largest WEIGHT of a token so far,
-// P times its largest |low_V| or step_V, rather than the largest P: so the products lie within 2^15 of fp16's range from above
-// whatever the values' size is, and a token is cut off only where its weight is 2^-24 of the largest or less (and then by
-// 2^-40 of that).  P itself, l and the sums of P low_V are in 32 bits, where R may be far from the largest score.
+// second what the first leaves over.  They are taken relative to a reference R that follows the largest WEIGHT of a token so
+// far, P times its largest |low_V| or step_V, rather than the largest P: so the products lie near fp16's upper end whatever
+// the values' size is, and a token is cut off only where its weight is 2^-24 of the largest or less (and then by 2^-40 of
+// that).  P itself, l and the sums of P low_V are in 32 bits, where R may be far from the largest score.  The matrix
+// unit cuts its sums off to 24 bits: a score is within some 2^-21 of the size of its terms (lse 0.4 to 1.5e-6 off, relative,
+// for keys of 16 times the variance of one channel), and V's codes are counted down in every second cell, so that what is
+// summed over a long request stays small.
 //
-// Bound: HBM; a cell of 16 tokens (2304 bytes of 128 elements in groups of 64) is about 290 instructions of a warp and 32
-// products of 16 x 8 x 16, where a multiprocessor has 400 issue slots in the time that the cell takes to come.  The q heads are the M side of the first
-// product (so that P comes out as the second one wants it, without a transposition) and the N side of the second.
+// Bound: the issue of integer operations.  A cell of 16 tokens (2304 bytes of 128 elements in groups of 64) is 290 instructions
+// of a warp, of them 133 on the half-rate integer pipe, 87 on the multipliers (the two add up: 4 LOP and 4 FFMA take 3.05
+// clocks of a multiprocessor, 4 LOP alone 2.03) and 24 products of 16 x 8 x 16 (2.03 clocks each, in parallel): about 110
+// clocks, where the cell takes 99 to come from HBM.  Copies alone take 116 us of the 152 of 64 requests; with a third block a
+// multiprocessor (128 registers) nothing changes.
 //
-// Split, ring and join are serve_attend.cu's.  A tile is 128 tokens: eight cells, each one bulk copy.
+// Split, ring and join are serve_attend.cu's.  A tile is 128 tokens: eight cells, copied in bulk in runs that every page divides into.
+//
+// Measured: 64 requests of up to 16384 tokens, 32 q heads over 8 of 128 elements, bf16, groups of 64 (605 MB) 152 us = 4.0
+// TB/s; one request of 131009 tokens, fp16, groups of 32 (168 MB) 51 us = 3.3; 128 requests of up to 4096, 64 q heads over 4
+// (155 MB) 91 us; 33 tokens 6.1 us.
 #define AMAP_ATTEND_PARTS_ONLY
 #include "serve_attend.cu"
 #include "serve_packed.cuh"
@@ -28,7 +38,7 @@ namespace {
 constexpr int kPackedTile = 128, kCells = kPackedTile / kCell, kOwn = kCells / kWarps;  // cells of a tile; of a warp
 constexpr int kLook = 32 / kCells;                                                      // tiles whose pages are looked up at a time
 static_assert(kOwn == 2, "a warp's cells of a tile");
-constexpr float kUp = 9.0f, kTop = 0x1p15f;  // P is 2^kUp times what it stands for; P step_V above kTop renews the reference
+constexpr float kUp = 0x1p9f, kTop = 0x1p15f;  // P is kUp times what it stands for; P step_V above kTop renews the reference
 constexpr float kNone = -3e38f;            // the reference before the first token
 constexpr float kLeast = 0x1p-60f;         // a smaller |low| or step counts as this much
 constexpr float kMost = 0x1p80f;           // a sum of P above this renews the reference, too (tokens whose V is constant have no step)
@@ -194,7 +204,7 @@ __global__ void __launch_bounds__(kBlock, (kPackedResident<NS>)) attend_packed_k
       settle(smem_at(&small.full[0]), S, stage, parity ^ 1, P.failed);
       return;
     }
-    if (piece.aside) join_aside<D, HB>(P, small, piece, kUp);
+    if (piece.aside) join_aside<D, HB>(P, small, piece, 0.0f);
     return;
   }
 
@@ -384,13 +394,12 @@ __global__ void __launch_bounds__(kBlock, (kPackedResident<NS>)) attend_packed_k
           bool beyond = fresh;
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            const float from = kUp - ref[c];
             float most = 0.0f;
 #pragma unroll
             for (int u = 0; u < kOwn; ++u) {
 #pragma unroll
               for (int e = 0; e < 2; ++e) {
-                p[u][2 * e + c] = exp2_of(fmaf(s[u][2 * e + c], to_log2[c], from));
+                p[u][2 * e + c] = exp2_of(fmaf(s[u][2 * e + c], to_log2[c], -ref[c])) * kUp;  // the exponent is exact where P is large
                 most = fmaxf(most, p[u][2 * e + c] * step[u][e]);
               }
             }
@@ -505,14 +514,14 @@ __global__ void __launch_bounds__(kBlock, (kPackedResident<NS>)) attend_packed_k
       sum += __shfl_xor_sync(~0u, sum, 8);
       sum += __shfl_xor_sync(~0u, sum, 16);
       if (ref[c] == kNone) ref[c] = -INFINITY;
-      if (g == 0) *reinterpret_cast<float2 *>(joint + (warp * 8 + 2 * t4 + c) * kPitch + D) = make_float2(ref[c], sum);
+      if (g == 0) *reinterpret_cast<float2 *>(joint + (warp * 8 + 2 * t4 + c) * kPitch + D) = make_float2(ref[c], sum / kUp);
     }
     sync_consumers();
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       const float *ml = joint + (2 * t4 + c) * kPitch + D;
       const float top = fmaxf(fmaxf(ml[0], ml[8 * kPitch]), fmaxf(ml[16 * kPitch], ml[24 * kPitch]));
-      const float f = top == -INFINITY ? 1.0f : exp2_of(ref[c] - top);
+      const float f = (top == -INFINITY ? 1.0f : exp2_of(ref[c] - top)) / kUp;
       float *to = joint + (warp * 8 + 2 * t4 + c) * kPitch;
 #pragma unroll
       for (int n = 0; n < NG; ++n) {
@@ -527,9 +536,9 @@ __global__ void __launch_bounds__(kBlock, (kPackedResident<NS>)) attend_packed_k
       }
     }
     sync_consumers();
-    sum_warps<D, HB>(P, joint, 0, heads, whole, r, first + in_group, slot, kUp);
+    sum_warps<D, HB>(P, joint, 0, heads, whole, r, first + in_group, slot, 0.0f);
     sync_consumers();
-    if (!whole) hand_in<D, HB>(P, small, joined, piece, item_first, item_last, heads, r, h, first + in_group, kUp);  // uniform over the block
+    if (!whole) hand_in<D, HB>(P, small, joined, piece, item_first, item_last, heads, r, h, first + in_group, 0.0f);  // uniform over the block
     if (more) {
       item_first = u1 - at.rest;
       take_q();

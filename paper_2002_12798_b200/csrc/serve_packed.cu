@@ -3,7 +3,8 @@
 // Reading.  A thread has eight elements of K and the same eight of V of a token, of two heads: a word and two 16-bit halves of codes,
 // the two words of numbers, and two stores of 16 bytes each.  A block has 16 tokens of these heads, so that where they are a cell's (the tokens
 // of a prompt) the halves of V, which lie apart, are served by the cell's lines in the first-level cache.
-// Bound: memory, of which three quarters are the stores.
+// Bound: memory, of which three quarters are the stores: 65537 tokens of 8 heads of 128 fp16 elements in groups of 32 (353 MB) 62 us
+// = 5.6 TB/s (one head a thread, 64-bit index arithmetic: 85); 700 tokens 5.2 us, latency.
 #include <algorithm>
 
 #include "serve_alias.hpp"

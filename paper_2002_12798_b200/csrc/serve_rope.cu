@@ -357,6 +357,8 @@ int widest(const Params &P, int es, int heads_es) {
 // in 64 bits: between two codes lies a border, and where k falls is the definition's only if k is not a rounding away from it
 // (with 32 bits about one of 2^19 codes would come out as its neighbour, and one of 2^15 steps as another number).  k and
 // v are a fifth of what the launch reads and writes at 4 q heads to a cache head, and the 64-bit units are idle otherwise.
+// Bound: latency, block after block (loads, angles, shuffles, codes): four blocks a multiprocessor instead of three took 4099
+// tokens of 32 + 8 + 8 heads of 128 bf16 elements from 55 to 36 us, fewer instructions by a quarter 2; memory would take 13.
 struct Packing {
   Params p;  // its one part is q; slots, positions, phases and by_page are k's and v's, too
   const char *k, *v;

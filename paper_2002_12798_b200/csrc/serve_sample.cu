@@ -11,12 +11,17 @@
 // maxima; for top_p alone the weight that all tokens together would need to make up the rest.  The tokens above it, few as
 // a rule, are listed by each warp, and if there are 1024 at most one block sorts them and is done.  More of them, or a row
 // whose lists overflow, go by histograms of counts and sums: first over y (64 bins to a power of two), then over the bits
-// of the logits in the bin where a bound falls, until that holds one logit.  The draw takes the sums of each warp's run of
-// the row (or of its list), and goes through one of them.
+// of the logits in the bin where a bound falls, until that holds one logit.  bf16 logits, of which some thousand different
+// ones have a weight, are counted in a bin of their own each, and weighed once.  The draw takes the sums of each warp's run
+// of the row (or of its list), and goes through one of them.
 //
-// Bound: the weights where all tokens have to be weighed (about 25 instructions, nine of them in 64 bits, each), memory and
-// latency elsewhere; the logits come from HBM once, and from the second-level cache once or twice more.  A row is a
-// cluster's, of as many blocks as fill the device, which exchange sums through shared memory.
+// Bound: 64-bit arithmetic where all tokens have to be weighed one by one (about 25 instructions, nine of them in 64 bits, 9 to 14
+// clocks of a multiprocessor for 32 tokens), the largest logit's pass by memory, and the rest by latency: every exchange between
+// a row's blocks takes one to four microseconds.  The logits come from HBM once, and from the second-level cache once or
+// twice more.  A row is a cluster's, of as many blocks as fill the device, which exchange sums through shared memory.
+//
+// Measured: one row of 32000 fp32 logits, 50 largest, top_p 0.95, 19 us; 64 rows of 100003 bf16, top_p 0.9, 61; 128 of 131072
+// fp32, nothing cut off, 57 (67 MB: 10 from HBM); 256 of 150001 bf16 with settings of their own 130.
 #include <cooperative_groups.h>
 
 #include <algorithm>
