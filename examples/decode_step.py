@@ -1,11 +1,11 @@
 """A decoder layer's serving steps from end to end: pages, rotary positions, paged cache, decode attention.
 
-    python examples/decode_step.py [--steps N] [--cache bf16|e4m3]
+    python examples/decode_step.py [--steps N] [--cache bf16|e4m3|4bit]
 
 A prompt of every request goes into the cache in one step (its own attention is left to the caller's prefill kernel), then
-tokens are generated one at a time: a step's `pages_extend`, `append` and `attend` are captured in a CUDA graph once and
-replayed, nothing is copied to the host in between.  Random projections stand in for the model; the last step is checked
-against plain torch.
+tokens are generated one at a time: a step's `pages_extend`, `append`, `attend` and `sample` are captured in a CUDA graph once
+and replayed, nothing is copied to the host in between.  Random projections stand in for the model; the last step is
+checked against plain torch.
 """
 import argparse
 import os
@@ -20,7 +20,7 @@ from paper_2002_12798_b200 import ops  # noqa: E402
 def main():
     p = argparse.ArgumentParser()
     p.add_argument("--steps", type=int, default=20)
-    p.add_argument("--cache", choices=["bf16", "e4m3"], default="bf16")
+    p.add_argument("--cache", choices=["bf16", "e4m3", "4bit"], default="bf16")
     a = p.parse_args()
     torch.manual_seed(0)
     requests, q_heads, heads, dim, page, row = 8, 32, 8, 128, 16, 64
@@ -32,10 +32,13 @@ def main():
     free = torch.randperm(pages, device=dev).to(torch.int32)
     free_count, seq_lens = torch.tensor([pages], **int32), torch.zeros(requests, **int32)
     held = torch.bfloat16 if a.cache == "bf16" else torch.float8_e4m3fn
-    k_cache = torch.zeros(pages, page, heads, dim, device=dev).to(held)
-    v_cache = torch.zeros(pages, page, heads, dim, device=dev).to(held)
     scale = 1.0 if a.cache == "bf16" else 1.0 / 64
-    cache = ops.PagedCache(k_cache, v_cache, k_scale=scale, v_scale=scale)
+    if a.cache == "4bit":
+        cache = ops.PackedCache.zeros(pages, page, heads, dim)
+    else:
+        k_cache = torch.zeros(pages, page, heads, dim, device=dev).to(held)
+        v_cache = torch.zeros(pages, page, heads, dim, device=dev).to(held)
+        cache = ops.PagedCache(k_cache, v_cache, k_scale=scale, v_scale=scale)
     rope = ops.RopePlan(dim, sections=[16, 24, 24])  # time, height, width; text moves along all three
     attention = ops.AttendPlan(requests, q_heads, heads, dim)
 
@@ -55,6 +58,8 @@ def main():
     # decoding: one token per request that has begun
     new = (prompt > 0).to(torch.int32)
     fused = torch.empty(requests, (q_heads + 2 * heads) * dim, device=dev, dtype=torch.bfloat16)
+    to_logits = torch.randn(q_heads * dim, 5000, device=dev, dtype=torch.bfloat16)
+    uniforms = torch.empty(requests, device=dev)
 
     def decode():
         s = ops.pages_extend(new, seq_lens, table, free, free_count, page, requests)
@@ -63,26 +68,29 @@ def main():
         rows = torch.zeros(requests + 1, q_heads, dim, device=dev, dtype=q.dtype)  # token -> its request's row
         rows[torch.where(s.requests < 0, requests, s.requests).long()] = q
         out = attention.attend(rows[:requests], cache, table, s.seq_lens)
+        token = ops.sample(out.flatten(1) @ to_logits, uniforms, temperature=0.8, top_k=50, top_p=0.95)
         seq_lens.copy_(s.seq_lens)
         free_count.copy_(s.free_count)
-        return rows, out, s
+        return rows, out, token
 
     before = seq_lens.clone(), free_count.clone(), table.clone()
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
         fused.normal_()
+        uniforms.uniform_()
         decode()  # warm-up
     torch.cuda.current_stream().wait_stream(side)
     for now, was in zip((seq_lens, free_count, table), before):
         now.copy_(was)
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
-        rows, out, s = decode()
+        rows, out, token = decode()
     start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
     start.record()
     for _ in range(a.steps):
         fused.normal_()
+        uniforms.uniform_()
         graph.replay()
     end.record()
     torch.cuda.synchronize()
@@ -96,12 +104,15 @@ def main():
             continue
         t = torch.arange(n, device=dev)
         at, off = table[r, t // page].long(), t % page
-        kk = k_cache.view(torch.uint8 if a.cache == "e4m3" else held)[at, off].view(held).float() * scale
-        vv = v_cache.view(torch.uint8 if a.cache == "e4m3" else held)[at, off].view(held).float() * scale
+        if a.cache == "4bit":
+            kk, vv = cache.read((at * page + off).to(torch.int32), dtype=torch.float32)
+        else:
+            kk, vv = (c.view(torch.uint8 if a.cache == "e4m3" else held)[at, off].view(held).float() * scale for c in (k_cache, v_cache))
         x = torch.einsum("hgd,thd->hgt", rows[r].float().view(heads, -1, dim), kk) * dim**-0.5
         want = torch.einsum("hgt,thd->hgd", torch.softmax(x, -1), vv).reshape(q_heads, dim)
         worst = max(worst, float((out[r].float() - want).abs().max() / want.abs().max()))
     assert worst < 0.01 and not attention.failed(), worst
+    assert ((token >= 0) & (token < 5000)).all()
     done = torch.ones(requests, dtype=torch.bool, device=dev)
     seq_lens, free_count = ops.pages_release(done, seq_lens, table, free, free_count, page)
     assert int(free_count) == pages and sorted(free.tolist()) == list(range(pages))

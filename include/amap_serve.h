@@ -1,7 +1,8 @@
 /*
  * amap_serve.h -- what a transformer does with the heads a composed map has
- * split: rotary positions, a paged key/value cache, and the attention of one
- * new token per request that reads it.  Their addresses depend on data that
+ * split: rotary positions, a paged key/value cache, the attention of one new
+ * token per request that reads it, and the choice of the next token.  Their
+ * addresses depend on data that
  * lives on the device (positions, slots, block tables, lengths), so they are
  * operators of their own beside amap_execute.
  *

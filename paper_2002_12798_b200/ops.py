@@ -1,5 +1,5 @@
-"""Operators on the heads that a composed map has split: rotary positions, a paged key/value cache, and the attention
-of one new token per request (include/amap_serve.h has the definitions; this module marshals arguments).
+"""Operators on the heads that a composed map has split: rotary positions, a paged key/value cache, the attention of one
+new token per request, and the choice of the next (include/amap_serve.h has the definitions; this module marshals arguments).
 
 One decoding step, for every layer the lines from `append` on:
 
@@ -10,7 +10,8 @@ One decoding step, for every layer the lines from `append` on:
     out = attention.attend(rows[:-1], cache, block_table, step.seq_lens)
 
 append takes the step's tokens, one behind the other; attend a row per request, of which some may have no token in the
-step (idle, or refused).  Where every request has one, `rows` is q.
+step (idle, or refused).  Where every request has one, `rows` is q.  cache is a PagedCache (16 bits, or 8 with a scale) or a
+PackedCache (4 bits, quantised as they are written).  Behind the last layer `sample` draws a token for every row of logits.
 
 Calls enqueue one kernel on the current CUDA stream (or `stream`) and neither synchronise nor copy to the host, so a
 step can be captured in a CUDA graph.  Tensors a call is given must stay alive and unchanged until that stream has run
