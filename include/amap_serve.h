@@ -330,7 +330,9 @@ int amap_packed_attend(const amap_attend_args *args /* host */, const amap_packe
  * less: the largest logit, the first of them.  A NaN counts as -infinity; a row
  * with no logit above -infinity gives -1; where the largest is +infinity, the
  * tokens that have it share the weight.
- * A uniform number outside counts as the nearest inside, NaN as 0.
+ * A uniform number outside counts as the nearest inside, NaN as 0; so do min_p
+ * and top_p of a row; those of a row that are NaN count as not given, a
+ * temperature that is as 0.
  * logprob[r] = log of the probability with which the token was drawn (0 for
  * temperature 0, -infinity with token -1).
  * The answer is the definition's in 64 bits: w is rounded to units of 2^-44 (of

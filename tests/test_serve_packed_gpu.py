@@ -459,3 +459,39 @@ def test_a_decoding_step_in_a_graph_and_on_another_stream(ops):
         want, _, bound, _ = ref.attend(f64(rows)[i], k, v, np.arange(40), plan.scale)
         assert (np.abs(f64(out)[i] - want) <= bound + 2.0**-8 * (np.abs(want) + bound)).all()
     assert not plan.failed()
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.2, 1e-30])
+def test_scales_of_either_sign(ops, scale):
+    r = np.random.default_rng(15)
+    cache, k, v = filled(ops, r, 320, 32, 2, 128, 64, "bf16")
+    table, lens = np.stack([r.permutation(10) for _ in range(3)]).astype(np.int32), np.array([320, 200, 7], dtype=np.int32)
+    q = cuda(r.standard_normal((3, 16, 128)), torch.bfloat16)
+    q[1, 2] = 0.0
+    check_attend(ops.AttendPlan(3, 16, 2, 128, scale=scale), q, cache, table, lens, k, v)
+    check_attend(ops.AttendPlan(3, 16, 2, 128, scale=scale, softcap=3.0), q, cache, table, lens, k, v)
+
+
+def test_two_plans_on_two_streams(ops):
+    r = np.random.default_rng(16)
+    cache, k, v = filled(ops, r, 4096, 16, 4, 128, 32, "bf16")
+    table, lens = cuda(np.stack([r.permutation(256) for _ in range(20)]).astype(np.int32)), cuda(r.integers(0, 4097, 20).astype(np.int32))
+    q = cuda(r.standard_normal((20, 32, 128)), torch.bfloat16)
+    plans, streams = [ops.AttendPlan(20, 32, 4, 128) for _ in range(2)], [torch.cuda.Stream() for _ in range(2)]
+    want = plans[0].attend(q, cache, table, lens)
+    torch.cuda.synchronize()
+    got = []
+    for i in range(40):
+        got.append(plans[i % 2].attend(q, cache, table, lens, stream=streams[i % 2]))
+        got.append(plans[i % 2].attend(q, cache, table, lens, stream=streams[1 - i % 2]))  # ordered by the plan
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, want) for x in got) and not plans[0].failed() and not plans[1].failed()
+
+
+def test_append_without_q(ops):
+    x = torch.randn(20, 2, 128, device="cuda", dtype=torch.float16)
+    slots, positions = torch.randperm(32, device="cuda")[:20].to(torch.int32), torch.arange(20, device="cuda")
+    cache, other = ops.PackedCache.zeros(2, 16, 2, 128), ops.PackedCache.zeros(2, 16, 2, 128)
+    out = ops.RopePlan(128).append(x[:, :0], x, x, positions, slots, cache)
+    ops.RopePlan(128).append(x, x, x, positions, slots, other)
+    assert out.shape == (20, 0, 128) and torch.equal(cache.data, other.data)

@@ -196,3 +196,42 @@ def test_drawn_as_often_as_their_weight(ops):
     token = ops.sample(x.expand(n, 50), (torch.arange(n, device="cuda") + 0.5) / n, temperature=1.3)
     p = torch.softmax(x[0].double() / float(np.float32(1.3)), 0).cpu().numpy()
     assert np.abs(np.bincount(token.cpu().numpy(), minlength=50) - n * p).max() <= 1.0 + n * 2.0**-23
+
+
+def test_settings_that_are_no_numbers_or_outside(ops):
+    x, u = torch.randn(4, 3000, device="cuda") * 3, torch.rand(4, device="cuda")
+    of = lambda *v: torch.tensor(v, device="cuda")  # noqa: E731
+    nan = float("nan")
+    plain = ops.sample(x, u)
+    assert torch.equal(ops.sample(x, u, top_p=of(nan, 1.0, 2.0, nan), min_p=of(nan, 0.0, -1.0, 0.0)), plain)
+    first = x.argmax(1).to(torch.int32)
+    assert torch.equal(ops.sample(x, u, temperature=of(nan, 0.0, -2.0, -0.0)), first)
+    assert torch.equal(ops.sample(x, u, top_p=of(-1.0, 0.0, -0.5, 1e-9), min_p=0.0), first)
+    assert torch.equal(ops.sample(x, u, min_p=of(1.0, 7.0, float("inf"), 1.5)), first)
+
+
+@pytest.mark.parametrize("rows,vocab", [(1, 200000), (30, 50000), (200, 20000)])
+def test_top_k_of_every_size(ops, rows, vocab):
+    """Bounds from a block's threads, from the row's, and none."""
+    g = torch.Generator(device="cuda").manual_seed(vocab)
+    for dtype in ("bf16", "fp32"):
+        x = (torch.randn(rows, vocab, generator=g, device="cuda") * 2).to(TYPES[dtype])
+        u = torch.rand(rows, generator=g, device="cuda")
+        for k in (2, 63, 64, 65, 129, 512, 513, 1023, 1025, 4097, vocab - 1):
+            check(ops, x[:3], u[:3], top_k=k)
+            check(ops, x[-2:], u[-2:], top_k=k, top_p=0.7)
+        token = ops.sample(x, u, top_k=100)
+        assert torch.equal(token[-2:], ops.sample(x[-2:], u[-2:], top_k=100))  # however many blocks a row has
+
+
+def test_flat_rows_keep_most_of_their_tokens(ops):
+    """Lists overflow, bounds fall deep into the row; bf16 logits around zero share a bin."""
+    g = torch.Generator(device="cuda").manual_seed(8)
+    for rows, vocab in ((3, 150001), (160, 30011)):
+        for spread in (0.01, 0.5):
+            for dtype in ("bf16", "fp16", "fp32"):
+                x = (torch.randn(rows, vocab, generator=g, device="cuda") * spread).to(TYPES[dtype])
+                u = torch.rand(rows, generator=g, device="cuda")
+                for settings in (dict(top_p=0.95), dict(top_p=0.4, temperature=0.3), dict(top_k=vocab // 2, top_p=0.9), dict(min_p=0.2, top_p=0.5)):
+                    check(ops, x[:3], u[:3], **settings)
+                    assert torch.equal(ops.sample(x, u, **settings)[:3], ops.sample(x[:3], u[:3], **settings))
