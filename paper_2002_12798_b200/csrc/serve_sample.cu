@@ -473,19 +473,15 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     float bound = z.least_value;
     if (min_p > 0.0f) bound = fmaxf(bound, __double2float_rd(z.top + 1024 * (log2((double)fminf(min_p, 1.0f)) - 1e-6) / z.by));
     if (by_k && top_k <= P.blocks * kThreads) {
-      // the top_k-th largest of the threads' own maxima: of this block's where that leaves few enough tokens (one row of 32000
-      // 19 -> 15 us), else of the row's
-      Z of = z;
-      if (top_k * P.blocks <= kThreads) of.blocks = 1;
-      of.clear_bins(kBins);
+      // the top_k-th largest of the threads' own maxima
+      z.clear_bins(kBins);
       int y;
-      const uint64_t w = of.weight(of.value(own), &y);
-      if (w) of.add(Z::bin_of(y), w);
-      const Tally mine = {w, w != 0};
-      if ((of.blocks == 1 ? of.block_sum(mine) : total(mine)).count >= (uint32_t)top_k) {
+      const uint64_t w = z.weight(z.value(own), &y);
+      if (w) z.add(Z::bin_of(y), w);
+      if (total({w, w != 0}).count >= (uint32_t)top_k) {
         int bin;
-        of.find_bin(kBins, true, top_k, 0, &bin);
-        bound = fmaxf(bound, of.value_of_bin(bin));
+        z.find_bin(kBins, true, top_k, 0, &bin);
+        bound = fmaxf(bound, z.value_of_bin(bin));
       }
     } else if (!by_k && !(min_p > 0.0f)) {
       Tally all = {0, 0};
