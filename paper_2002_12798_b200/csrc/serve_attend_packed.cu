@@ -47,7 +47,7 @@ template <int NS> constexpr int kPackedResident = NS >= 8 ? 1 : 2;
 // Stages of the ring: what a multiprocessor's shared memory has room for beside the rest of its blocks, up to eight.
 constexpr int least(int a, int b) { return a < b ? a : b; }
 template <int NS, int NG, int RESIDENT>
-constexpr int kPackedStages = least(8, (226 * 1024 / RESIDENT - 3072 - (int)sizeof(float) * kWarps * 8 * (32 * NS + 4)) / (kCells * cell_bytes(NS, NG)));
+constexpr int kPackedStages = least(8, (226 * 1024 / RESIDENT - 3 * 1024 - (int)sizeof(float) * kWarps * 8 * (32 * NS + 4)) / (kCells * cell_bytes(NS, NG)));
 
 struct PackedParams {
   Params p;
