@@ -738,7 +738,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   }
   uint64_t mass = 0;
   uint32_t same = 0;
-  const float last_value = last ? of_key(last) : -INFINITY;
+  // least_value has no weight, though the 16-bit logit whose bin it is in may have one (below zero a bin's logit is its upper end)
+  const float last_value = last ? of_key(last) : z.least_value;
   auto weigh = [&](float v) {
     const uint64_t w = z.weight(v);
     mass += v > last_value ? w : 0;

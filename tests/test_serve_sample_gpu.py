@@ -235,3 +235,36 @@ def test_flat_rows_keep_most_of_their_tokens(ops):
                 for settings in (dict(top_p=0.95), dict(top_p=0.4, temperature=0.3), dict(top_k=vocab // 2, top_p=0.9), dict(min_p=0.2, top_p=0.5)):
                     check(ops, x[:3], u[:3], **settings)
                     assert torch.equal(ops.sample(x, u, **settings)[:3], ops.sample(x[:3], u[:3], **settings))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("shift,temperature", [(-20.0, 0.001), (-100.0, 0.01), (-512.0, 0.05), (-200.0, 0.1), (-9984.0, 1.0), (-9984.0, 0.3), (0.0, 1e-4), (100.0, 0.01)])
+def test_largest_logits_below_zero(ops, dtype, shift, temperature):
+    """The lowest number with a weight lies between two 16-bit logits, next to a negative largest one: what is smaller, a NaN and what
+    lies outside the row have none.  Nothing cut off, min_p over more tokens than the lists hold, top_k of all; every row is written."""
+    g = torch.Generator(device="cuda").manual_seed(7)
+    for rows, vocab, offset in ((5, 3001, 0), (3, 20011, 3), (2, 777, 5)):
+        stride = vocab + 6
+        flat = torch.zeros(offset + rows * stride + 16, device="cuda", dtype=TYPES[dtype])
+        x = flat.as_strided((rows, vocab), (stride, 1), offset)
+        x.copy_(torch.randn(rows, vocab, generator=g, device="cuda") * 3 + shift)
+        x[0, ::3] = float("nan")
+        x[1, 1:] = -float("inf")
+        u = torch.rand(rows, generator=g, device="cuda")
+        for settings in (dict(), dict(min_p=1e-6), dict(top_k=vocab), dict(top_p=0.9), dict(top_k=vocab // 2, top_p=0.95)):
+            check(ops, x, u, temperature=temperature, **settings)
+            out = torch.full((rows,), -7, device="cuda", dtype=torch.int32)
+            ops.sample(x, u, temperature=temperature, out=out, **settings)
+            assert ((out >= 0) & (out < vocab)).all()
+
+
+def test_rows_of_the_lowest_numbers(ops):
+    """All of a row masked by the type's lowest number, with and without a NaN in it: the masked tokens share the weight."""
+    for dtype in ("bf16", "fp16", "fp32"):
+        for vocab in (1000, 1003, 30011):
+            x = torch.full((4, vocab), torch.finfo(TYPES[dtype]).min, device="cuda", dtype=TYPES[dtype])
+            x[2, ::2] = float("nan")
+            x[3, : vocab - 1] = -float("inf")
+            u = torch.tensor([0.1, 0.7, 0.6, 0.5], device="cuda")
+            for settings in (dict(), dict(temperature=0.01), dict(temperature=30.0), dict(min_p=0.5), dict(top_k=vocab), dict(top_p=0.9)):
+                check(ops, x, u, **settings)
