@@ -491,9 +491,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
       });
       all = total(all);
       if (tid == 0) S.total = all.mass;
-      // a token that is kept last has no less than its share of what is to be left out: a thousandth less, for the roundings
-      const double weight = (1.0 - (double)fmaxf(top_p, 0.0f)) * (double)all.mass / all.count * 0.999 / (double)(1ull << kUnit);
-      bound = fmaxf(bound, __double2float_rd(z.top + 1024 * (log2(fmin(weight, 1.0)) - 1e-6) / z.by));
+      // a token that is kept last has no less than its share of what is to be left out: a thousandth less, for the roundings, and
+      // half a unit, by which W may be above the weight (with less than that left there is no bound, and log2 gives a NaN)
+      const double share = (1.0 - (double)fmaxf(top_p, 0.0f)) * (double)all.mass / all.count * 0.999 - 0.5;
+      bound = fmaxf(bound, __double2float_rd(z.top + 1024 * (log2(fmin(share / (double)(1ull << kUnit), 1.0)) - 1e-6) / z.by));
     }
     // the tokens that reach it, in their order
     int n = 0;

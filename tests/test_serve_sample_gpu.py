@@ -268,3 +268,16 @@ def test_rows_of_the_lowest_numbers(ops):
             u = torch.tensor([0.1, 0.7, 0.6, 0.5], device="cuda")
             for settings in (dict(), dict(temperature=0.01), dict(temperature=30.0), dict(min_p=0.5), dict(top_k=vocab), dict(top_p=0.9)):
                 check(ops, x, u, **settings)
+
+
+def test_top_p_next_to_one_over_a_tail_of_few_units(ops):
+    """What top_p leaves out is less than the rounding of the weights of the tail: a tail token of 3.6 units of 2^-44 counts as 4."""
+    vocab = 1 << 19
+    x = torch.full((1, vocab), float(np.log(3.6 * 2.0**-44)), device="cuda")
+    x[0, 100::340] = float(np.log(2.0**-24))  # more than one block sorts, spread over the row
+    x[0, 5], x[0, 400_000] = 0.0, float(np.log(0.85))
+    x = x.expand(6, vocab)
+    u = torch.tensor([0.1, 0.5, 0.54, 0.6, 0.9, 0.99], device="cuda")
+    p = 1.0 - 2.0**-24
+    for settings in (dict(top_p=p), dict(top_p=torch.full((6,), p, device="cuda"))):
+        assert ops.sample(x, u, **settings).tolist() == [5, 5, 5, 400_000, 400_000, 400_000]
