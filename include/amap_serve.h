@@ -329,7 +329,7 @@ int amap_packed_attend(const amap_attend_args *args /* host */, const amap_packe
  * to it is above uniform times the sum over all kept ones.  temperature 0 or
  * less: the largest logit, the first of them.  A NaN counts as -infinity; a row
  * with no logit above -infinity gives -1; where the largest is +infinity, the
- * tokens that have it share the weight.
+ * tokens that have it share the weight.  A temperature above 1e30 counts as 1e30.
  * A uniform number outside counts as the nearest inside, NaN as 0; so do min_p
  * and top_p of a row; those of a row that are NaN count as not given, a
  * temperature that is as 0.

@@ -133,8 +133,8 @@ struct Sampler {
   int vocab, shift;      // shift: elements between the 16-byte boundary at or before x and x
   int begin, end;        // this warp's vectors, counted from that boundary
   int blocks, rank;
-  bool alone;            // only tokens with the largest logit have a weight, as it is +infinity or the lowest float: they count as 0, the
-                         // others as -1
+  bool alone;            // only tokens with the largest logit have a weight, as it is +infinity or next to the lowest float: they count as 0,
+                         // the others as -1
   float largest;
   double top, by;        // y = (x - top) by / 1024
   float least_value;     // smaller logits, and NaN, have no weight, and are taken to be this one
@@ -436,9 +436,12 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     return;
   }
   // ---- weights ----
-  z.alone = best == INFINITY || best == -FLT_MAX;
+  // kHottest: least_value lies above -FLT_MAX, which stands for -infinity and NaN, unless the largest logit itself is within 40 of
+  // them of it (in fp32 the two next to the lowest number)
+  constexpr double kHottest = 1e30;
+  z.alone = best == INFINITY || best < (float)(41 * kHottest - FLT_MAX);
   z.largest = best;
-  const double t = fmin((double)temperature, 1e36);
+  const double t = fmin((double)temperature, kHottest);
   z.top = z.alone ? 0.0f : best;
   z.by = 1024 * 1.4426950408889634 / t;
   z.least_value = fmaxf(__double2float_rd(z.top - (z.alone ? 1.0 : 40.0 * t)), -FLT_MAX);  // 2^-57.7

@@ -281,3 +281,28 @@ def test_top_p_next_to_one_over_a_tail_of_few_units(ops):
     p = 1.0 - 2.0**-24
     for settings in (dict(top_p=p), dict(top_p=torch.full((6,), p, device="cuda"))):
         assert ops.sample(x, u, **settings).tolist() == [5, 5, 5, 400_000, 400_000, 400_000]
+
+
+def test_temperatures_without_bound(ops):
+    """Above 1e30 they count as that, an infinite one of a row, too; NaN and -infinity are not drawn at any of them."""
+    rows = 6
+    x = torch.zeros(rows, 1003, device="cuda")
+    x[:, ::2] = float("nan")
+    x[:, 1::4] = -float("inf")
+    x[:, 3] = -3.3e38
+    x[1] -= 3.2e38
+    x[2] += 3.4e38
+    x[3, 3::4] = -torch.arange(1, 251, device="cuda") * 1e30  # the tokens 3, 7, 11, ..
+    x[4] = torch.finfo(torch.float32).min
+    x[4, ::5] = float("nan")
+    x[5] = torch.nextafter(x[4, 1], torch.tensor(0.0, device="cuda"))
+    x[5, ::3] = -float("inf")
+    u = torch.tensor([0.0213, 0.5077, 0.9713, 0.6071, 0.3019, 0.9037], device="cuda")
+    inf = torch.full((rows,), float("inf"), device="cuda")
+    for t in (1e29, 1e30, 1e35, 1e36, 3e38):
+        for settings in (dict(), dict(top_k=100), dict(top_p=0.5), dict(min_p=1e-3)):
+            want = ops.sample(x, u, temperature=min(t, 1e30), **settings)
+            check(ops, x, u, temperature=min(t, 1e30), **settings)
+            assert torch.equal(ops.sample(x, u, temperature=t, **settings), want)
+            if t == 1e36:
+                assert torch.equal(ops.sample(x, u, temperature=inf, **settings), want)
