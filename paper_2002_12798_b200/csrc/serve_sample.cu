@@ -216,6 +216,11 @@ struct Sampler {
     int y;
     return weight(v, &y);
   }
+  // of the draw of a token with logit v where the kept ones' W add up to `all`: by its weight unrounded, which may be a few units
+  __device__ __forceinline__ float log_probability(float v, uint64_t all) const {
+    constexpr double kLn2 = 0.6931471805599453;
+    return (float)(((double)v - top) * by * (kLn2 / 1024) - log((double)all / (double)(1ull << kUnit)));
+  }
   static __device__ __forceinline__ int bin_of(int y) { return -y >> 4; }
   // a value that every token with a bin up to this one reaches
   __device__ __forceinline__ float value_of_bin(int bin) const { return fmaxf(__double2float_rd(top - (16.0 * (bin + 1) + 1.0) / by), least_value); }
@@ -628,7 +633,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         for (int i = 0; i < 2; ++i) {
           if (w[i] && draw >= upto[i] - w[i] && draw < upto[i]) {
             P.a.tokens[row] = (int32_t)(0xFFFFFFFFu - (uint32_t)(S.order[2 * tid + i] >> 32));
-            if (P.a.logprobs) P.a.logprobs[row] = (float)log((double)w[i] / (double)all);
+            if (P.a.logprobs) P.a.logprobs[row] = z.log_probability(of_key((uint32_t)S.order[2 * tid + i]), all);
           }
         }
       }
@@ -894,7 +899,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
             for (int i = 0; i < N; ++i) {
               if (target >= at && target < at + w[i]) {
                 P.a.tokens[row] = index(j0 + lane, i);
-                if (P.a.logprobs) P.a.logprobs[row] = (float)log((double)w[i] / (double)all);
+                if (P.a.logprobs) P.a.logprobs[row] = z.log_probability(v[i], all);
               }
               at += w[i];
             }

@@ -306,3 +306,19 @@ def test_temperatures_without_bound(ops):
             assert torch.equal(ops.sample(x, u, temperature=t, **settings), want)
             if t == 1e36:
                 assert torch.equal(ops.sample(x, u, temperature=inf, **settings), want)
+
+
+def test_probabilities_of_unlikely_tokens(ops):
+    """A token of 2^-30 to 2^-44 of the largest one's weight, drawn because it comes first: the log of its probability is that of
+    its logit, not of its weight in whole units."""
+    for dtype in ("fp32", "fp16", "bf16"):
+        for d in (-21.0, -24.5, -27.25, -28.5, -30.0, -30.25):
+            for cut in (dict(), dict(top_k=2), dict(top_p=1.0 - 2.0**-24), dict(min_p=1e-14)):
+                x = torch.full((1, 40000 if not cut else 900), -100.0, device="cuda").to(TYPES[dtype])
+                x[0, 17], x[0, 500] = d, 0.0
+                token, logprob = ops.sample(x, torch.zeros(1, device="cuda"), return_logprob=True, **cut)
+                if int(token) == 500 and "top_p" in cut:
+                    continue  # what top_p leaves out may be all of the first
+                assert int(token) == 17
+                want = d - np.log1p(np.exp(d))
+                assert abs(float(logprob) - want) <= 2.0**-23 * abs(want), (dtype, d, float(logprob))
