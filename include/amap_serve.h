@@ -335,8 +335,11 @@ int amap_packed_attend(const amap_attend_args *args /* host */, const amap_packe
  * temperature that is as 0.
  * logprob[r] = log of the probability with which the token was drawn (0 for
  * temperature 0, -infinity with token -1).
- * The answer is the definition's in 64 bits: w is rounded to units of 2^-44 (of
- * the largest), sums are whole numbers, in no order.
+ * Sums are whole numbers, in no order: w is rounded to units of 2^-44 of the
+ * largest, so that a token with less than 2^-45 of it is never drawn, and the
+ * answer is the definition's in 64 bits but where uniform times the sum is
+ * within vocab * 2^-45 of a border between two tokens.  logprob is not rounded
+ * to these units.
  * ------------------------------------------------------------------------- */
 typedef struct amap_sample_args {
   int32_t rows;    /* 1 .. 65535 */

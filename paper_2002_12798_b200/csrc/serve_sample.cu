@@ -2,9 +2,10 @@
 //
 // Mathematics.  A token's weight w = 2^y, y = (x - max) log2(e) / temperature, by a table of 2^(i/1024) and a polynomial of degree 3
 // in 64 bits (Tang, ACM Transactions on Mathematical Software 15, 1989), is rounded to a whole number W of units of 2^-44.
-// Sums of W are whole numbers, so their order does not matter, and the answer is the 64-bit definition's but where the
-// uniform number is within some 2^-35 of a border between two tokens: with weights of 24 bits, rows of 10^5 tokens would often
-// come out otherwise.
+// Sums of W are whole numbers, so their order does not matter.  W is off by half a unit at most, and weights below 2^-45 are none: a
+// sum is off by 2^-45 of the largest weight for each token, 2^-26 of it at most (2^19 tokens just below 2^-45), as a rule by
+// far less, since roundings go either way.  The answer is the 64-bit definition's where the uniform number is further than that from
+// a border between two tokens: with weights of 24 bits, rows of 10^5 tokens would often come out otherwise.
 //
 // What the settings keep is a beginning of the order by (logit, index), given by a last logit and how many of the tokens
 // that have it are kept.  A first bound is cheap: min_p gives one; for top_k the top_k-th largest of the threads' own

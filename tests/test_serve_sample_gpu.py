@@ -322,3 +322,19 @@ def test_probabilities_of_unlikely_tokens(ops):
                 assert int(token) == 17
                 want = d - np.log1p(np.exp(d))
                 assert abs(float(logprob) - want) <= 2.0**-23 * abs(want), (dtype, d, float(logprob))
+
+
+def test_a_tail_below_the_unit(ops):
+    """Tokens of less than 2^-45 of the largest one's weight are not drawn, however many they are; the others' borders move by no
+    more than the tail's sum, 2^-27 here."""
+    vocab = 1 << 19
+    for dtype in ("fp32", "bf16"):
+        x = torch.full((1, vocab), -32.0, device="cuda").to(TYPES[dtype])  # 2^-46.2
+        x[0, [1000, 77_777, 300_000, 500_001]] = torch.tensor([-30.5, -2.0, 0.0, -0.5], device="cuda").to(TYPES[dtype])  # the first: 2^-44.0
+        w = torch.exp(x[0].double())
+        upto = torch.cumsum(w, 0) / w.sum()
+        u = torch.cat([torch.linspace(0, 1, 300, device="cuda")[1:-1], upto[[77_777, 300_000]].float() + 2.0**-22, upto[[77_777, 300_000]].float() - 2.0**-22])
+        want = torch.searchsorted(upto, u.double(), right=True)
+        for settings in (dict(), dict(temperature=torch.ones(len(u), device="cuda"), top_k=vocab), dict(min_p=1e-15)):
+            assert torch.equal(ops.sample(x.expand(len(u), vocab), u, **settings).long(), want)
+        assert ops.sample(x, torch.zeros(1, device="cuda")).tolist() == [1000]
