@@ -3,10 +3,10 @@
 // Mathematics.  That of serve_attend.cu with K = low_K + step_K c and V = low_V + step_V d by groups of elements:
 //   s_t = scale sum_g (step_K <q_g, c_tg> + low_K sum(q_g)),   O = sum_t sum_g (P_t step_V) d_tg + P_t low_V
 // so the matrix instructions see the codes themselves.  A code's four bits, masked out where they lie in a 16-bit half, are
-// an fp16 number: code x 2^-24 in bits 0 .. 3, code x 2^-20 in bits 4 .. 7 (fp16 counts evenly from 0 to 2^11 of its
+// an fp16 number: code x 2^-21 in bits 3 .. 6, code x 2^-17 in bits 7 .. 10 (fp16 counts evenly from 0 to 2^11 of its
 // smallest steps), exact in the products: no conversion.  q's elements that meet the lower kind of K's codes are taken 16
-// times as large.  Of V the lower kind's rows take whole bytes, lower + 16 upper, and what the upper rows have of them is taken off
-// at the end: four operations for eight codes.  Tokens are the M side of both products; P is transposed in between.
+// times as large; of O the lower kind's rows are scaled at the end.  Five operations for eight codes: four masks, and the
+// halves' bytes exchanged for the last two of four.  Tokens are the M side of both products; P is transposed in between.
 //
 // Precision.  q is fp16 times a power of two that brings its largest element near 2^11 (2^15 where it meets the lower kind):
 // elements down to 2^-27 of it are exact (of fp16's 11 bits, down to 2^-24).  P step_V enters as two fp16 terms of 11 bits, the
@@ -14,9 +14,11 @@
 // far, P times its largest |low_V| or step_V, rather than the largest P: so the products lie near fp16's upper end whatever
 // the values' size is, and a token is cut off only where its weight is 2^-24 of the largest or less (and then by 2^-40 of
 // that).  P itself, l and the sums of P low_V are in 32 bits, where R may be far from the largest score.  The matrix
-// unit cuts its sums off to 24 bits: a score is within some 2^-21 of the size of its terms (lse 0.4 to 1.5e-6 off, relative,
-// for keys of 16 times the variance of one channel), and V's codes are counted down in every second cell, so that what is
-// summed over a long request stays small.
+// unit cuts its sums off to 24 bits, counted from the largest of the exponent FIELDS: fp16 numbers below 2^-14 stand in line as if
+// they were 2^-14.  So codes in bits 0 .. 3 and 4 .. 7 lost up to four bits (sums of 16 products off by 2^-21.8 of the largest one,
+// in the bits 3 .. 10 by 2^-26.2 as with codes that are ordinary numbers; root mean squares): lse was off by 4e-7, relative,
+// for keys of 16 times the variance of one channel, and is by 4e-8 (products and sums in 32 bits: 3e-8).  V's codes are counted
+// down in every second cell, so that what is summed over a long request stays small beside what is cut off at every step.
 //
 // Bound: the issue of integer operations.  A cell of 16 tokens (2304 bytes of 128 elements in groups of 64) is 290 instructions
 // of a warp, of them 133 on the half-rate integer pipe, 87 on the multipliers (the two add up: 4 LOP and 4 FFMA take 3.05
@@ -99,6 +101,10 @@ __device__ __forceinline__ void load_v(const char *at, int lane, int slab, uint3
 }
 __device__ __forceinline__ float step_of(uint32_t w) { return __uint_as_float(w * 0x10000u); }
 __device__ __forceinline__ float low_of(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+// a lower and an upper code of both halves (kTurn); with the halves' bytes exchanged, the other two
+constexpr uint32_t kLower = 0x00780078u, kUpper = 0x07800780u;
+__device__ __forceinline__ uint32_t bytes_exchanged(uint32_t w) { return __byte_perm(w, 0, 0x2301); }
 
 // the larger step (the upper halves are not looked at)
 __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
@@ -250,7 +256,7 @@ __global__ void __launch_bounds__(kBlock, (kPackedResident<NS>)) attend_packed_k
     const int e = min(max((int)(__float_as_uint(big) >> 23) - 127 - 10, -120), 120);
     const float down = __uint_as_float((uint32_t)(127 - e) << 23);
     float up = unit * __uint_as_float((uint32_t)(127 + e) << 23);
-    up = copysignf(fminf(fmaxf(fabsf(up) * 0x1p20f, FLT_MIN), FLT_MAX), up);
+    up = copysignf(fminf(fmaxf(fabsf(up) * 0x1p17f, FLT_MIN), FLT_MAX), up);
     to_log2[0] = __shfl_sync(~0u, up, 8 * t4);
     to_log2[1] = __shfl_sync(~0u, up, 8 * t4 + 4);
 #pragma unroll
@@ -271,7 +277,7 @@ __global__ void __launch_bounds__(kBlock, (kPackedResident<NS>)) attend_packed_k
       }
       sum += __shfl_xor_sync(~0u, sum, 1);
       sum += __shfl_xor_sync(~0u, sum, 2);
-      sum *= 0x1p-20f;
+      sum *= 0x1p-17f;
       sums[n][0] = __shfl_sync(~0u, sum, 8 * t4);
       sums[n][1] = __shfl_sync(~0u, sum, 8 * t4 + 4);
     }
@@ -331,8 +337,8 @@ __global__ void __launch_bounds__(kBlock, (kPackedResident<NS>)) attend_packed_k
 #pragma unroll
                 for (int u = 0; u < kOwn; ++u) {
                   const int slab = (n0 + n) * SG + j;
-                  const uint32_t w0 = k[u][0][slab] >> (4 * i), w1 = k[u][1][slab] >> (4 * i);
-                  const uint32_t a0 = w0 & 0x000F000Fu, a1 = w1 & 0x000F000Fu, a2 = w0 & 0x00F000F0u, a3 = w1 & 0x00F000F0u;
+                  const uint32_t w0 = i ? bytes_exchanged(k[u][0][slab]) : k[u][0][slab], w1 = i ? bytes_exchanged(k[u][1][slab]) : k[u][1][slab];
+                  const uint32_t a0 = w0 & kLower, a1 = w1 & kLower, a2 = w0 & kUpper, a3 = w1 & kUpper;
                   if (j == 0 && i == 0) mma_first(acc[u][n], a0, a1, a2, a3, q[slab][i], q[slab][i + 1]);
                   else mma<AMAP_FP16>(acc[u][n], a0, a1, a2, a3, q[slab][i], q[slab][i + 1]);
                 }
@@ -471,12 +477,11 @@ __global__ void __launch_bounds__(kBlock, (kPackedResident<NS>)) attend_packed_k
             for (int j = 0; j < SG; ++j) {
 #pragma unroll
               for (int i = 0; i < 2; ++i) {
-                // rows g: whole bytes, of which 16 times rows g + 8, the upper codes, is taken off again at the end
-                const uint32_t x0 = u ? ~v[j][0] : v[j][0], x1 = u ? ~v[j][1] : v[j][1];
-                a[2 * j + i][0] = i ? __byte_perm(x0, 0, 0x4341) : x0 & 0x00FF00FFu;
-                a[2 * j + i][1] = (i ? a[2 * j + i][0] : x0) & 0x00F000F0u;
-                a[2 * j + i][2] = i ? __byte_perm(x1, 0, 0x4341) : x1 & 0x00FF00FFu;
-                a[2 * j + i][3] = (i ? a[2 * j + i][2] : x1) & 0x00F000F0u;
+                const uint32_t x0 = i ? bytes_exchanged(v[j][0]) : v[j][0], x1 = i ? bytes_exchanged(v[j][1]) : v[j][1];
+                a[2 * j + i][0] = (u ? ~x0 : x0) & kLower;
+                a[2 * j + i][1] = (u ? ~x0 : x0) & kUpper;
+                a[2 * j + i][2] = (u ? ~x1 : x1) & kLower;
+                a[2 * j + i][3] = (u ? ~x1 : x1) & kUpper;
               }
             }
 #pragma unroll
@@ -532,7 +537,7 @@ __global__ void __launch_bounds__(kBlock, (kPackedResident<NS>)) attend_packed_k
 #pragma unroll
         for (int i = 2 * n * SG; i < 2 * (n + 1) * SG; ++i)  // rows g and g + 8 are elements 4g + 2 (i mod 2) and the one behind it
           *reinterpret_cast<float2 *>(to + i / 2 * 32 + 4 * g + 2 * (i & 1)) =
-              make_float2(fmaf(o[i][c] - o[i][c + 2], 0x1p24f, low) * f, fmaf(o[i][c + 2], 0x1p20f, low) * f);
+              make_float2(fmaf(o[i][c], 0x1p21f, low) * f, fmaf(o[i][c + 2], 0x1p17f, low) * f);
       }
     }
     sync_consumers();

@@ -31,6 +31,14 @@ struct ReadParams {
 __device__ __forceinline__ float low_of(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 __device__ __forceinline__ float step_of(uint32_t w) { return __uint_as_float(w << 16); }
 
+// the i-th four bits of the lower half of a word as it lies in a cell, which with the half's bytes exchanged is `other`: masked out
+// where they are, beside 2^23, which goes together with the scale
+__device__ __forceinline__ float code_of(uint32_t w, uint32_t other, int i) {
+  const int at = kTurn + 4 * (i & 1);
+  return fmaf(__uint_as_float(((i < 2 ? w : other) & (15u << at)) | 0x4B000000u), 1.0f / (1 << at), -0x1p23f / (1 << at));
+}
+__device__ __forceinline__ uint32_t bytes_exchanged(uint32_t w) { return __byte_perm(w, 0, 0x2301); }
+
 template <int DT>
 __device__ __forceinline__ void put(char *p, int64_t at, const float (&x)[8], bool wide) {
   using T = typename Elem<DT>::T;
@@ -85,10 +93,11 @@ __global__ void __launch_bounds__(kThreads) read_kernel(const __grid_constant__ 
   for (int h = 0; h < kHeads; ++h) {
     if (head0 + h >= P.heads) break;
     float k[8], v[8];
+    const uint32_t kx = bytes_exchanged(kw[h]), x0 = bytes_exchanged(v0[h]), x1 = bytes_exchanged(v1[h]);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      k[i] = fmaf(step_of(numbers[h].x), (float)(kw[h] >> (4 * (i >> 1) + 16 * (i & 1)) & 15), low_of(numbers[h].x));
-      v[i] = fmaf(step_of(numbers[h].y), (float)((i < 4 ? v0[h] : v1[h]) >> (4 * (i & 3)) & 15), low_of(numbers[h].y));
+      k[i] = fmaf(step_of(numbers[h].x), i & 1 ? code_of(kw[h] >> 16, kx >> 16, i >> 1) : code_of(kw[h], kx, i >> 1), low_of(numbers[h].x));
+      v[i] = fmaf(step_of(numbers[h].y), i < 4 ? code_of(v0[h], x0, i) : code_of(v1[h], x1, i - 4), low_of(numbers[h].y));
     }
     put<DT>(P.k, row * P.k_row + (head0 + h) * P.k_head + c * 8, k, WIDE);
     put<DT>(P.v, row * P.v_row + (head0 + h) * P.v_head + c * 8, v, WIDE);

@@ -509,10 +509,14 @@ __device__ __forceinline__ void pack_rows(const Packing &A, uint32_t block, doub
       uint32_t w = 0;
 #pragma unroll
       for (int j = 0; j < 8; ++j) w |= code[j] << (4 * (j >> 1) + 16 * (j & 1));
-      *reinterpret_cast<uint32_t *>(cell + k_word_at(A.slabs, t, c)) = w;
+      *reinterpret_cast<uint32_t *>(cell + k_word_at(A.slabs, t, c)) = turn_halves(w);
     } else {
-      *reinterpret_cast<uint16_t *>(cell + v_half_at(A.slabs, t, 2 * c)) = (uint16_t)(code[0] | code[1] << 4 | code[2] << 8 | code[3] << 12);
-      *reinterpret_cast<uint16_t *>(cell + v_half_at(A.slabs, t, 2 * c + 1)) = (uint16_t)(code[4] | code[5] << 4 | code[6] << 8 | code[7] << 12);
+      uint32_t w = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w |= code[j] << (4 * j);
+      w = turn_halves(w);
+      *reinterpret_cast<uint16_t *>(cell + v_half_at(A.slabs, t, 2 * c)) = (uint16_t)w;
+      *reinterpret_cast<uint16_t *>(cell + v_half_at(A.slabs, t, 2 * c + 1)) = (uint16_t)(w >> 16);
     }
     if (d0 % A.group == 0)
       *reinterpret_cast<uint32_t *>(cell + numbers_at(A.slabs, t, d0 / A.group) + (is_k ? 0 : 4)) = (uint32_t)__bfloat16_as_ushort(low) << 16 | __bfloat16_as_ushort(step);

@@ -259,3 +259,27 @@ def test_python_refusals():
 def test_the_kernel_and_the_layout_name_the_same_cell():
     text = open(os.path.join(CSRC, "serve_packed.cuh")).read()
     assert int(re.search(r"constexpr int kCell = (\d+);", text).group(1)) == 16
+
+
+def test_codes_lie_where_the_masks_find_them(tmp_path):
+    """The two masks of attention (serve_attend_packed.cu) on a word, and on it with its halves' bytes exchanged, give all eight codes."""
+    cxx = shutil.which("g++")
+    if not cxx:
+        pytest.skip("no C++ compiler")
+    (tmp_path / "codes.cpp").write_text("""
+#include <cstdio>
+#include "serve_packed.cuh"
+int main() {
+  for (uint32_t i = 0, w = 0x12345678u; i < 200; ++i, w = w * 1664525u + 1013904223u)
+    printf("%u %u\\n", w, amap_serve::turn_halves(w));
+}
+""")
+    flags = ["-std=c++17", "-O1", "-Wall", "-Werror", "-I", CSRC, "-I", os.path.join(ROOT, "include"), "-x", "c++"]
+    subprocess.check_call([cxx, *flags, str(tmp_path / "codes.cpp"), "-o", str(tmp_path / "codes")])
+    text = open(os.path.join(CSRC, "serve_attend_packed.cu")).read()
+    lower, upper = (int(x, 16) for x in re.search(r"kLower = (0x\w+)u, kUpper = (0x\w+)u;", text).groups())
+    for line in subprocess.check_output([str(tmp_path / "codes")], text=True).splitlines():
+        plain, held = (int(x) for x in line.split())
+        other = (held & 0x00FF00FF) << 8 | held >> 8 & 0x00FF00FF
+        got = [(x & mask) >> shift >> 16 * o & 0xFFFF for x in (held, other) for mask, shift in ((lower, 3), (upper, 7)) for o in (0, 1)]
+        assert got == [plain >> (4 * i + 16 * o) & 15 for i in range(4) for o in (0, 1)]
