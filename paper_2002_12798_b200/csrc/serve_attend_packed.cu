@@ -11,9 +11,10 @@
 // Precision.  q is fp16 times a power of two that brings its largest element near 2^11 (2^15 where it meets the lower kind):
 // elements down to 2^-27 of it are exact (of fp16's 11 bits, down to 2^-24).  P step_V enters as two fp16 terms of 11 bits, the
 // second what the first leaves over.  They are taken relative to a reference R that follows the largest WEIGHT of a token so
-// far, P times its largest |low_V| or step_V, rather than the largest P: so the products lie near fp16's upper end whatever
-// the values' size is, and a token is cut off only where its weight is 2^-24 of the largest or less (and then by 2^-40 of
-// that).  P itself, l and the sums of P low_V are in 32 bits, where R may be far from the largest score.  The matrix
+// far, P times its largest |low_V| or step_V, rather than the largest P: so the products lie near fp16's upper end for values of
+// any size (2^-110 and more), and a token is cut off only where its weight is 2^-24 of the largest or less (and then by 2^-33
+// of that).  P itself, l and the sums of P low_V are in 32 bits, where R may be far from the largest score; values above 2^24 are
+// scaled, so that neither end of their range is met (kLarge).  The matrix
 // unit cuts its sums off to 24 bits, counted from the largest of the exponent FIELDS: fp16 numbers below 2^-14 stand in line as if
 // they were 2^-14.  So codes in bits 0 .. 3 and 4 .. 7 lost up to four bits (sums of 16 products off by 2^-21.8 of the largest one,
 // in the bits 3 .. 10 by 2^-26.2 as with codes that are ordinary numbers; root mean squares): lse was off by 4e-7, relative,
@@ -42,8 +43,14 @@ constexpr int kLook = 32 / kCells;                                              
 static_assert(kOwn == 2, "a warp's cells of a tile");
 constexpr float kUp = 0x1p9f, kTop = 0x1p15f;  // P is kUp times what it stands for; P step_V above kTop renews the reference
 constexpr float kNone = -3e38f;            // the reference before the first token
-constexpr float kLeast = 0x1p-60f;         // a smaller |low| or step counts as this much
-constexpr float kMost = 0x1p80f;           // a sum of P above this renews the reference, too (tokens whose V is constant have no step)
+constexpr float kLeast = 0x1p-90f;         // a smaller |low| or step counts as this much
+constexpr float kMost = 0x1p72f;           // a sum of P above this renews the reference, too (tokens whose V is constant have no step)
+// Where a |low| or step is above kLarge the item's numbers of V are taken times a power of 2 from then on, which brings the largest
+// below 1.  So P |low| is below kMost kLarge (and below 2 kUp where the reference is new), with room for a sum of 2^27 of them, and the
+// most probable token's P is 2^-24 at least, far enough from 2^-126 for 32 bits to hold what l adds up.
+constexpr float kLarge = 0x1p24f;
+// O is handed over as this much of itself, so that a sum of the largest values has room; what divides it by l takes that off
+constexpr float kRoom = 0x1p-24f;
 
 template <int NS> constexpr int kPackedResident = NS >= 8 ? 1 : 2;
 // Stages of the ring: what a multiprocessor's shared memory has room for beside the rest of its blocks, up to eight.
@@ -106,10 +113,17 @@ __device__ __forceinline__ float low_of(uint32_t w) { return __uint_as_float(w &
 constexpr uint32_t kLower = 0x00780078u, kUpper = 0x07800780u;
 __device__ __forceinline__ uint32_t bytes_exchanged(uint32_t w) { return __byte_perm(w, 0, 0x2301); }
 
-// the larger step (the upper halves are not looked at)
+__device__ __forceinline__ float power_of_2(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }  // -126 .. 127
+// low and step times 2^e
+__device__ __forceinline__ uint32_t scaled(uint32_t w, int e) {
+  uint32_t r;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"((uint32_t)(127 + e) * (0x10001u << 7)));
+  return r;
+}
+// the larger step, and the larger |low| with one sign or the other; NaN counts for nothing
 __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
   uint32_t r;
-  asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  asm("max.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
 
@@ -286,9 +300,11 @@ __global__ void __launch_bounds__(kBlock, (kPackedResident<NS>)) attend_packed_k
   // o: codes' part of O^T, elements by heads 2 t4 and 2 t4 + 1; of these heads: low's part of a group over this lane's tokens,
   // the same of l, and the reference
   float o[2 * NS][4], lows[NG][2], l[2], ref[2];
-  bool fresh;  // nothing is in them yet
+  bool fresh;   // nothing is in them yet
+  int scale_v;  // V's numbers are taken times 2^scale_v
   auto clear = [&]() {
     fresh = true;
+    scale_v = 0;
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       l[c] = 0.0f;
@@ -317,6 +333,15 @@ __global__ void __launch_bounds__(kBlock, (kPackedResident<NS>)) attend_packed_k
       const uint32_t rows = small.rows_there[stage][warp];
       char *const base = smem + stage * kStage + warp * kOwn * C;
       if (rows) {
+        if (scale_v != 0) {  // where they lie: it is seldom
+#pragma unroll 1
+          for (int i = lane; i < kOwn * NG * kCell; i += 32) {
+            uint32_t *const at = reinterpret_cast<uint32_t *>(base + i / (NG * kCell) * C + NS * 512 + i % (NG * kCell) * 8 + 4);
+            *at = scaled(*at, scale_v);
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // ahead of the copy that overwrites them
+          __syncwarp();
+        }
         float s[kOwn][4];    // tokens g, g + 8 of a cell by heads 2 t4, 2 t4 + 1
         uint32_t w[kOwn][2][NG];  // V's numbers
         uint32_t k[kOwn][2][NS];
@@ -384,20 +409,26 @@ __global__ void __launch_bounds__(kBlock, (kPackedResident<NS>)) attend_packed_k
             }
           }
         }
-        float step[kOwn][2];      // the largest
+        float step[kOwn][2];  // a token's largest
+        uint32_t all;         // the largest of all of these
+        auto look_over = [&]() {
+          all = 0;
 #pragma unroll
-        for (int u = 0; u < kOwn; ++u) {
+          for (int u = 0; u < kOwn; ++u) {
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            uint32_t most = w[u][e][0];
+            for (int e = 0; e < 2; ++e) {
+              uint32_t most = w[u][e][0];
 #pragma unroll
-            for (int n = 1; n < NG; ++n) most = larger(most, w[u][e][n]);
-            step[u][e] = step_of(most);
+              for (int n = 1; n < NG; ++n) most = larger(most, w[u][e][n]);
+              step[u][e] = step_of(most);
+              all = larger(all, most);
+            }
           }
-        }
+        };
+        look_over();
         float p[kOwn][4], sum[2];
         auto weigh = [&]() {
-          bool beyond = fresh;
+          bool beyond = fresh || fmaxf(fabsf(low_of(all)), step_of(all)) > kLarge;
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
             float most = 0.0f;
@@ -416,6 +447,16 @@ __global__ void __launch_bounds__(kBlock, (kPackedResident<NS>)) attend_packed_k
         };
         // seldom after the first tile: the reference, and all that is relative to it, go by this step's weights, too
         auto renew = [&]() {
+          float by = 1.0f;  // for a new scale of V
+          const float size = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(fmaxf(fabsf(low_of(all)), step_of(all)))));
+          if (size > kLarge) {
+            const int down = min((int)(__float_as_uint(size) >> 23) - 126, 126 + scale_v);
+            scale_v -= down;
+            by = power_of_2(-down);
+#pragma unroll
+            for (int i = 0; i < 2 * kOwn * NG; ++i) w[i / (2 * NG)][i / NG % 2][i % NG] = scaled(w[i / (2 * NG)][i / NG % 2][i % NG], -down);
+            look_over();
+          }
           float weight[kOwn][2];  // log2 of the larger of |low| and step
 #pragma unroll
           for (int u = 0; u < kOwn; ++u) {
@@ -440,11 +481,11 @@ __global__ void __launch_bounds__(kBlock, (kPackedResident<NS>)) attend_packed_k
             ref[c] = top;
             l[c] *= keep;
 #pragma unroll
-            for (int n = 0; n < NG; ++n) lows[n][c] *= keep;
+            for (int n = 0; n < NG; ++n) lows[n][c] *= keep * by;
 #pragma unroll
             for (int i = 0; i < 2 * NS; ++i) {
-              o[i][c] *= keep;
-              o[i][c + 2] *= keep;
+              o[i][c] *= keep * by;
+              o[i][c + 2] *= keep * by;
             }
           }
           fresh = false;
@@ -526,7 +567,7 @@ __global__ void __launch_bounds__(kBlock, (kPackedResident<NS>)) attend_packed_k
     for (int c = 0; c < 2; ++c) {
       const float *ml = joint + (2 * t4 + c) * kPitch + D;
       const float top = fmaxf(fmaxf(ml[0], ml[8 * kPitch]), fmaxf(ml[16 * kPitch], ml[24 * kPitch]));
-      const float f = (top == -INFINITY ? 1.0f : exp2_of(ref[c] - top)) / kUp;
+      const float f = (top == -INFINITY ? 1.0f : exp2_of(ref[c] - top)) / kUp, unscale = power_of_2(-scale_v);
       float *to = joint + (warp * 8 + 2 * t4 + c) * kPitch;
 #pragma unroll
       for (int n = 0; n < NG; ++n) {
@@ -534,10 +575,11 @@ __global__ void __launch_bounds__(kBlock, (kPackedResident<NS>)) attend_packed_k
         low += __shfl_xor_sync(~0u, low, 4);
         low += __shfl_xor_sync(~0u, low, 8);
         low += __shfl_xor_sync(~0u, low, 16);
+        low *= kRoom;
 #pragma unroll
         for (int i = 2 * n * SG; i < 2 * (n + 1) * SG; ++i)  // rows g and g + 8 are elements 4g + 2 (i mod 2) and the one behind it
           *reinterpret_cast<float2 *>(to + i / 2 * 32 + 4 * g + 2 * (i & 1)) =
-              make_float2(fmaf(o[i][c], 0x1p21f, low) * f, fmaf(o[i][c + 2], 0x1p17f, low) * f);
+              make_float2(fmaf(o[i][c], 0x1p21f * kRoom, low) * f * unscale, fmaf(o[i][c + 2], 0x1p17f * kRoom, low) * f * unscale);
       }
     }
     sync_consumers();
@@ -574,7 +616,7 @@ extern "C" int amap_packed_attend(const amap_attend_args *a, const amap_packed *
   P.a.maps = nullptr;
   P.a.cache = {};
   P.a.cache.n_pages = c.n_pages, P.a.cache.page_size = c.page_size, P.a.cache.heads = c.heads, P.a.cache.head_dim = c.head_dim;
-  P.a.cache.k_scale = P.a.cache.v_scale = 1.0f;
+  P.a.cache.k_scale = 1.0f, P.a.cache.v_scale = 1.0f / kRoom;
   PP.data = static_cast<const char *>(c.data), PP.page = c.page, PP.head = c.head;
   PP.run = 1;
   while (PP.run < kCells && c.page_size / kCell % (2 * PP.run) == 0) PP.run *= 2;

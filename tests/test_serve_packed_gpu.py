@@ -527,3 +527,23 @@ def test_scores_are_as_good_as_in_32_bits(ops, dim, group, dtype, heavy):
         size = np.sqrt((terms**2).sum(-1)).max(0) * plan.scale
         off.append((lse[i].cpu().double().numpy() - want) / np.maximum(size, 1.0))
     assert np.sqrt(np.mean(np.square(off))) <= 4 * 2.0**-24
+
+
+@pytest.mark.parametrize("group", [32, 64])
+@pytest.mark.parametrize("size", [2.0**40, 2.0**58, -(2.0**70), 2.0**100, -(2.0**120)])
+@pytest.mark.parametrize("rise", [0.0, 0.05, 2.0])
+def test_constant_values_behind_zeros(ops, group, size, rise):
+    """Groups of one value have no step: the weight that they have is their value's.  Zeros, then large values, with scores that
+    stay as they are or rise."""
+    r = np.random.default_rng(17)
+    tokens, dim = 512, 128
+    k, v = np.zeros((tokens, 1, dim)), np.zeros((tokens, 1, dim))
+    k[:, 0, 0] = np.maximum(0, np.arange(tokens) - 64) * rise / 4
+    v[128:] = size
+    v[300:, :, dim // 2 :] = size / 2.0**20  # the second half's values grow smaller on the way
+    v[400:420] = 0.0
+    cache, *held = filled(ops, r, tokens, 64, 1, dim, group, "bf16", k=k, v=v)
+    q = torch.zeros(3, 8, dim, device="cuda", dtype=torch.bfloat16)
+    q[:, :, 0] = torch.tensor([1.0, 0.5, 0.0, 2.0, -1.0, 0.25, 4.0, 1.0], device="cuda")
+    table = np.stack([np.arange(8), np.arange(8), np.arange(8)[::-1]]).astype(np.int32)
+    check_attend(ops.AttendPlan(3, 8, 1, dim, scale=1.0), q, cache, table, np.array([512, 140, 500], dtype=np.int32), *held)
