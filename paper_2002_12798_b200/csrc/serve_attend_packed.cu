@@ -447,12 +447,11 @@ __global__ void __launch_bounds__(kBlock, (kPackedResident<NS>)) attend_packed_k
         };
         // seldom after the first tile: the reference, and all that is relative to it, go by this step's weights, too
         auto renew = [&]() {
-          float by = 1.0f;  // for a new scale of V
+          int down = 0;  // V's new scale is 2^-down of the one so far
           const float size = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(fmaxf(fabsf(low_of(all)), step_of(all)))));
           if (size > kLarge) {
-            const int down = min((int)(__float_as_uint(size) >> 23) - 126, 126 + scale_v);
+            down = min((int)(__float_as_uint(size) >> 23) - 126, 126 + scale_v);
             scale_v -= down;
-            by = power_of_2(-down);
 #pragma unroll
             for (int i = 0; i < 2 * kOwn * NG; ++i) w[i / (2 * NG)][i / NG % 2][i % NG] = scaled(w[i / (2 * NG)][i / NG % 2][i % NG], -down);
             look_over();
@@ -470,22 +469,22 @@ __global__ void __launch_bounds__(kBlock, (kPackedResident<NS>)) attend_packed_k
           }
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            float top = kNone;
+            float top = ref[c] + __log2f(l[c]) - 100.0f;  // l has room
 #pragma unroll
             for (int u = 0; u < kOwn; ++u) top = fmaxf(top, fmaxf(fmaf(s[u][c], to_log2[c], weight[u][0]), fmaf(s[u][c + 2], to_log2[c], weight[u][1])));
             top = fmaxf(top, __shfl_xor_sync(~0u, top, 4));
             top = fmaxf(top, __shfl_xor_sync(~0u, top, 8));
             top = fmaxf(top, __shfl_xor_sync(~0u, top, 16));
-            top = fmaxf(top, ref[c]);
-            const float keep = exp2_of(ref[c] - top);
+            top = fmaxf(top, ref[c] - (float)down);  // weights so far are smaller by this, too
+            const float keep = exp2_of(ref[c] - top), keep_o = keep * power_of_2(-down);
             ref[c] = top;
             l[c] *= keep;
 #pragma unroll
-            for (int n = 0; n < NG; ++n) lows[n][c] *= keep * by;
+            for (int n = 0; n < NG; ++n) lows[n][c] *= keep_o;
 #pragma unroll
             for (int i = 0; i < 2 * NS; ++i) {
-              o[i][c] *= keep * by;
-              o[i][c + 2] *= keep * by;
+              o[i][c] *= keep_o;
+              o[i][c + 2] *= keep_o;
             }
           }
           fresh = false;

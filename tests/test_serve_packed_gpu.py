@@ -547,3 +547,20 @@ def test_constant_values_behind_zeros(ops, group, size, rise):
     q[:, :, 0] = torch.tensor([1.0, 0.5, 0.0, 2.0, -1.0, 0.25, 4.0, 1.0], device="cuda")
     table = np.stack([np.arange(8), np.arange(8), np.arange(8)[::-1]]).astype(np.int32)
     check_attend(ops.AttendPlan(3, 8, 1, dim, scale=1.0), q, cache, table, np.array([512, 140, 500], dtype=np.int32), *held)
+
+
+def test_values_of_every_size(ops):
+    """From 2^-105 to 2^120, all of one size, and from token to token."""
+    r = np.random.default_rng(18)
+    tokens, dim = 512, 128
+    k = r.standard_normal((tokens, 1, dim))
+    q = cuda(r.standard_normal((1, 8, dim)), torch.bfloat16)
+    table, lens = np.arange(8, dtype=np.int32)[None], np.array([tokens], dtype=np.int32)
+    plan = ops.AttendPlan(1, 8, 1, dim)
+    for low, high in ((-105, -105), (-80, -80), (-40, -40), (23, 25), (60, 60), (118, 118), (-105, 60), (-60, 118), (-20, 30)):
+        v = r.standard_normal((tokens, 1, dim)) * 2.0 ** r.integers(low, high + 1, (tokens, 1, 1))
+        cache, *held = filled(ops, r, tokens, 64, 1, dim, 64, "bf16", k=k, v=v)
+        check_attend(plan, q, cache, table, lens, *held)
+        v = np.sort(np.abs(v), axis=0)  # growing, so that the scale is renewed on the way
+        cache, *held = filled(ops, r, tokens, 64, 1, dim, 32, "bf16", k=k, v=v)
+        check_attend(plan, q, cache, table, lens, *held)
