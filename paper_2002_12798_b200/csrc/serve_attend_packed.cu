@@ -12,8 +12,9 @@
 // elements down to 2^-27 of it are exact (of fp16's 11 bits, down to 2^-24).  P step_V enters as two fp16 terms of 11 bits, the
 // second what the first leaves over.  They are taken relative to a reference R that follows the largest WEIGHT of a token so
 // far, P times its largest |low_V| or step_V, rather than the largest P: so the products lie near fp16's upper end for values of
-// any size (2^-110 and more), and a token is cut off only where its weight is 2^-24 of the largest or less (and then by 2^-33
-// of that).  P itself, l and the sums of P low_V are in 32 bits, where R may be far from the largest score; values above 2^24 are
+// any size (2^-110 and more), and an element is off by 2^-30 of the largest weight of a token, over all groups of the head, at most:
+// a token is cut off only where its weight is 2^-24 of that, and so are a group's codes whose steps are 2^-24 of another group's (down
+// to 2^-18 a 16-bit output does not show it).  A lift of its own for each group would be 8 more multiplications for two.  P itself, l and the sums of P low_V are in 32 bits, where R may be far from the largest score; values above 2^24 are
 // scaled, so that neither end of their range is met (kLarge).  The matrix
 // unit cuts its sums off to 24 bits, counted from the largest of the exponent FIELDS: fp16 numbers below 2^-14 stand in line as if
 // they were 2^-14.  So codes in bits 0 .. 3 and 4 .. 7 lost up to four bits (sums of 16 products off by 2^-21.8 of the largest one,

@@ -549,6 +549,33 @@ def test_constant_values_behind_zeros(ops, group, size, rise):
     check_attend(ops.AttendPlan(3, 8, 1, dim, scale=1.0), q, cache, table, np.array([512, 140, 500], dtype=np.int32), *held)
 
 
+@pytest.mark.parametrize("group", [32, 64])
+@pytest.mark.parametrize("apart", [10, 18, 26])
+def test_groups_of_values_far_apart(ops, group, apart):
+    """The second half of a head has values 2^-apart of the first's: they are right to 15 / 2 x 2^-25 / 2^9 of the first's for each token
+    (codes of at most 15, half of fp16's smallest step, the largest weight at 2^9 or more), and to 16 bits where that is far below."""
+    r = np.random.default_rng(apart)
+    tokens, dim = 256, 128
+    v = r.standard_normal((tokens, 1, dim))
+    v[..., dim // 2 :] *= 2.0**-apart
+    for dtype, spread in (("bf16", 0.0), ("bf16", 1.0), ("fp16", 0.0)):
+        if dtype == "fp16" and apart > 10:
+            continue  # fp16 has no such numbers
+        k = r.standard_normal((tokens, 1, dim)) * spread
+        cache, held_k, held_v = filled(ops, r, tokens, 32, 1, dim, group, dtype, k=k, v=v)
+        q = cuda(r.standard_normal((2, 8, dim)), TYPES[dtype])
+        table, lens = np.stack([r.permutation(8) for _ in range(2)]).astype(np.int32), np.array([256, 199], dtype=np.int32)
+        plan = ops.AttendPlan(2, 8, 1, dim)
+        out, _ = check_attend(plan, q, cache, table, lens, held_k, held_v)
+        for i, n in enumerate(lens):
+            t = np.arange(n)
+            want, _, bound, _ = ref.attend(f64(q)[i], held_k, held_v, table[i, t // 32] * 32 + t % 32, plan.scale)
+            off, size = np.abs(f64(out)[i] - want)[:, dim // 2 :], np.abs(want)[:, dim // 2 :]
+            # a score's error moves a weight, of values of up to 6 (and the softmax's, beside 2^-apart, is the same for both halves)
+            own = (4 * 2.0**-20 + 2.0**-8 * (dtype == "bf16") + 2.0**-11 * (dtype == "fp16")) * size + 2.0**-apart * 6 * 2.0**-15
+            assert (off <= own + 7.5 * 2.0**-34 * 6).all(), (dtype, i, (off / own).max())
+
+
 def test_values_of_every_size(ops):
     """From 2^-105 to 2^120, all of one size, and from token to token."""
     r = np.random.default_rng(18)
