@@ -259,7 +259,7 @@ int amap_attend_workspace(int32_t n_requests, int32_t q_heads, int32_t kv_heads,
 /* ---------------------------------------------------------------------------
  * A paged cache of 4 bits.  A head's elements are held in groups of 32 or 64:
  *   low  = the group's smallest element, rounded down to bf16;
- *   step = (its largest element - low) / 15, rounded to bf16;
+ *   step = (its largest element - low) / 15, rounded to fp32 and that to bf16;
  *   code = (element - low) / step, rounded to nearest even, within 0 .. 15 (0
  *          where step is 0), and stands for low + step * code.
  * A group that holds a NaN or an infinity, or whose low or step is none of

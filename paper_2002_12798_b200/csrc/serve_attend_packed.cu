@@ -22,17 +22,19 @@
 // for keys of 16 times the variance of one channel, and is by 4e-8 (products and sums in 32 bits: 3e-8).  V's codes are counted
 // down in every second cell, so that what is summed over a long request stays small beside what is cut off at every step.
 //
-// Bound: the issue of integer operations.  A cell of 16 tokens (2304 bytes of 128 elements in groups of 64) is 290 instructions
-// of a warp, of them 133 on the half-rate integer pipe, 87 on the multipliers (the two add up: 4 LOP and 4 FFMA take 3.05
-// clocks of a multiprocessor, 4 LOP alone 2.03) and 24 products of 16 x 8 x 16 (2.03 clocks each, in parallel): about 110
-// clocks, where the cell takes 99 to come from HBM.  Copies alone take 116 us of the 152 of 64 requests; with a third block a
-// multiprocessor (128 registers) nothing changes.
+// Bound: a warp's own chain, with two computing warps to a scheduler.  A cell of 16 tokens (2304 bytes of 128 elements in groups of
+// 64) is 300 instructions of a warp, of them 135 on the half-rate integer pipe, 90 on the multipliers and 24 products of 16 x 8 x 16
+// (2.03 clocks of a multiprocessor each): at full issue some 115 clocks, where the cell takes 99 to come from HBM and is
+// there after 165.  No unit is at its limit (issue slots 49 %, integer pipe 46, products 31, DRAM 45); warps wait for their own
+// last instruction first, for one another and the pipes next, and a quarter as long for instructions to come: the loop with its
+// rare branches is larger than the nearest instruction memory, and ptxas' order of it is worth some 4 % either way.  Copies alone
+// take 116 us of the 162 of 64 requests; a third block a multiprocessor (128 registers) brings nothing.
 //
 // Split, ring and join are serve_attend.cu's.  A tile is 128 tokens: eight cells, copied in bulk in runs that every page divides into.
 //
-// Measured: 64 requests of up to 16384 tokens, 32 q heads over 8 of 128 elements, bf16, groups of 64 (605 MB) 152 us = 4.0
-// TB/s; one request of 131009 tokens, fp16, groups of 32 (168 MB) 51 us = 3.3; 128 requests of up to 4096, 64 q heads over 4
-// (155 MB) 91 us; 33 tokens 6.1 us.
+// Measured: 64 requests of up to 16384 tokens, 32 q heads over 8 of 128 elements, bf16, groups of 64 (605 MB) 162 us = 3.7
+// TB/s; one request of 131009 tokens, fp16, groups of 32 (168 MB) 53 us = 3.2; 128 requests of up to 4096, 64 q heads over 4
+// (155 MB) 95 us; 33 tokens 6.3 us.
 #define AMAP_ATTEND_PARTS_ONLY
 #include "serve_attend.cu"
 #include "serve_packed.cuh"

@@ -16,13 +16,16 @@
 // ones have a weight, are counted in a bin of their own each, and weighed once.  The draw takes the sums of each warp's run
 // of the row (or of its list), and goes through one of them.
 //
-// Bound: 64-bit arithmetic where all tokens have to be weighed one by one (about 25 instructions, nine of them in 64 bits, 9 to 14
-// clocks of a multiprocessor for 32 tokens), the largest logit's pass by memory, and the rest by latency: every exchange between
-// a row's blocks takes one to four microseconds.  The logits come from HBM once, and from the second-level cache once or
-// twice more.  A row is a cluster's, of as many blocks as fill the device, which exchange sums through shared memory.
+// Bound: latency.  Where all tokens are weighed one by one (about 25 instructions, nine of them in 64 bits) no unit is near its
+// limit: 128 x 131072 fp32 have 49 % of the issue slots, 15 % of the 64-bit pipe, and wait for loads first, for one another
+// and for barriers next; 64 registers a thread, for two blocks of 16 warps, leave 56 to 76 bytes of spills (240 to 316 read back).  The largest logit's
+// pass is memory's.  The rest are chains: one row, of 1000 logits in one block or of 32000 in eight, is 15 to 19 us of bins
+// cleared and scanned for a bound, two sorts of 15 barriers and more, and scans, with exchanges of one to four us where
+// there are blocks to exchange with.  The logits come from HBM once, and from the second-level cache once or twice more.  A row is a
+// cluster's, of as many blocks as fill the device, which exchange sums through shared memory.
 //
-// Measured: one row of 32000 fp32 logits, 50 largest, top_p 0.95, 19 us; 64 rows of 100003 bf16, top_p 0.9, 61; 128 of 131072
-// fp32, nothing cut off, 57 (67 MB: 10 from HBM); 256 of 150001 bf16 with settings of their own 130.
+// Measured: one row of 32000 fp32 logits, 50 largest, top_p 0.95, 20 us; 64 rows of 100003 bf16, top_p 0.9, 61; 128 of 131072
+// fp32, nothing cut off, 62 (67 MB: 10 from HBM); 256 of 150001 bf16 with settings of their own 130 to 142, by the settings drawn.
 #include <cooperative_groups.h>
 
 #include <algorithm>
